@@ -24,6 +24,10 @@
  *   dv_spec_verify  proposed tokens the constraint admits, and greedy
  *                   verification of the proposals against the model's logits
  *                   at every proposed position.
+ *   dv_head_loss,   training a proposer or a model under the same constraint:
+ *   dv_distill_loss, softmax cross entropy over the allowed tokens from hidden
+ *   dv_embed and    states and head weights, divergence from a teacher's top
+ *   their _backward logits, and the embedding, each with its gradients.
  *
  * Conventions shared by every call:
  *   - Every array argument is a DEVICE pointer (hipMalloc'd or a torch CUDA
@@ -66,6 +70,8 @@ extern "C" {
 #define DV_MAX_PROPOSED 1024       /* num_proposed in [0, DV_MAX_PROPOSED];
                                       batch * (num_proposed + 1) <= DV_MAX_BATCH */
 #define DV_NOALLOC_MAX_BATCH 65536 /* batch of dv_masked_step_noalloc          */
+#define DV_MAX_HIDDEN 65536        /* hidden      in [1, DV_MAX_HIDDEN]  */
+#define DV_MAX_TOP    1024         /* num_top     in [1, DV_MAX_TOP]     */
 
 typedef enum dv_status {
     DV_OK = 0,
@@ -411,6 +417,168 @@ DV_API dv_status dv_spec_verify(const int32_t *next_state, const uint32_t *allow
                          const void *logits, int32_t dtype, int64_t ld_row, int64_t ld_pos,
                          int32_t batch, int32_t *token, int32_t *accepted, int32_t *new_state,
                          void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Training under a constraint
+ * ---------------------------
+ * The calls below take rows instead of sequences: row n (a token position of
+ * a batch, `rows` of them in [0, DV_MAX_BATCH]) has an automaton state, and
+ * the tokens its state allows are the only ones with a probability:
+ *
+ *   allow, num_states, states   allow [S][ceil(V/32)] uint32 as written by
+ *       dv_align and states [rows] int32: row n's allowed tokens A_n are those
+ *       with bit (states[n], v) set; none when states[n] is outside [0, S).
+ *       allow = NULL (states then also NULL, num_states 0): every token.
+ *
+ * What is masked has no effect on any result, whatever its logit (infinities
+ * and NaN included).  Elements are of `dtype` (DV_F32 or DV_BF16) and aligned
+ * to their size; every array with a row stride ld_* (in elements, at least the
+ * row's length) has unit stride along its rows, and rows may start at any
+ * alignment.  Products, sums, softmax statistics and losses are in fp32, each
+ * result rounded once; no call adds with atomics: the same call gives the same
+ * bits.  Workspaces hold nothing between calls and need no clearing; 256-byte
+ * aligned; calls that share one must be ordered on one stream.  Outputs must
+ * not overlap each other, an input or the workspace, except where said.
+ */
+
+/*
+ * dv_head_loss_workspace_bytes -- device workspace of dv_head_loss.  Returns 0
+ * when an argument is outside its limit.
+ */
+DV_API size_t dv_head_loss_workspace_bytes(int32_t rows, int32_t hidden, int32_t num_tokens, int32_t dtype);
+
+/*
+ * dv_head_loss -- softmax cross entropy over the allowed tokens, from hidden
+ * states and head weights, without the logits in memory.
+ *
+ * For row n with z_v = sum_d x[n][d] weight[v][d] and t = targets[n]:
+ *     lse[n]  = ln sum over v in A_n of exp(z_v), -infinity when A_n is empty;
+ *     loss[n] = lse[n] - z_t where t is in A_n; else (t outside [0, V), not
+ *               allowed, or a dead row) the row takes no part: loss[n] = 0.
+ *
+ * x [rows][ld_x], weight [V][ld_weight] of `dtype`; targets [rows] int32.
+ * fp32 operands are multiplied as sums of three bf16 parts each: the products
+ * of parts below 2^-22 of the whole are left out.
+ * loss, lse [rows] fp32.
+ * rows = 0 is valid and enqueues nothing.
+ * Errors: DV_ERR_INVALID_ARG (NULL, misaligned elements, or only one of allow
+ *   and states), DV_ERR_SHAPE, DV_ERR_DTYPE, DV_ERR_ALIAS, DV_ERR_WORKSPACE,
+ *   DV_ERR_HIP.
+ */
+DV_API dv_status dv_head_loss(const void *x, int64_t ld_x, const void *weight, int64_t ld_weight, int32_t dtype,
+                              int32_t rows, int32_t hidden, int32_t num_tokens, const int32_t *targets,
+                              const uint32_t *allow, int32_t num_states, const int32_t *states,
+                              float *loss, float *lse, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * dv_head_loss_backward_workspace_bytes -- device workspace of
+ * dv_head_loss_backward (a piece of the vocabulary at a time: it grows with
+ * rows and hidden, and with num_tokens only up to one piece).  Returns 0 when
+ * an argument is outside its limit.
+ */
+DV_API size_t dv_head_loss_backward_workspace_bytes(int32_t rows, int32_t hidden, int32_t num_tokens, int32_t dtype);
+
+/*
+ * dv_head_loss_backward -- the gradients of sum_n grad_loss[n] loss[n].
+ *
+ * With G[n][v] = grad_loss[n] (exp(z_v - lse[n]) - [v = targets[n]]) for v in
+ * A_n of rows that take part, 0 elsewhere:
+ *     grad_x[n]      = sum_v G[n][v] weight[v]     [rows][hidden]
+ *     grad_weight[v] = sum_n G[n][v] x[n]          [V][hidden]
+ * both contiguous, of `dtype`; either may be NULL and is then not computed.
+ * lse [rows] fp32 as dv_head_loss wrote it for the same inputs; grad_loss
+ * [rows] fp32.  The logits are computed again a piece at a time.  For bf16
+ * inputs G is rounded to bf16 on its way into the two products (a relative
+ * error of 2^-8 of each term, of the size of the outputs' own rounding).
+ * x and weight must be finite.
+ * rows = 0 is valid: grad_weight is filled with zeros.
+ * Errors as dv_head_loss.
+ */
+DV_API dv_status dv_head_loss_backward(const void *x, int64_t ld_x, const void *weight, int64_t ld_weight,
+                                       int32_t dtype, int32_t rows, int32_t hidden, int32_t num_tokens,
+                                       const int32_t *targets, const uint32_t *allow, int32_t num_states,
+                                       const int32_t *states, const float *lse, const float *grad_loss, void *grad_x,
+                                       void *grad_weight, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * dv_distill_loss_workspace_bytes -- device workspace of dv_distill_loss and
+ * dv_distill_loss_backward (for either dtype).  Returns 0 when an argument is
+ * outside its limit.  For one num_top it never falls as rows grow.
+ */
+DV_API size_t dv_distill_loss_workspace_bytes(int32_t rows, int32_t num_tokens, int32_t num_top);
+
+/*
+ * dv_distill_loss -- divergence of a model's distribution over the allowed
+ * tokens from a teacher's top logits.
+ *
+ * With c = inv_temperature = 1/T and row n's entries k in [0, num_top),
+ * L_n = {k : teacher_ids[n][k] in A_n and teacher_logits[n][k] > -infinity}:
+ *     q_k = softmax of c teacher_logits[n] over L_n,
+ *     p_v = softmax of c logits[n] over A_n,
+ *     loss[n] = sum over L_n of q_k (ln q_k - ln p_{id_k}).
+ * An id listed more than once counts with the sum of its entries.  Where L_n is
+ * empty, or no allowed logit is above -infinity, the row takes no part: loss 0.
+ *
+ * logits [rows][ld_logits] of `dtype`; teacher_ids [rows][num_top] int32 (ids
+ * outside [0, V) take no part), teacher_logits [rows][num_top] fp32; loss
+ * [rows] fp32.  inv_temperature finite and > 0.
+ * rows = 0 is valid and enqueues nothing.
+ * Errors as dv_head_loss.
+ */
+DV_API dv_status dv_distill_loss(const void *logits, int64_t ld_logits, int32_t dtype, int32_t rows,
+                                 int32_t num_tokens, const int32_t *teacher_ids, const float *teacher_logits,
+                                 int32_t num_top, float inv_temperature, const uint32_t *allow, int32_t num_states,
+                                 const int32_t *states, float *loss, void *workspace, size_t workspace_bytes,
+                                 void *stream);
+
+/*
+ * dv_distill_loss_backward -- the gradient of sum_n grad_loss[n] loss[n], and
+ * the loss with it, in one call (a training step needs no dv_distill_loss):
+ *     grad[n][v] = grad_loss[n] c (p_v - sum of q_k with id_k = v)  on A_n,
+ *                  0 elsewhere and on rows that take no part.
+ * grad [rows][ld_grad] of `dtype`; it may be the logits themselves (the same
+ * address and row stride), which are then overwritten.  loss may be NULL;
+ * grad_loss [rows] fp32.  Other arguments and errors as dv_distill_loss.
+ */
+DV_API dv_status dv_distill_loss_backward(const void *logits, int64_t ld_logits, int32_t dtype, int32_t rows,
+                                          int32_t num_tokens, const int32_t *teacher_ids,
+                                          const float *teacher_logits, int32_t num_top, float inv_temperature,
+                                          const uint32_t *allow, int32_t num_states, const int32_t *states,
+                                          const float *grad_loss, float *loss, void *grad, int64_t ld_grad,
+                                          void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * dv_embed -- rows of a table by token, scaled:
+ *     out[n] = scale weight[ids[n]], zeros where ids[n] is outside [0, V).
+ * weight [V][ld_weight] and out [rows][hidden] (contiguous) of `dtype`, ids
+ * [rows] int32.  rows = 0 is valid and enqueues nothing.
+ * Errors as dv_head_loss (no workspace; DV_ERR_SHAPE also for a scale that is
+ *   not finite).
+ */
+DV_API dv_status dv_embed(const void *weight, int64_t ld_weight, int32_t dtype, int32_t num_tokens, int32_t hidden,
+                          const int32_t *ids, int32_t rows, float scale, void *out, void *stream);
+
+/*
+ * dv_embed_backward_workspace_bytes -- device workspace of dv_embed_backward;
+ * for one hidden it never falls as rows grow.  Returns 0 when an argument is
+ * outside its limit.
+ */
+DV_API size_t dv_embed_backward_workspace_bytes(int32_t rows, int32_t hidden, int32_t num_tokens);
+
+/*
+ * dv_embed_backward -- the table's gradient, rows added in their order:
+ *     grad_weight[v] = scale * (sum over n with ids[n] = v of grad_out[n]),
+ * zeros for tokens that no row names; with accumulate != 0 added to what
+ * grad_weight holds (a table shared with the head: after
+ * dv_head_loss_backward), and rows of tokens that no row names stay as they are.
+ * grad_out [rows][ld_grad_out] and grad_weight [V][hidden] (contiguous) of
+ * `dtype`.  rows = 0 is valid: zeros, or nothing with accumulate.
+ * Errors as dv_embed, and DV_ERR_WORKSPACE.
+ */
+DV_API dv_status dv_embed_backward(const void *grad_out, int64_t ld_grad_out, int32_t dtype, int32_t rows,
+                                   int32_t hidden, const int32_t *ids, int32_t num_tokens, float scale,
+                                   int32_t accumulate, void *grad_weight, void *workspace, size_t workspace_bytes,
+                                   void *stream);
 
 /* Static, human-readable name of a status code ("DV_OK", ...). */
 DV_API const char *dv_status_string(int32_t status);

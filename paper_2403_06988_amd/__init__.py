@@ -12,6 +12,10 @@ importing this package fails if the library is not built.
 Algorithm 2, walked to full depth as in Sec. 3.5) for a byte-level DFA;
 ``masked_step`` is one step of its Algorithm 1 with greedy decoding;
 ``spec_walk`` / ``spec_verify`` are the speculative chain check of Sec. 3.6.
+
+For training under the same constraint (a proposer for the speculation, or a
+model): ``head_loss``, ``distill_loss`` and ``embed`` with their ``_backward``
+calls; the ``autograd`` module has them as differentiable functions.
 """
 from __future__ import annotations
 
@@ -22,7 +26,10 @@ import torch
 
 __all__ = ["align", "validate_vocab", "masked_step", "masked_step_noalloc", "masked_sample", "spec_walk", "spec_verify", "align_workspace_bytes",
            "masked_step_workspace_bytes", "masked_sample_workspace_bytes", "spec_verify_workspace_bytes",
-           "step_workspace", "sample_workspace", "spec_workspace", "DvError", "DEAD", "library_path", "lib"]
+           "step_workspace", "sample_workspace", "spec_workspace", "head_loss", "head_loss_backward",
+           "head_loss_workspace_bytes", "head_loss_backward_workspace_bytes", "distill_loss", "distill_loss_backward",
+           "distill_loss_workspace_bytes", "embed", "embed_backward", "embed_backward_workspace_bytes", "DvError", "DEAD",
+           "library_path", "lib"]
 
 DEAD = -1
 DV_OK = 0
@@ -81,6 +88,28 @@ def _load():
     lib.dv_spec_verify.restype = ctypes.c_int
     lib.dv_spec_verify.argtypes = [vp, vp, i32, i32, vp, vp, i32, i64, vp, i32, i64, i64, i32, vp, vp, vp,
                                    vp, sz, vp]
+    f32 = ctypes.c_float
+    mask = [vp, i32, vp]
+    lib.dv_head_loss_workspace_bytes.restype = sz
+    lib.dv_head_loss_workspace_bytes.argtypes = [i32, i32, i32, i32]
+    lib.dv_head_loss.restype = ctypes.c_int
+    lib.dv_head_loss.argtypes = [vp, i64, vp, i64, i32, i32, i32, i32, vp, *mask, vp, vp, vp, sz, vp]
+    lib.dv_head_loss_backward_workspace_bytes.restype = sz
+    lib.dv_head_loss_backward_workspace_bytes.argtypes = [i32, i32, i32, i32]
+    lib.dv_head_loss_backward.restype = ctypes.c_int
+    lib.dv_head_loss_backward.argtypes = [vp, i64, vp, i64, i32, i32, i32, i32, vp, *mask, vp, vp, vp, vp, vp, sz, vp]
+    lib.dv_distill_loss_workspace_bytes.restype = sz
+    lib.dv_distill_loss_workspace_bytes.argtypes = [i32, i32, i32]
+    lib.dv_distill_loss.restype = ctypes.c_int
+    lib.dv_distill_loss.argtypes = [vp, i64, i32, i32, i32, vp, vp, i32, f32, *mask, vp, vp, sz, vp]
+    lib.dv_distill_loss_backward.restype = ctypes.c_int
+    lib.dv_distill_loss_backward.argtypes = [vp, i64, i32, i32, i32, vp, vp, i32, f32, *mask, vp, vp, vp, i64, vp, sz, vp]
+    lib.dv_embed.restype = ctypes.c_int
+    lib.dv_embed.argtypes = [vp, i64, i32, i32, i32, vp, i32, f32, vp, vp]
+    lib.dv_embed_backward_workspace_bytes.restype = sz
+    lib.dv_embed_backward_workspace_bytes.argtypes = [i32, i32, i32]
+    lib.dv_embed_backward.restype = ctypes.c_int
+    lib.dv_embed_backward.argtypes = [vp, i64, i32, i32, i32, vp, i32, f32, i32, vp, vp, sz, vp]
     return lib
 
 
@@ -404,3 +433,213 @@ def spec_verify(next_state, allow, states, proposals, logits, token=None, accept
                             _ptr(workspace), nbytes, _stream(stream, dev))
     _check(st, "dv_spec_verify")
     return token, accepted, new_state
+
+
+# ------------------------------------------------------------------ training
+
+def head_loss_workspace_bytes(rows: int, hidden: int, num_tokens: int, dtype) -> int:
+    return int(lib.dv_head_loss_workspace_bytes(rows, hidden, num_tokens, _code(dtype)))
+
+
+def head_loss_backward_workspace_bytes(rows: int, hidden: int, num_tokens: int, dtype) -> int:
+    return int(lib.dv_head_loss_backward_workspace_bytes(rows, hidden, num_tokens, _code(dtype)))
+
+
+def distill_loss_workspace_bytes(rows: int, num_tokens: int, num_top: int) -> int:
+    return int(lib.dv_distill_loss_workspace_bytes(rows, num_tokens, num_top))
+
+
+def embed_backward_workspace_bytes(rows: int, hidden: int, num_tokens: int) -> int:
+    return int(lib.dv_embed_backward_workspace_bytes(rows, hidden, num_tokens))
+
+
+def _code(dtype) -> int:
+    if dtype == torch.float32:
+        return DV_F32
+    if dtype == torch.bfloat16:
+        return DV_BF16
+    raise TypeError(f"dtype must be float32 or bfloat16, got {dtype}")
+
+
+def _matrix(t, name, dev, dtype=None):
+    """Checks of a [rows][n] array with unit stride along its rows; returns its
+    row stride (at least n)."""
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if not t.is_cuda or t.device != dev:
+        raise ValueError(f"{name} must be a device tensor on {dev}")
+    if t.dim() != 2:
+        raise ValueError(f"{name} must have two dimensions")
+    rows, n = t.shape
+    if rows and n > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name} must have unit stride along its rows")
+    if rows > 1 and t.stride(0) < n:
+        raise ValueError(f"the rows of {name} must not overlap")
+    return t.stride(0) if rows > 1 else n
+
+
+def _vector(t, name, n, dtype, dev):
+    _want(t, name, dtype, dev)
+    if t.dim() != 1 or t.shape[0] != n:
+        raise ValueError(f"{name} must be [{n}]")
+
+
+def _mask_args(allow, states, rows, V, dev):
+    """(allow pointer, number of states, states pointer) of a call's mask."""
+    if (allow is None) != (states is None):
+        raise ValueError("allow and states must be given together")
+    if allow is None:
+        return None, 0, None
+    _want(allow, "allow", torch.int32, dev)
+    if allow.dim() != 2 or allow.shape[1] != (V + 31) // 32:
+        raise ValueError("allow must be [S][ceil(V/32)]")
+    _vector(states, "states", rows, torch.int32, dev)
+    return _ptr(allow), allow.shape[0], _ptr(states)
+
+
+def _result(t, name, shape, dtype, dev):
+    """A caller-supplied contiguous output (or a new one)."""
+    if t is None:
+        return torch.empty(shape, dtype=dtype, device=dev)
+    _want(t, name, dtype, dev)
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
+    return t
+
+
+def _scratch(workspace, need, dev):
+    return _workspace(workspace, need, dev, lambda: torch.empty(max(need, 1), dtype=torch.uint8, device=dev))
+
+
+def _head_args(x, weight, targets, allow, states):
+    dev = weight.device
+    ld_x, ld_w = _matrix(x, "x", dev), _matrix(weight, "weight", dev, x.dtype)
+    dt = _code(x.dtype)
+    (N, D), V = x.shape, weight.shape[0]
+    if weight.shape[1] != D:
+        raise ValueError(f"weight must be [V][{D}]")
+    _vector(targets, "targets", N, torch.int32, dev)
+    mask = _mask_args(allow, states, N, V, dev)
+    return dev, (_ptr(x), ld_x, _ptr(weight), ld_w, dt, N, D, V, _ptr(targets), *mask), (N, D, V, dt)
+
+
+def head_loss(x, weight, targets, allow=None, states=None, loss=None, lse=None, workspace=None, stream=None):
+    """Softmax cross entropy over the allowed tokens, from hidden states
+    x [N][D] and head weights weight [V][D] (bf16 or fp32, any row stride),
+    without keeping the logits.
+
+    targets [N] int32; a row whose target is outside [0, V) or not allowed
+    takes no part (loss 0).  allow [S][ceil(V/32)] int32 (as from ``align``)
+    with states [N] int32: the tokens each row's state allows; without them
+    every token.  Returns (loss [N], lse [N]) fp32."""
+    dev, args, (N, D, V, dt) = _head_args(x, weight, targets, allow, states)
+    loss = _result(loss, "loss", (N,), torch.float32, dev)
+    lse = _result(lse, "lse", (N,), torch.float32, dev)
+    workspace, nbytes = _scratch(workspace, int(lib.dv_head_loss_workspace_bytes(N, D, V, dt)), dev)
+    st = lib.dv_head_loss(*args, _ptr(loss), _ptr(lse), _ptr(workspace), nbytes, _stream(stream, dev))
+    _check(st, "dv_head_loss")
+    return loss, lse
+
+
+def head_loss_backward(x, weight, targets, lse, grad_loss, allow=None, states=None, grad_x=None, grad_weight=None,
+                       want_x=True, want_weight=True, workspace=None, stream=None):
+    """Gradients of sum(grad_loss * loss) of ``head_loss``; lse [N] as it
+    returned it.  Returns (grad_x [N][D], grad_weight [V][D]) in the inputs'
+    dtype; ``want_x`` / ``want_weight`` false: None in its place, not computed."""
+    dev, args, (N, D, V, dt) = _head_args(x, weight, targets, allow, states)
+    _vector(lse, "lse", N, torch.float32, dev)
+    _vector(grad_loss, "grad_loss", N, torch.float32, dev)
+    if not (want_x or want_weight):
+        return None, None
+    grad_x = _result(grad_x, "grad_x", (N, D), x.dtype, dev) if want_x else None
+    grad_weight = _result(grad_weight, "grad_weight", (V, D), x.dtype, dev) if want_weight else None
+    workspace, nbytes = _scratch(workspace, int(lib.dv_head_loss_backward_workspace_bytes(N, D, V, dt)), dev)
+    st = lib.dv_head_loss_backward(*args, _ptr(lse), _ptr(grad_loss), _ptr(grad_x), _ptr(grad_weight), _ptr(workspace),
+                                   nbytes, _stream(stream, dev))
+    _check(st, "dv_head_loss_backward")
+    return grad_x, grad_weight
+
+
+def _distill_args(logits, teacher_ids, teacher_logits, inv_temperature, allow, states):
+    dev = logits.device
+    ld = _matrix(logits, "logits", dev)
+    dt = _code(logits.dtype)
+    N, V = logits.shape
+    _want(teacher_ids, "teacher_ids", torch.int32, dev)
+    _want(teacher_logits, "teacher_logits", torch.float32, dev)
+    if teacher_ids.dim() != 2 or teacher_ids.shape[0] != N or teacher_ids.shape != teacher_logits.shape:
+        raise ValueError(f"teacher_ids and teacher_logits must both be [{N}][K]")
+    K = teacher_ids.shape[1]
+    mask = _mask_args(allow, states, N, V, dev)
+    return dev, (_ptr(logits), ld, dt, N, V, _ptr(teacher_ids), _ptr(teacher_logits), K, float(inv_temperature),
+                 *mask), (N, V, K)
+
+
+def distill_loss(logits, teacher_ids, teacher_logits, inv_temperature=1.0, allow=None, states=None, loss=None,
+                 workspace=None, stream=None):
+    """Divergence KL(teacher || model) over the allowed tokens: the teacher's
+    softmax over its listed tokens (teacher_ids [N][K] int32, teacher_logits
+    [N][K] fp32), the model's over all allowed tokens of logits [N][V] (bf16 or
+    fp32, any row stride), both at temperature 1 / inv_temperature.  Returns
+    loss [N] fp32 (0 for rows with nothing listed or nothing allowed)."""
+    dev, args, (N, V, K) = _distill_args(logits, teacher_ids, teacher_logits, inv_temperature, allow, states)
+    loss = _result(loss, "loss", (N,), torch.float32, dev)
+    workspace, nbytes = _scratch(workspace, distill_loss_workspace_bytes(N, V, K), dev)
+    st = lib.dv_distill_loss(*args, _ptr(loss), _ptr(workspace), nbytes, _stream(stream, dev))
+    _check(st, "dv_distill_loss")
+    return loss
+
+
+def distill_loss_backward(logits, teacher_ids, teacher_logits, grad_loss, inv_temperature=1.0, allow=None, states=None,
+                          loss=None, grad=None, workspace=None, stream=None):
+    """``distill_loss`` together with the gradient of sum(grad_loss * loss)
+    in the logits: (loss [N], grad [N][V] in the logits' dtype).  ``grad`` may
+    be a [N][V] array of any row stride, or the logits themselves."""
+    dev, args, (N, V, K) = _distill_args(logits, teacher_ids, teacher_logits, inv_temperature, allow, states)
+    _vector(grad_loss, "grad_loss", N, torch.float32, dev)
+    loss = _result(loss, "loss", (N,), torch.float32, dev)
+    if grad is None:
+        grad = torch.empty((N, V), dtype=logits.dtype, device=dev)
+    ld_grad = _matrix(grad, "grad", dev, logits.dtype)
+    if tuple(grad.shape) != (N, V):
+        raise ValueError(f"grad must be [{N}][{V}]")
+    workspace, nbytes = _scratch(workspace, distill_loss_workspace_bytes(N, V, K), dev)
+    st = lib.dv_distill_loss_backward(*args, _ptr(grad_loss), _ptr(loss), _ptr(grad), ld_grad, _ptr(workspace), nbytes,
+                                      _stream(stream, dev))
+    _check(st, "dv_distill_loss_backward")
+    return loss, grad
+
+
+def embed(weight, ids, scale=1.0, out=None, stream=None):
+    """Rows of weight [V][D] (bf16 or fp32) by token, scaled: out [N][D] with
+    out[n] = scale * weight[ids[n]], zeros for ids outside [0, V)."""
+    dev = weight.device
+    ld = _matrix(weight, "weight", dev)
+    dt = _code(weight.dtype)
+    V, D = weight.shape
+    N = ids.shape[0]
+    _vector(ids, "ids", N, torch.int32, dev)
+    out = _result(out, "out", (N, D), weight.dtype, dev)
+    st = lib.dv_embed(_ptr(weight), ld, dt, V, D, _ptr(ids), N, float(scale), _ptr(out), _stream(stream, dev))
+    _check(st, "dv_embed")
+    return out
+
+
+def embed_backward(grad_out, ids, num_tokens, scale=1.0, grad_weight=None, accumulate=False, workspace=None, stream=None):
+    """Gradient of ``embed`` in its table: grad_weight [num_tokens][D] with
+    the scaled rows of grad_out [N][D] summed by token, in their order;
+    ``accumulate``: added to the given grad_weight (a table that the head
+    shares)."""
+    dev = grad_out.device
+    ld = _matrix(grad_out, "grad_out", dev)
+    dt = _code(grad_out.dtype)
+    N, D = grad_out.shape
+    _vector(ids, "ids", N, torch.int32, dev)
+    if accumulate and grad_weight is None:
+        raise ValueError("accumulate adds to a given grad_weight")
+    grad_weight = _result(grad_weight, "grad_weight", (num_tokens, D), grad_out.dtype, dev)
+    workspace, nbytes = _scratch(workspace, embed_backward_workspace_bytes(N, D, num_tokens), dev)
+    st = lib.dv_embed_backward(_ptr(grad_out), ld, dt, N, D, _ptr(ids), num_tokens, float(scale), int(bool(accumulate)),
+                               _ptr(grad_weight), _ptr(workspace), nbytes, _stream(stream, dev))
+    _check(st, "dv_embed_backward")
+    return grad_weight

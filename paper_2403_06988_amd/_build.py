@@ -10,7 +10,8 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
-SOURCES = ["dv_api.hip", "dv_align.hip", "dv_step.hip", "dv_spec.hip", "dv_sample.hip"]
+SOURCES = ["dv_api.hip", "dv_align.hip", "dv_step.hip", "dv_spec.hip", "dv_sample.hip",
+           "dv_head.hip", "dv_distill.hip", "dv_embed.hip"]
 PROBE_SOURCES = ["dv_probes.hip"]
 LIB = os.path.join(HERE, "libdv.so")
 PROBE_LIB = os.path.join(HERE, "libdv_probes.so")

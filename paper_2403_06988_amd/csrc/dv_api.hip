@@ -10,6 +10,7 @@
 #include "../../include/dv.h"
 #include "dv_internal.h"
 #include "dv_sample.h"
+#include "dv_train.h"
 
 namespace {
 
@@ -466,6 +467,345 @@ dv_status dv_spec_verify(const int32_t *next_state, const uint32_t *allow, int32
                                              ld_pos, batch, token, accepted, new_state, workspace,
                                              static_cast<hipStream_t>(stream)),
                       "dv_spec_verify launch");
+}
+
+}  // extern "C"
+
+// ---------------------------------------------------------------- training
+
+namespace {
+
+constexpr int64_t kMaxRowStride = (int64_t)1 << 40;
+
+size_t element_size(int32_t dtype) { return dtype == DV_F32 ? 4 : 2; }
+
+// Bytes that `rows` rows of n elements take, ld elements apart.
+Range rows_range(const void *p, int64_t rows, int64_t n, int64_t ld, size_t elt)
+{
+    return range_of(p, p && rows ? ((size_t)(rows - 1) * (size_t)ld + (size_t)n) * elt : 0);
+}
+
+struct TrainSizes {
+    int32_t rows, num_tokens, dtype;
+};
+
+dv_status train_sizes(const char *name, TrainSizes s)
+{
+    if (s.num_tokens < 1 || s.num_tokens > DV_MAX_TOKENS)
+        return fail(DV_ERR_SHAPE, "%s: num_tokens=%d outside [1, %d]", name, s.num_tokens, DV_MAX_TOKENS);
+    if (s.rows < 0 || s.rows > DV_MAX_BATCH)
+        return fail(DV_ERR_SHAPE, "%s: rows=%d outside [0, %d]", name, s.rows, DV_MAX_BATCH);
+    if (s.dtype != DV_F32 && s.dtype != DV_BF16)
+        return fail(DV_ERR_DTYPE, "%s: unknown dtype %d", name, s.dtype);
+    return DV_OK;
+}
+
+dv_status hidden_size(const char *name, int32_t hidden)
+{
+    if (hidden < 1 || hidden > DV_MAX_HIDDEN)
+        return fail(DV_ERR_SHAPE, "%s: hidden=%d outside [1, %d]", name, hidden, DV_MAX_HIDDEN);
+    return DV_OK;
+}
+
+dv_status row_stride(const char *name, const char *what, int64_t ld, int64_t least)
+{
+    if (ld < least || ld > kMaxRowStride)
+        return fail(DV_ERR_SHAPE, "%s: %s=%lld must be at least %lld", name, what, (long long)ld, (long long)least);
+    return DV_OK;
+}
+
+dv_status aligned(const char *name, const char *what, const void *p, size_t elt)
+{
+    if (reinterpret_cast<uintptr_t>(p) % elt)
+        return fail(DV_ERR_INVALID_ARG, "%s: %s must be aligned to its element size (%zu bytes)", name, what, elt);
+    return DV_OK;
+}
+
+// The allowed tokens' arguments: all or none of them (states may be NULL with
+// no rows).
+dv_status mask_args(const char *name, const uint32_t *allow, int32_t num_states, const int32_t *states, int32_t rows)
+{
+    if ((allow && !states && rows > 0) || (!allow && states))
+        return fail(DV_ERR_INVALID_ARG, "%s: allow and states must be given together", name);
+    if (allow && (num_states < 1 || num_states > DV_MAX_STATES))
+        return fail(DV_ERR_SHAPE, "%s: num_states=%d outside [1, %d]", name, num_states, DV_MAX_STATES);
+    return DV_OK;
+}
+
+Range allow_range(const uint32_t *allow, int32_t num_states, int32_t num_tokens)
+{
+    return range_of(allow, allow ? (size_t)num_states * (((size_t)num_tokens + 31) / 32) * 4 : 0);
+}
+
+template <size_t OUT, size_t IN>
+dv_status no_overlap(const char *name, const Range (&outs)[OUT], const Range (&ins)[IN])
+{
+    for (size_t i = 0; i < OUT; ++i) {
+        for (size_t j = 0; j < i; ++j)
+            if (overlap(outs[i], outs[j]))
+                return fail(DV_ERR_ALIAS, "%s: two outputs, or an output and the workspace, overlap", name);
+        for (const Range &in : ins)
+            if (overlap(outs[i], in))
+                return fail(DV_ERR_ALIAS, "%s: an output or the workspace overlaps an input", name);
+    }
+    return DV_OK;
+}
+
+dv_status workspace_args(const char *name, const void *workspace, size_t bytes, size_t need)
+{
+    if (!workspace || bytes < need)
+        return fail(DV_ERR_WORKSPACE, "%s: workspace of %zu bytes given, %zu needed", name, bytes, need);
+    if (reinterpret_cast<uintptr_t>(workspace) & 255)
+        return fail(DV_ERR_WORKSPACE, "%s: workspace must be 256-byte aligned", name);
+    return DV_OK;
+}
+
+bool head_sizes_ok(int32_t rows, int32_t hidden, int32_t num_tokens, int32_t dtype)
+{
+    return rows >= 0 && rows <= DV_MAX_BATCH && hidden >= 1 && hidden <= DV_MAX_HIDDEN && num_tokens >= 1 &&
+           num_tokens <= DV_MAX_TOKENS && (dtype == DV_F32 || dtype == DV_BF16);
+}
+
+#define DV_CHECK(call)                \
+    do {                              \
+        const dv_status st_ = (call); \
+        if (st_ != DV_OK)             \
+            return st_;               \
+    } while (0)
+
+// The inputs that both head calls share.
+dv_status head_args(const char *name, const void *x, int64_t ld_x, const void *weight, int64_t ld_weight,
+                    int32_t dtype, int32_t rows, int32_t hidden, int32_t num_tokens, const int32_t *targets,
+                    const uint32_t *allow, int32_t num_states, const int32_t *states)
+{
+    if (!weight || (rows > 0 && (!x || !targets)))
+        return fail(DV_ERR_INVALID_ARG, "%s: weight must be non-NULL, x and targets when rows > 0", name);
+    DV_CHECK(train_sizes(name, {rows, num_tokens, dtype}));
+    DV_CHECK(hidden_size(name, hidden));
+    DV_CHECK(row_stride(name, "ld_x", ld_x, hidden));
+    DV_CHECK(row_stride(name, "ld_weight", ld_weight, hidden));
+    DV_CHECK(mask_args(name, allow, num_states, states, rows));
+    DV_CHECK(aligned(name, "x", x, element_size(dtype)));
+    return aligned(name, "weight", weight, element_size(dtype));
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t dv_head_loss_workspace_bytes(int32_t rows, int32_t hidden, int32_t num_tokens, int32_t dtype)
+{
+    return head_sizes_ok(rows, hidden, num_tokens, dtype) ? dv::head_workspace_bytes(rows, hidden, num_tokens, dtype) : 0;
+}
+
+dv_status dv_head_loss(const void *x, int64_t ld_x, const void *weight, int64_t ld_weight, int32_t dtype, int32_t rows,
+                       int32_t hidden, int32_t num_tokens, const int32_t *targets, const uint32_t *allow,
+                       int32_t num_states, const int32_t *states, float *loss, float *lse, void *workspace,
+                       size_t workspace_bytes, void *stream)
+{
+    g_error[0] = '\0';
+    const char *name = "dv_head_loss";
+    DV_CHECK(head_args(name, x, ld_x, weight, ld_weight, dtype, rows, hidden, num_tokens, targets, allow, num_states,
+                       states));
+    if (rows == 0)
+        return DV_OK;
+    if (!loss || !lse)
+        return fail(DV_ERR_INVALID_ARG, "%s: loss and lse must be non-NULL when rows > 0", name);
+    const size_t elt = element_size(dtype), need = dv::head_workspace_bytes(rows, hidden, num_tokens, dtype);
+    DV_CHECK(workspace_args(name, workspace, workspace_bytes, need));
+    const Range outs[] = {range_of(loss, (size_t)rows * 4), range_of(lse, (size_t)rows * 4), range_of(workspace, need)};
+    const Range ins[] = {rows_range(x, rows, hidden, ld_x, elt), rows_range(weight, num_tokens, hidden, ld_weight, elt),
+                         range_of(targets, (size_t)rows * 4), allow_range(allow, num_states, num_tokens),
+                         range_of(states, states ? (size_t)rows * 4 : 0)};
+    DV_CHECK(no_overlap(name, outs, ins));
+    const dv::HeadArgs a{x, ld_x, weight, ld_weight, dtype, rows, hidden, num_tokens, targets, {allow, states, num_states}};
+    return hip_status(dv::launch_head_loss(a, loss, lse, workspace, static_cast<hipStream_t>(stream)),
+                      "dv_head_loss launch");
+}
+
+size_t dv_head_loss_backward_workspace_bytes(int32_t rows, int32_t hidden, int32_t num_tokens, int32_t dtype)
+{
+    return head_sizes_ok(rows, hidden, num_tokens, dtype)
+               ? dv::head_backward_workspace_bytes(rows, hidden, num_tokens, dtype)
+               : 0;
+}
+
+dv_status dv_head_loss_backward(const void *x, int64_t ld_x, const void *weight, int64_t ld_weight, int32_t dtype,
+                                int32_t rows, int32_t hidden, int32_t num_tokens, const int32_t *targets,
+                                const uint32_t *allow, int32_t num_states, const int32_t *states, const float *lse,
+                                const float *grad_loss, void *grad_x, void *grad_weight, void *workspace,
+                                size_t workspace_bytes, void *stream)
+{
+    g_error[0] = '\0';
+    const char *name = "dv_head_loss_backward";
+    DV_CHECK(head_args(name, x, ld_x, weight, ld_weight, dtype, rows, hidden, num_tokens, targets, allow, num_states,
+                       states));
+    if (rows > 0 && (!lse || !grad_loss))
+        return fail(DV_ERR_INVALID_ARG, "%s: lse and grad_loss must be non-NULL when rows > 0", name);
+    if (!grad_weight && (rows == 0 || !grad_x))
+        return rows == 0 ? DV_OK : fail(DV_ERR_INVALID_ARG, "%s: grad_x or grad_weight must be non-NULL", name);
+    const size_t elt = element_size(dtype);
+    DV_CHECK(aligned(name, "grad_x", grad_x, elt));
+    DV_CHECK(aligned(name, "grad_weight", grad_weight, elt));
+    const size_t need = dv::head_backward_workspace_bytes(rows, hidden, num_tokens, dtype);
+    DV_CHECK(workspace_args(name, workspace, workspace_bytes, need));
+    const Range outs[] = {rows_range(grad_x, rows, hidden, hidden, elt),
+                          rows_range(grad_weight, num_tokens, hidden, hidden, elt), range_of(workspace, need)};
+    const Range ins[] = {rows_range(x, rows, hidden, ld_x, elt), rows_range(weight, num_tokens, hidden, ld_weight, elt),
+                         range_of(targets, (size_t)rows * 4), allow_range(allow, num_states, num_tokens),
+                         range_of(states, states ? (size_t)rows * 4 : 0), range_of(lse, (size_t)rows * 4),
+                         range_of(grad_loss, (size_t)rows * 4)};
+    DV_CHECK(no_overlap(name, outs, ins));
+    const dv::HeadArgs a{x, ld_x, weight, ld_weight, dtype, rows, hidden, num_tokens, targets, {allow, states, num_states}};
+    return hip_status(dv::launch_head_loss_backward(a, lse, grad_loss, grad_x, grad_weight, workspace,
+                                                    static_cast<hipStream_t>(stream)),
+                      "dv_head_loss_backward launch");
+}
+
+size_t dv_distill_loss_workspace_bytes(int32_t rows, int32_t num_tokens, int32_t num_top)
+{
+    if (rows < 0 || rows > DV_MAX_BATCH || num_tokens < 1 || num_tokens > DV_MAX_TOKENS || num_top < 1 ||
+        num_top > DV_MAX_TOP)
+        return 0;
+    return dv::distill_workspace_bytes(rows, num_tokens, num_top);
+}
+
+namespace {
+
+// Both distillation calls; `grad_wanted`: the backward one.
+dv_status distill_common(const char *name, bool grad_wanted, const void *logits, int64_t ld_logits, int32_t dtype,
+                         int32_t rows, int32_t num_tokens, const int32_t *teacher_ids, const float *teacher_logits,
+                         int32_t num_top, float inv_temperature, const uint32_t *allow, int32_t num_states,
+                         const int32_t *states, const float *grad_loss, float *loss, void *grad, int64_t ld_grad,
+                         void *workspace, size_t workspace_bytes, void *stream)
+{
+    g_error[0] = '\0';
+    if (rows > 0 && (!logits || !teacher_ids || !teacher_logits))
+        return fail(DV_ERR_INVALID_ARG, "%s: logits, teacher_ids and teacher_logits must be non-NULL when rows > 0", name);
+    DV_CHECK(train_sizes(name, {rows, num_tokens, dtype}));
+    if (num_top < 1 || num_top > DV_MAX_TOP)
+        return fail(DV_ERR_SHAPE, "%s: num_top=%d outside [1, %d]", name, num_top, DV_MAX_TOP);
+    if (!(inv_temperature > 0.0f && inv_temperature <= 3.0e38f))
+        return fail(DV_ERR_SHAPE, "%s: inv_temperature=%g must be finite and > 0", name, (double)inv_temperature);
+    DV_CHECK(row_stride(name, "ld_logits", ld_logits, num_tokens));
+    if (grad_wanted)
+        DV_CHECK(row_stride(name, "ld_grad", ld_grad, num_tokens));
+    DV_CHECK(mask_args(name, allow, num_states, states, rows));
+    const size_t elt = element_size(dtype);
+    DV_CHECK(aligned(name, "logits", logits, elt));
+    if (rows == 0)
+        return DV_OK;
+    if (grad_wanted ? !grad || !grad_loss : !loss)
+        return fail(DV_ERR_INVALID_ARG, "%s: %s must be non-NULL when rows > 0", name,
+                    grad_wanted ? "grad and grad_loss" : "loss");
+    DV_CHECK(aligned(name, "grad", grad, elt));
+    const size_t need = dv::distill_workspace_bytes(rows, num_tokens, num_top);
+    DV_CHECK(workspace_args(name, workspace, workspace_bytes, need));
+    const size_t entries = (size_t)rows * (size_t)num_top * 4;
+    const Range r_logits = rows_range(logits, rows, num_tokens, ld_logits, elt);
+    const bool in_place = grad == logits && ld_grad == ld_logits;
+    const Range outs[] = {range_of(loss, loss ? (size_t)rows * 4 : 0), rows_range(grad, rows, num_tokens, ld_grad, elt),
+                          range_of(workspace, need)};
+    const Range ins[] = {in_place ? range_of(nullptr, 0) : r_logits, range_of(teacher_ids, entries),
+                         range_of(teacher_logits, entries), allow_range(allow, num_states, num_tokens),
+                         range_of(states, states ? (size_t)rows * 4 : 0),
+                         range_of(grad_loss, grad_loss ? (size_t)rows * 4 : 0)};
+    DV_CHECK(no_overlap(name, outs, ins));
+    const dv::DistillArgs a{logits,         ld_logits, dtype,           rows, num_tokens, teacher_ids,
+                            teacher_logits, num_top,   inv_temperature, {allow, states, num_states}};
+    return hip_status(dv::launch_distill(a, grad_loss, loss, grad, ld_grad, workspace, static_cast<hipStream_t>(stream)),
+                      name);
+}
+
+}  // namespace
+
+dv_status dv_distill_loss(const void *logits, int64_t ld_logits, int32_t dtype, int32_t rows, int32_t num_tokens,
+                          const int32_t *teacher_ids, const float *teacher_logits, int32_t num_top,
+                          float inv_temperature, const uint32_t *allow, int32_t num_states, const int32_t *states,
+                          float *loss, void *workspace, size_t workspace_bytes, void *stream)
+{
+    return distill_common("dv_distill_loss", false, logits, ld_logits, dtype, rows, num_tokens, teacher_ids,
+                          teacher_logits, num_top, inv_temperature, allow, num_states, states, nullptr, loss, nullptr,
+                          0, workspace, workspace_bytes, stream);
+}
+
+dv_status dv_distill_loss_backward(const void *logits, int64_t ld_logits, int32_t dtype, int32_t rows,
+                                   int32_t num_tokens, const int32_t *teacher_ids, const float *teacher_logits,
+                                   int32_t num_top, float inv_temperature, const uint32_t *allow, int32_t num_states,
+                                   const int32_t *states, const float *grad_loss, float *loss, void *grad,
+                                   int64_t ld_grad, void *workspace, size_t workspace_bytes, void *stream)
+{
+    return distill_common("dv_distill_loss_backward", true, logits, ld_logits, dtype, rows, num_tokens, teacher_ids,
+                          teacher_logits, num_top, inv_temperature, allow, num_states, states, grad_loss, loss, grad,
+                          ld_grad, workspace, workspace_bytes, stream);
+}
+
+namespace {
+
+dv_status embed_args(const char *name, int32_t dtype, int32_t num_tokens, int32_t hidden, int32_t rows, float scale,
+                     const char *stride_name, int64_t ld)
+{
+    DV_CHECK(train_sizes(name, {rows, num_tokens, dtype}));
+    DV_CHECK(hidden_size(name, hidden));
+    DV_CHECK(row_stride(name, stride_name, ld, hidden));
+    if (!(scale >= -3.0e38f && scale <= 3.0e38f))
+        return fail(DV_ERR_SHAPE, "%s: scale=%g must be finite", name, (double)scale);
+    return DV_OK;
+}
+
+}  // namespace
+
+dv_status dv_embed(const void *weight, int64_t ld_weight, int32_t dtype, int32_t num_tokens, int32_t hidden,
+                   const int32_t *ids, int32_t rows, float scale, void *out, void *stream)
+{
+    g_error[0] = '\0';
+    const char *name = "dv_embed";
+    if (!weight || (rows > 0 && (!ids || !out)))
+        return fail(DV_ERR_INVALID_ARG, "%s: weight must be non-NULL, ids and out when rows > 0", name);
+    DV_CHECK(embed_args(name, dtype, num_tokens, hidden, rows, scale, "ld_weight", ld_weight));
+    const size_t elt = element_size(dtype);
+    DV_CHECK(aligned(name, "weight", weight, elt));
+    DV_CHECK(aligned(name, "out", out, elt));
+    if (rows == 0)
+        return DV_OK;
+    const Range outs[] = {rows_range(out, rows, hidden, hidden, elt)};
+    const Range ins[] = {rows_range(weight, num_tokens, hidden, ld_weight, elt), range_of(ids, (size_t)rows * 4)};
+    DV_CHECK(no_overlap(name, outs, ins));
+    return hip_status(dv::launch_embed(weight, ld_weight, dtype, num_tokens, hidden, ids, rows, scale, out,
+                                       static_cast<hipStream_t>(stream)),
+                      "dv_embed launch");
+}
+
+size_t dv_embed_backward_workspace_bytes(int32_t rows, int32_t hidden, int32_t num_tokens)
+{
+    if (!head_sizes_ok(rows, hidden, num_tokens, DV_F32))
+        return 0;
+    return dv::embed_backward_workspace_bytes(rows, hidden, num_tokens);
+}
+
+dv_status dv_embed_backward(const void *grad_out, int64_t ld_grad_out, int32_t dtype, int32_t rows, int32_t hidden,
+                            const int32_t *ids, int32_t num_tokens, float scale, int32_t accumulate, void *grad_weight,
+                            void *workspace, size_t workspace_bytes, void *stream)
+{
+    g_error[0] = '\0';
+    const char *name = "dv_embed_backward";
+    if (!grad_weight || (rows > 0 && (!grad_out || !ids)))
+        return fail(DV_ERR_INVALID_ARG, "%s: grad_weight must be non-NULL, grad_out and ids when rows > 0", name);
+    DV_CHECK(embed_args(name, dtype, num_tokens, hidden, rows, scale, "ld_grad_out", ld_grad_out));
+    const size_t elt = element_size(dtype);
+    DV_CHECK(aligned(name, "grad_out", grad_out, elt));
+    DV_CHECK(aligned(name, "grad_weight", grad_weight, elt));
+    const size_t need = dv::embed_backward_workspace_bytes(rows, hidden, num_tokens);
+    DV_CHECK(workspace_args(name, workspace, workspace_bytes, need));
+    const Range outs[] = {rows_range(grad_weight, num_tokens, hidden, hidden, elt), range_of(workspace, need)};
+    const Range ins[] = {rows_range(grad_out, rows, hidden, ld_grad_out, elt), range_of(ids, (size_t)rows * 4)};
+    DV_CHECK(no_overlap(name, outs, ins));
+    if (rows == 0 && accumulate)
+        return DV_OK;
+    return hip_status(dv::launch_embed_backward(grad_out, ld_grad_out, dtype, rows, hidden, ids, num_tokens, scale,
+                                                accumulate != 0, grad_weight, workspace,
+                                                static_cast<hipStream_t>(stream)),
+                      "dv_embed_backward launch");
 }
 
 }  // extern "C"

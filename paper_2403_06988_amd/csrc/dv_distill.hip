@@ -1,0 +1,394 @@
+// Distillation from a teacher's top logits over the allowed tokens.
+//
+// Per row, with the allowed tokens A of the row's state, c = 1/T, and the
+// listed teacher entries L = {k : id_k in A, top_k > -inf}:
+//     q_k = exp(c (top_k - max)) / sum over L,   p_v = exp(c (z_v - m)) / s,
+//     loss = sum_L q_k (ln q_k - ln p_{id_k}),
+//     dloss/dz_v = c (p_v - sum of q_k with id_k = v)   on A, 0 elsewhere.
+//
+// The loss needs one read of the row, loss and gradient one read and one
+// write of it: both are bound by memory.  The gradient kernel keeps the row in no
+// wider place than the caches between its two passes: a row is 0.25 to 1 MB.
+#include "dv_train.h"
+
+namespace dv {
+namespace {
+
+constexpr int kThreads = 512;
+constexpr int kWaves = kThreads / kWave;
+constexpr int kMaxTop = 1024;
+
+template <typename T>
+struct Vec;
+template <>
+struct Vec<float> {
+    static constexpr int kN = 4;
+    float x[4];
+    static __device__ __forceinline__ Vec load(const float *p)
+    {
+        Vec v;
+        __builtin_memcpy(v.x, p, 16);
+        return v;
+    }
+    __device__ __forceinline__ float get(int i) const { return x[i]; }
+    static __device__ __forceinline__ void store(float *p, const float (&y)[4]) { __builtin_memcpy(p, y, 16); }
+    static __device__ __forceinline__ float one(const float *p) { return *p; }
+    static __device__ __forceinline__ void put(float *p, float y) { *p = y; }
+};
+template <>
+struct Vec<uint16_t> {
+    static constexpr int kN = 8;
+    uint32_t x[4];
+    static __device__ __forceinline__ Vec load(const uint16_t *p)
+    {
+        Vec v;
+        __builtin_memcpy(v.x, p, 16);
+        return v;
+    }
+    __device__ __forceinline__ float get(int i) const
+    {
+        return __uint_as_float(i & 1 ? x[i >> 1] & 0xFFFF0000u : x[i >> 1] << 16);
+    }
+    static __device__ __forceinline__ void store(uint16_t *p, const float (&y)[8])
+    {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            w[i] = (uint32_t)narrow(y[2 * i]) | (uint32_t)narrow(y[2 * i + 1]) << 16;
+        __builtin_memcpy(p, w, 16);
+    }
+    static __device__ __forceinline__ float one(const uint16_t *p) { return widen(*p); }
+    static __device__ __forceinline__ void put(uint16_t *p, float y) { *p = narrow(y); }
+};
+
+// The mask bits of vector j of a row (kN tokens from kN j on).
+template <int N>
+__device__ __forceinline__ uint32_t vector_bits(const RowMask &m, int j)
+{
+    if (!m.words)
+        return (1u << N) - 1u;
+    const uint8_t *bytes = reinterpret_cast<const uint8_t *>(m.words);
+    return N == 8 ? bytes[j] : (uint32_t)bytes[j >> 1] >> ((j & 1) * 4);
+}
+
+struct Shared {
+    float wave_a[kWaves], wave_b[kWaves];
+    int id[kMaxTop];
+    float q[kMaxTop];
+    float z[kMaxTop];
+};
+
+__device__ __forceinline__ float block_sum(float v, Shared &sh)
+{
+    v = wave_sum(v);
+    __syncthreads();
+    if ((threadIdx.x & (kWave - 1)) == 0)
+        sh.wave_a[threadIdx.x / kWave] = v;
+    __syncthreads();
+    float t = 0.f;
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i)
+        t += sh.wave_a[i];
+    return t;
+}
+
+__device__ __forceinline__ Softmax block_join(Softmax v, float c2, Shared &sh)
+{
+#pragma unroll
+    for (int d = 32; d; d >>= 1)
+        v = softmax_join(v, {__shfl_xor(v.max, d), __shfl_xor(v.sum, d)}, c2);
+    __syncthreads();
+    if ((threadIdx.x & (kWave - 1)) == 0) {
+        sh.wave_a[threadIdx.x / kWave] = v.max;
+        sh.wave_b[threadIdx.x / kWave] = v.sum;
+    }
+    __syncthreads();
+    Softmax t{sh.wave_a[0], sh.wave_b[0]};
+#pragma unroll
+    for (int i = 1; i < kWaves; ++i)
+        t = softmax_join(t, {sh.wave_a[i], sh.wave_b[i]}, c2);
+    return t;
+}
+
+// The teacher's entries of a row: ids (-1 where an entry takes no part) and
+// probabilities in LDS; returns the maximum and the sum of exp(c (top - max)).
+__device__ __forceinline__ Softmax teacher(const DistillArgs &a, const RowMask &m, int row, float c2, Shared &sh)
+{
+    Softmax own{-INFINITY, 0.f};
+    for (int k = threadIdx.x; k < a.K; k += kThreads) {
+        const int id = a.ids[(size_t)row * a.K + k];
+        const float t = a.top[(size_t)row * a.K + k];
+        const bool in = m.has(id) && t != -INFINITY;
+        sh.id[k] = in ? id : -1;
+        sh.q[k] = t;
+        if (in)
+            own = softmax_join(own, {t, 1.f}, c2);
+    }
+    const Softmax all = block_join(own, c2, sh);
+    for (int k = threadIdx.x; k < a.K; k += kThreads)
+        sh.q[k] = sh.id[k] < 0 ? 0.f : softmax_term(sh.q[k], all.max, c2) / all.sum;
+    return all;
+}
+
+// The softmax state of tokens [from, to) of a row (from a multiple of 8).
+template <typename T>
+__device__ __forceinline__ Softmax row_stats(const T *z, const RowMask &m, int from, int to, float c2)
+{
+    using V = Vec<T>;
+    constexpr int N = V::kN;
+    constexpr int U = 4;  // vectors on the way per lane
+    Softmax own{-INFINITY, 0.f};
+    const int j0 = from / N, j1 = to / N;
+    for (int j = j0 + threadIdx.x; j < j1; j += kThreads * U) {
+        V v[U];
+        uint32_t bits[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int ju = j + u * kThreads;
+            const bool in = ju < j1;
+            v[u] = V::load(z + (size_t)(in ? ju : j) * N);
+            bits[u] = in ? vector_bits<N>(m, ju) : 0u;
+        }
+        float top = own.max;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                top = fmaxf(top, bits[u] >> i & 1u ? v[u].get(i) : -INFINITY);
+        if (top == -INFINITY) {  // nothing so far, unless NaN
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int i = 0; i < N; ++i)
+                    own.sum = (bits[u] >> i & 1u) && v[u].get(i) != v[u].get(i) ? v[u].get(i) : own.sum;
+            continue;
+        }
+        float sum = own.max == -INFINITY ? own.sum : own.sum * softmax_term(own.max, top, c2);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                sum += bits[u] >> i & 1u ? softmax_term(v[u].get(i), top, c2) : 0.f;
+        own = {top, sum};
+    }
+    for (int i = j1 * N + threadIdx.x; i < to; i += kThreads)
+        if (m.has(i)) {
+            const float x = V::one(z + i);
+            own = x == -INFINITY ? own : softmax_join(own, {x, 1.f}, c2);
+        }
+    return own;
+}
+
+// The row's part of the loss: needs sh.id, sh.q and sh.z.
+__device__ __forceinline__ float row_loss(const DistillArgs &a, int row, Softmax t, Softmax s, Shared &sh)
+{
+    const float c = a.inv_temperature;
+    const float lnt = logf(t.sum), lns = logf(s.sum);
+    float sum = 0.f;
+    for (int k = threadIdx.x; k < a.K; k += kThreads) {
+        const float q = sh.q[k];
+        if (!(q == 0.f))  // NaN counts
+            sum += q * (((a.top[(size_t)row * a.K + k] - t.max) * c - lnt) - ((sh.z[k] - s.max) * c - lns));
+    }
+    return block_sum(sum, sh);
+}
+
+// Writes the gradient of tokens [from, to): w (p - q).  `part` false: zeros.
+template <typename T>
+__device__ __forceinline__ void row_grad(const T *z, T *grad, const RowMask &m, int from, int to, float c2, Softmax s,
+                                         float w, bool part, int K, Shared &sh)
+{
+    using V = Vec<T>;
+    constexpr int N = V::kN;
+    constexpr int U = 4;
+    const int j0 = from / N, j1 = to / N;
+    const float scale = part ? w / s.sum : 0.f;
+    for (int j = j0 + threadIdx.x; j < j1; j += kThreads * U) {
+        V v[U];
+        uint32_t bits[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int ju = j + u * kThreads;
+            const bool in = ju < j1;
+            v[u] = V::load(z + (size_t)(in ? ju : j) * N);
+            bits[u] = in && part ? vector_bits<N>(m, ju) : 0u;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            float y[N];
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                y[i] = bits[u] >> i & 1u ? softmax_term(v[u].get(i), s.max, c2) * scale : 0.f;
+            const int ju = j + u * kThreads;
+            if (ju < j1)
+                V::store(grad + (size_t)ju * N, y);
+        }
+    }
+    for (int i = j1 * N + threadIdx.x; i < to; i += kThreads)
+        V::put(grad + i, part && m.has(i) ? softmax_term(V::one(z + i), s.max, c2) * scale : 0.f);
+    if (!part)
+        return;
+    // the listed tokens, once the block's stores above are done: an id listed
+    // more than once takes the sum of its entries, in their order, from each
+    __syncthreads();
+    for (int k = threadIdx.x; k < K; k += kThreads) {
+        const int id = sh.id[k];
+        if (id < from || id >= to)
+            continue;
+        float q = 0.f;
+        for (int i = 0; i < K; ++i)
+            q += sh.id[i] == id ? sh.q[i] : 0.f;
+        V::put(grad + id, softmax_term(sh.z[k], s.max, c2) * scale - w * q);
+    }
+}
+
+// One block per row: the row's softmax, the loss, and with GRAD the gradient
+// from a second pass over the row, which its first pass left in the caches.
+template <typename T, bool GRAD>
+__global__ __launch_bounds__(kThreads) void distill_row_kernel(DistillArgs a, const float *grad_loss, float *loss,
+                                                                T *grad, int64_t ld_grad)
+{
+    __shared__ Shared sh;
+    const int row = blockIdx.x;
+    const float c2 = a.inv_temperature * kLog2e;
+    const RowMask m(a.masks, a.V, row);
+    const T *z = static_cast<const T *>(a.logits) + (size_t)row * a.ld;
+    const Softmax t = teacher(a, m, row, c2, sh);
+    for (int k = threadIdx.x; k < a.K; k += kThreads)
+        sh.z[k] = sh.id[k] < 0 ? 0.f : Vec<T>::one(z + sh.id[k]);
+    Softmax s{-INFINITY, 0.f};
+    bool part = !t.empty();
+    if (part)
+        s = block_join(row_stats(z, m, 0, a.V, c2), c2, sh);
+    part = part && !s.empty();
+    if (loss) {
+        const float l = part ? row_loss(a, row, t, s, sh) : 0.f;
+        if (threadIdx.x == 0)
+            loss[row] = l;
+    }
+    if (GRAD)
+        row_grad(z, grad + (size_t)row * ld_grad, m, 0, a.V, c2, s, part ? grad_loss[row] * a.inv_temperature : 0.f,
+                 part, a.K, sh);
+}
+
+// Rows split over blocks (few rows): the chunks' softmax states, and the
+// logits of the listed tokens (the gradient may overwrite the logits) ...
+template <typename T>
+__global__ __launch_bounds__(kThreads) void distill_stats_kernel(DistillArgs a, int chunk, Softmax *part, float *listed)
+{
+    __shared__ Shared sh;
+    const int row = blockIdx.y, c = blockIdx.x;
+    const float c2 = a.inv_temperature * kLog2e;
+    const RowMask m(a.masks, a.V, row);
+    const T *z = static_cast<const T *>(a.logits) + (size_t)row * a.ld;
+    const int from = c * chunk, to = a.V - from < chunk ? a.V : from + chunk;
+    if (c == 0)
+        for (int k = threadIdx.x; k < a.K; k += kThreads) {
+            const int id = a.ids[(size_t)row * a.K + k];
+            listed[(size_t)row * a.K + k] = m.has(id) ? Vec<T>::one(z + id) : 0.f;
+        }
+    Softmax s{-INFINITY, 0.f};
+    if (!m.dead)
+        s = block_join(row_stats(z, m, from, to, c2), c2, sh);
+    if (threadIdx.x == 0)
+        part[(size_t)row * gridDim.x + c] = s;
+}
+
+// ... and then the loss (chunk 0's block) and each chunk's gradient.
+template <typename T, bool GRAD>
+__global__ __launch_bounds__(kThreads) void distill_finish_kernel(DistillArgs a, int chunk, int chunks,
+                                                                   const Softmax *parts, const float *listed,
+                                                                   const float *grad_loss, float *loss, T *grad,
+                                                                   int64_t ld_grad)
+{
+    __shared__ Shared sh;
+    const int row = blockIdx.y, c = blockIdx.x;
+    const float c2 = a.inv_temperature * kLog2e;
+    const RowMask m(a.masks, a.V, row);
+    const Softmax t = teacher(a, m, row, c2, sh);
+    for (int k = threadIdx.x; k < a.K; k += kThreads)
+        sh.z[k] = listed[(size_t)row * a.K + k];
+    Softmax s{-INFINITY, 0.f};
+    for (int i = threadIdx.x; i < chunks; i += kThreads)
+        s = softmax_join(s, parts[(size_t)row * chunks + i], c2);
+    s = block_join(s, c2, sh);
+    const bool part = !t.empty() && !s.empty();
+    if (loss && c == 0) {
+        const float l = part ? row_loss(a, row, t, s, sh) : 0.f;
+        if (threadIdx.x == 0)
+            loss[row] = l;
+    }
+    if (GRAD) {
+        const int from = c * chunk, to = a.V - from < chunk ? a.V : from + chunk;
+        const T *z = static_cast<const T *>(a.logits) + (size_t)row * a.ld;
+        row_grad(z, grad + (size_t)row * ld_grad, m, from, to, c2, s, part ? grad_loss[row] * a.inv_temperature : 0.f,
+                 part, a.K, sh);
+    }
+}
+
+struct Split {
+    int chunk, chunks;  // tokens of a chunk (a multiple of 8), chunks of a row
+};
+
+// Rows are split until the launch has two blocks a compute unit, each with at
+// least one pass of its lanes' vectors.
+constexpr int kSplitBlocks = 512;
+constexpr int kWholeRows = 256;
+
+Split split_of(int rows, int V, int dtype)
+{
+    const int pass = kThreads * (dtype == 1 ? 8 : 4);
+    int want = rows >= kWholeRows || rows < 1 ? 1 : kSplitBlocks / rows;
+    const int most = V / pass > 1 ? V / pass : 1;
+    want = want < most ? want : most;
+    int chunk = (int)align_up((size_t)(V + want - 1) / want, 8);
+    return {chunk, (V + chunk - 1) / chunk};
+}
+
+template <typename T>
+hipError_t launch(const DistillArgs &a, const float *grad_loss, float *loss, T *grad, int64_t ld_grad, void *workspace,
+                  hipStream_t stream)
+{
+    const Split s = split_of(a.rows, a.V, a.dtype);
+    if (s.chunks == 1) {
+        if (grad)
+            distill_row_kernel<T, true><<<a.rows, kThreads, 0, stream>>>(a, grad_loss, loss, grad, ld_grad);
+        else
+            distill_row_kernel<T, false><<<a.rows, kThreads, 0, stream>>>(a, nullptr, loss, nullptr, 0);
+        return last_launch();
+    }
+    Softmax *parts = static_cast<Softmax *>(workspace);
+    float *listed = reinterpret_cast<float *>(parts + (size_t)a.rows * s.chunks);
+    const dim3 grid(s.chunks, a.rows);
+    distill_stats_kernel<T><<<grid, kThreads, 0, stream>>>(a, s.chunk, parts, listed);
+    hipError_t e = last_launch();
+    if (e != hipSuccess)
+        return e;
+    if (grad)
+        distill_finish_kernel<T, true><<<grid, kThreads, 0, stream>>>(a, s.chunk, s.chunks, parts, listed, grad_loss,
+                                                                      loss, grad, ld_grad);
+    else
+        distill_finish_kernel<T, false><<<dim3(1, a.rows), kThreads, 0, stream>>>(a, s.chunk, s.chunks, parts, listed,
+                                                                                  nullptr, loss, nullptr, 0);
+    return last_launch();
+}
+
+}  // namespace
+
+// At most 512 chunks in all, of rows that are split (fewer than kWholeRows).
+size_t distill_workspace_bytes(int rows, int V, int K)
+{
+    (void)V;
+    const int split = rows < kWholeRows ? rows : kWholeRows - 1;
+    return align_up((size_t)kSplitBlocks * sizeof(Softmax) + (size_t)split * (size_t)K * 4, 256);
+}
+
+hipError_t launch_distill(const DistillArgs &a, const float *grad_loss, float *loss, void *grad, int64_t ld_grad,
+                          void *workspace, hipStream_t stream)
+{
+    if (a.dtype == 1)
+        return launch(a, grad_loss, loss, static_cast<uint16_t *>(grad), ld_grad, workspace, stream);
+    return launch(a, grad_loss, loss, static_cast<float *>(grad), ld_grad, workspace, stream);
+}
+
+}  // namespace dv

@@ -1,0 +1,618 @@
+// Head loss: softmax cross entropy over the allowed tokens, from hidden
+// states x [N][D] and head weights w [V][D], in pieces of the vocabulary.
+//
+//     z_nv = <x_n, w_v>,  lse_n = ln sum over allowed v of exp(z_nv),
+//     loss_n = lse_n - z_nt                (t the target; 0 where it is not allowed)
+//     G_nv = g_n (exp(z_nv - lse_n) - [v = t]) over allowed v, 0 elsewhere
+//     dx = G w,  dw = G^T x.
+//
+// The logits (4 N V bytes) never reach memory.  Forward: a tile of logits stays
+// in the registers of the product that made it and leaves as each row's
+// maximum and sum of exponentials over the tile; a second kernel joins the
+// tiles.  Backward: a piece of the vocabulary at a time, the same product again,
+// its tiles leaving as G in bf16, and from the piece's G the two other products.
+// Four products of 2 N D V operations against six N D V that cannot be avoided:
+// the price of not keeping the logits.
+//
+// All products are the one of dv_gemm.h (k contiguous in both operands), so x,
+// w's piece and G are also laid out transposed.  fp32 operands go through it
+// as three bf16 planes each.
+#include <type_traits>
+
+#include "dv_gemm.h"
+#include "dv_train.h"
+
+namespace dv {
+namespace {
+
+// ------------------------------------------------------------- preparation
+
+// x as a sum of P bf16 numbers, each the rest rounded to nearest (three hold
+// all 24 bits of an fp32 significand: the sum is exact).  What is infinite or
+// NaN stays in the first; a first part that would round up to infinity is
+// cut instead.
+template <int P>
+__device__ __forceinline__ void split_planes(float x, __bf16 (&out)[P])
+{
+    out[0] = (__bf16)x;
+    if constexpr (P > 1) {
+        const bool finite = fabsf(x) <= 3.4028235e38f;
+        if (finite && fabsf((float)out[0]) > 3.4028235e38f)
+            out[0] = (__bf16)__uint_as_float(__float_as_uint(x) & 0xFFFF0000u);
+        float left = finite ? x - (float)out[0] : 0.f;
+#pragma unroll
+        for (int p = 1; p < P; ++p) {
+            out[p] = (__bf16)left;
+            left -= (float)out[p];
+        }
+    }
+}
+
+// src [rows][cols] (row stride ld) to bf16 planes [P][rows][out_cols], zeros past cols.
+template <typename T, int P>
+__global__ void pack_kernel(const T *src, int64_t ld, int rows, int cols, int out_cols, __bf16 *dst, int64_t plane)
+{
+    const int64_t row = blockIdx.y + (int64_t)blockIdx.z * 65535;
+    const int col = (blockIdx.x * blockDim.x + threadIdx.x) * 2;
+    if (row >= rows || col >= out_cols)
+        return;
+    __bf16 a[P], b[P];
+    float x = 0.f, y = 0.f;
+    if constexpr (sizeof(T) == 4) {
+        x = col < cols ? src[row * ld + col] : 0.f;
+        y = col + 1 < cols ? src[row * ld + col + 1] : 0.f;
+    } else {
+        x = col < cols ? widen(src[row * ld + col]) : 0.f;
+        y = col + 1 < cols ? widen(src[row * ld + col + 1]) : 0.f;
+    }
+    split_planes<P>(x, a);
+    split_planes<P>(y, b);
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+        __bf16 both[2] = {a[p], b[p]};
+        __builtin_memcpy(dst + p * plane + row * out_cols + col, both, 4);
+    }
+}
+
+// bf16 src [rows][cols] (row stride ld, of plane z) to dst [cols][out_rows], zeros past rows.
+__global__ __launch_bounds__(256) void transpose_kernel(const uint16_t *src, int64_t ld, int64_t src_plane, int rows, int cols,
+                                                         uint16_t *dst, int out_rows, int64_t dst_plane)
+{
+    __shared__ uint16_t tile[64][66];
+    src += blockIdx.z * src_plane;
+    dst += blockIdx.z * dst_plane;
+    const int r0 = blockIdx.x * 64, c0 = blockIdx.y * 64;
+    const int tx = threadIdx.x & 63, ty = threadIdx.x >> 6;
+#pragma unroll
+    for (int i = 0; i < 64; i += 4) {
+        const int r = r0 + i + ty, c = c0 + tx;
+        tile[i + ty][tx] = r < rows && c < cols ? src[(int64_t)r * ld + c] : (uint16_t)0;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 64; i += 4) {
+        const int c = c0 + i + ty, r = r0 + tx;
+        if (c < cols && r < out_rows)
+            dst[(int64_t)c * out_rows + r] = tile[tx][i + ty];
+    }
+}
+
+// --------------------------------------------------------------- the logits
+
+// Per row and tile: maximum and sum of exponentials of the allowed logits;
+// the target's logit.  i runs over the piece's tokens, j over rows.
+template <int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(WM *WN *kWave, 2) void stats_kernel(GemmShape g, int v0, int V, int rows, Masks masks,
+                                                                 const int32_t *targets, Softmax *parts,
+                                                                 float *target_logit, int tiles_i, int tiles_j)
+{
+    using G = Gemm<BM, BN, WM, WN>;
+    __shared__ __attribute__((aligned(1024))) char lds[G::kLdsBytes];
+    int ti, tj;
+    tile_of_block(blockIdx.x, tiles_i, tiles_j, ti, tj);
+    f32x4 acc[G::kTm][G::kTn] = {};
+    G::run(acc, g, ti * BM, tj * BN, 0, g.k / kGemmStageK * g.segments, lds);
+
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+    const int wm = wave / WN, wn = wave % WN;
+    const int vw = v0 + ti * BM + wm * (BM / WM);  // the wave's first token
+    const int quarter = lane >> 4;
+    constexpr int kWords = BM / WM / 32;
+#pragma unroll
+    for (int b = 0; b < G::kTn; ++b) {
+        const int n = tj * BN + wn * (BN / WN) + b * 16 + (lane & 15);
+        const bool live = n < rows;
+        const RowMask m(masks, V, live ? n : 0);
+        uint32_t word[kWords];
+#pragma unroll
+        for (int i = 0; i < kWords; ++i)
+            word[i] = m.word((vw >> 5) + i) >> (quarter * 4);
+        float top = -INFINITY;
+#pragma unroll
+        for (int a = 0; a < G::kTm; ++a)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const bool in = word[a >> 1] >> ((a & 1) * 16 + e) & 1u;
+                const float z = in ? acc[a][b][e] : -INFINITY;
+                top = fmaxf(top, z);
+            }
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float base = top == -INFINITY ? 0.f : top;
+        float sum = 0.f;
+#pragma unroll
+        for (int a = 0; a < G::kTm; ++a)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const bool in = word[a >> 1] >> ((a & 1) * 16 + e) & 1u;
+                sum += in ? softmax_term(acc[a][b][e], base, kLog2e) : 0.f;
+            }
+        sum += __shfl_xor(sum, 16);
+        sum += __shfl_xor(sum, 32);
+        const int t = live ? targets[n] - vw : -1;
+        if (live && quarter == 0)
+            parts[(size_t)(vw / (BM / WM)) * rows + n] = {top, sum};
+        const bool here = (uint32_t)t < (uint32_t)(BM / WM) && ((t >> 2) & 3) == quarter;
+        if (__ballot(here)) {
+            float z = 0.f;
+#pragma unroll
+            for (int a = 0; a < G::kTm; ++a)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    z = t == a * 16 + quarter * 4 + e ? acc[a][b][e] : z;
+            if (here)
+                target_logit[n] = z;
+        }
+    }
+}
+
+// Joins the tiles of each row: blocks of 256 threads take 256 / slices rows.
+__global__ __launch_bounds__(256) void finish_kernel(const Softmax *parts, int nparts, int rows, int V, Masks masks,
+                                                      const int32_t *targets, const float *target_logit, float *loss,
+                                                      float *lse, int slices)
+{
+    __shared__ Softmax sh[256];
+    const int per_block = 256 / slices;
+    const int slice = threadIdx.x / per_block;
+    const int n = blockIdx.x * per_block + threadIdx.x % per_block;
+    Softmax s{-INFINITY, 0.f};
+    if (n < rows) {
+#pragma unroll 4
+        for (int p = slice; p < nparts; p += slices)
+            s = softmax_join(s, parts[(size_t)p * rows + n], kLog2e);
+    }
+    sh[threadIdx.x] = s;
+    __syncthreads();
+    if (slice || n >= rows)
+        return;
+    for (int i = 1; i < slices; ++i)
+        s = softmax_join(s, sh[i * per_block + threadIdx.x], kLog2e);
+    const int t = targets[n];
+    const RowMask m(masks, V, n);
+    const float lns = s.empty() ? 0.f : logf(s.sum);
+    lse[n] = s.empty() ? -INFINITY : s.max + lns;
+    loss[n] = m.has(t) ? (s.max - target_logit[n]) + lns : 0.f;
+}
+
+// The weight of each row's gradient: grad_loss where the target is allowed, else 0.
+__global__ void weights_kernel(int rows, int V, Masks masks, const int32_t *targets, const float *grad_loss, float *weight)
+{
+    const int n = blockIdx.x * blockDim.x + threadIdx.x;
+    if (n < rows)
+        weight[n] = RowMask(masks, V, n).has(targets[n]) ? grad_loss[n] : 0.f;
+}
+
+// A piece of G in bf16 (P planes of it for fp32 operands): [rows][ld] with
+// the piece's tokens along a row, zeros up to the next multiple of 64 both ways.
+template <int BM, int BN, int WM, int WN, int P>
+__global__ __launch_bounds__(WM *WN *kWave, 2) void grad_kernel(GemmShape g, int v0, int V, int rows, Masks masks,
+                                                                const int32_t *targets, const float *lse,
+                                                                const float *weight, __bf16 *out, int64_t ld,
+                                                                int64_t plane, int tiles_i, int tiles_j)
+{
+    using G = Gemm<BM, BN, WM, WN>;
+    __shared__ __attribute__((aligned(1024))) char lds[G::kLdsBytes];
+    int ti, tj;
+    tile_of_block(blockIdx.x, tiles_i, tiles_j, ti, tj);
+    f32x4 acc[G::kTm][G::kTn] = {};
+    G::run(acc, g, ti * BM, tj * BN, 0, g.k / kGemmStageK * g.segments, lds);
+
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+    const int wm = wave / WN, wn = wave % WN;
+    const int lw = ti * BM + wm * (BM / WM);  // the wave's first token in the piece
+    const int vw = v0 + lw;
+    const int quarter = lane >> 4;
+    const int rows64 = (rows + 63) & ~63;
+#pragma unroll
+    for (int b = 0; b < G::kTn; ++b) {
+        const int n = tj * BN + wn * (BN / WN) + b * 16 + (lane & 15);
+        if (n >= rows64)
+            continue;
+        const bool live = n < rows;
+        const RowMask m(masks, V, live ? n : 0);
+        const float w = live ? weight[n] : 0.f;
+        const float base = w != 0.f ? lse[n] : 0.f;
+        const int t = live ? targets[n] - vw : -1;
+#pragma unroll
+        for (int a = 0; a < G::kTm; ++a) {
+            const uint32_t bits = m.word((vw >> 5) + (a >> 1)) >> (quarter * 4 + (a & 1) * 16);
+            __bf16 y[4][P];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                float p = (bits >> e & 1u) && w != 0.f ? softmax_term(acc[a][b][e], base, kLog2e) : 0.f;
+                p -= t == a * 16 + quarter * 4 + e ? 1.f : 0.f;
+                split_planes<P>(p * w, y[e]);
+            }
+            const int col = lw + a * 16 + quarter * 4;
+            if (col < ld)
+#pragma unroll
+                for (int p = 0; p < P; ++p) {
+                    __bf16 four[4] = {y[0][p], y[1][p], y[2][p], y[3][p]};
+                    __builtin_memcpy(out + p * plane + (int64_t)n * ld + col, four, 8);
+                }
+        }
+    }
+}
+
+// ------------------------------------------------------- the other products
+
+enum class Out { kStore, kPartial, kPartialAdd };
+
+// C[j][i] of a product as rows of `cols` elements: in T, or in fp32 as (or on
+// top of) the partial sums of this block's share of k.
+template <int BM, int BN, int WM, int WN, typename T, Out OUT>
+__global__ __launch_bounds__(WM *WN *kWave, 2) void product_kernel(GemmShape g, T *out, int cols, int64_t split_stride,
+                                                                   int split_stages, int tiles_i, int tiles_j)
+{
+    using G = Gemm<BM, BN, WM, WN>;
+    __shared__ __attribute__((aligned(1024))) char lds[G::kLdsBytes];
+    int ti, tj;
+    tile_of_block(blockIdx.x, tiles_i, tiles_j, ti, tj);
+    const int total = g.k / kGemmStageK * g.segments;
+    const int from = blockIdx.y * split_stages;
+    const int stages = total - from < split_stages ? total - from : split_stages;
+    f32x4 acc[G::kTm][G::kTn] = {};
+    G::run(acc, g, ti * BM, tj * BN, from, stages, lds);
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+    const int wm = wave / WN, wn = wave % WN;
+    out += blockIdx.y * split_stride;
+#pragma unroll
+    for (int b = 0; b < G::kTn; ++b) {
+        const int r = tj * BN + wn * (BN / WN) + b * 16 + (lane & 15);
+        if (r >= g.b.rows)
+            continue;
+#pragma unroll
+        for (int a = 0; a < G::kTm; ++a) {
+            const int c = ti * BM + wm * (BM / WM) + a * 16 + (lane >> 4) * 4;
+            T *p = out + (int64_t)r * cols + c;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (c + e < cols) {
+                    float y = acc[a][b][e];
+                    if (OUT == Out::kPartialAdd)
+                        y += (float)p[e];
+                    p[e] = (T)y;
+                }
+        }
+    }
+}
+
+template <typename T>
+__global__ void join_splits_kernel(const float *parts, int splits, int64_t n, T *out)
+{
+    const int64_t i = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x);
+    if (i >= n)
+        return;
+    float s = 0.f;
+    for (int k = 0; k < splits; ++k)
+        s += parts[(int64_t)k * n + i];
+    out[i] = (T)s;
+}
+
+template <typename T>
+__global__ void zero_kernel(T *p, int64_t n)
+{
+    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += (int64_t)gridDim.x * blockDim.x)
+        p[i] = (T)0.f;
+}
+
+// --------------------------------------------------------------- the plans
+
+constexpr int kLargeTiles = 160;  // 256 x 256 tiles from here on
+constexpr int64_t kPieceElements = (int64_t)1 << 27;
+constexpr int kPieceTokens = 1 << 18;
+
+int tile_side(int64_t rows_i, int64_t rows_j)
+{
+    const auto tiles = [&](int s) { return ((rows_i + s - 1) / s) * ((rows_j + s - 1) / s); };
+    if (rows_j > 128 && rows_i > 128 && tiles(256) >= kLargeTiles)
+        return 256;
+    if (rows_j > 64 && rows_i > 64 && tiles(128) >= kLargeTiles)
+        return 128;
+    return 64;
+}
+
+int64_t up64(int64_t n) { return (n + 63) / 64 * 64; }
+
+struct HeadLayout {
+    int planes, segments;
+    int64_t k;        // hidden size as the products see it
+    int piece;        // tokens of a piece, a multiple of 256 (or all)
+    int pieces;
+    int splits;       // of the k of dx
+    size_t x, w, parts, target_logit;                        // forward
+    size_t x_t, w_t, g, g_t, weight, dx;                      // backward
+    size_t forward_bytes, backward_bytes;
+};
+
+HeadLayout head_layout(int rows, int hidden, int V, int dtype)
+{
+    HeadLayout l{};
+    l.planes = dtype == 1 ? 1 : 3;
+    l.segments = dtype == 1 ? 1 : kGemmSegments;
+    l.k = up64(hidden);
+    const int64_t r64 = up64(rows > 0 ? rows : 1);
+    int64_t piece = kPieceElements / r64 / 256 * 256;
+    piece = piece < 4096 ? 4096 : piece;
+    piece = piece > kPieceTokens ? kPieceTokens : piece;
+    l.pieces = (int)((V + piece - 1) / piece);
+    // pieces of about the same size
+    piece = ((V + l.pieces - 1) / l.pieces + 255) / 256 * 256;
+    l.piece = (int)(piece < V ? piece : V);
+    l.pieces = (int)((V + l.piece - 1) / l.piece);
+    const int64_t p64 = up64(l.piece);
+    size_t at = 0;
+    const auto take = [&](size_t bytes) {
+        const size_t here = at;
+        at += align_up(bytes, 256);
+        return here;
+    };
+    const size_t planes = (size_t)l.planes;
+    l.x = take(planes * r64 * l.k * 2);
+    l.w = take(planes * p64 * l.k * 2);
+    const size_t shared = at;
+    l.parts = take(((size_t)V / 32 + 8) * r64 * sizeof(Softmax));
+    l.target_logit = take((size_t)r64 * 4);
+    l.forward_bytes = at;
+    at = shared;
+    l.x_t = take(planes * hidden * r64 * 2);
+    l.w_t = take(planes * hidden * p64 * 2);
+    l.g = take(planes * r64 * p64 * 2);
+    l.g_t = take(planes * r64 * p64 * 2);
+    l.weight = take((size_t)r64 * 4);
+    // dx over a piece: few tiles and a long k, so k is split until they fill the compute units
+    const int side = tile_side(hidden, rows);
+    const int64_t tiles = ((int64_t)(hidden + side - 1) / side) * ((rows + side - 1) / side);
+    const int64_t k_stages = p64 / kGemmStageK * l.segments;
+    int64_t splits = tiles > 0 ? 256 / tiles : 1;
+    splits = splits > k_stages / 16 ? k_stages / 16 : splits;
+    splits = splits > 16 ? 16 : splits;
+    l.splits = (int)(splits < 1 ? 1 : splits);
+    l.dx = take((size_t)l.splits * rows * hidden * 4);
+    l.backward_bytes = at;
+    return l;
+}
+
+hipError_t pack(const void *src, int64_t ld, int dtype, int64_t rows, int cols, int out_cols, __bf16 *dst, int64_t plane,
+                hipStream_t s)
+{
+    const int threads = 128;
+    const dim3 grid((out_cols / 2 + threads - 1) / threads, (unsigned)(rows < 65535 ? rows : 65535),
+                    (unsigned)((rows + 65534) / 65535));
+    if (dtype == 1)
+        pack_kernel<uint16_t, 1><<<grid, threads, 0, s>>>(static_cast<const uint16_t *>(src), ld, (int)rows, cols,
+                                                          out_cols, dst, plane);
+    else
+        pack_kernel<float, 3><<<grid, threads, 0, s>>>(static_cast<const float *>(src), ld, (int)rows, cols, out_cols,
+                                                       dst, plane);
+    return last_launch();
+}
+
+hipError_t transpose(const __bf16 *src, int64_t ld, int64_t src_plane, int planes, int rows, int cols, __bf16 *dst,
+                     int64_t out_rows, int64_t dst_plane, hipStream_t s)
+{
+    const dim3 grid((unsigned)((out_rows + 63) / 64), (unsigned)((cols + 63) / 64), planes);
+    transpose_kernel<<<grid, 256, 0, s>>>(reinterpret_cast<const uint16_t *>(src), ld, src_plane, rows, cols,
+                                          reinterpret_cast<uint16_t *>(dst), (int)out_rows, dst_plane);
+    return last_launch();
+}
+
+// An operand as the products need it: in place, or packed into `buffer`.
+bool in_place(const void *p, int64_t ld, int dtype, int hidden)
+{
+    return dtype == 1 && hidden % 64 == 0 && ld % 8 == 0 && reinterpret_cast<uintptr_t>(p) % 16 == 0 &&
+           ld <= ((int64_t)1 << 20);
+}
+
+hipError_t operand(const void *p, int64_t ld, int dtype, int rows, int hidden, const HeadLayout &l, __bf16 *buffer,
+                   GemmOperand &out, hipStream_t s)
+{
+    if (in_place(p, ld, dtype, hidden)) {
+        out = {static_cast<const __bf16 *>(p), ld, 0, rows};
+        return hipSuccess;
+    }
+    out = {buffer, l.k, (int64_t)rows * l.k, rows};
+    return pack(p, ld, dtype, rows, hidden, (int)l.k, buffer, out.plane, s);
+}
+
+#define DV_TRY(call)                   \
+    do {                               \
+        const hipError_t e_ = (call);  \
+        if (e_ != hipSuccess)          \
+            return e_;                 \
+    } while (0)
+
+template <typename F>
+hipError_t with_tile(int side, F &&f)
+{
+    if (side == 256)
+        f(std::integral_constant<int, 256>{}, std::integral_constant<int, 4>{});
+    else if (side == 128)
+        f(std::integral_constant<int, 128>{}, std::integral_constant<int, 2>{});
+    else
+        f(std::integral_constant<int, 64>{}, std::integral_constant<int, 2>{});
+    return last_launch();
+}
+
+// How k is split `splits` ways: whole pairs of 32-k steps each, and no split empty
+// (`used` of them may be fewer).
+struct Splits {
+    int stages, used;
+};
+Splits splits_of(const GemmShape &g, int splits)
+{
+    const int total = g.k / kGemmStageK * g.segments;
+    const int stages = ((total + splits - 1) / splits + 1) & ~1;
+    return {stages, (total + stages - 1) / stages};
+}
+
+template <typename T, Out OUT>
+hipError_t product(const GemmShape &g, T *out, int cols, int splits, int64_t split_stride, hipStream_t s)
+{
+    return with_tile(tile_side(g.a.rows, g.b.rows), [&](auto side, auto wn) {
+        constexpr int B = decltype(side)::value, WN = decltype(wn)::value;
+        const int ti = (g.a.rows + B - 1) / B, tj = (g.b.rows + B - 1) / B;
+        const Splits k = splits_of(g, splits);
+        product_kernel<B, B, 2, WN, T, OUT><<<dim3(ti * tj, k.used), 2 * WN * kWave, 0, s>>>(g, out, cols, split_stride,
+                                                                                             k.stages, ti, tj);
+    });
+}
+
+template <typename T>
+hipError_t zero(T *p, int64_t n, hipStream_t s)
+{
+    if (n == 0)
+        return hipSuccess;
+    const int64_t blocks = (n + 255) / 256;
+    zero_kernel<T><<<(unsigned)(blocks < 4096 ? blocks : 4096), 256, 0, s>>>(p, n);
+    return last_launch();
+}
+
+const void *weight_rows(const HeadArgs &a, int v0)
+{
+    return static_cast<const char *>(a.weight) + (int64_t)v0 * a.ld_w * (a.dtype == 1 ? 2 : 4);
+}
+
+template <typename T>
+hipError_t backward(const HeadArgs &a, const float *lse, const float *grad_loss, T *grad_x, T *grad_weight, char *ws,
+                    hipStream_t s)
+{
+    const HeadLayout l = head_layout(a.rows, a.hidden, a.V, a.dtype);
+    const int64_t r64 = up64(a.rows);
+    const auto at = [&](size_t off) { return reinterpret_cast<__bf16 *>(ws + off); };
+    float *weight = reinterpret_cast<float *>(ws + l.weight), *dx = reinterpret_cast<float *>(ws + l.dx);
+    GemmOperand x;
+    DV_TRY(operand(a.x, a.ld_x, a.dtype, a.rows, a.hidden, l, at(l.x), x, s));
+    weights_kernel<<<(a.rows + 255) / 256, 256, 0, s>>>(a.rows, a.V, a.masks, a.targets, grad_loss, weight);
+    DV_TRY(last_launch());
+    const GemmOperand x_t{at(l.x_t), r64, (int64_t)a.hidden * r64, a.hidden};
+    if (grad_weight)
+        DV_TRY(transpose(x.p, x.ld, x.plane, l.planes, a.rows, a.hidden, at(l.x_t), r64, x_t.plane, s));
+    int splits = 1;
+    for (int piece = 0; piece < l.pieces; ++piece) {
+        const int v0 = piece * l.piece;
+        const int n = a.V - v0 < l.piece ? a.V - v0 : l.piece;
+        const int64_t n64 = up64(n);
+        GemmOperand w;
+        DV_TRY(operand(weight_rows(a, v0), a.ld_w, a.dtype, n, a.hidden, l, at(l.w), w, s));
+        const GemmShape logits{w, x, (int)l.k, l.segments};
+        const GemmOperand g{at(l.g), n64, r64 * n64, a.rows};
+        DV_TRY(with_tile(tile_side(n, a.rows), [&](auto side, auto wn) {
+            constexpr int B = decltype(side)::value, WN = decltype(wn)::value;
+            const int ti = (n + B - 1) / B, tj = (a.rows + B - 1) / B;
+            constexpr int P = sizeof(T) == 2 ? 1 : 3;
+            grad_kernel<B, B, 2, WN, P><<<ti * tj, 2 * WN * kWave, 0, s>>>(logits, v0, a.V, a.rows, a.masks, a.targets,
+                                                                          lse, weight, at(l.g), n64, g.plane, ti, tj);
+        }));
+        if (grad_x) {
+            const GemmOperand w_t{at(l.w_t), n64, (int64_t)a.hidden * n64, a.hidden};
+            DV_TRY(transpose(w.p, w.ld, w.plane, l.planes, n, a.hidden, at(l.w_t), n64, w_t.plane, s));
+            const GemmShape shape{w_t, g, (int)n64, l.segments};
+            const int64_t stride = (int64_t)a.rows * a.hidden;
+            if (piece == 0) {
+                // later pieces have no longer a k, so they use no more splits
+                splits = splits_of(shape, l.splits).used;
+                if (l.pieces == 1 && splits == 1)
+                    DV_TRY((product<T, Out::kStore>(shape, grad_x, a.hidden, 1, 0, s)));
+                else
+                    DV_TRY((product<float, Out::kPartial>(shape, dx, a.hidden, splits, stride, s)));
+            } else {
+                DV_TRY((product<float, Out::kPartialAdd>(shape, dx, a.hidden, splits, stride, s)));
+            }
+        }
+        if (grad_weight) {
+            const GemmOperand g_t{at(l.g_t), r64, n64 * r64, n};
+            DV_TRY(transpose(g.p, g.ld, g.plane, l.planes, (int)r64, n, at(l.g_t), r64, g_t.plane, s));
+            const GemmShape shape{x_t, g_t, (int)r64, l.segments};
+            DV_TRY((product<T, Out::kStore>(shape, grad_weight + (int64_t)v0 * a.hidden, a.hidden, 1, 0, s)));
+        }
+    }
+    if (grad_x && !(l.pieces == 1 && splits == 1)) {
+        const int64_t n = (int64_t)a.rows * a.hidden;
+        join_splits_kernel<T><<<(unsigned)((n + 255) / 256), 256, 0, s>>>(dx, splits, n, grad_x);
+        DV_TRY(last_launch());
+    }
+    return hipSuccess;
+}
+
+}  // namespace
+
+size_t head_workspace_bytes(int rows, int hidden, int V, int dtype)
+{
+    return head_layout(rows, hidden, V, dtype).forward_bytes;
+}
+
+size_t head_backward_workspace_bytes(int rows, int hidden, int V, int dtype)
+{
+    return head_layout(rows, hidden, V, dtype).backward_bytes;
+}
+
+hipError_t launch_head_loss(const HeadArgs &a, float *loss, float *lse, void *workspace, hipStream_t s)
+{
+    const HeadLayout l = head_layout(a.rows, a.hidden, a.V, a.dtype);
+    char *ws = static_cast<char *>(workspace);
+    Softmax *parts = reinterpret_cast<Softmax *>(ws + l.parts);
+    float *target_logit = reinterpret_cast<float *>(ws + l.target_logit);
+    GemmOperand x;
+    DV_TRY(operand(a.x, a.ld_x, a.dtype, a.rows, a.hidden, l, reinterpret_cast<__bf16 *>(ws + l.x), x, s));
+    const bool whole = in_place(a.weight, a.ld_w, a.dtype, a.hidden);  // nothing to pack: one piece
+    const int step = whole ? a.V : l.piece;
+    const int side = tile_side(step, a.rows);
+    for (int v0 = 0; v0 < a.V; v0 += step) {
+        const int n = a.V - v0 < step ? a.V - v0 : step;
+        GemmOperand w;
+        DV_TRY(operand(weight_rows(a, v0), a.ld_w, a.dtype, n, a.hidden, l, reinterpret_cast<__bf16 *>(ws + l.w), w, s));
+        const GemmShape g{w, x, (int)l.k, l.segments};
+        DV_TRY(with_tile(side, [&](auto sd, auto wn) {
+            constexpr int B = decltype(sd)::value, WN = decltype(wn)::value;
+            const int ti = (n + B - 1) / B, tj = (a.rows + B - 1) / B;
+            stats_kernel<B, B, 2, WN><<<ti * tj, 2 * WN * kWave, 0, s>>>(g, v0, a.V, a.rows, a.masks, a.targets, parts,
+                                                                        target_logit, ti, tj);
+        }));
+    }
+    const int nparts = (a.V + side - 1) / side * 2;
+    int slices = 16;
+    while (slices < 256 && 256 / slices > a.rows)
+        slices *= 2;
+    const int per_block = 256 / slices;
+    finish_kernel<<<(a.rows + per_block - 1) / per_block, 256, 0, s>>>(parts, nparts, a.rows, a.V, a.masks, a.targets,
+                                                                      target_logit, loss, lse, slices);
+    return last_launch();
+}
+
+hipError_t launch_head_loss_backward(const HeadArgs &a, const float *lse, const float *grad_loss, void *grad_x,
+                                     void *grad_weight, void *workspace, hipStream_t s)
+{
+    if (a.rows == 0) {
+        const int64_t n = (int64_t)a.V * a.hidden;
+        if (!grad_weight)
+            return hipSuccess;
+        return a.dtype == 1 ? zero(static_cast<__bf16 *>(grad_weight), n, s) : zero(static_cast<float *>(grad_weight), n, s);
+    }
+    char *ws = static_cast<char *>(workspace);
+    if (a.dtype == 1)
+        return backward(a, lse, grad_loss, static_cast<__bf16 *>(grad_x), static_cast<__bf16 *>(grad_weight), ws, s);
+    return backward(a, lse, grad_loss, static_cast<float *>(grad_x), static_cast<float *>(grad_weight), ws, s);
+}
+
+}  // namespace dv

@@ -1,0 +1,263 @@
+"""dv_head_loss and its backward pass against their 64-bit forms, element by
+element within derived bounds; gradients also against differences of the
+loss; edges of masks, targets, strides and sizes; refusals."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from tests.train_common import check, head_reference, masks, pack_mask, row_mask
+
+pytestmark = pytest.mark.gpu
+DEV = torch.device("cuda:0")
+
+
+@pytest.fixture(scope="module")
+def dv():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import paper_2403_06988_amd as dv_mod
+    return dv_mod
+
+
+def on_device(t, pad):
+    """t on the device with rows `pad` elements further apart, the first off a 16-byte boundary when pad is odd."""
+    if pad == 0:
+        return t.to(DEV)
+    wide = torch.full((t.shape[0], t.shape[1] + pad), float("nan"), dtype=t.dtype, device=DEV)
+    view = wide[:, pad // 2:pad // 2 + t.shape[1]]
+    view.copy_(t)
+    return view
+
+
+def make(seed, N, D, V, dtype, S, shares=(0.0, 0.02, 0.5, 1.0), std=3.0):
+    rng = np.random.default_rng(seed)
+    x = torch.from_numpy(rng.normal(size=(N, D))).to(dtype)
+    w = torch.from_numpy(rng.normal(size=(V, D)) * std / math.sqrt(D)).to(dtype)
+    may = masks(rng, S, V, shares) if S else None
+    states = torch.from_numpy(rng.integers(-1, S + 1, N).astype(np.int32)) if S else None
+    mask = row_mask(may, states, N, V)
+    targets = torch.zeros(N, dtype=torch.int32)
+    for n in range(N):
+        allowed = torch.nonzero(mask[n])[:, 0]
+        if allowed.numel() and n % 7:
+            targets[n] = int(allowed[rng.integers(allowed.numel())])
+        else:  # padding, past the end, or any token
+            targets[n] = [-1, V, -2147483648, int(rng.integers(V))][rng.integers(4)]
+    g = torch.from_numpy(rng.normal(size=N)).float()
+    return x, w, targets, may, states, mask, g
+
+
+def run(dv, x, w, targets, may, states, g, pad=0):
+    kw = {}
+    if may is not None:
+        kw = dict(allow=pack_mask(may).to(DEV), states=states.to(DEV))
+    xd, wd, td = on_device(x, pad), on_device(w, pad), targets.to(DEV)
+    loss, lse = dv.head_loss(xd, wd, td, **kw)
+    gx, gw = dv.head_loss_backward(xd, wd, td, lse, g.to(DEV), **kw)
+    torch.cuda.synchronize()
+    return loss, lse, gx, gw
+
+
+# rows, hidden, tokens: one of each, below and above the tiles' sides and their k, odd ones
+SIZES = [(1, 1, 1), (1, 64, 32), (2, 8, 33), (3, 65, 100), (17, 100, 257), (64, 64, 256), (65, 128, 255), (33, 192, 1000),
+         (130, 63, 513), (200, 256, 300), (300, 72, 2049)]
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("masked", [False, True])
+@pytest.mark.parametrize("N,D,V", SIZES)
+def test_matches_the_64_bit_form(dv, N, D, V, dtype, masked):
+    print(f"head N={N} D={D} V={V} {dtype} masked={masked}", flush=True)
+    x, w, t, may, states, mask, g = make(N * 7 + D + V, N, D, V, dtype, 5 if masked else 0)
+    ref = head_reference(x, w, t, mask, g)
+    for pad in (0, 3):
+        loss, lse, gx, gw = run(dv, x, w, t, may, states, g, pad)
+        check(lse, ref["lse"], ref["lse_tol"], "lse")
+        check(loss, ref["loss"], ref["loss_tol"], "loss")
+        check(gx, ref["grad_x"], ref["grad_x_tol"], "grad_x")
+        check(gw, ref["grad_weight"], ref["grad_weight_tol"], "grad_weight")
+        assert gx.dtype == dtype and gw.dtype == dtype
+
+
+@pytest.mark.parametrize("N,D,V,dtype", [
+    (700, 640, 5000, torch.bfloat16),     # 128-sided tiles, split k
+    (2100, 512, 6200, torch.bfloat16),    # 256-sided tiles
+    (1100, 256, 5003, torch.float32),
+])
+def test_larger_tiles(dv, N, D, V, dtype):
+    print(f"head large N={N} D={D} V={V} {dtype}", flush=True)
+    x, w, t, may, states, mask, g = make(3, N, D, V, dtype, 6)
+    ref = head_reference(x, w, t, mask, g)
+    loss, lse, gx, gw = run(dv, x, w, t, may, states, g)
+    check(lse, ref["lse"], ref["lse_tol"], "lse")
+    check(loss, ref["loss"], ref["loss_tol"], "loss")
+    check(gx, ref["grad_x"], ref["grad_x_tol"], "grad_x")
+    check(gw, ref["grad_weight"], ref["grad_weight_tol"], "grad_weight")
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_several_pieces_of_the_vocabulary(dv, dtype):
+    """More rows than a piece of the vocabulary covers in one go."""
+    N, D, V = 20000, 64, 9000
+    print(f"head pieces N={N} D={D} V={V} {dtype}", flush=True)
+    assert N * V > 1 << 27
+    g = torch.Generator(device=DEV).manual_seed(5)
+    x = torch.randn((N, D), generator=g, device=DEV).to(dtype)
+    w = (torch.randn((V, D), generator=g, device=DEV) * 0.3).to(dtype)
+    t = torch.randint(0, V, (N,), generator=g, device=DEV, dtype=torch.int32)
+    gl = torch.randn(N, generator=g, device=DEV)
+    loss, lse = dv.head_loss(x, w, t)
+    gx, gw = dv.head_loss_backward(x, w, t, lse, gl)
+    pick = torch.arange(0, N, 997)
+    ref = head_reference(x[pick].cpu(), w.cpu(), t[pick].cpu(), torch.ones((len(pick), V), dtype=torch.bool), gl[pick].cpu())
+    check(loss[pick], ref["loss"], ref["loss_tol"], "loss")
+    check(lse[pick], ref["lse"], ref["lse_tol"], "lse")
+    check(gx[pick], ref["grad_x"], ref["grad_x_tol"], "grad_x")
+    # the weight's gradient takes every row: its sums against those over float64 on the device, whole
+    z = x.double() @ w.double().t()
+    G = torch.softmax(z, 1)
+    G[torch.arange(N, device=DEV), t.long()] -= 1
+    G *= gl.double()[:, None]
+    want = G.t().contiguous() @ x.double()
+    mags = G.abs().t().contiguous() @ x.double().abs()
+    # the terms' error (2^-8 of bf16 G; fp32: logits within 2^-14 of e) and N terms' sum
+    term = 2.0 ** -8 + 2.0 ** -12 if dtype == torch.bfloat16 else 2.0 ** -13
+    out = 2.0 ** -8 if dtype == torch.bfloat16 else 2.0 ** -24
+    tol = (term + 6 * N * 2.0 ** -24) * mags + out * want.abs()
+    check(gw, want.cpu(), tol.cpu(), "grad_weight")
+
+
+def test_gradient_against_differences(dv):
+    N, D, V = 6, 24, 70
+    x, w, t, may, states, mask, g = make(11, N, D, V, torch.float32, 4, shares=(0.6, 1.0))
+    t = t.clamp(0, V - 1)
+    kw = dict(allow=pack_mask(may).to(DEV), states=states.to(DEV))
+    g = g.to(DEV)
+
+    def total(x, w):
+        loss, lse = dv.head_loss(x.to(DEV), w.to(DEV), t.to(DEV), **kw)
+        return float((loss.double() * g.double()).sum()), lse
+
+    _, lse = total(x, w)
+    gx, gw = dv.head_loss_backward(x.to(DEV), w.to(DEV), t.to(DEV), lse, g, **kw)
+    rng = np.random.default_rng(2)
+    for _ in range(6):
+        dx = torch.from_numpy(rng.normal(size=x.shape)).float()
+        dw = torch.from_numpy(rng.normal(size=w.shape)).float()
+        h = 2.0 ** -7
+        diff = (total(x + h * dx, w + h * dw)[0] - total(x - h * dx, w - h * dw)[0]) / (2 * h)
+        along = float((gx.cpu().double() * dx.double()).sum() + (gw.cpu().double() * dw.double()).sum())
+        # third derivatives of the loss along (dx, dw) times h^2 / 6, and the losses' rounding over 2 h
+        assert abs(diff - along) < 0.02 * (1 + abs(along)), (diff, along)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_rows_that_take_no_part(dv, dtype):
+    """Empty masks, dead states, targets that are padding or not allowed: loss
+    0, no gradient, and no trace of them in the others' gradients."""
+    N, D, V = 40, 64, 300
+    x, w, t, may, states, mask, g = make(21, N, D, V, dtype, 3, shares=(0.0, 1.0, 0.3))
+    states[:] = 1
+    states[3], states[4], states[5] = 0, -1, 77
+    t[:] = 5
+    t[6], t[7] = -1, V
+    states[8] = 2
+    t[8] = int(torch.nonzero(~may[2])[0, 0])
+    out = [3, 4, 5, 6, 7, 8]
+    loss, lse, gx, gw = run(dv, x, w, t, may, states, g)
+    assert torch.equal(loss[out].cpu(), torch.zeros(len(out)))
+    assert torch.equal(gx[out].float().cpu(), torch.zeros((len(out), D)))
+    assert bool((lse[[3, 4, 5]] == -math.inf).all()) and bool(torch.isfinite(lse[[6, 7, 8]]).all())
+    keep = [n for n in range(N) if n not in out]
+    ref = head_reference(x, w, t, row_mask(may, states, N, V), g)
+    check(gw, ref["grad_weight"], ref["grad_weight_tol"], "grad_weight")
+    check(gx[keep], ref["grad_x"][keep], ref["grad_x_tol"][keep], "grad_x")
+    # all of them: zeros everywhere
+    loss, lse, gx, gw = run(dv, x, w, torch.full_like(t, -1), may, states, g)
+    assert not loss.any() and not gx.any() and not gw.any()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_what_is_masked_has_no_effect(dv, dtype):
+    """Weight rows that make masked logits huge change nothing; logits beyond
+    exp's range on allowed tokens stay exact."""
+    N, D, V = 9, 64, 200
+    x, w, t, may, states, mask, g = make(31, N, D, V, dtype, 1, shares=(0.5,))
+    states[:] = 0
+    allowed = torch.nonzero(may[0])[:, 0]
+    t[:] = int(allowed[0])
+    x[0] *= 60  # logits of several hundred
+    first = run(dv, x, w, t, may, states, g)
+    w2 = w.clone()
+    w2[~may[0]] *= 1e30
+    second = run(dv, x, w2, t, may, states, g)
+    assert torch.equal(first[0], second[0]) and torch.equal(first[1], second[1])
+    ref = head_reference(x, w, t, row_mask(may, states, N, V), g)
+    check(first[0], ref["loss"], ref["loss_tol"], "loss")
+    assert torch.equal(first[3][~may[0]], torch.zeros_like(first[3][~may[0]]))
+    assert torch.equal(first[3][may[0]], second[3][may[0]])
+
+
+def test_nan_is_seen(dv):
+    N, D, V = 5, 64, 100
+    x, w, t, may, states, mask, g = make(41, N, D, V, torch.float32, 0)
+    t[:] = 1
+    x[2] = float("nan")
+    loss, lse, gx, gw = run(dv, x, w, t, None, None, g)
+    assert bool(torch.isnan(loss[2])) and bool(torch.isnan(lse[2]))
+    assert bool(torch.isfinite(loss[[0, 1, 3, 4]]).all())
+
+
+def test_one_gradient_alone_and_no_rows(dv):
+    N, D, V = 50, 96, 500
+    x, w, t, may, states, mask, g = make(51, N, D, V, torch.bfloat16, 0)
+    loss, lse, gx, gw = run(dv, x, w, t, None, None, g)
+    args = (x.to(DEV), w.to(DEV), t.to(DEV), lse, g.to(DEV))
+    ax, none = dv.head_loss_backward(*args, want_weight=False)
+    assert none is None and torch.equal(ax, gx)
+    none, aw = dv.head_loss_backward(*args, want_x=False)
+    assert none is None and torch.equal(aw, gw)
+    e = torch.empty((0, D), dtype=torch.bfloat16, device=DEV)
+    none_t = torch.empty(0, dtype=torch.int32, device=DEV)
+    none_f = torch.empty(0, device=DEV)
+    loss, lse = dv.head_loss(e, w.to(DEV), none_t)
+    assert loss.numel() == 0
+    gw.fill_(7)
+    gx, gw = dv.head_loss_backward(e, w.to(DEV), none_t, none_f, none_f, grad_weight=gw)
+    assert gx.shape == (0, D) and not gw.any()
+
+
+def test_same_bits_each_time_and_on_another_stream(dv):
+    x, w, t, may, states, mask, g = make(61, 300, 256, 3000, torch.bfloat16, 4)
+    first = run(dv, x, w, t, may, states, g)
+    side = torch.cuda.Stream()
+    kw = dict(allow=pack_mask(may).to(DEV), states=states.to(DEV))
+    xd, wd, td, gd = x.to(DEV), w.to(DEV), t.to(DEV), g.to(DEV)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        loss, lse = dv.head_loss(xd, wd, td, **kw)
+        gx, gw = dv.head_loss_backward(xd, wd, td, lse, gd, **kw)
+    torch.cuda.synchronize()
+    for a, b in zip(first, (loss, lse, gx, gw)):
+        assert torch.equal(a, b)
+
+
+def test_refusals(dv):
+    x = torch.zeros((4, 64), dtype=torch.bfloat16, device=DEV)
+    w = torch.zeros((100, 64), dtype=torch.bfloat16, device=DEV)
+    t = torch.zeros(4, dtype=torch.int32, device=DEV)
+    al = torch.zeros((2, 4), dtype=torch.int32, device=DEV)
+    for bad in (lambda: dv.head_loss(x.half(), w.half(), t), lambda: dv.head_loss(x, w.float(), t),
+                lambda: dv.head_loss(x, w, t.long()), lambda: dv.head_loss(x, w, t[:3]),
+                lambda: dv.head_loss(x[:, :32], w, t), lambda: dv.head_loss(x.t(), w, t),
+                lambda: dv.head_loss(x, w, t, allow=al), lambda: dv.head_loss(x, w, t, allow=al[:, :3], states=t),
+                lambda: dv.head_loss(x, w, t, workspace=torch.zeros(16, dtype=torch.uint8, device=DEV)),
+                lambda: dv.head_loss_backward(x, w, t, torch.zeros(3, device=DEV), torch.zeros(4, device=DEV)),
+                lambda: dv.head_loss_backward(x, w, t, torch.zeros(4, device=DEV), torch.zeros(4, device=DEV),
+                                              grad_x=torch.zeros((4, 32), dtype=torch.bfloat16, device=DEV))):
+        with pytest.raises((TypeError, ValueError)):
+            bad()
+    with pytest.raises(dv.DvError):  # an output over an input
+        dv.head_loss_backward(x, w, t, torch.zeros(4, device=DEV), torch.zeros(4, device=DEV), grad_x=x)
