@@ -35,27 +35,32 @@ __device__ __forceinline__ int segment_plane_b(int s) { return (0x210100 >> (4 *
 
 // The waves of a block split its BM x BN tile into WM x WN parts.
 //
-// A stage holds 32 k of both tiles in LDS as groups of 16 rows x 64 bytes
-// (1 KiB, what one wave's direct-to-LDS load writes).  In a group the 16-byte
-// piece c of row r sits at place 4 r + (c ^ f(r)), f(r) = (r / 2 mod 4) ^ (r / 8),
+// A stage holds 64 k of both tiles in LDS as groups of 8 rows x 128 bytes
+// (1 KiB, what one wave's direct-to-LDS load writes; whole lines of memory: with 32 k
+// stages the same product ran 15 to 20 % slower on twice the requests).  In a
+// tile the 16-byte piece c of row r sits at place c ^ (r / 2 mod 8) of its row,
 // so that the lanes of a fragment read (row l mod 16, piece l / 16) meet
-// distinct banks.  kStages stages are in flight or in use: while the matrix
-// instructions work on the registers of stage k, stage k + 1 goes from LDS to
-// registers and stage k + 3 from memory to LDS.
-constexpr int kGemmStages = 4;
-constexpr int kGemmStageK = 32;
+// distinct banks.  Two stages: while the matrix instructions work on one half of a
+// stage's k in registers, its other half (then the next stage's first) goes
+// from LDS to registers, and the stage after it from memory to LDS.  One barrier
+// a stage: past it every wave has the stage's fragments in registers, so its
+// buffer is free, and the next stage has arrived.
+//
+// What it reaches with 256 x 256 tiles: 16384 x 8192 x 4096 1.31 PFLOP/s, 4096 x
+// 8192 x 16384 1.26 (the library 1.55 and 1.57); 128 x 128 tiles 1.10 and 1.06,
+// 64 x 64 tiles 0.71 and 0.69.
+constexpr int kGemmStageK = 64;
 
 template <int BM, int BN, int WM, int WN>
 struct Gemm {
     static constexpr int kWaves = WM * WN;
-    static constexpr int kThreads = kWaves * kWave;
     static constexpr int kTm = BM / WM / 16;  // 16-row fragments of a wave
     static constexpr int kTn = BN / WN / 16;
-    static constexpr int kGroupsA = BM / 16;
-    static constexpr int kGroups = (BM + BN) / 16;
+    static constexpr int kGroupsA = BM / 8;
+    static constexpr int kGroups = (BM + BN) / 8;
     static constexpr int kLoads = kGroups / kWaves;  // of one wave per stage
     static constexpr int kStageBytes = kGroups * 1024;
-    static constexpr int kLdsBytes = kGemmStages * kStageBytes;
+    static constexpr int kLdsBytes = 2 * kStageBytes;
     static_assert(kGroups % kWaves == 0, "whole groups per wave");
 
     using Lds = __attribute__((address_space(3))) void *;
@@ -64,18 +69,18 @@ struct Gemm {
         bf16x8 a[kTm], b[kTn];
     };
 
-    static __device__ __forceinline__ int swizzle(int r) { return ((r >> 1) & 3) ^ (r >> 3); }
-
     static __device__ __forceinline__ void read(Fragments &f, const char *stage, int wm, int wn, int place)
     {
 #pragma unroll
         for (int i = 0; i < kTn; ++i)
-            f.b[i] = *reinterpret_cast<const bf16x8 *>(stage + (kGroupsA + wn * kTn + i) * 1024 + place);
+            f.b[i] = *reinterpret_cast<const bf16x8 *>(stage + kGroupsA * 1024 + (wn * kTn + i) * 2048 + place);
 #pragma unroll
         for (int i = 0; i < kTm; ++i)
-            f.a[i] = *reinterpret_cast<const bf16x8 *>(stage + (wm * kTm + i) * 1024 + place);
+            f.a[i] = *reinterpret_cast<const bf16x8 *>(stage + (wm * kTm + i) * 2048 + place);
     }
 
+    // acc += a b^T, with the LDS reads issued just before dealt out between
+    // the matrix instructions.
     static __device__ __forceinline__ void multiply(f32x4 (&acc)[kTm][kTn], const Fragments &f)
     {
 #pragma unroll
@@ -83,26 +88,32 @@ struct Gemm {
 #pragma unroll
             for (int j = 0; j < kTn; ++j)
                 acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.a[i], f.b[j], acc[i][j], 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < kTm + kTn; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // a matrix instruction
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);  // an LDS read
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
     }
 
-    // vmcnt: at most n of this wave's loads still on the way
+    // s_waitcnt: at most N of this wave's loads on the way; LDS reads done too with 0
     template <int N>
     static __device__ __forceinline__ void wait_loads()
     {
         static_assert(N < 64, "six bits of the count");
-        __builtin_amdgcn_s_waitcnt(0x0F70 | (N & 15) | (N >> 4) << 14);
+        __builtin_amdgcn_s_waitcnt((N ? 0x0F70 : 0x0070) | (N & 15) | (N >> 4) << 14);
     }
 
-    // acc += the tile at rows i0 of A and j0 of B.  lane l of a wave ends
+    // acc += the tile at rows i0 of A and j0 of B.  Lane l of a wave ends
     // with acc[ti][tj][e] = C[i0 + wm BM/WM + 16 ti + 4 (l / 16) + e][j0 + wn BN/WN + 16 tj + l mod 16].
-    // `from`, `stages`: this block's part of the 32-k steps (both even).
+    // `from`, `stages` (at least 1): this block's part of the 64-k stages.
     static __device__ __forceinline__ void run(f32x4 (&acc)[kTm][kTn], const GemmShape &g, int i0, int j0, int from,
                                                int stages, char *lds)
     {
         const int lane = threadIdx.x & (kWave - 1);
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
         const int wm = wave / WN, wn = wave % WN;
-        const int lr = lane >> 2, lc = (lane & 3) ^ swizzle(lr);
         int voff[kLoads];
         bool is_a[kLoads];
 #pragma unroll
@@ -111,9 +122,10 @@ struct Gemm {
             is_a[i] = group < kGroupsA;
             const GemmOperand &o = is_a[i] ? g.a : g.b;
             const int r0 = is_a[i] ? i0 : j0;
-            int r = (is_a[i] ? group : group - kGroupsA) * 16 + lr;
+            int r = (is_a[i] ? group : group - kGroupsA) * 8 + (lane >> 3);
+            const int c = (lane & 7) ^ ((r >> 1) & 7);
             r = r < o.rows - r0 ? r : o.rows - 1 - r0;
-            voff[i] = r * (int)(o.ld * 2) + lc * 16;
+            voff[i] = r * (int)(o.ld * 2) + c * 16;
         }
         const char *pa = reinterpret_cast<const char *>(g.a.p + (int64_t)i0 * g.a.ld);
         const char *pb = reinterpret_cast<const char *>(g.b.p + (int64_t)j0 * g.b.ld);
@@ -140,36 +152,32 @@ struct Gemm {
             }
         };
 
-        const int place = ((lane & 15) * 4 + ((lane >> 4) ^ swizzle(lane & 15))) * 16;
-        Fragments f[2];
+        const int r = lane & 15;
+        const int place0 = r * 128 + ((lane >> 4) ^ (r >> 1)) * 16;        // first half of a stage's k
+        const int place1 = r * 128 + ((4 + (lane >> 4)) ^ (r >> 1)) * 16;  // second half
+        Fragments f0, f1;
         load(0);
-        load(1);
-        if (stages > 2) {
-            load(2);
-            wait_loads<2 * kLoads>();
-        } else {
+        if (stages > 1) {
+            load(1);
             wait_loads<kLoads>();
+        } else {
+            wait_loads<0>();
         }
         __builtin_amdgcn_s_barrier();
-        read(f[0], lds, wm, wn, place);
-        auto step = [&](int k, const Fragments &cur, Fragments &next) {
-            if (k + 1 < stages) {
-                if (k + 2 < stages)
-                    wait_loads<kLoads>();
-                else
-                    wait_loads<0>();
+        asm volatile("" ::: "memory");
+        read(f0, lds, wm, wn, place0);
+        for (int s = 0; s < stages; ++s) {
+            read(f1, lds + (s & 1) * kStageBytes, wm, wn, place1);
+            multiply(acc, f0);
+            if (s + 1 < stages) {
+                wait_loads<0>();
                 __builtin_amdgcn_s_barrier();
                 asm volatile("" ::: "memory");
-                if (k + 3 < stages)
-                    load((k + 3) & (kGemmStages - 1));
-                read(next, lds + ((k + 1) & (kGemmStages - 1)) * kStageBytes, wm, wn, place);
-                __builtin_amdgcn_sched_barrier(0);
+                if (s + 2 < stages)
+                    load(s & 1);
+                read(f0, lds + ((s + 1) & 1) * kStageBytes, wm, wn, place0);
             }
-            multiply(acc, cur);
-        };
-        for (int k = 0; k < stages; k += 2) {
-            step(k, f[0], f[1]);
-            step(k + 1, f[1], f[0]);
+            multiply(acc, f1);
         }
     }
 };

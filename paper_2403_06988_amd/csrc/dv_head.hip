@@ -385,7 +385,7 @@ HeadLayout head_layout(int rows, int hidden, int V, int dtype)
     const int64_t tiles = ((int64_t)(hidden + side - 1) / side) * ((rows + side - 1) / side);
     const int64_t k_stages = p64 / kGemmStageK * l.segments;
     int64_t splits = tiles > 0 ? 256 / tiles : 1;
-    splits = splits > k_stages / 16 ? k_stages / 16 : splits;
+    splits = splits > k_stages / 8 ? k_stages / 8 : splits;
     splits = splits > 16 ? 16 : splits;
     l.splits = (int)(splits < 1 ? 1 : splits);
     l.dx = take((size_t)l.splits * rows * hidden * 4);
@@ -454,15 +454,15 @@ hipError_t with_tile(int side, F &&f)
     return last_launch();
 }
 
-// How k is split `splits` ways: whole pairs of 32-k steps each, and no split empty
-// (`used` of them may be fewer).
+// How k is split `splits` ways: whole stages, and no split empty (`used` of
+// them may be fewer).
 struct Splits {
     int stages, used;
 };
 Splits splits_of(const GemmShape &g, int splits)
 {
     const int total = g.k / kGemmStageK * g.segments;
-    const int stages = ((total + splits - 1) / splits + 1) & ~1;
+    const int stages = (total + splits - 1) / splits;
     return {stages, (total + stages - 1) / stages};
 }
 
