@@ -1,6 +1,7 @@
-// Tiled bf16 matrix product C[i][j] = sum_k A[i][k] B[j][k] with fp32 sums,
-// the core of the head loss (dv_head.hip).  Both operands are stored with k
-// contiguous, rows on 16-byte boundaries, k a multiple of 64.
+// Tiled bf16 matrix product C[i][j] = sum_k A(i, k) B(j, k) with fp32 sums,
+// the core of the head loss (dv_head.hip).  Each operand is stored with k
+// along its rows ("rows": i by k) or with k from row to row ("columns": k by i);
+// row starts are on 16-byte boundaries and k is a multiple of 64.
 #pragma once
 
 #include "dv_internal.h"
@@ -10,14 +11,18 @@ namespace dv {
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 
-// One operand: rows of `ld` elements; row indices past `rows` read the last
-// row (the epilogue drops what comes of them).  An fp32 operand is held as
-// three bf16 planes, `plane` elements apart, that add up to it exactly.
+// One operand, rows of `ld` elements.  Stored by rows: `n` rows (indices past
+// them read the last one).  Stored by columns: rows of `n` elements, n a
+// multiple of 8 (pieces past them read the last one), of which k_rows exist (past
+// them the last one is read again: the other operand holds zeros there).  What
+// comes of indices past n is dropped by the epilogue.  An fp32 operand is held
+// as three bf16 planes, `plane` elements apart, that add up to it exactly.
 struct GemmOperand {
     const __bf16 *p;
     int64_t ld;
     int64_t plane;
-    int rows;
+    int n;
+    int k_rows;
 };
 
 struct GemmShape {
@@ -33,35 +38,129 @@ constexpr int kGemmSegments = 6;
 __device__ __forceinline__ int segment_plane_a(int s) { return (0x012010 >> (4 * (5 - s))) & 15; }
 __device__ __forceinline__ int segment_plane_b(int s) { return (0x210100 >> (4 * (5 - s))) & 15; }
 
-// The waves of a block split its BM x BN tile into WM x WN parts.
+// The waves of a block split its BM x BN tile into WM x WN parts; COLS_A and
+// COLS_B say which operands are stored by columns.
 //
-// A stage holds 64 k of both tiles in LDS as groups of 8 rows x 128 bytes
-// (1 KiB, what one wave's direct-to-LDS load writes; whole lines of memory: with 32 k
-// stages the same product ran 15 to 20 % slower on twice the requests).  In a
-// tile the 16-byte piece c of row r sits at place c ^ (r / 2 mod 8) of its row,
-// so that the lanes of a fragment read (row l mod 16, piece l / 16) meet
-// distinct banks.  Two stages: while the matrix instructions work on one half of a
-// stage's k in registers, its other half (then the next stage's first) goes
-// from LDS to registers, and the stage after it from memory to LDS.  One barrier
-// a stage: past it every wave has the stage's fragments in registers, so its
-// buffer is free, and the next stage has arrived.
+// A stage holds 64 k of both tiles in LDS, laid out in groups of 1 KiB (what
+// one wave's direct-to-LDS load writes; whole lines of memory: with 32 k stages
+// the same product ran 15 to 20 % slower on twice the requests).
 //
-// What it reaches with 256 x 256 tiles: 16384 x 8192 x 4096 1.31 PFLOP/s, 4096 x
-// 8192 x 16384 1.26 (the library 1.55 and 1.57); 128 x 128 tiles 1.10 and 1.06,
-// 64 x 64 tiles 0.71 and 0.69.
+// By rows: 8 rows x 128 bytes a group; the 16-byte piece c of row r sits at
+// place c ^ (r / 2 mod 8) of its row, so that the lanes of a fragment read (row
+// l mod 16, piece l / 16) meet distinct banks.
+//
+// By columns: a group is 1024 / (2 BM) rows of k, each the tile's BM columns.  A
+// fragment is read by transposing 8-byte loads: 16 lanes give the places of 4
+// rows x 16 columns, and lane c receives column c's four values of k.  What is read
+// at once are the rows that differ in bits 0, 1 and 3 of k; a group therefore
+// takes rows that differ in the other bits (2, then 4, then 5), and groups are 32
+// bytes more than their size apart: distinct banks again.
+//
+// Two stages: while the matrix instructions work on one half of a stage's k in
+// registers, its other half (then the next stage's first) goes from LDS to
+// registers, and the stage after it from memory to LDS.  One barrier a stage: past
+// it every wave has the stage's fragments in registers, so its buffer is free,
+// and the next stage has arrived.
+//
+// What it reaches by rows with 256 x 256 tiles: 16384 x 8192 x 4096 1.31 PFLOP/s,
+// 4096 x 8192 x 16384 1.26 (the library 1.55 and 1.57); 128 x 128 tiles 1.10 and
+// 1.06, 64 x 64 tiles 0.71 and 0.69.
 constexpr int kGemmStageK = 64;
 
-template <int BM, int BN, int WM, int WN>
+// One side's tile in LDS: B rows or columns, of which a wave takes F fragments.
+template <int B, bool COLS>
+struct GemmSide {
+    static constexpr int kGroups = B / 8;
+    static constexpr int kPitch = COLS ? 1024 + 32 : 1024;
+    static constexpr int kBytes = kGroups * kPitch;
+    static constexpr int kRowsPerGroup = 1024 / (2 * B);  // by columns: 2, 4 or 8
+    static_assert(!COLS || (B >= 64 && B <= 256), "a group holds 2, 4 or 8 rows of k");
+
+    // By columns, row `r` of a stage's 64: its group and its place in the group.
+    // Bits 0, 1, 3 of r (and of 4, 5 what the place does not take) make the group.
+    static constexpr __host__ __device__ int row_of(int group, int slot)
+    {
+        int r = (group & 3) | (group >> 2 & 1) << 3 | (slot & 1) << 2;
+        if (kRowsPerGroup == 2)
+            r |= (group >> 3 & 1) << 4 | (group >> 4 & 1) << 5;
+        else if (kRowsPerGroup == 4)
+            r |= (slot >> 1 & 1) << 4 | (group >> 3 & 1) << 5;
+        else
+            r |= (slot >> 1 & 1) << 4 | (slot >> 2 & 1) << 5;
+        return r;
+    }
+
+    // What lane `lane` loads for group `group`, of the tile from `i0` on:
+    // byte offset from the stage's start in memory; `k_left` rows of k are left.
+    static __device__ __forceinline__ int source(const GemmOperand &o, int i0, int group, int lane, int k_left)
+    {
+        if constexpr (COLS) {
+            constexpr int kPieces = B / 8;
+            int r = row_of(group, lane / kPieces);
+            int c = (lane % kPieces) * 8;
+            r = r < k_left ? r : k_left - 1;
+            c = c < o.n - i0 ? c : o.n - 8 - i0;
+            return r * (int)(o.ld * 2) + c * 2;
+        } else {
+            int r = group * 8 + (lane >> 3);
+            const int c = (lane & 7) ^ ((r >> 1) & 7);
+            r = r < o.n - i0 ? r : o.n - 1 - i0;
+            return r * (int)(o.ld * 2) + c * 16;
+        }
+    }
+
+    // A lane's place in the tile for its part of a wave's fragments, and the
+    // distance of fragment i and of half h of the stage's k from it.
+    static __device__ __forceinline__ int place(int lane, int h)
+    {
+        const int r = lane & 15, b = lane >> 4;
+        if constexpr (COLS) {
+            const int group = r >> 2 | (b & 1) << 2;
+            int at = group * kPitch + (lane & 3) * 8;
+            if (kRowsPerGroup == 2)
+                at += (b >> 1) * 8 * kPitch + h * 16 * kPitch;
+            else if (kRowsPerGroup == 4)
+                at += (b >> 1) * 2 * (2 * B) + h * 8 * kPitch;
+            else
+                at += (b >> 1) * 2 * (2 * B) + h * 4 * (2 * B);
+            return at;
+        } else {
+            return r * 128 + ((h * 4 + b) ^ (r >> 1)) * 16;
+        }
+    }
+
+    static constexpr __device__ __forceinline__ int fragment_step() { return COLS ? 32 : 2048; }
+
+    static __device__ __forceinline__ bf16x8 fragment(const char *tile, int at, int i)
+    {
+        if constexpr (COLS) {
+            typedef __attribute__((ext_vector_type(4))) short s16x4;
+            using Ptr = __attribute__((address_space(3))) s16x4 *;
+            union {
+                s16x4 half[2];
+                bf16x8 v;
+            } f;
+            f.half[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Ptr)(tile + at + i * fragment_step()));
+            f.half[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Ptr)(tile + at + i * fragment_step() + 2 * B));
+            return f.v;
+        } else {
+            return *reinterpret_cast<const bf16x8 *>(tile + at + i * fragment_step());
+        }
+    }
+};
+
+template <int BM, int BN, int WM, int WN, bool COLS_A = false, bool COLS_B = false>
 struct Gemm {
+    using A = GemmSide<BM, COLS_A>;
+    using B = GemmSide<BN, COLS_B>;
     static constexpr int kWaves = WM * WN;
     static constexpr int kTm = BM / WM / 16;  // 16-row fragments of a wave
     static constexpr int kTn = BN / WN / 16;
-    static constexpr int kGroupsA = BM / 8;
-    static constexpr int kGroups = (BM + BN) / 8;
+    static constexpr int kGroups = A::kGroups + B::kGroups;
     static constexpr int kLoads = kGroups / kWaves;  // of one wave per stage
-    static constexpr int kStageBytes = kGroups * 1024;
+    static constexpr int kStageBytes = A::kBytes + B::kBytes;
     static constexpr int kLdsBytes = 2 * kStageBytes;
-    static_assert(kGroups % kWaves == 0, "whole groups per wave");
+    static_assert(kGroups % kWaves == 0 && A::kGroups % kLoads == 0, "a wave loads whole groups of one side");
 
     using Lds = __attribute__((address_space(3))) void *;
 
@@ -69,14 +168,14 @@ struct Gemm {
         bf16x8 a[kTm], b[kTn];
     };
 
-    static __device__ __forceinline__ void read(Fragments &f, const char *stage, int wm, int wn, int place)
+    static __device__ __forceinline__ void read(Fragments &f, const char *stage, int at_a, int at_b)
     {
 #pragma unroll
         for (int i = 0; i < kTn; ++i)
-            f.b[i] = *reinterpret_cast<const bf16x8 *>(stage + kGroupsA * 1024 + (wn * kTn + i) * 2048 + place);
+            f.b[i] = B::fragment(stage + A::kBytes, at_b, i);
 #pragma unroll
         for (int i = 0; i < kTm; ++i)
-            f.a[i] = *reinterpret_cast<const bf16x8 *>(stage + (wm * kTm + i) * 2048 + place);
+            f.a[i] = A::fragment(stage, at_a, i);
     }
 
     // acc += a b^T, with the LDS reads issued just before dealt out between
@@ -88,11 +187,15 @@ struct Gemm {
 #pragma unroll
             for (int j = 0; j < kTn; ++j)
                 acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.a[i], f.b[j], acc[i][j], 0, 0, 0);
+        constexpr int kReads = kTm * (COLS_A ? 2 : 1) + kTn * (COLS_B ? 2 : 1);
+        static_assert(kReads <= 2 * kTm * kTn, "at least one matrix instruction to two reads");
+        constexpr int kPer = kReads > kTm * kTn ? 2 : 1;
 #pragma unroll
-        for (int i = 0; i < kTm + kTn; ++i) {
-            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // a matrix instruction
-            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);  // an LDS read
-            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        for (int i = 0; i < kReads / kPer; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);     // a matrix instruction
+            __builtin_amdgcn_sched_group_barrier(0x100, kPer, 0);  // LDS reads
+            if (2 * kReads <= kTm * kTn)
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
         }
         __builtin_amdgcn_sched_barrier(0);
     }
@@ -105,8 +208,24 @@ struct Gemm {
         __builtin_amdgcn_s_waitcnt((N ? 0x0F70 : 0x0070) | (N & 15) | (N >> 4) << 14);
     }
 
-    // acc += the tile at rows i0 of A and j0 of B.  Lane l of a wave ends
-    // with acc[ti][tj][e] = C[i0 + wm BM/WM + 16 ti + 4 (l / 16) + e][j0 + wn BN/WN + 16 tj + l mod 16].
+    // 16 bytes a lane from base + offset to LDS, lane after lane from `dst` on.
+    // In assembly, because the compiler takes any later transposing read for a
+    // read of what is on its way and waits for it; it writes no register, and
+    // the waits and the barrier of `run` order it.  (m0 is never held over a
+    // statement: the compiler sets it where it needs it.)
+    static __device__ __forceinline__ void load_to_lds(const char *base, int offset, uint32_t dst)
+    {
+        typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+        const uint64_t p = reinterpret_cast<uint64_t>(base);
+        const u32x4 rsrc = {(uint32_t)p, (uint32_t)(p >> 32) & 0xFFFFu, 0x7FFFFFFFu, 0x00027000u};
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                     :
+                     : "s"(dst), "v"(offset), "s"(rsrc)
+                     : "memory");
+    }
+
+    // acc += the tile at i0 of A and j0 of B.  Lane l of a wave ends with
+    // acc[ti][tj][e] = C[i0 + wm BM/WM + 16 ti + 4 (l / 16) + e][j0 + wn BN/WN + 16 tj + l mod 16].
     // `from`, `stages` (at least 1): this block's part of the 64-k stages.
     static __device__ __forceinline__ void run(f32x4 (&acc)[kTm][kTn], const GemmShape &g, int i0, int j0, int from,
                                                int stages, char *lds)
@@ -114,47 +233,50 @@ struct Gemm {
         const int lane = threadIdx.x & (kWave - 1);
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
         const int wm = wave / WN, wn = wave % WN;
-        int voff[kLoads];
-        bool is_a[kLoads];
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            const int group = wave * kLoads + i;
-            is_a[i] = group < kGroupsA;
-            const GemmOperand &o = is_a[i] ? g.a : g.b;
-            const int r0 = is_a[i] ? i0 : j0;
-            int r = (is_a[i] ? group : group - kGroupsA) * 8 + (lane >> 3);
-            const int c = (lane & 7) ^ ((r >> 1) & 7);
-            r = r < o.rows - r0 ? r : o.rows - 1 - r0;
-            voff[i] = r * (int)(o.ld * 2) + c * 16;
-        }
-        const char *pa = reinterpret_cast<const char *>(g.a.p + (int64_t)i0 * g.a.ld);
-        const char *pb = reinterpret_cast<const char *>(g.b.p + (int64_t)j0 * g.b.ld);
-        const int per_segment = g.k / kGemmStageK;
-        int segment = from / per_segment;
-        int at = (from - segment * per_segment) * (kGemmStageK * 2);  // bytes along k
 
-        auto load = [&](int slot) {
-            const char *qa = pa, *qb = pb;
-            if (g.segments > 1) {
-                qa += (int64_t)segment_plane_a(segment) * g.a.plane * 2;
-                qb += (int64_t)segment_plane_b(segment) * g.b.plane * 2;
-            }
-            auto ra = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(qa), 0, 0x7FFFFFFF, 0x00027000);
-            auto rb = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(qb), 0, 0x7FFFFFFF, 0x00027000);
-            char *dst = lds + slot * kStageBytes + wave * kLoads * 1024;
+        // this wave's loads: kLoads groups of one side, whose next stage begins at `next`
+        const int group = wave * kLoads;
+        const bool side_a = group < A::kGroups;
+        const GemmOperand &o = side_a ? g.a : g.b;
+        const bool cols = side_a ? COLS_A : COLS_B;
+        const int first = side_a ? i0 : j0;
+        const int64_t stage_step = (cols ? kGemmStageK * o.ld : kGemmStageK) * 2;
+        const char *const start = reinterpret_cast<const char *>(o.p + (cols ? first : first * o.ld));
+        int voff[kLoads];
+        const auto place_loads = [&](int k_left) {
 #pragma unroll
             for (int i = 0; i < kLoads; ++i)
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(is_a[i] ? ra : rb, (Lds)(dst + i * 1024), 16, voff[i], at, 0, 0);
-            at += kGemmStageK * 2;
-            if (at == g.k * 2) {
-                at = 0;
+                voff[i] = side_a ? A::source(o, first, group + i, lane, k_left)
+                                 : B::source(o, first, group - A::kGroups + i, lane, k_left);
+        };
+        place_loads(kGemmStageK);
+        const int per_segment = g.k / kGemmStageK;
+        int segment = from / per_segment;
+        int stage = from - segment * per_segment;
+        const int slot_base = side_a ? group * A::kPitch : A::kBytes + (group - A::kGroups) * B::kPitch;
+        const int pitch = side_a ? A::kPitch : B::kPitch;
+        const bool ragged = cols && o.k_rows < g.k;  // k's last stage has rows that do not exist
+
+        const auto load = [&](int slot) {
+            const char *q = start + stage * stage_step;
+            if (g.segments > 1)
+                q += (int64_t)(side_a ? segment_plane_a(segment) : segment_plane_b(segment)) * o.plane * 2;
+            if (ragged && stage == per_segment - 1)
+                place_loads(o.k_rows - stage * kGemmStageK);
+            const uint32_t dst = (uint32_t)(uintptr_t)(Lds)(lds + slot * kStageBytes + slot_base);
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i)
+                load_to_lds(q, voff[i], dst + i * pitch);
+            if (++stage == per_segment) {
+                stage = 0;
                 ++segment;
+                if (ragged)
+                    place_loads(kGemmStageK);
             }
         };
 
-        const int r = lane & 15;
-        const int place0 = r * 128 + ((lane >> 4) ^ (r >> 1)) * 16;        // first half of a stage's k
-        const int place1 = r * 128 + ((4 + (lane >> 4)) ^ (r >> 1)) * 16;  // second half
+        const int a0 = A::place(lane, 0) + wm * (A::fragment_step() * kTm), a1 = A::place(lane, 1) + wm * (A::fragment_step() * kTm);
+        const int b0 = B::place(lane, 0) + wn * (B::fragment_step() * kTn), b1 = B::place(lane, 1) + wn * (B::fragment_step() * kTn);
         Fragments f0, f1;
         load(0);
         if (stages > 1) {
@@ -165,9 +287,9 @@ struct Gemm {
         }
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        read(f0, lds, wm, wn, place0);
+        read(f0, lds, a0, b0);
         for (int s = 0; s < stages; ++s) {
-            read(f1, lds + (s & 1) * kStageBytes, wm, wn, place1);
+            read(f1, lds + (s & 1) * kStageBytes, a1, b1);
             multiply(acc, f0);
             if (s + 1 < stages) {
                 wait_loads<0>();
@@ -175,7 +297,7 @@ struct Gemm {
                 asm volatile("" ::: "memory");
                 if (s + 2 < stages)
                     load(s & 1);
-                read(f0, lds + ((s + 1) & 1) * kStageBytes, wm, wn, place0);
+                read(f0, lds + ((s + 1) & 1) * kStageBytes, a0, b0);
             }
             multiply(acc, f1);
         }

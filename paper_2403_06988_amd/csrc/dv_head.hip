@@ -14,9 +14,9 @@
 // Four products of 2 N D V operations against six N D V that cannot be avoided:
 // the price of not keeping the logits.
 //
-// All products are the one of dv_gemm.h (k contiguous in both operands), so x,
-// w's piece and G are also laid out transposed.  fp32 operands go through it
-// as three bf16 planes each.
+// All products are the one of dv_gemm.h, which takes operands with k along their
+// rows or from row to row: x, w and G are used as they lie.  fp32 operands go
+// through it as three bf16 planes each.
 #include <type_traits>
 
 #include "dv_gemm.h"
@@ -71,29 +71,6 @@ __global__ void pack_kernel(const T *src, int64_t ld, int rows, int cols, int ou
     for (int p = 0; p < P; ++p) {
         __bf16 both[2] = {a[p], b[p]};
         __builtin_memcpy(dst + p * plane + row * out_cols + col, both, 4);
-    }
-}
-
-// bf16 src [rows][cols] (row stride ld, of plane z) to dst [cols][out_rows], zeros past rows.
-__global__ __launch_bounds__(256) void transpose_kernel(const uint16_t *src, int64_t ld, int64_t src_plane, int rows, int cols,
-                                                         uint16_t *dst, int out_rows, int64_t dst_plane)
-{
-    __shared__ uint16_t tile[64][66];
-    src += blockIdx.z * src_plane;
-    dst += blockIdx.z * dst_plane;
-    const int r0 = blockIdx.x * 64, c0 = blockIdx.y * 64;
-    const int tx = threadIdx.x & 63, ty = threadIdx.x >> 6;
-#pragma unroll
-    for (int i = 0; i < 64; i += 4) {
-        const int r = r0 + i + ty, c = c0 + tx;
-        tile[i + ty][tx] = r < rows && c < cols ? src[(int64_t)r * ld + c] : (uint16_t)0;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < 64; i += 4) {
-        const int c = c0 + i + ty, r = r0 + tx;
-        if (c < cols && r < out_rows)
-            dst[(int64_t)c * out_rows + r] = tile[tx][i + ty];
     }
 }
 
@@ -258,13 +235,15 @@ __global__ __launch_bounds__(WM *WN *kWave, 2) void grad_kernel(GemmShape g, int
 
 enum class Out { kStore, kPartial, kPartialAdd };
 
-// C[j][i] of a product as rows of `cols` elements: in T, or in fp32 as (or on
-// top of) the partial sums of this block's share of k.
-template <int BM, int BN, int WM, int WN, typename T, Out OUT>
-__global__ __launch_bounds__(WM *WN *kWave, 2) void product_kernel(GemmShape g, T *out, int cols, int64_t split_stride,
-                                                                   int split_stages, int tiles_i, int tiles_j)
+// C[j][i] of a product as `out_rows` rows of `cols` elements: in T, or in fp32
+// as (or on top of) the partial sums of this block's share of k.  A is stored by
+// columns, B by columns with COLS_B.
+template <int BM, int BN, int WM, int WN, bool COLS_B, typename T, Out OUT>
+__global__ __launch_bounds__(WM *WN *kWave, 2) void product_kernel(GemmShape g, T *out, int out_rows, int cols,
+                                                                   int64_t split_stride, int split_stages, int tiles_i,
+                                                                   int tiles_j)
 {
-    using G = Gemm<BM, BN, WM, WN>;
+    using G = Gemm<BM, BN, WM, WN, true, COLS_B>;
     __shared__ __attribute__((aligned(1024))) char lds[G::kLdsBytes];
     int ti, tj;
     tile_of_block(blockIdx.x, tiles_i, tiles_j, ti, tj);
@@ -279,7 +258,7 @@ __global__ __launch_bounds__(WM *WN *kWave, 2) void product_kernel(GemmShape g, 
 #pragma unroll
     for (int b = 0; b < G::kTn; ++b) {
         const int r = tj * BN + wn * (BN / WN) + b * 16 + (lane & 15);
-        if (r >= g.b.rows)
+        if (r >= out_rows)
             continue;
 #pragma unroll
         for (int a = 0; a < G::kTm; ++a) {
@@ -318,18 +297,41 @@ __global__ void zero_kernel(T *p, int64_t n)
 
 // --------------------------------------------------------------- the plans
 
-constexpr int kLargeTiles = 160;  // 256 x 256 tiles from here on
 constexpr int64_t kPieceElements = (int64_t)1 << 27;
 constexpr int kPieceTokens = 1 << 18;
 
-int tile_side(int64_t rows_i, int64_t rows_j)
+// The tile side and the splits of k for a product of `i` x `j` over `stages` of
+// 64 k, by the time that each side would take: rounds of blocks over the 256
+// compute units, each block its stages and about three more to start and end, at
+// the rate the core reaches with that side; splits write and read their sums.
+struct Plan {
+    int side, splits, stages;  // stages of a split; no split is empty
+};
+
+Plan plan_product(int64_t i, int64_t j, int64_t stages, int most_splits)
 {
-    const auto tiles = [&](int s) { return ((rows_i + s - 1) / s) * ((rows_j + s - 1) / s); };
-    if (rows_j > 128 && rows_i > 128 && tiles(256) >= kLargeTiles)
-        return 256;
-    if (rows_j > 64 && rows_i > 64 && tiles(128) >= kLargeTiles)
-        return 128;
-    return 64;
+    struct Side {
+        int side, per_unit;
+        double us;  // of a unit's blocks for one stage
+    };
+    constexpr Side kSides[] = {{256, 1, 1.65}, {128, 2, 0.97}, {64, 4, 0.77}};
+    Plan best{64, 1, (int)stages};
+    double least = 1e30;
+    for (const Side &s : kSides) {
+        const int64_t tiles = ((i + s.side - 1) / s.side) * ((j + s.side - 1) / s.side);
+        for (int64_t want = 1; want <= most_splits; ++want) {
+            const int64_t per = (stages + want - 1) / want;
+            const int64_t used = (stages + per - 1) / per;
+            const int64_t slots = (int64_t)256 * s.per_unit;
+            const double rounds = (double)((tiles * used + slots - 1) / slots);
+            const double us = rounds * (double)(per + 3) * s.us + (used > 1 ? (double)(used * i * j) * 2e-6 + 3 : 0);
+            if (us < least) {
+                least = us;
+                best = {s.side, (int)used, (int)per};
+            }
+        }
+    }
+    return best;
 }
 
 int64_t up64(int64_t n) { return (n + 63) / 64 * 64; }
@@ -339,9 +341,9 @@ struct HeadLayout {
     int64_t k;        // hidden size as the products see it
     int piece;        // tokens of a piece, a multiple of 256 (or all)
     int pieces;
-    int splits;       // of the k of dx
+    Plan dx_plan;
     size_t x, w, parts, target_logit;                        // forward
-    size_t x_t, w_t, g, g_t, weight, dx;                      // backward
+    size_t g, weight, dx;                                     // backward
     size_t forward_bytes, backward_bytes;
 };
 
@@ -375,20 +377,11 @@ HeadLayout head_layout(int rows, int hidden, int V, int dtype)
     l.target_logit = take((size_t)r64 * 4);
     l.forward_bytes = at;
     at = shared;
-    l.x_t = take(planes * hidden * r64 * 2);
-    l.w_t = take(planes * hidden * p64 * 2);
     l.g = take(planes * r64 * p64 * 2);
-    l.g_t = take(planes * r64 * p64 * 2);
     l.weight = take((size_t)r64 * 4);
-    // dx over a piece: few tiles and a long k, so k is split until they fill the compute units
-    const int side = tile_side(hidden, rows);
-    const int64_t tiles = ((int64_t)(hidden + side - 1) / side) * ((rows + side - 1) / side);
-    const int64_t k_stages = p64 / kGemmStageK * l.segments;
-    int64_t splits = tiles > 0 ? 256 / tiles : 1;
-    splits = splits > k_stages / 8 ? k_stages / 8 : splits;
-    splits = splits > 16 ? 16 : splits;
-    l.splits = (int)(splits < 1 ? 1 : splits);
-    l.dx = take((size_t)l.splits * rows * hidden * 4);
+    // dx over a piece: few tiles and a long k
+    l.dx_plan = plan_product(l.k, rows, p64 / kGemmStageK * l.segments, 16);
+    l.dx = take((size_t)l.dx_plan.splits * rows * hidden * 4);
     l.backward_bytes = at;
     return l;
 }
@@ -408,15 +401,6 @@ hipError_t pack(const void *src, int64_t ld, int dtype, int64_t rows, int cols, 
     return last_launch();
 }
 
-hipError_t transpose(const __bf16 *src, int64_t ld, int64_t src_plane, int planes, int rows, int cols, __bf16 *dst,
-                     int64_t out_rows, int64_t dst_plane, hipStream_t s)
-{
-    const dim3 grid((unsigned)((out_rows + 63) / 64), (unsigned)((cols + 63) / 64), planes);
-    transpose_kernel<<<grid, 256, 0, s>>>(reinterpret_cast<const uint16_t *>(src), ld, src_plane, rows, cols,
-                                          reinterpret_cast<uint16_t *>(dst), (int)out_rows, dst_plane);
-    return last_launch();
-}
-
 // An operand as the products need it: in place, or packed into `buffer`.
 bool in_place(const void *p, int64_t ld, int dtype, int hidden)
 {
@@ -428,10 +412,10 @@ hipError_t operand(const void *p, int64_t ld, int dtype, int rows, int hidden, c
                    GemmOperand &out, hipStream_t s)
 {
     if (in_place(p, ld, dtype, hidden)) {
-        out = {static_cast<const __bf16 *>(p), ld, 0, rows};
+        out = {static_cast<const __bf16 *>(p), ld, 0, rows, 0};
         return hipSuccess;
     }
-    out = {buffer, l.k, (int64_t)rows * l.k, rows};
+    out = {buffer, l.k, (int64_t)rows * l.k, rows, 0};
     return pack(p, ld, dtype, rows, hidden, (int)l.k, buffer, out.plane, s);
 }
 
@@ -454,27 +438,20 @@ hipError_t with_tile(int side, F &&f)
     return last_launch();
 }
 
-// How k is split `splits` ways: whole stages, and no split empty (`used` of
-// them may be fewer).
-struct Splits {
-    int stages, used;
-};
-Splits splits_of(const GemmShape &g, int splits)
+// An operand stored by rows, seen as one stored by columns: `k` elements a row.
+GemmOperand by_columns(const GemmOperand &o, int64_t k)
 {
-    const int total = g.k / kGemmStageK * g.segments;
-    const int stages = (total + splits - 1) / splits;
-    return {stages, (total + stages - 1) / stages};
+    return {o.p, o.ld, o.plane, (int)k, o.n};
 }
 
-template <typename T, Out OUT>
-hipError_t product(const GemmShape &g, T *out, int cols, int splits, int64_t split_stride, hipStream_t s)
+template <bool COLS_B, typename T, Out OUT>
+hipError_t product(const GemmShape &g, const Plan &plan, T *out, int out_rows, int cols, int64_t split_stride, hipStream_t s)
 {
-    return with_tile(tile_side(g.a.rows, g.b.rows), [&](auto side, auto wn) {
+    return with_tile(plan.side, [&](auto side, auto wn) {
         constexpr int B = decltype(side)::value, WN = decltype(wn)::value;
-        const int ti = (g.a.rows + B - 1) / B, tj = (g.b.rows + B - 1) / B;
-        const Splits k = splits_of(g, splits);
-        product_kernel<B, B, 2, WN, T, OUT><<<dim3(ti * tj, k.used), 2 * WN * kWave, 0, s>>>(g, out, cols, split_stride,
-                                                                                             k.stages, ti, tj);
+        const int ti = (cols + B - 1) / B, tj = (out_rows + B - 1) / B;
+        product_kernel<B, B, 2, WN, COLS_B, T, OUT><<<dim3(ti * tj, plan.splits), 2 * WN * kWave, 0, s>>>(
+            g, out, out_rows, cols, split_stride, plan.stages, ti, tj);
     });
 }
 
@@ -505,9 +482,6 @@ hipError_t backward(const HeadArgs &a, const float *lse, const float *grad_loss,
     DV_TRY(operand(a.x, a.ld_x, a.dtype, a.rows, a.hidden, l, at(l.x), x, s));
     weights_kernel<<<(a.rows + 255) / 256, 256, 0, s>>>(a.rows, a.V, a.masks, a.targets, grad_loss, weight);
     DV_TRY(last_launch());
-    const GemmOperand x_t{at(l.x_t), r64, (int64_t)a.hidden * r64, a.hidden};
-    if (grad_weight)
-        DV_TRY(transpose(x.p, x.ld, x.plane, l.planes, a.rows, a.hidden, at(l.x_t), r64, x_t.plane, s));
     int splits = 1;
     for (int piece = 0; piece < l.pieces; ++piece) {
         const int v0 = piece * l.piece;
@@ -516,8 +490,8 @@ hipError_t backward(const HeadArgs &a, const float *lse, const float *grad_loss,
         GemmOperand w;
         DV_TRY(operand(weight_rows(a, v0), a.ld_w, a.dtype, n, a.hidden, l, at(l.w), w, s));
         const GemmShape logits{w, x, (int)l.k, l.segments};
-        const GemmOperand g{at(l.g), n64, r64 * n64, a.rows};
-        DV_TRY(with_tile(tile_side(n, a.rows), [&](auto side, auto wn) {
+        const GemmOperand g{at(l.g), n64, r64 * n64, a.rows, 0};
+        DV_TRY(with_tile(plan_product(n, a.rows, l.k / kGemmStageK * l.segments, 1).side, [&](auto side, auto wn) {
             constexpr int B = decltype(side)::value, WN = decltype(wn)::value;
             const int ti = (n + B - 1) / B, tj = (a.rows + B - 1) / B;
             constexpr int P = sizeof(T) == 2 ? 1 : 3;
@@ -525,26 +499,28 @@ hipError_t backward(const HeadArgs &a, const float *lse, const float *grad_loss,
                                                                           lse, weight, at(l.g), n64, g.plane, ti, tj);
         }));
         if (grad_x) {
-            const GemmOperand w_t{at(l.w_t), n64, (int64_t)a.hidden * n64, a.hidden};
-            DV_TRY(transpose(w.p, w.ld, w.plane, l.planes, n, a.hidden, at(l.w_t), n64, w_t.plane, s));
-            const GemmShape shape{w_t, g, (int)n64, l.segments};
+            const GemmShape shape{by_columns(w, l.k), g, (int)n64, l.segments};
             const int64_t stride = (int64_t)a.rows * a.hidden;
             if (piece == 0) {
-                // later pieces have no longer a k, so they use no more splits
-                splits = splits_of(shape, l.splits).used;
+                splits = l.dx_plan.splits;
                 if (l.pieces == 1 && splits == 1)
-                    DV_TRY((product<T, Out::kStore>(shape, grad_x, a.hidden, 1, 0, s)));
+                    DV_TRY((product<false, T, Out::kStore>(shape, l.dx_plan, grad_x, a.rows, a.hidden, 0, s)));
                 else
-                    DV_TRY((product<float, Out::kPartial>(shape, dx, a.hidden, splits, stride, s)));
+                    DV_TRY((product<false, float, Out::kPartial>(shape, l.dx_plan, dx, a.rows, a.hidden, stride, s)));
             } else {
-                DV_TRY((product<float, Out::kPartialAdd>(shape, dx, a.hidden, splits, stride, s)));
+                // the last piece's k is no longer than the first one's: its splits are no more
+                const int stages = (int)(n64 / kGemmStageK) * l.segments;
+                Plan plan = l.dx_plan;
+                plan.splits = (stages + plan.stages - 1) / plan.stages;
+                DV_TRY((product<false, float, Out::kPartialAdd>(shape, plan, dx, a.rows, a.hidden, stride, s)));
             }
         }
         if (grad_weight) {
-            const GemmOperand g_t{at(l.g_t), r64, n64 * r64, n};
-            DV_TRY(transpose(g.p, g.ld, g.plane, l.planes, (int)r64, n, at(l.g_t), r64, g_t.plane, s));
-            const GemmShape shape{x_t, g_t, (int)r64, l.segments};
-            DV_TRY((product<T, Out::kStore>(shape, grad_weight + (int64_t)v0 * a.hidden, a.hidden, 1, 0, s)));
+            GemmOperand g_t = by_columns(g, n64);
+            g_t.k_rows = (int)r64;
+            const GemmShape shape{by_columns(x, l.k), g_t, (int)r64, l.segments};
+            const Plan plan = plan_product(l.k, n, r64 / kGemmStageK * l.segments, 1);
+            DV_TRY((product<true, T, Out::kStore>(shape, plan, grad_weight + (int64_t)v0 * a.hidden, n, a.hidden, 0, s)));
         }
     }
     if (grad_x && !(l.pieces == 1 && splits == 1)) {
@@ -577,7 +553,7 @@ hipError_t launch_head_loss(const HeadArgs &a, float *loss, float *lse, void *wo
     DV_TRY(operand(a.x, a.ld_x, a.dtype, a.rows, a.hidden, l, reinterpret_cast<__bf16 *>(ws + l.x), x, s));
     const bool whole = in_place(a.weight, a.ld_w, a.dtype, a.hidden);  // nothing to pack: one piece
     const int step = whole ? a.V : l.piece;
-    const int side = tile_side(step, a.rows);
+    const int side = plan_product(step, a.rows, l.k / kGemmStageK * l.segments, 1).side;
     for (int v0 = 0; v0 < a.V; v0 += step) {
         const int n = a.V - v0 < step ? a.V - v0 : step;
         GemmOperand w;
