@@ -96,6 +96,18 @@ __device__ __forceinline__ uint16_t narrow(float x)
     return c.u;
 }
 
+// Two at once, the first in the low half.
+__device__ __forceinline__ uint32_t narrow_pair(float lo, float hi)
+{
+    typedef __attribute__((ext_vector_type(2))) __bf16 Pair;
+    union {
+        Pair b;
+        uint32_t u;
+    } c;
+    c.b = Pair{(__bf16)lo, (__bf16)hi};
+    return c.u;
+}
+
 inline hipError_t last_launch() { return hipGetLastError(); }
 
 // --------------------------------------------------------------- head loss
