@@ -128,8 +128,14 @@ def _ptr(t) -> int | None:
     return None if t is None else t.data_ptr()
 
 
+# the current stream's handle without a Stream object around it (2 us of a call)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream(stream, device) -> int:
     if stream is None:
+        if _raw_stream is not None and device.index is not None:
+            return _raw_stream(device.index)
         stream = torch.cuda.current_stream(device)
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 

@@ -16,8 +16,8 @@
 namespace dv {
 namespace {
 
-constexpr int kThreads = 512;  // of the blocks that share a row, or pass over it twice
-constexpr int kMaxWaves = 1024 / kWave;
+constexpr int kThreads = 512;
+constexpr int kWaves = kThreads / kWave;
 constexpr int kMaxTop = 1024;
 
 // Vectors of 16 bytes at any element's alignment.  The gradient's are stored
@@ -91,13 +91,13 @@ struct Vec<uint16_t> {
 };
 
 struct Shared {
-    float wave_a[kMaxWaves], wave_b[kMaxWaves];
+    float wave_a[kWaves], wave_b[kWaves];
     int id[kMaxTop];
     float q[kMaxTop];
     float z[kMaxTop];
 };
 
-// Over the block's waves: sums and maxima in every lane.
+// Over the block's waves, in every lane.
 __device__ __forceinline__ float block_sum(float v, Shared &sh)
 {
     v = wave_sum(v);
@@ -106,25 +106,29 @@ __device__ __forceinline__ float block_sum(float v, Shared &sh)
         sh.wave_a[threadIdx.x / kWave] = v;
     __syncthreads();
     float t = 0.f;
-    for (int i = 0; i < (int)blockDim.x / kWave; ++i)
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i)
         t += sh.wave_a[i];
     return t;
 }
 
 __device__ __forceinline__ Softmax block_join(Softmax v, float c2, Shared &sh)
 {
-#pragma unroll
-    for (int d = 32; d; d >>= 1)
-        v = softmax_join(v, {__shfl_xor(v.max, d), __shfl_xor(v.sum, d)}, c2);
+    const float top = wave_max(v.max);
+    const float sum = wave_sum(v.max == -INFINITY ? v.sum : v.sum * softmax_term(v.max, top, c2));
     __syncthreads();
     if ((threadIdx.x & (kWave - 1)) == 0) {
-        sh.wave_a[threadIdx.x / kWave] = v.max;
-        sh.wave_b[threadIdx.x / kWave] = v.sum;
+        sh.wave_a[threadIdx.x / kWave] = top;
+        sh.wave_b[threadIdx.x / kWave] = sum;
     }
     __syncthreads();
-    Softmax t{sh.wave_a[0], sh.wave_b[0]};
-    for (int i = 1; i < (int)blockDim.x / kWave; ++i)
-        t = softmax_join(t, {sh.wave_a[i], sh.wave_b[i]}, c2);
+    Softmax t{-INFINITY, 0.f};
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i)
+        t.max = fmaxf(t.max, sh.wave_a[i]);
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i)
+        t.sum += sh.wave_a[i] == -INFINITY ? sh.wave_b[i] : sh.wave_b[i] * softmax_term(sh.wave_a[i], t.max, c2);
     return t;
 }
 
@@ -133,7 +137,7 @@ __device__ __forceinline__ Softmax block_join(Softmax v, float c2, Shared &sh)
 __device__ __forceinline__ Softmax teacher(const DistillArgs &a, const RowMask &m, int row, float c2, Shared &sh)
 {
     Softmax own{-INFINITY, 0.f};
-    for (int k = threadIdx.x; k < a.K; k += blockDim.x) {
+    for (int k = threadIdx.x; k < a.K; k += kThreads) {
         const int id = a.ids[(size_t)row * a.K + k];
         const float t = a.top[(size_t)row * a.K + k];
         const bool in = m.has(id) && t != -INFINITY;
@@ -143,7 +147,7 @@ __device__ __forceinline__ Softmax teacher(const DistillArgs &a, const RowMask &
             own = softmax_join(own, {t, 1.f}, c2);
     }
     const Softmax all = block_join(own, c2, sh);
-    for (int k = threadIdx.x; k < a.K; k += blockDim.x)
+    for (int k = threadIdx.x; k < a.K; k += kThreads)
         sh.q[k] = sh.id[k] < 0 ? 0.f : softmax_term(sh.q[k], all.max, c2) / all.sum;
     return all;
 }
@@ -264,7 +268,7 @@ __device__ __forceinline__ float row_loss(const DistillArgs &a, int row, Softmax
     const float c = a.inv_temperature;
     const float lnt = logf(t.sum), lns = logf(s.sum);
     float sum = 0.f;
-    for (int k = threadIdx.x; k < a.K; k += blockDim.x) {
+    for (int k = threadIdx.x; k < a.K; k += kThreads) {
         const float q = sh.q[k];
         if (!(q == 0.f))  // NaN counts
             sum += q * (((a.top[(size_t)row * a.K + k] - t.max) * c - lnt) - ((sh.z[k] - s.max) * c - lns));
@@ -280,7 +284,7 @@ __device__ __forceinline__ void listed_grad(T *grad, int from, int to, float c2,
                                             Shared &sh)
 {
     __syncthreads();
-    for (int k = threadIdx.x; k < K; k += blockDim.x) {
+    for (int k = threadIdx.x; k < K; k += kThreads) {
         const int id = sh.id[k];
         if (id < from || id >= to)
             continue;
@@ -346,7 +350,7 @@ __global__ __launch_bounds__(kThreads) void distill_row_kernel(DistillArgs a, co
     const RowMask m(a.masks, a.V, row);
     const T *z = static_cast<const T *>(a.logits) + (size_t)row * a.ld;
     const Softmax t = teacher(a, m, row, c2, sh);
-    for (int k = threadIdx.x; k < a.K; k += blockDim.x)
+    for (int k = threadIdx.x; k < a.K; k += kThreads)
         sh.z[k] = sh.id[k] < 0 ? 0.f : Vec<T>::one(z + sh.id[k]);
     Softmax s{-INFINITY, 0.f};
     bool part = !m.dead && !t.empty();
@@ -375,7 +379,7 @@ __global__ __launch_bounds__(kThreads) void distill_stats_kernel(DistillArgs a, 
     const T *z = static_cast<const T *>(a.logits) + (size_t)row * a.ld;
     const int from = c * chunk, to = a.V - from < chunk ? a.V : from + chunk;
     if (c == 0)
-        for (int k = threadIdx.x; k < a.K; k += blockDim.x) {
+        for (int k = threadIdx.x; k < a.K; k += kThreads) {
             const int id = a.ids[(size_t)row * a.K + k];
             listed[(size_t)row * a.K + k] = m.has(id) ? Vec<T>::one(z + id) : 0.f;
         }
@@ -398,7 +402,7 @@ __global__ __launch_bounds__(kThreads) void distill_finish_kernel(DistillArgs a,
     const float c2 = a.inv_temperature * kLog2e;
     const RowMask m(a.masks, a.V, row);
     const Softmax t = teacher(a, m, row, c2, sh);
-    for (int k = threadIdx.x; k < a.K; k += blockDim.x)
+    for (int k = threadIdx.x; k < a.K; k += kThreads)
         sh.z[k] = listed[(size_t)row * a.K + k];
     Softmax s{-INFINITY, 0.f};
     for (int i = threadIdx.x; i < chunks; i += kThreads)
@@ -422,15 +426,22 @@ struct Split {
     int chunk, chunks;  // tokens of a chunk (a multiple of 8), chunks of a row
 };
 
-// Rows are split until the launch has two blocks a compute unit, each with at
-// least one pass of its lanes' vectors.
+// A row is one block's when rows are many or short: a split row costs a second
+// launch and the chunks' meeting (us a call, whole rows and split ones, loss and
+// gradient: 40 x 64,000 bf16 12.6 and 14.4, 40 x 128,256 18.5 and 14.3, 100 x 128,256
+// 20.9 and 17.3, 200 x 128,256 29.1 and 31.1; the loss alone: 40 x 128,256 10.8 and
+// 12.7, 8 x 256,000 16.7 and 12.5).  Else rows are split until the launch has two
+// blocks a compute unit, each with at least one pass of its lanes' vectors.
 constexpr int kSplitBlocks = 512;
-constexpr int kWholeRows = 256;
+constexpr int kWholeRows = 160;
 
-Split split_of(int rows, int V, int dtype)
+Split split_of(int rows, int V, int dtype, bool grad)
 {
+    const int64_t row_bytes = (int64_t)V * (dtype == 1 ? 2 : 4);
     const int pass = kThreads * (dtype == 1 ? 8 : 4);
-    int want = rows >= kWholeRows || rows < 1 ? 1 : kSplitBlocks / rows;
+    int want = kSplitBlocks / (rows > 0 ? rows : 1);
+    if (rows >= kWholeRows || row_bytes <= (grad ? 131072 : 262144))
+        want = 1;
     const int most = V / pass > 1 ? V / pass : 1;
     want = want < most ? want : most;
     int chunk = (int)align_up((size_t)(V + want - 1) / want, 8);
@@ -441,7 +452,7 @@ template <typename T, bool MASK>
 hipError_t launch(const DistillArgs &a, const float *grad_loss, float *loss, T *grad, int64_t ld_grad, void *workspace,
                   hipStream_t stream)
 {
-    const Split s = split_of(a.rows, a.V, a.dtype);
+    const Split s = split_of(a.rows, a.V, a.dtype, grad != nullptr);
     if (s.chunks == 1) {
         if (grad)
             distill_row_kernel<T, MASK, true><<<a.rows, kThreads, 0, stream>>>(a, grad_loss, loss, grad, ld_grad);

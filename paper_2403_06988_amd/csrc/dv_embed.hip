@@ -14,10 +14,33 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// Elements of one lane: as many bytes as row starts share alignment with.
-template <typename T, int N>
+// Elements of one lane, 16 bytes from any element on; rows end where they end, so
+// a row's last lane may hold fewer (`n` of them).
+template <typename T>
 struct Pack {
-    T x[N];
+    static constexpr int kN = 16 / sizeof(T);
+    T x[kN];
+    __device__ __forceinline__ void load(const T *p, int n)
+    {
+        if (n >= kN) {
+            __builtin_memcpy(x, p, 16);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kN; ++i)
+                x[i] = i < n ? p[i] : T(0);
+        }
+    }
+    __device__ __forceinline__ void store(T *p, int n) const
+    {
+        if (n >= kN) {
+            __builtin_memcpy(p, x, 16);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kN; ++i)
+                if (i < n)
+                    p[i] = x[i];
+        }
+    }
 };
 
 __device__ __forceinline__ float to_float(float x) { return x; }
@@ -25,44 +48,37 @@ __device__ __forceinline__ float to_float(uint16_t x) { return widen(x); }
 __device__ __forceinline__ void from_float(float y, float &x) { x = y; }
 __device__ __forceinline__ void from_float(float y, uint16_t &x) { x = narrow(y); }
 
-template <typename T, int N>
-__device__ __forceinline__ Pack<T, N> load_pack(const T *p)
-{
-    Pack<T, N> v;
-    __builtin_memcpy(&v, p, sizeof v);
-    return v;
-}
-template <typename T, int N>
-__device__ __forceinline__ void store_pack(T *p, const Pack<T, N> &v)
-{
-    __builtin_memcpy(p, &v, sizeof v);
-}
-
-// A lane group of 2^lanes_log2 lanes copies one row, N elements a lane at a
-// time (the last lanes of a row that N does not divide go one by one).
-template <typename T, int N>
+// A lane group of 2^lanes_log2 lanes copies ROWS rows at once, `step` apart.
+template <typename T, int ROWS>
 __global__ __launch_bounds__(kThreads) void embed_kernel(const T *weight, int64_t ld, int V, int D, const int32_t *ids,
-                                                          int rows, float scale, T *out, int lanes_log2)
+                                                          int rows, int64_t step, float scale, T *out, int lanes_log2)
 {
+    constexpr int N = Pack<T>::kN;
     const int lanes = 1 << lanes_log2;
     const int64_t row = (int64_t)blockIdx.x * (kThreads >> lanes_log2) + (threadIdx.x >> lanes_log2);
-    if (row >= rows)
+    if (row >= step)
         return;
-    const int id = ids[row];
-    const bool in = (uint32_t)id < (uint32_t)V;
-    const T *src = weight + (int64_t)(in ? id : 0) * ld;
-    T *dst = out + row * D;
-    const int first = blockIdx.y * lanes + (threadIdx.x & (lanes - 1));
-    const int whole = D / N;
-    for (int j = first; j < whole; j += lanes * gridDim.y) {
-        Pack<T, N> v = load_pack<T, N>(src + (int64_t)j * N);
+    int id[ROWS];
 #pragma unroll
-        for (int i = 0; i < N; ++i)
-            from_float(in ? to_float(v.x[i]) * scale : 0.f, v.x[i]);
-        store_pack(dst + (int64_t)j * N, v);
+    for (int r = 0; r < ROWS; ++r)
+        id[r] = row + r * step < rows ? ids[row + r * step] : -1;
+    for (int64_t col = (int64_t)(blockIdx.y * lanes + (threadIdx.x & (lanes - 1))) * N; col < D;
+         col += (int64_t)lanes * gridDim.y * N) {
+        const int n = (int)(D - col);
+        Pack<T> v[ROWS];
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r)
+            v[r].load(weight + (int64_t)((uint32_t)id[r] < (uint32_t)V ? id[r] : 0) * ld + col, n);
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) {
+            const bool in = (uint32_t)id[r] < (uint32_t)V;
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                from_float(in ? to_float(v[r].x[i]) * scale : 0.f, v[r].x[i]);
+            if (row + r * step < rows)
+                v[r].store(out + (row + r * step) * D + col, n);
+        }
     }
-    for (int i = whole * N + first; i < D; i += lanes * gridDim.y)
-        from_float(in ? to_float(src[i]) * scale : 0.f, dst[i]);
 }
 
 // ------------------------------------------------------------------ sorting
@@ -308,86 +324,88 @@ __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(const int32_t 
 // chunk is finished there.  Of a run that crosses chunks, each chunk keeps its
 // part in fp32: slot 0 of the chunk if the run came in from the chunk before,
 // slot 1 if it began here; the second kernel adds the parts in chunk order.
-template <typename T, int N>
-__device__ __forceinline__ void emit(T *grad, int64_t at, float (&acc)[N], float scale, bool accumulate)
+template <typename T>
+__device__ __forceinline__ void emit(T *grad, const float (&acc)[Pack<T>::kN], int n, float scale, bool accumulate)
 {
-    Pack<T, N> v;
+    Pack<T> v;
     if (accumulate)
-        v = load_pack<T, N>(grad + at);
+        v.load(grad, n);
 #pragma unroll
-    for (int i = 0; i < N; ++i)
+    for (int i = 0; i < Pack<T>::kN; ++i)
         from_float(accumulate ? to_float(v.x[i]) + acc[i] * scale : acc[i] * scale, v.x[i]);
-    store_pack(grad + at, v);
+    v.store(grad, n);
 }
 
-template <typename T, int N>
+template <typename T>
 __global__ __launch_bounds__(kThreads) void sum_chunks_kernel(const T *grad_out, int64_t ld, int D, const int *keys,
                                                                const int *order, int rows, int V, int chunk,
-                                                               float scale, bool accumulate, T *grad, float *parts)
+                                                               float scale, bool accumulate, T *grad, float *parts,
+                                                               int part_ld)
 {
+    constexpr int N = Pack<T>::kN;
+    constexpr int U = 8;  // rows on their way at once
     const int c = blockIdx.x;
     const int64_t from = (int64_t)c * chunk;
     const int64_t to = from + chunk < rows ? from + chunk : rows;
     const int col = (blockIdx.y * blockDim.x + threadIdx.x) * N;
     if (col >= D)
         return;
+    const int n = D - col;
     const bool came = from > 0 && keys[from - 1] == keys[from];
     const bool goes = to < rows && keys[to] == keys[to - 1];
-    constexpr int U = 8;
     float acc[N] = {};
     bool first = true;  // still in the chunk's first run
     int key = keys[from];
+    const auto keep = [&](int slot) {
+        __builtin_memcpy(parts + ((int64_t)c * 2 + slot) * part_ld + col, acc, sizeof acc);
+    };
     for (int64_t i = from; i < to && key < V; i += U) {
-        Pack<T, N> v[U];
+        Pack<T> v[U];
         int k[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int64_t at = i + u < to ? i + u : to - 1;
-            k[u] = i + u < to ? keys[at] : V;
-            v[u] = load_pack<T, N>(grad_out + (int64_t)order[at] * ld + col);
+            k[u] = keys[at];
+            v[u].load(grad_out + (int64_t)order[at] * ld + col, n);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
+            if (i + u >= to)
+                break;
             if (k[u] != key) {
-                if (key < V && !(i + u >= to)) {
-                    if (first && came) {
-                        float *p = parts + ((int64_t)c * 2) * D + col;
-#pragma unroll
-                        for (int e = 0; e < N; ++e)
-                            p[e] = acc[e];
-                    } else {
-                        emit<T, N>(grad, (int64_t)key * D + col, acc, scale, accumulate);
-                    }
-                    first = false;
-                    key = k[u];
-#pragma unroll
-                    for (int e = 0; e < N; ++e)
-                        acc[e] = 0.f;
+                if (key < V) {
+                    if (first && came)
+                        keep(0);
+                    else
+                        emit<T>(grad + (int64_t)key * D + col, acc, n, scale, accumulate);
                 }
-            }
-            if (i + u < to && key < V)
+                first = false;
+                key = k[u];
 #pragma unroll
                 for (int e = 0; e < N; ++e)
-                    acc[e] += to_float(v[u].x[e]);
+                    acc[e] = 0.f;
+            }
+#pragma unroll
+            for (int e = 0; e < N; ++e)
+                acc[e] += to_float(v[u].x[e]);
         }
     }
     if (key >= V)
         return;
-    if ((first && came) || goes) {
-        float *p = parts + ((int64_t)c * 2 + (first && came ? 0 : 1)) * D + col;
-#pragma unroll
-        for (int e = 0; e < N; ++e)
-            p[e] = acc[e];
-    } else {
-        emit<T, N>(grad, (int64_t)key * D + col, acc, scale, accumulate);
-    }
+    if (first && came)
+        keep(0);
+    else if (goes)
+        keep(1);
+    else
+        emit<T>(grad + (int64_t)key * D + col, acc, n, scale, accumulate);
 }
 
-template <typename T, int N>
+template <typename T>
 __global__ __launch_bounds__(kThreads) void sum_parts_kernel(int D, const int *keys, int rows, int V, int chunk,
                                                               int chunks, float scale, bool accumulate, T *grad,
-                                                              const float *parts)
+                                                              const float *parts, int part_ld)
 {
+    constexpr int N = Pack<T>::kN;
     const int c = blockIdx.x;
     const int64_t from = (int64_t)c * chunk;
     const int64_t to = from + chunk;
@@ -397,33 +415,54 @@ __global__ __launch_bounds__(kThreads) void sum_parts_kernel(int D, const int *k
     // a run that begins in this chunk and goes on into the next
     if (key >= V || keys[to] != key || (from > 0 && keys[from] == key && keys[from - 1] == key))
         return;
+    // the chunks that the run goes on into, a wave's lanes looking at 64 at a time
+    int last = c;
+    for (;;) {
+        const int d = last + 1 + (int)(threadIdx.x & (kWave - 1));
+        const uint64_t on = __ballot(d < chunks && keys[(int64_t)(d < chunks ? d : c) * chunk] == key);
+        if (~on) {
+            last += __builtin_ctzll(~on);
+            break;
+        }
+        last += kWave;
+    }
     const int col = (blockIdx.y * blockDim.x + threadIdx.x) * N;
     if (col >= D)
         return;
     float acc[N];
-    const float *own = parts + ((int64_t)c * 2 + 1) * D + col;
+    const float *p = parts + ((int64_t)c * 2 + 1) * part_ld + col;
+    __builtin_memcpy(acc, p, sizeof acc);
+    p += part_ld;  // slot 0 of the next chunk
+    constexpr int U = 8;
+    for (int d = c + 1; d <= last; d += U) {
+        float part[U][N];
 #pragma unroll
-    for (int e = 0; e < N; ++e)
-        acc[e] = own[e];
-    for (int d = c + 1; d < chunks && keys[(int64_t)d * chunk] == key; ++d) {
-        const float *p = parts + ((int64_t)d * 2) * D + col;
+        for (int u = 0; u < U; ++u)
+            __builtin_memcpy(part[u], p + (int64_t)(d + u <= last ? u : 0) * 2 * part_ld, sizeof acc);
 #pragma unroll
-        for (int e = 0; e < N; ++e)
-            acc[e] += p[e];
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int e = 0; e < N; ++e)
+                acc[e] += d + u <= last ? part[u][e] : 0.f;
+        p += (int64_t)U * 2 * part_ld;
     }
-    emit<T, N>(grad, (int64_t)key * D + col, acc, scale, accumulate);
+    emit<T>(grad + (int64_t)key * D + col, acc, D - col, scale, accumulate);
 }
 
-// Chunks of 32 rows, doubled until there are at most kMaxChunks.
-constexpr int kMaxChunks = 512;
+// Chunks of 8 rows, doubled until there are at most kMaxChunks: short ones keep
+// many rows on their way, and a token's parts are added one after the other.
+constexpr int kLeastChunk = 8;
+constexpr int kMaxChunks = 1024;
 
 int chunk_of(int rows)
 {
-    int c = 32;
+    int c = kLeastChunk;
     while ((int64_t)c * kMaxChunks < rows)
         c *= 2;
     return c;
 }
+
+int part_stride(int hidden) { return (hidden + 7) & ~7; }
 
 struct EmbedLayout {
     size_t keys[2], order[2], hist, parts, bytes;
@@ -445,52 +484,63 @@ EmbedLayout embed_layout(int rows, int hidden)
     at += align_up((blocks ? blocks : 1) * kBins * 4, 256);
     l.parts = at;
     // chunk_of's chunks, or more (the size never falls as rows grow)
-    const size_t chunks = rows < 32 * kMaxChunks ? ((size_t)rows + 31) / 32 : (size_t)kMaxChunks;
-    at += align_up(chunks * 2 * (size_t)hidden * 4 + 4, 256);
+    const size_t chunks = rows < kLeastChunk * kMaxChunks ? ((size_t)rows + kLeastChunk - 1) / kLeastChunk
+                                                          : (size_t)kMaxChunks;
+    at += align_up(chunks * 2 * (size_t)part_stride(hidden) * 4 + 4, 256);
     l.bytes = at;
     return l;
 }
 
-// Bytes that every row start of a [..][ld] array is a multiple of, 16 at most.
-int row_alignment(const void *p, int64_t ld, int elt)
-{
-    const uintptr_t a = reinterpret_cast<uintptr_t>(p) | (uintptr_t)(ld * elt) | 16;
-    return (int)(a & (~a + 1));
-}
-
-template <typename T, int N>
+template <typename T, int ROWS>
 hipError_t embed_with(const T *weight, int64_t ld, int V, int D, const int32_t *ids, int rows, float scale, T *out,
                       hipStream_t stream)
 {
-    const int vecs = (D + N - 1) / N;
+    const int vecs = (D + Pack<T>::kN - 1) / Pack<T>::kN;
     int log2 = 0;
     while (log2 < 8 && (1 << log2) < vecs)
         ++log2;
-    const int rows_per_block = kThreads >> log2;
-    const int gx = (rows + rows_per_block - 1) / rows_per_block;
+    const int64_t step = ((int64_t)rows + ROWS - 1) / ROWS;
+    const int64_t per_block = kThreads >> log2;
     int gy = (vecs + (1 << log2) - 1) >> log2;
     gy = gy < 64 ? gy : 64;
-    embed_kernel<T, N><<<dim3(gx, gy), kThreads, 0, stream>>>(weight, ld, V, D, ids, rows, scale, out, log2);
+    embed_kernel<T, ROWS><<<dim3((unsigned)((step + per_block - 1) / per_block), gy), kThreads, 0, stream>>>(
+        weight, ld, V, D, ids, rows, step, scale, out, log2);
     return last_launch();
 }
 
-template <typename T, int N>
-hipError_t sums_with(const T *grad_out, int64_t ld, int D, const int *keys, const int *order, int rows, int V,
-                     float scale, bool accumulate, T *grad, float *parts, hipStream_t stream)
+// Four rows a lane once that leaves the compute units enough blocks: each row's
+// load waits for its id.
+template <typename T>
+hipError_t embed(const void *weight, int64_t ld, int V, int D, const int32_t *ids, int rows, float scale, void *out,
+                 hipStream_t stream)
 {
+    const T *w = static_cast<const T *>(weight);
+    T *o = static_cast<T *>(out);
+    if ((int64_t)rows * D >= (int64_t)4 * 1024 * kThreads * Pack<T>::kN)
+        return embed_with<T, 4>(w, ld, V, D, ids, rows, scale, o, stream);
+    return embed_with<T, 1>(w, ld, V, D, ids, rows, scale, o, stream);
+}
+
+template <typename T>
+hipError_t sums(const void *grad_out, int64_t ld, int D, const int *keys, const int *order, int rows, int V, float scale,
+                bool accumulate, void *grad_weight, float *parts, hipStream_t stream)
+{
+    const T *g = static_cast<const T *>(grad_out);
+    T *w = static_cast<T *>(grad_weight);
     const int chunk = chunk_of(rows), chunks = (rows + chunk - 1) / chunk;
-    const int vecs = (D + N - 1) / N;
+    const int vecs = (D + Pack<T>::kN - 1) / Pack<T>::kN;
     int threads = kWave;
     while (threads < kThreads && threads < vecs)
         threads *= 2;
     const dim3 grid(chunks, (vecs + threads - 1) / threads);
-    sum_chunks_kernel<T, N><<<grid, threads, 0, stream>>>(grad_out, ld, D, keys, order, rows, V, chunk, scale,
-                                                          accumulate, grad, parts);
+    const int part_ld = part_stride(D);
+    sum_chunks_kernel<T><<<grid, threads, 0, stream>>>(g, ld, D, keys, order, rows, V, chunk, scale, accumulate, w, parts,
+                                                       part_ld);
     hipError_t e = last_launch();
     if (e != hipSuccess || chunks == 1)
         return e;
-    sum_parts_kernel<T, N><<<grid, threads, 0, stream>>>(D, keys, rows, V, chunk, chunks, scale, accumulate, grad,
-                                                         parts);
+    sum_parts_kernel<T><<<grid, threads, 0, stream>>>(D, keys, rows, V, chunk, chunks, scale, accumulate, w, parts,
+                                                      part_ld);
     return last_launch();
 }
 
@@ -499,21 +549,8 @@ hipError_t sums_with(const T *grad_out, int64_t ld, int D, const int *keys, cons
 hipError_t launch_embed(const void *weight, int64_t ld_w, int dtype, int V, int hidden, const int32_t *ids, int rows,
                         float scale, void *out, hipStream_t stream)
 {
-    const int elt = dtype == 1 ? 2 : 4;
-    const int in = row_alignment(weight, ld_w, elt), to = row_alignment(out, hidden, elt);
-    const int bytes = in < to ? in : to;
-    if (dtype == 1) {
-        const uint16_t *w = static_cast<const uint16_t *>(weight);
-        uint16_t *o = static_cast<uint16_t *>(out);
-        if (bytes == 16)
-            return embed_with<uint16_t, 8>(w, ld_w, V, hidden, ids, rows, scale, o, stream);
-        return embed_with<uint16_t, 2>(w, ld_w, V, hidden, ids, rows, scale, o, stream);
-    }
-    const float *w = static_cast<const float *>(weight);
-    float *o = static_cast<float *>(out);
-    if (bytes == 16)
-        return embed_with<float, 4>(w, ld_w, V, hidden, ids, rows, scale, o, stream);
-    return embed_with<float, 1>(w, ld_w, V, hidden, ids, rows, scale, o, stream);
+    return dtype == 1 ? embed<uint16_t>(weight, ld_w, V, hidden, ids, rows, scale, out, stream)
+                      : embed<float>(weight, ld_w, V, hidden, ids, rows, scale, out, stream);
 }
 
 size_t embed_backward_workspace_bytes(int rows, int hidden, int V)
@@ -567,20 +604,10 @@ hipError_t launch_embed_backward(const void *grad_out, int64_t ld, int dtype, in
     }
     if (rows == 0)
         return hipSuccess;
-    const int in = row_alignment(grad_out, ld, elt), to = row_alignment(grad_weight, hidden, elt);
-    const bool wide = in == 16 && to == 16 && hidden % (16 / elt) == 0;
-    if (dtype == 1) {
-        const uint16_t *g = static_cast<const uint16_t *>(grad_out);
-        uint16_t *w = static_cast<uint16_t *>(grad_weight);
-        if (wide)
-            return sums_with<uint16_t, 8>(g, ld, hidden, keys[at], order[at], rows, V, scale, accumulate, w, parts, stream);
-        return sums_with<uint16_t, 1>(g, ld, hidden, keys[at], order[at], rows, V, scale, accumulate, w, parts, stream);
-    }
-    const float *g = static_cast<const float *>(grad_out);
-    float *w = static_cast<float *>(grad_weight);
-    if (wide)
-        return sums_with<float, 4>(g, ld, hidden, keys[at], order[at], rows, V, scale, accumulate, w, parts, stream);
-    return sums_with<float, 1>(g, ld, hidden, keys[at], order[at], rows, V, scale, accumulate, w, parts, stream);
+    return dtype == 1 ? sums<uint16_t>(grad_out, ld, hidden, keys[at], order[at], rows, V, scale, accumulate, grad_weight,
+                                       parts, stream)
+                      : sums<float>(grad_out, ld, hidden, keys[at], order[at], rows, V, scale, accumulate, grad_weight,
+                                    parts, stream);
 }
 
 }  // namespace dv
