@@ -15,8 +15,7 @@
 // the price of not keeping the logits.
 //
 // All products are the one of dv_gemm.h, which takes operands with k along their
-// rows or from row to row: x, w and G are used as they lie.  fp32 operands go
-// through it as three bf16 planes each.
+// rows or from row to row: x, w and G are used as they lie.
 #include <type_traits>
 
 #include "dv_gemm.h"
@@ -27,50 +26,27 @@ namespace {
 
 // ------------------------------------------------------------- preparation
 
-// x as a sum of P bf16 numbers, each the rest rounded to nearest (three hold
-// all 24 bits of an fp32 significand: the sum is exact).  What is infinite or
-// NaN stays in the first; a first part that would round up to infinity is
-// cut instead.
-template <int P>
-__device__ __forceinline__ void split_planes(float x, __bf16 (&out)[P])
+// src [rows][cols] (row stride ld) to rows of out_cols (a multiple of 64), zeros
+// past cols: a lane copies 16 bytes, from any element's alignment.
+template <typename T>
+__global__ __launch_bounds__(256) void pack_kernel(const T *src, int64_t ld, int rows, int cols, int out_cols, T *dst)
 {
-    out[0] = (__bf16)x;
-    if constexpr (P > 1) {
-        const bool finite = fabsf(x) <= 3.4028235e38f;
-        if (finite && fabsf((float)out[0]) > 3.4028235e38f)
-            out[0] = (__bf16)__uint_as_float(__float_as_uint(x) & 0xFFFF0000u);
-        float left = finite ? x - (float)out[0] : 0.f;
+    constexpr int N = 16 / (int)sizeof(T);
+    const int vecs = out_cols / N;
+    const int64_t total = (int64_t)rows * vecs;
+    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < total; i += (int64_t)gridDim.x * blockDim.x) {
+        const int64_t row = i / vecs;
+        const int col = (int)(i - row * vecs) * N;
+        const T *p = src + row * ld + col;
+        T x[N];
+        if (col + N <= cols) {
+            __builtin_memcpy(x, p, 16);
+        } else {
 #pragma unroll
-        for (int p = 1; p < P; ++p) {
-            out[p] = (__bf16)left;
-            left -= (float)out[p];
+            for (int e = 0; e < N; ++e)
+                x[e] = col + e < cols ? p[e] : T(0);
         }
-    }
-}
-
-// src [rows][cols] (row stride ld) to bf16 planes [P][rows][out_cols], zeros past cols.
-template <typename T, int P>
-__global__ void pack_kernel(const T *src, int64_t ld, int rows, int cols, int out_cols, __bf16 *dst, int64_t plane)
-{
-    const int64_t row = blockIdx.y + (int64_t)blockIdx.z * 65535;
-    const int col = (blockIdx.x * blockDim.x + threadIdx.x) * 2;
-    if (row >= rows || col >= out_cols)
-        return;
-    __bf16 a[P], b[P];
-    float x = 0.f, y = 0.f;
-    if constexpr (sizeof(T) == 4) {
-        x = col < cols ? src[row * ld + col] : 0.f;
-        y = col + 1 < cols ? src[row * ld + col + 1] : 0.f;
-    } else {
-        x = col < cols ? widen(src[row * ld + col]) : 0.f;
-        y = col + 1 < cols ? widen(src[row * ld + col + 1]) : 0.f;
-    }
-    split_planes<P>(x, a);
-    split_planes<P>(y, b);
-#pragma unroll
-    for (int p = 0; p < P; ++p) {
-        __bf16 both[2] = {a[p], b[p]};
-        __builtin_memcpy(dst + p * plane + row * out_cols + col, both, 4);
+        *reinterpret_cast<uint4 *>(dst + row * out_cols + col) = *reinterpret_cast<const uint4 *>(x);
     }
 }
 
@@ -78,17 +54,17 @@ __global__ void pack_kernel(const T *src, int64_t ld, int rows, int cols, int ou
 
 // Per row and tile: maximum and sum of exponentials of the allowed logits;
 // the target's logit.  i runs over the piece's tokens, j over rows.
-template <int BM, int BN, int WM, int WN>
+template <typename E, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__(WM *WN *kWave, 2) void stats_kernel(GemmShape g, int v0, int V, int rows, Masks masks,
                                                                  const int32_t *targets, Softmax *parts,
                                                                  float *target_logit, int tiles_i, int tiles_j)
 {
-    using G = Gemm<BM, BN, WM, WN>;
+    using G = Gemm<E, BM, BN, WM, WN>;
     __shared__ __attribute__((aligned(1024))) char lds[G::kLdsBytes];
     int ti, tj;
     tile_of_block(blockIdx.x, tiles_i, tiles_j, ti, tj);
     f32x4 acc[G::kTm][G::kTn] = {};
-    G::run(acc, g, ti * BM, tj * BN, 0, g.k / kGemmStageK * g.segments, lds);
+    G::run(acc, g, ti * BM, tj * BN, 0, g.k / G::kStageK, lds);
 
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
     const int wm = wave / WN, wn = wave % WN;
@@ -179,20 +155,20 @@ __global__ void weights_kernel(int rows, int V, Masks masks, const int32_t *targ
         weight[n] = RowMask(masks, V, n).has(targets[n]) ? grad_loss[n] : 0.f;
 }
 
-// A piece of G in bf16 (P planes of it for fp32 operands): [rows][ld] with
-// the piece's tokens along a row, zeros up to the next multiple of 64 both ways.
-template <int BM, int BN, int WM, int WN, int P>
+// A piece of G in the operands' type: [rows][ld] with the piece's tokens along a
+// row, zeros up to the next multiple of 64 both ways.
+template <typename E, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__(WM *WN *kWave, 2) void grad_kernel(GemmShape g, int v0, int V, int rows, Masks masks,
                                                                 const int32_t *targets, const float *lse,
-                                                                const float *weight, __bf16 *out, int64_t ld,
-                                                                int64_t plane, int tiles_i, int tiles_j)
+                                                                const float *weight, E *out, int64_t ld, int tiles_i,
+                                                                int tiles_j)
 {
-    using G = Gemm<BM, BN, WM, WN>;
+    using G = Gemm<E, BM, BN, WM, WN>;
     __shared__ __attribute__((aligned(1024))) char lds[G::kLdsBytes];
     int ti, tj;
     tile_of_block(blockIdx.x, tiles_i, tiles_j, ti, tj);
     f32x4 acc[G::kTm][G::kTn] = {};
-    G::run(acc, g, ti * BM, tj * BN, 0, g.k / kGemmStageK * g.segments, lds);
+    G::run(acc, g, ti * BM, tj * BN, 0, g.k / G::kStageK, lds);
 
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
     const int wm = wave / WN, wn = wave % WN;
@@ -213,20 +189,16 @@ __global__ __launch_bounds__(WM *WN *kWave, 2) void grad_kernel(GemmShape g, int
 #pragma unroll
         for (int a = 0; a < G::kTm; ++a) {
             const uint32_t bits = m.word((vw >> 5) + (a >> 1)) >> (quarter * 4 + (a & 1) * 16);
-            __bf16 y[4][P];
+            E y[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 float p = (bits >> e & 1u) && w != 0.f ? softmax_term(acc[a][b][e], base, kLog2e) : 0.f;
                 p -= t == a * 16 + quarter * 4 + e ? 1.f : 0.f;
-                split_planes<P>(p * w, y[e]);
+                y[e] = (E)(p * w);
             }
             const int col = lw + a * 16 + quarter * 4;
             if (col < ld)
-#pragma unroll
-                for (int p = 0; p < P; ++p) {
-                    __bf16 four[4] = {y[0][p], y[1][p], y[2][p], y[3][p]};
-                    __builtin_memcpy(out + p * plane + (int64_t)n * ld + col, four, 8);
-                }
+                __builtin_memcpy(out + (int64_t)n * ld + col, y, sizeof y);
         }
     }
 }
@@ -238,16 +210,16 @@ enum class Out { kStore, kPartial, kPartialAdd };
 // C[j][i] of a product as `out_rows` rows of `cols` elements: in T, or in fp32
 // as (or on top of) the partial sums of this block's share of k.  A is stored by
 // columns, B by columns with COLS_B.
-template <int BM, int BN, int WM, int WN, bool COLS_B, typename T, Out OUT>
+template <typename E, int BM, int BN, int WM, int WN, bool COLS_B, typename T, Out OUT>
 __global__ __launch_bounds__(WM *WN *kWave, 2) void product_kernel(GemmShape g, T *out, int out_rows, int cols,
                                                                    int64_t split_stride, int split_stages, int tiles_i,
                                                                    int tiles_j)
 {
-    using G = Gemm<BM, BN, WM, WN, true, COLS_B>;
+    using G = Gemm<E, BM, BN, WM, WN, true, COLS_B>;
     __shared__ __attribute__((aligned(1024))) char lds[G::kLdsBytes];
     int ti, tj;
     tile_of_block(blockIdx.x, tiles_i, tiles_j, ti, tj);
-    const int total = g.k / kGemmStageK * g.segments;
+    const int total = g.k / G::kStageK;
     const int from = blockIdx.y * split_stages;
     const int stages = total - from < split_stages ? total - from : split_stages;
     f32x4 acc[G::kTm][G::kTn] = {};
@@ -264,14 +236,20 @@ __global__ __launch_bounds__(WM *WN *kWave, 2) void product_kernel(GemmShape g, 
         for (int a = 0; a < G::kTm; ++a) {
             const int c = ti * BM + wm * (BM / WM) + a * 16 + (lane >> 4) * 4;
             T *p = out + (int64_t)r * cols + c;
+            T y[4];
+            if (c + 4 <= cols) {  // four elements of a row, at any element's alignment
+                if (OUT == Out::kPartialAdd)
+                    __builtin_memcpy(y, p, sizeof y);
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (c + e < cols) {
-                    float y = acc[a][b][e];
-                    if (OUT == Out::kPartialAdd)
-                        y += (float)p[e];
-                    p[e] = (T)y;
-                }
+                for (int e = 0; e < 4; ++e)
+                    y[e] = (T)(acc[a][b][e] + (OUT == Out::kPartialAdd ? (float)y[e] : 0.f));
+                __builtin_memcpy(p, y, sizeof y);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (c + e < cols)
+                        p[e] = (T)(acc[a][b][e] + (OUT == Out::kPartialAdd ? (float)p[e] : 0.f));
+            }
         }
     }
 }
@@ -301,14 +279,14 @@ constexpr int64_t kPieceElements = (int64_t)1 << 27;
 constexpr int kPieceTokens = 1 << 18;
 
 // The tile side and the splits of k for a product of `i` x `j` over `stages` of
-// 64 k, by the time that each side would take: rounds of blocks over the 256
+// k (64 of bf16, 32 of fp32), by the time that each side would take: rounds of blocks over the 256
 // compute units, each block its stages and about three more to start and end, at
 // the rate the core reaches with that side; splits write and read their sums.
 struct Plan {
     int side, splits, stages;  // stages of a split; no split is empty
 };
 
-Plan plan_product(int64_t i, int64_t j, int64_t stages, int most_splits)
+Plan plan_product(int64_t i, int64_t j, int64_t stages, int most_splits, bool bf16)
 {
     struct Side {
         int side, per_unit;
@@ -324,7 +302,7 @@ Plan plan_product(int64_t i, int64_t j, int64_t stages, int most_splits)
             const int64_t used = (stages + per - 1) / per;
             const int64_t slots = (int64_t)256 * s.per_unit;
             const double rounds = (double)((tiles * used + slots - 1) / slots);
-            const double us = rounds * (double)(per + 3) * s.us + (used > 1 ? (double)(used * i * j) * 2e-6 + 3 : 0);
+            const double us = rounds * (double)(per + 3) * s.us * (bf16 ? 1.0 : 3.0) + (used > 1 ? (double)(used * i * j) * 2e-6 + 3 : 0);
             if (us < least) {
                 least = us;
                 best = {s.side, (int)used, (int)per};
@@ -337,22 +315,22 @@ Plan plan_product(int64_t i, int64_t j, int64_t stages, int most_splits)
 int64_t up64(int64_t n) { return (n + 63) / 64 * 64; }
 
 struct HeadLayout {
-    int planes, segments;
     int64_t k;        // hidden size as the products see it
+    int stage_k;
     int piece;        // tokens of a piece, a multiple of 256 (or all)
     int pieces;
     Plan dx_plan;
-    size_t x, w, parts, target_logit;                        // forward
-    size_t g, weight, dx;                                     // backward
+    size_t x, w, parts, target_logit;  // forward
+    size_t g, weight, dx;              // backward
     size_t forward_bytes, backward_bytes;
 };
 
 HeadLayout head_layout(int rows, int hidden, int V, int dtype)
 {
     HeadLayout l{};
-    l.planes = dtype == 1 ? 1 : 3;
-    l.segments = dtype == 1 ? 1 : kGemmSegments;
+    const size_t elt = dtype == 1 ? 2 : 4;
     l.k = up64(hidden);
+    l.stage_k = 128 / (int)elt;
     const int64_t r64 = up64(rows > 0 ? rows : 1);
     int64_t piece = kPieceElements / r64 / 256 * 256;
     piece = piece < 4096 ? 4096 : piece;
@@ -369,54 +347,47 @@ HeadLayout head_layout(int rows, int hidden, int V, int dtype)
         at += align_up(bytes, 256);
         return here;
     };
-    const size_t planes = (size_t)l.planes;
-    l.x = take(planes * r64 * l.k * 2);
-    l.w = take(planes * p64 * l.k * 2);
+    l.x = take(r64 * l.k * elt);
+    l.w = take(p64 * l.k * elt);
     const size_t shared = at;
     l.parts = take(((size_t)V / 32 + 8) * r64 * sizeof(Softmax));
     l.target_logit = take((size_t)r64 * 4);
     l.forward_bytes = at;
     at = shared;
-    l.g = take(planes * r64 * p64 * 2);
+    l.g = take(r64 * p64 * elt);
     l.weight = take((size_t)r64 * 4);
     // dx over a piece: few tiles and a long k
-    l.dx_plan = plan_product(l.k, rows, p64 / kGemmStageK * l.segments, 16);
+    l.dx_plan = plan_product(l.k, rows, p64 / l.stage_k, 16, dtype == 1);
     l.dx = take((size_t)l.dx_plan.splits * rows * hidden * 4);
     l.backward_bytes = at;
     return l;
 }
 
-hipError_t pack(const void *src, int64_t ld, int dtype, int64_t rows, int cols, int out_cols, __bf16 *dst, int64_t plane,
-                hipStream_t s)
-{
-    const int threads = 128;
-    const dim3 grid((out_cols / 2 + threads - 1) / threads, (unsigned)(rows < 65535 ? rows : 65535),
-                    (unsigned)((rows + 65534) / 65535));
-    if (dtype == 1)
-        pack_kernel<uint16_t, 1><<<grid, threads, 0, s>>>(static_cast<const uint16_t *>(src), ld, (int)rows, cols,
-                                                          out_cols, dst, plane);
-    else
-        pack_kernel<float, 3><<<grid, threads, 0, s>>>(static_cast<const float *>(src), ld, (int)rows, cols, out_cols,
-                                                       dst, plane);
-    return last_launch();
-}
-
 // An operand as the products need it: in place, or packed into `buffer`.
 bool in_place(const void *p, int64_t ld, int dtype, int hidden)
 {
-    return dtype == 1 && hidden % 64 == 0 && ld % 8 == 0 && reinterpret_cast<uintptr_t>(p) % 16 == 0 &&
+    return hidden % 64 == 0 && ld % (dtype == 1 ? 8 : 4) == 0 && reinterpret_cast<uintptr_t>(p) % 16 == 0 &&
            ld <= ((int64_t)1 << 20);
 }
 
-hipError_t operand(const void *p, int64_t ld, int dtype, int rows, int hidden, const HeadLayout &l, __bf16 *buffer,
+hipError_t operand(const void *p, int64_t ld, int dtype, int rows, int hidden, const HeadLayout &l, void *buffer,
                    GemmOperand &out, hipStream_t s)
 {
     if (in_place(p, ld, dtype, hidden)) {
-        out = {static_cast<const __bf16 *>(p), ld, 0, rows, 0};
+        out = {p, ld, rows, 0};
         return hipSuccess;
     }
-    out = {buffer, l.k, (int64_t)rows * l.k, rows, 0};
-    return pack(p, ld, dtype, rows, hidden, (int)l.k, buffer, out.plane, s);
+    out = {buffer, l.k, rows, 0};
+    const int64_t vecs = (int64_t)rows * (l.k / (dtype == 1 ? 8 : 4));
+    const int64_t blocks = (vecs + 255) / 256;
+    const unsigned grid = (unsigned)(blocks < 8192 ? blocks : 8192);
+    if (dtype == 1)
+        pack_kernel<uint16_t><<<grid, 256, 0, s>>>(static_cast<const uint16_t *>(p), ld, rows, hidden, (int)l.k,
+                                                   static_cast<uint16_t *>(buffer));
+    else
+        pack_kernel<float><<<grid, 256, 0, s>>>(static_cast<const float *>(p), ld, rows, hidden, (int)l.k,
+                                                static_cast<float *>(buffer));
+    return last_launch();
 }
 
 #define DV_TRY(call)                   \
@@ -441,16 +412,16 @@ hipError_t with_tile(int side, F &&f)
 // An operand stored by rows, seen as one stored by columns: `k` elements a row.
 GemmOperand by_columns(const GemmOperand &o, int64_t k)
 {
-    return {o.p, o.ld, o.plane, (int)k, o.n};
+    return {o.p, o.ld, (int)k, o.n};
 }
 
-template <bool COLS_B, typename T, Out OUT>
+template <typename E, bool COLS_B, typename T, Out OUT>
 hipError_t product(const GemmShape &g, const Plan &plan, T *out, int out_rows, int cols, int64_t split_stride, hipStream_t s)
 {
     return with_tile(plan.side, [&](auto side, auto wn) {
         constexpr int B = decltype(side)::value, WN = decltype(wn)::value;
         const int ti = (cols + B - 1) / B, tj = (out_rows + B - 1) / B;
-        product_kernel<B, B, 2, WN, COLS_B, T, OUT><<<dim3(ti * tj, plan.splits), 2 * WN * kWave, 0, s>>>(
+        product_kernel<E, B, B, 2, WN, COLS_B, T, OUT><<<dim3(ti * tj, plan.splits), 2 * WN * kWave, 0, s>>>(
             g, out, out_rows, cols, split_stride, plan.stages, ti, tj);
     });
 }
@@ -476,10 +447,11 @@ hipError_t backward(const HeadArgs &a, const float *lse, const float *grad_loss,
 {
     const HeadLayout l = head_layout(a.rows, a.hidden, a.V, a.dtype);
     const int64_t r64 = up64(a.rows);
-    const auto at = [&](size_t off) { return reinterpret_cast<__bf16 *>(ws + off); };
     float *weight = reinterpret_cast<float *>(ws + l.weight), *dx = reinterpret_cast<float *>(ws + l.dx);
+    T *g_piece = reinterpret_cast<T *>(ws + l.g);
+    constexpr bool kBf16 = sizeof(T) == 2;
     GemmOperand x;
-    DV_TRY(operand(a.x, a.ld_x, a.dtype, a.rows, a.hidden, l, at(l.x), x, s));
+    DV_TRY(operand(a.x, a.ld_x, a.dtype, a.rows, a.hidden, l, ws + l.x, x, s));
     weights_kernel<<<(a.rows + 255) / 256, 256, 0, s>>>(a.rows, a.V, a.masks, a.targets, grad_loss, weight);
     DV_TRY(last_launch());
     int splits = 1;
@@ -488,39 +460,38 @@ hipError_t backward(const HeadArgs &a, const float *lse, const float *grad_loss,
         const int n = a.V - v0 < l.piece ? a.V - v0 : l.piece;
         const int64_t n64 = up64(n);
         GemmOperand w;
-        DV_TRY(operand(weight_rows(a, v0), a.ld_w, a.dtype, n, a.hidden, l, at(l.w), w, s));
-        const GemmShape logits{w, x, (int)l.k, l.segments};
-        const GemmOperand g{at(l.g), n64, r64 * n64, a.rows, 0};
-        DV_TRY(with_tile(plan_product(n, a.rows, l.k / kGemmStageK * l.segments, 1).side, [&](auto side, auto wn) {
+        DV_TRY(operand(weight_rows(a, v0), a.ld_w, a.dtype, n, a.hidden, l, ws + l.w, w, s));
+        const GemmShape logits{w, x, (int)l.k};
+        const GemmOperand g{g_piece, n64, a.rows, 0};
+        DV_TRY(with_tile(plan_product(n, a.rows, l.k / l.stage_k, 1, kBf16).side, [&](auto side, auto wn) {
             constexpr int B = decltype(side)::value, WN = decltype(wn)::value;
             const int ti = (n + B - 1) / B, tj = (a.rows + B - 1) / B;
-            constexpr int P = sizeof(T) == 2 ? 1 : 3;
-            grad_kernel<B, B, 2, WN, P><<<ti * tj, 2 * WN * kWave, 0, s>>>(logits, v0, a.V, a.rows, a.masks, a.targets,
-                                                                          lse, weight, at(l.g), n64, g.plane, ti, tj);
+            grad_kernel<T, B, B, 2, WN><<<ti * tj, 2 * WN * kWave, 0, s>>>(logits, v0, a.V, a.rows, a.masks, a.targets, lse,
+                                                                          weight, g_piece, n64, ti, tj);
         }));
         if (grad_x) {
-            const GemmShape shape{by_columns(w, l.k), g, (int)n64, l.segments};
+            const GemmShape shape{by_columns(w, l.k), g, (int)n64};
             const int64_t stride = (int64_t)a.rows * a.hidden;
             if (piece == 0) {
                 splits = l.dx_plan.splits;
                 if (l.pieces == 1 && splits == 1)
-                    DV_TRY((product<false, T, Out::kStore>(shape, l.dx_plan, grad_x, a.rows, a.hidden, 0, s)));
+                    DV_TRY((product<T, false, T, Out::kStore>(shape, l.dx_plan, grad_x, a.rows, a.hidden, 0, s)));
                 else
-                    DV_TRY((product<false, float, Out::kPartial>(shape, l.dx_plan, dx, a.rows, a.hidden, stride, s)));
+                    DV_TRY((product<T, false, float, Out::kPartial>(shape, l.dx_plan, dx, a.rows, a.hidden, stride, s)));
             } else {
                 // the last piece's k is no longer than the first one's: its splits are no more
-                const int stages = (int)(n64 / kGemmStageK) * l.segments;
+                const int stages = (int)(n64 / l.stage_k);
                 Plan plan = l.dx_plan;
                 plan.splits = (stages + plan.stages - 1) / plan.stages;
-                DV_TRY((product<false, float, Out::kPartialAdd>(shape, plan, dx, a.rows, a.hidden, stride, s)));
+                DV_TRY((product<T, false, float, Out::kPartialAdd>(shape, plan, dx, a.rows, a.hidden, stride, s)));
             }
         }
         if (grad_weight) {
             GemmOperand g_t = by_columns(g, n64);
             g_t.k_rows = (int)r64;
-            const GemmShape shape{by_columns(x, l.k), g_t, (int)r64, l.segments};
-            const Plan plan = plan_product(l.k, n, r64 / kGemmStageK * l.segments, 1);
-            DV_TRY((product<true, T, Out::kStore>(shape, plan, grad_weight + (int64_t)v0 * a.hidden, n, a.hidden, 0, s)));
+            const GemmShape shape{by_columns(x, l.k), g_t, (int)r64};
+            const Plan plan = plan_product(l.k, n, r64 / l.stage_k, 1, kBf16);
+            DV_TRY((product<T, true, T, Out::kStore>(shape, plan, grad_weight + (int64_t)v0 * a.hidden, n, a.hidden, 0, s)));
         }
     }
     if (grad_x && !(l.pieces == 1 && splits == 1)) {
@@ -550,25 +521,30 @@ hipError_t launch_head_loss(const HeadArgs &a, float *loss, float *lse, void *wo
     Softmax *parts = reinterpret_cast<Softmax *>(ws + l.parts);
     float *target_logit = reinterpret_cast<float *>(ws + l.target_logit);
     GemmOperand x;
-    DV_TRY(operand(a.x, a.ld_x, a.dtype, a.rows, a.hidden, l, reinterpret_cast<__bf16 *>(ws + l.x), x, s));
+    DV_TRY(operand(a.x, a.ld_x, a.dtype, a.rows, a.hidden, l, ws + l.x, x, s));
     const bool whole = in_place(a.weight, a.ld_w, a.dtype, a.hidden);  // nothing to pack: one piece
     const int step = whole ? a.V : l.piece;
-    const int side = plan_product(step, a.rows, l.k / kGemmStageK * l.segments, 1).side;
+    const int side = plan_product(step, a.rows, l.k / l.stage_k, 1, a.dtype == 1).side;
     for (int v0 = 0; v0 < a.V; v0 += step) {
         const int n = a.V - v0 < step ? a.V - v0 : step;
         GemmOperand w;
-        DV_TRY(operand(weight_rows(a, v0), a.ld_w, a.dtype, n, a.hidden, l, reinterpret_cast<__bf16 *>(ws + l.w), w, s));
-        const GemmShape g{w, x, (int)l.k, l.segments};
-        DV_TRY(with_tile(side, [&](auto sd, auto wn) {
-            constexpr int B = decltype(sd)::value, WN = decltype(wn)::value;
-            const int ti = (n + B - 1) / B, tj = (a.rows + B - 1) / B;
-            stats_kernel<B, B, 2, WN><<<ti * tj, 2 * WN * kWave, 0, s>>>(g, v0, a.V, a.rows, a.masks, a.targets, parts,
-                                                                        target_logit, ti, tj);
-        }));
+        DV_TRY(operand(weight_rows(a, v0), a.ld_w, a.dtype, n, a.hidden, l, ws + l.w, w, s));
+        const GemmShape g{w, x, (int)l.k};
+        const auto run = [&](auto zero) {
+            using E = decltype(zero);
+            return with_tile(side, [&](auto sd, auto wn) {
+                constexpr int B = decltype(sd)::value, WN = decltype(wn)::value;
+                const int ti = (n + B - 1) / B, tj = (a.rows + B - 1) / B;
+                stats_kernel<E, B, B, 2, WN><<<ti * tj, 2 * WN * kWave, 0, s>>>(g, v0, a.V, a.rows, a.masks, a.targets,
+                                                                                parts, target_logit, ti, tj);
+            });
+        };
+        DV_TRY(a.dtype == 1 ? run((__bf16)0.f) : run(0.f));
     }
     const int nparts = (a.V + side - 1) / side * 2;
+    // a thread's share of the parts: about 16, more of them only for many rows
     int slices = 16;
-    while (slices < 256 && 256 / slices > a.rows)
+    while (slices < (a.rows < 64 ? 256 : 64) && slices * 16 < nparts)
         slices *= 2;
     const int per_block = 256 / slices;
     finish_kernel<<<(a.rows + per_block - 1) / per_block, 256, 0, s>>>(parts, nparts, a.rows, a.V, a.masks, a.targets,
