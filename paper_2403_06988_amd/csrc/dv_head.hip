@@ -50,6 +50,40 @@ __global__ __launch_bounds__(256) void pack_kernel(const T *src, int64_t ld, int
     }
 }
 
+// A wave's results on their way out: 16 rows (index j of the product, one a lane of
+// each 16) of COLS columns (index i, four a lane) go through LDS, so that they
+// leave as 16-byte pieces of whole lines (8-byte stores of 16 rows at a time,
+// straight from the registers, wrote 1 GB at 1.3 TB/s).
+template <typename T, int COLS>
+struct RowStage {
+    static constexpr int kPitch = COLS * (int)sizeof(T) + 16;
+    static constexpr int kBytes = 16 * kPitch;
+    static constexpr int kN = 16 / (int)sizeof(T);        // elements of a piece
+    static constexpr int kLanesPerRow = COLS / kN;
+    static constexpr int kRowsAtOnce = kWave / kLanesPerRow;
+    static_assert(kLanesPerRow <= kWave && kWave % kLanesPerRow == 0, "whole rows at once");
+
+    // four elements of fragment a, from lane `lane`
+    static __device__ __forceinline__ void put(char *lds, int lane, int a, const T (&y)[4])
+    {
+        __builtin_memcpy(lds + (lane & 15) * kPitch + (a * 16 + (lane >> 4) * 4) * (int)sizeof(T), y, sizeof y);
+    }
+    // f(row of the 16, first column, piece) for each of this lane's pieces
+    template <typename F>
+    static __device__ __forceinline__ void each(const char *lds, int lane, F &&f)
+    {
+        wave_lds_sync();
+#pragma unroll
+        for (int r = 0; r < 16; r += kRowsAtOnce) {
+            const int row = r + lane / kLanesPerRow, piece = lane % kLanesPerRow;
+            T y[kN];
+            __builtin_memcpy(y, lds + row * kPitch + piece * 16, 16);
+            f(row, piece * kN, y);
+        }
+        wave_lds_sync();
+    }
+};
+
 // --------------------------------------------------------------- the logits
 
 // Per row and tile: maximum and sum of exponentials of the allowed logits;
@@ -135,11 +169,14 @@ __global__ __launch_bounds__(256) void finish_kernel(const Softmax *parts, int n
             s = softmax_join(s, parts[(size_t)p * rows + n], kLog2e);
     }
     sh[threadIdx.x] = s;
-    __syncthreads();
+    for (int half = slices / 2; half; half /= 2) {
+        __syncthreads();
+        if (slice < half)
+            sh[threadIdx.x] = softmax_join(sh[threadIdx.x], sh[threadIdx.x + half * per_block], kLog2e);
+    }
     if (slice || n >= rows)
         return;
-    for (int i = 1; i < slices; ++i)
-        s = softmax_join(s, sh[i * per_block + threadIdx.x], kLog2e);
+    s = sh[threadIdx.x];
     const int t = targets[n];
     const RowMask m(masks, V, n);
     const float lns = s.empty() ? 0.f : logf(s.sum);
@@ -176,11 +213,16 @@ __global__ __launch_bounds__(WM *WN *kWave, 2) void grad_kernel(GemmShape g, int
     const int vw = v0 + lw;
     const int quarter = lane >> 4;
     const int rows64 = (rows + 63) & ~63;
+    using Rows = RowStage<E, BM / WM>;
+    static_assert(WM * WN * Rows::kBytes <= G::kLdsBytes, "every wave has its rows");
+    char *mine = lds + wave * Rows::kBytes;
+    G::barrier();  // the last stage is read
 #pragma unroll
     for (int b = 0; b < G::kTn; ++b) {
-        const int n = tj * BN + wn * (BN / WN) + b * 16 + (lane & 15);
-        if (n >= rows64)
-            continue;
+        const int n0 = tj * BN + wn * (BN / WN) + b * 16;
+        if (n0 >= rows64)
+            break;
+        const int n = n0 + (lane & 15);
         const bool live = n < rows;
         const RowMask m(masks, V, live ? n : 0);
         const float w = live ? weight[n] : 0.f;
@@ -196,10 +238,12 @@ __global__ __launch_bounds__(WM *WN *kWave, 2) void grad_kernel(GemmShape g, int
                 p -= t == a * 16 + quarter * 4 + e ? 1.f : 0.f;
                 y[e] = (E)(p * w);
             }
-            const int col = lw + a * 16 + quarter * 4;
-            if (col < ld)
-                __builtin_memcpy(out + (int64_t)n * ld + col, y, sizeof y);
+            Rows::put(mine, lane, a, y);
         }
+        Rows::each(mine, lane, [&](int row, int col, const E (&y)[Rows::kN]) {
+            if (lw + col < ld)  // 64 divides ld
+                __builtin_memcpy(out + (int64_t)(n0 + row) * ld + lw + col, y, sizeof y);
+        });
     }
 }
 
@@ -227,43 +271,72 @@ __global__ __launch_bounds__(WM *WN *kWave, 2) void product_kernel(GemmShape g, 
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
     const int wm = wave / WN, wn = wave % WN;
     out += blockIdx.y * split_stride;
+    using Rows = RowStage<T, BM / WM>;
+    static_assert(WM * WN * Rows::kBytes <= G::kLdsBytes, "every wave has its rows");
+    char *mine = lds + wave * Rows::kBytes;
+    G::barrier();  // the last stage is read
+    const int c0 = ti * BM + wm * (BM / WM);
 #pragma unroll
     for (int b = 0; b < G::kTn; ++b) {
-        const int r = tj * BN + wn * (BN / WN) + b * 16 + (lane & 15);
-        if (r >= out_rows)
-            continue;
+        const int r0 = tj * BN + wn * (BN / WN) + b * 16;
+        if (r0 >= out_rows)
+            break;
 #pragma unroll
         for (int a = 0; a < G::kTm; ++a) {
-            const int c = ti * BM + wm * (BM / WM) + a * 16 + (lane >> 4) * 4;
-            T *p = out + (int64_t)r * cols + c;
             T y[4];
-            if (c + 4 <= cols) {  // four elements of a row, at any element's alignment
-                if (OUT == Out::kPartialAdd)
-                    __builtin_memcpy(y, p, sizeof y);
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    y[e] = (T)(acc[a][b][e] + (OUT == Out::kPartialAdd ? (float)y[e] : 0.f));
+            for (int e = 0; e < 4; ++e)
+                y[e] = (T)acc[a][b][e];
+            Rows::put(mine, lane, a, y);
+        }
+        Rows::each(mine, lane, [&](int row, int col, T (&y)[Rows::kN]) {
+            T *p = out + (int64_t)(r0 + row) * cols + c0 + col;
+            const int left = r0 + row < out_rows ? cols - c0 - col : 0;
+            if (left >= Rows::kN) {  // at any element's alignment
+                if (OUT == Out::kPartialAdd) {
+                    T before[Rows::kN];
+                    __builtin_memcpy(before, p, sizeof before);
+#pragma unroll
+                    for (int e = 0; e < Rows::kN; ++e)
+                        y[e] += before[e];
+                }
                 __builtin_memcpy(p, y, sizeof y);
             } else {
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (c + e < cols)
-                        p[e] = (T)(acc[a][b][e] + (OUT == Out::kPartialAdd ? (float)p[e] : 0.f));
+                for (int e = 0; e < Rows::kN; ++e)
+                    if (e < left)
+                        p[e] = OUT == Out::kPartialAdd ? (T)(p[e] + y[e]) : y[e];
             }
-        }
+        });
     }
 }
 
+// The sum of the splits' parts, n elements each (a lane four of them), in T.
 template <typename T>
-__global__ void join_splits_kernel(const float *parts, int splits, int64_t n, T *out)
+__global__ __launch_bounds__(256) void join_splits_kernel(const float *parts, int splits, int64_t n, T *out)
 {
-    const int64_t i = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x);
+    const int64_t i = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) * 4;
     if (i >= n)
         return;
-    float s = 0.f;
-    for (int k = 0; k < splits; ++k)
-        s += parts[(int64_t)k * n + i];
-    out[i] = (T)s;
+    const int left = (int)(n - i < 4 ? n - i : 4);
+    float s[4] = {};
+    for (int k = 0; k < splits; ++k) {
+        float x[4];
+        if (left == 4)
+            __builtin_memcpy(x, parts + k * n + i, sizeof x);
+        else
+            for (int e = 0; e < 4; ++e)
+                x[e] = e < left ? parts[k * n + i + e] : 0.f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            s[e] += x[e];
+    }
+    const T y[4] = {(T)s[0], (T)s[1], (T)s[2], (T)s[3]};
+    if (left == 4)
+        __builtin_memcpy(out + i, y, sizeof y);
+    else
+        for (int e = 0; e < left; ++e)
+            out[i + e] = y[e];
 }
 
 template <typename T>
@@ -279,9 +352,13 @@ constexpr int64_t kPieceElements = (int64_t)1 << 27;
 constexpr int kPieceTokens = 1 << 18;
 
 // The tile side and the splits of k for a product of `i` x `j` over `stages` of
-// k (64 of bf16, 32 of fp32), by the time that each side would take: rounds of blocks over the 256
-// compute units, each block its stages and about three more to start and end, at
-// the rate the core reaches with that side; splits write and read their sums.
+// k (64 of bf16, 32 of fp32), by the time that each choice would take.  Up to
+// per_unit blocks share a compute unit: a stage of all of them takes `us` (PFLOP/s
+// at 8192 x 8192 x 4096, bf16 and fp32: side 256 1.17 and 0.205, 128 1.09 and 0.181, 64
+// 0.66 and 0.122), one alone two fifths of that and more; a block takes about three
+// stages more to start and end; its results leave at the unit's share of the
+// memory, hidden behind another block's work where units have several.  Splits
+// write and read their sums.
 struct Plan {
     int side, splits, stages;  // stages of a split; no split is empty
 };
@@ -290,9 +367,11 @@ Plan plan_product(int64_t i, int64_t j, int64_t stages, int most_splits, bool bf
 {
     struct Side {
         int side, per_unit;
-        double us;  // of a unit's blocks for one stage
+        double us[2];
     };
-    constexpr Side kSides[] = {{256, 1, 1.65}, {128, 2, 0.97}, {64, 4, 0.77}};
+    constexpr Side kSides[] = {{256, 1, {1.72, 5.2}}, {128, 2, {0.98, 3.0}}, {64, 4, {0.80, 2.3}}};
+    constexpr int kUnits = 256;
+    constexpr double kBytesPerUs = 19500;  // of a unit
     Plan best{64, 1, (int)stages};
     double least = 1e30;
     for (const Side &s : kSides) {
@@ -300,9 +379,17 @@ Plan plan_product(int64_t i, int64_t j, int64_t stages, int most_splits, bool bf
         for (int64_t want = 1; want <= most_splits; ++want) {
             const int64_t per = (stages + want - 1) / want;
             const int64_t used = (stages + per - 1) / per;
-            const int64_t slots = (int64_t)256 * s.per_unit;
-            const double rounds = (double)((tiles * used + slots - 1) / slots);
-            const double us = rounds * (double)(per + 3) * s.us * (bf16 ? 1.0 : 3.0) + (used > 1 ? (double)(used * i * j) * 2e-6 + 3 : 0);
+            const int64_t blocks = tiles * used, slots = (int64_t)kUnits * s.per_unit;
+            const double tile_bytes = (double)s.side * s.side * (used > 1 || !bf16 ? 4 : 2);
+            const auto round = [&](int64_t per_unit) {
+                const double work = (double)(per + 3) * s.us[bf16 ? 0 : 1] * (0.4 + 0.6 * (double)per_unit / s.per_unit);
+                const double store = (double)per_unit * tile_bytes / kBytesPerUs;
+                return per_unit > 1 ? (work > store ? work : store) : work + store;
+            };
+            const int64_t rest = blocks % slots;
+            const double us = (double)(blocks / slots) * round(s.per_unit) +
+                              (rest ? round((rest + kUnits - 1) / kUnits) : 0) +
+                              (used > 1 ? (double)(used * i * j) * 2e-6 + 5 : 0);
             if (us < least) {
                 least = us;
                 best = {s.side, (int)used, (int)per};
@@ -321,9 +408,14 @@ struct HeadLayout {
     int pieces;
     Plan dx_plan;
     size_t x, w, parts, target_logit;  // forward
-    size_t g, weight, dx;              // backward
+    size_t g, weight, dx, dw;          // backward
     size_t forward_bytes, backward_bytes;
 };
+
+Plan dw_plan(const HeadLayout &l, int rows, int64_t n, bool bf16)
+{
+    return plan_product(l.k, n, up64(rows > 0 ? rows : 1) / l.stage_k, 8, bf16);
+}
 
 HeadLayout head_layout(int rows, int hidden, int V, int dtype)
 {
@@ -359,6 +451,13 @@ HeadLayout head_layout(int rows, int hidden, int V, int dtype)
     // dx over a piece: few tiles and a long k
     l.dx_plan = plan_product(l.k, rows, p64 / l.stage_k, 16, dtype == 1);
     l.dx = take((size_t)l.dx_plan.splits * rows * hidden * 4);
+    // dw over a piece, and over the last one: split where hidden and tokens make few tiles
+    const auto dw_sums = [&](int64_t n) {
+        const Plan p = dw_plan(l, rows, n, dtype == 1);
+        return p.splits > 1 ? (size_t)p.splits * n * hidden * 4 : 0;
+    };
+    const size_t whole = dw_sums(l.piece), last = dw_sums(V - (int64_t)(l.pieces - 1) * l.piece);
+    l.dw = take(whole > last ? whole : last);
     l.backward_bytes = at;
     return l;
 }
@@ -436,6 +535,13 @@ hipError_t zero(T *p, int64_t n, hipStream_t s)
     return last_launch();
 }
 
+template <typename T>
+hipError_t join_splits(const float *parts, int splits, int64_t n, T *out, hipStream_t s)
+{
+    join_splits_kernel<T><<<(unsigned)((n + 1023) / 1024), 256, 0, s>>>(parts, splits, n, out);
+    return last_launch();
+}
+
 const void *weight_rows(const HeadArgs &a, int v0)
 {
     return static_cast<const char *>(a.weight) + (int64_t)v0 * a.ld_w * (a.dtype == 1 ? 2 : 4);
@@ -490,14 +596,20 @@ hipError_t backward(const HeadArgs &a, const float *lse, const float *grad_loss,
             GemmOperand g_t = by_columns(g, n64);
             g_t.k_rows = (int)r64;
             const GemmShape shape{by_columns(x, l.k), g_t, (int)r64};
-            const Plan plan = plan_product(l.k, n, r64 / l.stage_k, 1, kBf16);
-            DV_TRY((product<T, true, T, Out::kStore>(shape, plan, grad_weight + (int64_t)v0 * a.hidden, n, a.hidden, 0, s)));
+            const Plan plan = dw_plan(l, a.rows, n, kBf16);
+            T *out = grad_weight + (int64_t)v0 * a.hidden;
+            if (plan.splits == 1) {
+                DV_TRY((product<T, true, T, Out::kStore>(shape, plan, out, n, a.hidden, 0, s)));
+            } else {
+                const int64_t size = (int64_t)n * a.hidden;
+                float *dw = reinterpret_cast<float *>(ws + l.dw);
+                DV_TRY((product<T, true, float, Out::kPartial>(shape, plan, dw, n, a.hidden, size, s)));
+                DV_TRY(join_splits(dw, plan.splits, size, out, s));
+            }
         }
     }
     if (grad_x && !(l.pieces == 1 && splits == 1)) {
-        const int64_t n = (int64_t)a.rows * a.hidden;
-        join_splits_kernel<T><<<(unsigned)((n + 255) / 256), 256, 0, s>>>(dx, splits, n, grad_x);
-        DV_TRY(last_launch());
+        DV_TRY(join_splits(dx, splits, (int64_t)a.rows * a.hidden, grad_x, s));
     }
     return hipSuccess;
 }
