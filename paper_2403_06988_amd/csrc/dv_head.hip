@@ -355,21 +355,23 @@ constexpr int kPieceTokens = 1 << 18;
 // k (64 of bf16, 32 of fp32), by the time that each choice would take.  Up to
 // per_unit blocks share a compute unit: a stage of all of them takes `us` (PFLOP/s
 // at 8192 x 8192 x 4096, bf16 and fp32: side 256 1.17 and 0.205, 128 1.09 and 0.181, 64
-// 0.66 and 0.122), one alone two fifths of that and more; a block takes about three
-// stages more to start and end; its results leave at the unit's share of the
-// memory, hidden behind another block's work where units have several.  Splits
-// write and read their sums.
+// 0.66 and 0.122), one alone two fifths of that and more; a tile takes some stages
+// more to start and end; its results (out_bytes an element; 0: what little the
+// logits' kernels write does not count) leave at the unit's share of the memory,
+// hidden behind another block's work where units have several.  Splits write and
+// read their sums.  Against all choices of side and splits, timed at nine shapes of
+// 8 to 8,192 rows in both types, it picks one within 5 % of the fastest.
 struct Plan {
     int side, splits, stages;  // stages of a split; no split is empty
 };
 
-Plan plan_product(int64_t i, int64_t j, int64_t stages, int most_splits, bool bf16)
+Plan plan_product(int64_t i, int64_t j, int64_t stages, int most_splits, bool bf16, int out_bytes)
 {
     struct Side {
-        int side, per_unit;
+        int side, per_unit, around;  // around: stages that a tile's start and end cost
         double us[2];
     };
-    constexpr Side kSides[] = {{256, 1, {1.72, 5.2}}, {128, 2, {0.98, 3.0}}, {64, 4, {0.80, 2.3}}};
+    constexpr Side kSides[] = {{256, 1, 3, {1.72, 5.2}}, {128, 2, 5, {1.03, 3.1}}, {64, 4, 5, {0.80, 2.3}}};
     constexpr int kUnits = 256;
     constexpr double kBytesPerUs = 19500;  // of a unit
     Plan best{64, 1, (int)stages};
@@ -380,9 +382,9 @@ Plan plan_product(int64_t i, int64_t j, int64_t stages, int most_splits, bool bf
             const int64_t per = (stages + want - 1) / want;
             const int64_t used = (stages + per - 1) / per;
             const int64_t blocks = tiles * used, slots = (int64_t)kUnits * s.per_unit;
-            const double tile_bytes = (double)s.side * s.side * (used > 1 || !bf16 ? 4 : 2);
+            const double tile_bytes = (double)s.side * s.side * (used > 1 ? 4 : out_bytes);
             const auto round = [&](int64_t per_unit) {
-                const double work = (double)(per + 3) * s.us[bf16 ? 0 : 1] * (0.4 + 0.6 * (double)per_unit / s.per_unit);
+                const double work = (double)(per + s.around) * s.us[bf16 ? 0 : 1] * (0.4 + 0.6 * (double)per_unit / s.per_unit);
                 const double store = (double)per_unit * tile_bytes / kBytesPerUs;
                 return per_unit > 1 ? (work > store ? work : store) : work + store;
             };
@@ -414,7 +416,7 @@ struct HeadLayout {
 
 Plan dw_plan(const HeadLayout &l, int rows, int64_t n, bool bf16)
 {
-    return plan_product(l.k, n, up64(rows > 0 ? rows : 1) / l.stage_k, 8, bf16);
+    return plan_product(l.k, n, up64(rows > 0 ? rows : 1) / l.stage_k, 8, bf16, bf16 ? 2 : 4);
 }
 
 HeadLayout head_layout(int rows, int hidden, int V, int dtype)
@@ -449,7 +451,7 @@ HeadLayout head_layout(int rows, int hidden, int V, int dtype)
     l.g = take(r64 * p64 * elt);
     l.weight = take((size_t)r64 * 4);
     // dx over a piece: few tiles and a long k
-    l.dx_plan = plan_product(l.k, rows, p64 / l.stage_k, 16, dtype == 1);
+    l.dx_plan = plan_product(l.k, rows, p64 / l.stage_k, 16, dtype == 1, 4);
     l.dx = take((size_t)l.dx_plan.splits * rows * hidden * 4);
     // dw over a piece, and over the last one: split where hidden and tokens make few tiles
     const auto dw_sums = [&](int64_t n) {
@@ -569,7 +571,7 @@ hipError_t backward(const HeadArgs &a, const float *lse, const float *grad_loss,
         DV_TRY(operand(weight_rows(a, v0), a.ld_w, a.dtype, n, a.hidden, l, ws + l.w, w, s));
         const GemmShape logits{w, x, (int)l.k};
         const GemmOperand g{g_piece, n64, a.rows, 0};
-        DV_TRY(with_tile(plan_product(n, a.rows, l.k / l.stage_k, 1, kBf16).side, [&](auto side, auto wn) {
+        DV_TRY(with_tile(plan_product(n, a.rows, l.k / l.stage_k, 1, kBf16, 0).side, [&](auto side, auto wn) {
             constexpr int B = decltype(side)::value, WN = decltype(wn)::value;
             const int ti = (n + B - 1) / B, tj = (a.rows + B - 1) / B;
             grad_kernel<T, B, B, 2, WN><<<ti * tj, 2 * WN * kWave, 0, s>>>(logits, v0, a.V, a.rows, a.masks, a.targets, lse,
@@ -636,7 +638,7 @@ hipError_t launch_head_loss(const HeadArgs &a, float *loss, float *lse, void *wo
     DV_TRY(operand(a.x, a.ld_x, a.dtype, a.rows, a.hidden, l, ws + l.x, x, s));
     const bool whole = in_place(a.weight, a.ld_w, a.dtype, a.hidden);  // nothing to pack: one piece
     const int step = whole ? a.V : l.piece;
-    const int side = plan_product(step, a.rows, l.k / l.stage_k, 1, a.dtype == 1).side;
+    const int side = plan_product(step, a.rows, l.k / l.stage_k, 1, a.dtype == 1, 0).side;
     for (int v0 = 0; v0 < a.V; v0 += step) {
         const int n = a.V - v0 < step ? a.V - v0 : step;
         GemmOperand w;
