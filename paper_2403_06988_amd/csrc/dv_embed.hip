@@ -14,39 +14,63 @@ namespace {
 
 constexpr int kThreads = 256;
 
+__device__ __forceinline__ float to_float(float x) { return x; }
+__device__ __forceinline__ float to_float(uint16_t x) { return widen(x); }
+__device__ __forceinline__ void from_float(float y, float &x) { x = y; }
+__device__ __forceinline__ void from_float(float y, uint16_t &x) { x = narrow(y); }
+
 // Elements of one lane, 16 bytes from any element on; rows end where they end, so
 // a row's last lane may hold fewer (`n` of them).
 template <typename T>
 struct Pack {
     static constexpr int kN = 16 / sizeof(T);
-    T x[kN];
+    Words w;
+    __device__ __forceinline__ T get(int i) const { return element<T>(w, i); }
     __device__ __forceinline__ void load(const T *p, int n)
     {
         if (n >= kN) {
-            __builtin_memcpy(x, p, 16);
+            w = load_words(p);
         } else {
+            T x[kN];
 #pragma unroll
             for (int i = 0; i < kN; ++i)
                 x[i] = i < n ? p[i] : T(0);
+            set(x);
         }
     }
     __device__ __forceinline__ void store(T *p, int n) const
     {
         if (n >= kN) {
-            __builtin_memcpy(p, x, 16);
+            store_words(p, w);
         } else {
 #pragma unroll
             for (int i = 0; i < kN; ++i)
                 if (i < n)
-                    p[i] = x[i];
+                    p[i] = get(i);
         }
     }
+    __device__ __forceinline__ void set(const T (&x)[kN])
+    {
+        union {
+            T t[kN];
+            Words w;
+        } u;
+#pragma unroll
+        for (int i = 0; i < kN; ++i)
+            u.t[i] = x[i];
+        w = u.w;
+    }
+    // f(i) in T, for every element
+    template <typename F>
+    __device__ __forceinline__ void fill(F &&f)
+    {
+        T x[kN];
+#pragma unroll
+        for (int i = 0; i < kN; ++i)
+            from_float(f(i), x[i]);
+        set(x);
+    }
 };
-
-__device__ __forceinline__ float to_float(float x) { return x; }
-__device__ __forceinline__ float to_float(uint16_t x) { return widen(x); }
-__device__ __forceinline__ void from_float(float y, float &x) { x = y; }
-__device__ __forceinline__ void from_float(float y, uint16_t &x) { x = narrow(y); }
 
 // A lane group of 2^lanes_log2 lanes copies ROWS rows at once, `step` apart.
 template <typename T, int ROWS>
@@ -72,11 +96,10 @@ __global__ __launch_bounds__(kThreads) void embed_kernel(const T *weight, int64_
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) {
             const bool in = (uint32_t)id[r] < (uint32_t)V;
-#pragma unroll
-            for (int i = 0; i < N; ++i)
-                from_float(in ? to_float(v[r].x[i]) * scale : 0.f, v[r].x[i]);
+            Pack<T> y;
+            y.fill([&](int i) { return in ? to_float(v[r].get(i)) * scale : 0.f; });
             if (row + r * step < rows)
-                v[r].store(out + (row + r * step) * D + col, n);
+                y.store(out + (row + r * step) * D + col, n);
         }
     }
 }
@@ -330,10 +353,9 @@ __device__ __forceinline__ void emit(T *grad, const float (&acc)[Pack<T>::kN], i
     Pack<T> v;
     if (accumulate)
         v.load(grad, n);
-#pragma unroll
-    for (int i = 0; i < Pack<T>::kN; ++i)
-        from_float(accumulate ? to_float(v.x[i]) + acc[i] * scale : acc[i] * scale, v.x[i]);
-    v.store(grad, n);
+    Pack<T> y;
+    y.fill([&](int i) { return accumulate ? to_float(v.get(i)) + acc[i] * scale : acc[i] * scale; });
+    y.store(grad, n);
 }
 
 template <typename T>
@@ -357,7 +379,10 @@ __global__ __launch_bounds__(kThreads) void sum_chunks_kernel(const T *grad_out,
     bool first = true;  // still in the chunk's first run
     int key = keys[from];
     const auto keep = [&](int slot) {
-        __builtin_memcpy(parts + ((int64_t)c * 2 + slot) * part_ld + col, acc, sizeof acc);
+        float *p = parts + ((int64_t)c * 2 + slot) * part_ld + col;
+#pragma unroll
+        for (int e = 0; e < N; e += 4)
+            *reinterpret_cast<float4 *>(p + e) = make_float4(acc[e], acc[e + 1], acc[e + 2], acc[e + 3]);
     };
     for (int64_t i = from; i < to && key < V; i += U) {
         Pack<T> v[U];
@@ -387,7 +412,7 @@ __global__ __launch_bounds__(kThreads) void sum_chunks_kernel(const T *grad_out,
             }
 #pragma unroll
             for (int e = 0; e < N; ++e)
-                acc[e] += to_float(v[u].x[e]);
+                acc[e] += to_float(v[u].get(e));
         }
     }
     if (key >= V)
@@ -398,6 +423,20 @@ __global__ __launch_bounds__(kThreads) void sum_chunks_kernel(const T *grad_out,
         keep(1);
     else
         emit<T>(grad + (int64_t)key * D + col, acc, n, scale, accumulate);
+}
+
+// N floats of a part (16-byte aligned: parts are a multiple of 8 floats apart).
+template <int N>
+__device__ __forceinline__ void read_part(float (&x)[N], const float *p)
+{
+#pragma unroll
+    for (int e = 0; e < N; e += 4) {
+        const float4 f = *reinterpret_cast<const float4 *>(p + e);
+        x[e] = f.x;
+        x[e + 1] = f.y;
+        x[e + 2] = f.z;
+        x[e + 3] = f.w;
+    }
 }
 
 template <typename T>
@@ -431,14 +470,14 @@ __global__ __launch_bounds__(kThreads) void sum_parts_kernel(int D, const int *k
         return;
     float acc[N];
     const float *p = parts + ((int64_t)c * 2 + 1) * part_ld + col;
-    __builtin_memcpy(acc, p, sizeof acc);
+    read_part(acc, p);
     p += part_ld;  // slot 0 of the next chunk
     constexpr int U = 8;
     for (int d = c + 1; d <= last; d += U) {
         float part[U][N];
 #pragma unroll
         for (int u = 0; u < U; ++u)
-            __builtin_memcpy(part[u], p + (int64_t)(d + u <= last ? u : 0) * 2 * part_ld, sizeof acc);
+            read_part(part[u], p + (int64_t)(d + u <= last ? u : 0) * 2 * part_ld);
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll

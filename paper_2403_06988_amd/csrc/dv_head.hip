@@ -38,15 +38,20 @@ __global__ __launch_bounds__(256) void pack_kernel(const T *src, int64_t ld, int
         const int64_t row = i / vecs;
         const int col = (int)(i - row * vecs) * N;
         const T *p = src + row * ld + col;
-        T x[N];
+        Words x;
         if (col + N <= cols) {
-            __builtin_memcpy(x, p, 16);
+            x = load_words(p);
         } else {
+            union {
+                T t[N];
+                Words w;
+            } part;
 #pragma unroll
             for (int e = 0; e < N; ++e)
-                x[e] = col + e < cols ? p[e] : T(0);
+                part.t[e] = col + e < cols ? p[e] : T(0);
+            x = part.w;
         }
-        *reinterpret_cast<uint4 *>(dst + row * out_cols + col) = *reinterpret_cast<const uint4 *>(x);
+        *reinterpret_cast<Words *>(dst + row * out_cols + col) = x;
     }
 }
 
@@ -76,9 +81,7 @@ struct RowStage {
 #pragma unroll
         for (int r = 0; r < 16; r += kRowsAtOnce) {
             const int row = r + lane / kLanesPerRow, piece = lane % kLanesPerRow;
-            T y[kN];
-            __builtin_memcpy(y, lds + row * kPitch + piece * 16, 16);
-            f(row, piece * kN, y);
+            f(row, piece * kN, *reinterpret_cast<const Words *>(lds + row * kPitch + piece * 16));
         }
         wave_lds_sync();
     }
@@ -240,9 +243,9 @@ __global__ __launch_bounds__(WM *WN *kWave, 2) void grad_kernel(GemmShape g, int
             }
             Rows::put(mine, lane, a, y);
         }
-        Rows::each(mine, lane, [&](int row, int col, const E (&y)[Rows::kN]) {
+        Rows::each(mine, lane, [&](int row, int col, Words y) {
             if (lw + col < ld)  // 64 divides ld
-                __builtin_memcpy(out + (int64_t)(n0 + row) * ld + lw + col, y, sizeof y);
+                store_words(out + (int64_t)(n0 + row) * ld + lw + col, y);
         });
     }
 }
@@ -289,23 +292,27 @@ __global__ __launch_bounds__(WM *WN *kWave, 2) void product_kernel(GemmShape g, 
                 y[e] = (T)acc[a][b][e];
             Rows::put(mine, lane, a, y);
         }
-        Rows::each(mine, lane, [&](int row, int col, T (&y)[Rows::kN]) {
+        Rows::each(mine, lane, [&](int row, int col, Words y) {
             T *p = out + (int64_t)(r0 + row) * cols + c0 + col;
             const int left = r0 + row < out_rows ? cols - c0 - col : 0;
-            if (left >= Rows::kN) {  // at any element's alignment
-                if (OUT == Out::kPartialAdd) {
-                    T before[Rows::kN];
-                    __builtin_memcpy(before, p, sizeof before);
+            if constexpr (OUT == Out::kPartialAdd) {
+                f32x4 before = {};
+                if (left >= Rows::kN) {
+                    before = __builtin_bit_cast(f32x4, load_words(p));
+                } else {
 #pragma unroll
                     for (int e = 0; e < Rows::kN; ++e)
-                        y[e] += before[e];
+                        before[e] = e < left ? p[e] : 0.f;
                 }
-                __builtin_memcpy(p, y, sizeof y);
+                y = __builtin_bit_cast(Words, before + __builtin_bit_cast(f32x4, y));
+            }
+            if (left >= Rows::kN) {
+                store_words(p, y);
             } else {
 #pragma unroll
                 for (int e = 0; e < Rows::kN; ++e)
                     if (e < left)
-                        p[e] = OUT == Out::kPartialAdd ? (T)(p[e] + y[e]) : y[e];
+                        p[e] = element<T>(y, e);
             }
         });
     }
@@ -319,17 +326,15 @@ __global__ __launch_bounds__(256) void join_splits_kernel(const float *parts, in
     if (i >= n)
         return;
     const int left = (int)(n - i < 4 ? n - i : 4);
-    float s[4] = {};
+    f32x4 s = {};
     for (int k = 0; k < splits; ++k) {
-        float x[4];
+        f32x4 x = {};
         if (left == 4)
-            __builtin_memcpy(x, parts + k * n + i, sizeof x);
+            x = __builtin_bit_cast(f32x4, load_words(parts + k * n + i));
         else
-            for (int e = 0; e < 4; ++e)
-                x[e] = e < left ? parts[k * n + i + e] : 0.f;
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            s[e] += x[e];
+            for (int e = 0; e < left; ++e)
+                x[e] = parts[k * n + i + e];
+        s += x;
     }
     const T y[4] = {(T)s[0], (T)s[1], (T)s[2], (T)s[3]};
     if (left == 4)

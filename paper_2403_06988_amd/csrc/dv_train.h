@@ -108,6 +108,24 @@ __device__ __forceinline__ uint32_t narrow_pair(float lo, float hi)
     return c.u;
 }
 
+// 16 bytes from and to any element's alignment, as one access (arrays of
+// elements copied with memcpy come apart into smaller ones).
+typedef __attribute__((ext_vector_type(4))) uint32_t Words;
+typedef __attribute__((ext_vector_type(4), aligned(2))) uint32_t AnyWords;
+__device__ __forceinline__ Words load_words(const void *p) { return *static_cast<const AnyWords *>(p); }
+__device__ __forceinline__ void store_words(void *p, Words w) { *static_cast<AnyWords *>(p) = w; }
+// Element i of 16 bytes of T.
+template <typename T>
+__device__ __forceinline__ T element(const Words &w, int i)
+{
+    union {
+        Words w;
+        T t[16 / sizeof(T)];
+    } u;
+    u.w = w;
+    return u.t[i];
+}
+
 inline hipError_t last_launch() { return hipGetLastError(); }
 
 // --------------------------------------------------------------- head loss
