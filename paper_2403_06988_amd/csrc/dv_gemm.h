@@ -1,7 +1,7 @@
 // Tiled matrix product C[i][j] = sum_k A(i, k) B(j, k) of bf16 or fp32 operands with
 // fp32 sums, the core of the head loss (dv_head.hip).  Each operand is stored with
 // k along its rows ("rows": i by k) or with k from row to row ("columns": k by i);
-// row starts are on 16-byte boundaries and k is a multiple of 64.
+// row starts are on 16-byte boundaries.
 #pragma once
 
 #include "dv_internal.h"
@@ -25,7 +25,7 @@ struct GemmOperand {
 
 struct GemmShape {
     GemmOperand a, b;
-    int k;  // a multiple of 64
+    int k;  // whole stages: a multiple of 64 (bf16) or 32 (fp32)
 };
 
 // The waves of a block split its BM x BN tile into WM x WN parts; COLS_A and
@@ -212,7 +212,7 @@ struct Gemm {
     static constexpr int kLoads = kGroups / kWaves;  // of one wave per stage
     static constexpr int kStageBytes = A::kBytes + B::kBytes;
     static constexpr int kLdsBytes = 2 * kStageBytes;
-    static_assert(kGroups % kWaves == 0 && A::kGroups % kLoads == 0, "a wave loads whole groups of one side");
+    static_assert(kGroups % kWaves == 0, "a wave loads whole groups");
 
     using Lds = __attribute__((address_space(3))) void *;
 
@@ -292,39 +292,50 @@ struct Gemm {
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
         const int wm = wave / WN, wn = wave % WN;
 
-        // this wave's loads: kLoads groups of one side
+        // this wave's loads: kLoads groups, of one side (or, in tiles of uneven
+        // sides, of both)
         const int group = wave * kLoads;
-        const bool side_a = group < A::kGroups;
-        const GemmOperand &o = side_a ? g.a : g.b;
-        const bool cols = side_a ? COLS_A : COLS_B;
-        const int first = side_a ? i0 : j0;
-        const int64_t stage_step = (cols ? kStageK * o.ld : kStageK) * (int64_t)sizeof(E);
-        const char *const start = reinterpret_cast<const char *>(static_cast<const E *>(o.p) + (cols ? first : first * o.ld));
+        const auto side_a = [&](int i) {
+            constexpr bool kMixed = A::kGroups % kLoads != 0;
+            return group + (kMixed ? i : 0) < A::kGroups;
+        };
+        const auto start = [&](const GemmOperand &o, bool cols, int first) {
+            return reinterpret_cast<const char *>(static_cast<const E *>(o.p) + (cols ? first : first * o.ld));
+        };
+        const auto step = [&](const GemmOperand &o, bool cols) {
+            return (cols ? kStageK * o.ld : kStageK) * (int64_t)sizeof(E);
+        };
+        const char *const start_a = start(g.a, COLS_A, i0), *const start_b = start(g.b, COLS_B, j0);
+        const int64_t step_a = step(g.a, COLS_A), step_b = step(g.b, COLS_B);
         int voff[kLoads];
-        const auto place_loads = [&](int k_left) {
+        const auto place_loads = [&](int left_a, int left_b) {
 #pragma unroll
             for (int i = 0; i < kLoads; ++i)
-                voff[i] = side_a ? A::source(o, first, group + i, lane, k_left)
-                                 : B::source(o, first, group - A::kGroups + i, lane, k_left);
+                voff[i] = side_a(i) ? A::source(g.a, i0, group + i, lane, left_a)
+                                    : B::source(g.b, j0, group + i - A::kGroups, lane, left_b);
         };
-        place_loads(kStageK);
+        place_loads(kStageK, kStageK);
         int stage = from;
-        const int slot_base = side_a ? group * A::kPitch : A::kBytes + (group - A::kGroups) * B::kPitch;
-        const int pitch = side_a ? A::kPitch : B::kPitch;
-        const bool ragged = cols && o.k_rows < g.k;  // k's last rows do not exist
 
         const auto load = [&](int slot) {
-            const char *q = start + stage * stage_step;
-            if (ragged && (stage + 1) * kStageK > o.k_rows) {
-                const int left = o.k_rows - stage * kStageK;
-                place_loads(left > 0 ? left : 1);
-                if (left <= 0)  // a whole stage of them: the last row
-                    q = start + (int64_t)(o.k_rows - 1) * o.ld * (int64_t)sizeof(E);
-            }
-            const uint32_t dst = (uint32_t)(uintptr_t)(Lds)(lds + slot * kStageBytes + slot_base);
+            // rows of k that do not exist, by columns: the last one again
+            const auto left = [&](const GemmOperand &o, bool cols) {
+                return cols ? o.k_rows - stage * kStageK : kStageK;
+            };
+            const auto place = [&](const char *start, int64_t step, const GemmOperand &o, int left) {
+                return left > 0 ? start + stage * step : start + (int64_t)(o.k_rows - 1) * o.ld * (int64_t)sizeof(E);
+            };
+            const int left_a = left(g.a, COLS_A), left_b = left(g.b, COLS_B);
+            if (left_a < kStageK || left_b < kStageK)
+                place_loads(left_a > 0 ? left_a : 1, left_b > 0 ? left_b : 1);
+            const char *const qa = place(start_a, step_a, g.a, left_a), *const qb = place(start_b, step_b, g.b, left_b);
+            const uint32_t dst = (uint32_t)(uintptr_t)(Lds)(lds + slot * kStageBytes);
 #pragma unroll
-            for (int i = 0; i < kLoads; ++i)
-                load_to_lds(q, voff[i], dst + i * pitch);
+            for (int i = 0; i < kLoads; ++i) {
+                const int at = group + i;
+                load_to_lds(side_a(i) ? qa : qb, voff[i],
+                            dst + (side_a(i) ? at * A::kPitch : A::kBytes + (at - A::kGroups) * B::kPitch));
+            }
             ++stage;
         };
 

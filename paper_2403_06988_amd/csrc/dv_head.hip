@@ -196,7 +196,8 @@ __global__ void weights_kernel(int rows, int V, Masks masks, const int32_t *targ
 }
 
 // A piece of G in the operands' type: [rows][ld] with the piece's tokens along a
-// row, zeros up to the next multiple of 64 both ways.
+// row, zeros up to the next multiple of 64 of them, and up to the next whole stage
+// of rows.
 template <typename E, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__(WM *WN *kWave, 2) void grad_kernel(GemmShape g, int v0, int V, int rows, Masks masks,
                                                                 const int32_t *targets, const float *lse,
@@ -215,7 +216,7 @@ __global__ __launch_bounds__(WM *WN *kWave, 2) void grad_kernel(GemmShape g, int
     const int lw = ti * BM + wm * (BM / WM);  // the wave's first token in the piece
     const int vw = v0 + lw;
     const int quarter = lane >> 4;
-    const int rows64 = (rows + 63) & ~63;
+    const int rows_k = (rows + G::kStageK - 1) / G::kStageK * G::kStageK;
     using Rows = RowStage<E, BM / WM>;
     static_assert(WM * WN * Rows::kBytes <= G::kLdsBytes, "every wave has its rows");
     char *mine = lds + wave * Rows::kBytes;
@@ -223,7 +224,7 @@ __global__ __launch_bounds__(WM *WN *kWave, 2) void grad_kernel(GemmShape g, int
 #pragma unroll
     for (int b = 0; b < G::kTn; ++b) {
         const int n0 = tj * BN + wn * (BN / WN) + b * 16;
-        if (n0 >= rows64)
+        if (n0 >= rows_k)
             break;
         const int n = n0 + (lane & 15);
         const bool live = n < rows;
@@ -256,14 +257,15 @@ enum class Out { kStore, kPartial, kPartialAdd };
 
 // C[j][i] of a product as `out_rows` rows of `cols` elements: in T, or in fp32
 // as (or on top of) the partial sums of this block's share of k.  A is stored by
-// columns, B by columns with COLS_B.
-template <typename E, int BM, int BN, int WM, int WN, bool COLS_B, typename T, Out OUT>
+// columns, B by columns with COLS_B.  One buffer where k is one stage: three
+// blocks a compute unit instead of two (64 rows x 2048 x 128,256 bf16: 103 us and 128).
+template <typename E, int BM, int BN, int WM, int WN, bool COLS_B, typename T, Out OUT, int BUFFERS>
 __global__ __launch_bounds__(WM *WN *kWave, 2) void product_kernel(GemmShape g, T *out, int out_rows, int cols,
                                                                    int64_t split_stride, int split_stages, int tiles_i,
                                                                    int tiles_j)
 {
     using G = Gemm<E, BM, BN, WM, WN, true, COLS_B>;
-    __shared__ __attribute__((aligned(1024))) char lds[G::kLdsBytes];
+    __shared__ __attribute__((aligned(1024))) char lds[BUFFERS * G::kStageBytes];
     int ti, tj;
     tile_of_block(blockIdx.x, tiles_i, tiles_j, ti, tj);
     const int total = g.k / G::kStageK;
@@ -275,7 +277,7 @@ __global__ __launch_bounds__(WM *WN *kWave, 2) void product_kernel(GemmShape g, 
     const int wm = wave / WN, wn = wave % WN;
     out += blockIdx.y * split_stride;
     using Rows = RowStage<T, BM / WM>;
-    static_assert(WM * WN * Rows::kBytes <= G::kLdsBytes, "every wave has its rows");
+    static_assert(WM * WN * Rows::kBytes <= BUFFERS * G::kStageBytes, "every wave has its rows");
     char *mine = lds + wave * Rows::kBytes;
     G::barrier();  // the last stage is read
     const int c0 = ti * BM + wm * (BM / WM);
@@ -307,7 +309,12 @@ __global__ __launch_bounds__(WM *WN *kWave, 2) void product_kernel(GemmShape g, 
                 y = __builtin_bit_cast(Words, before + __builtin_bit_cast(f32x4, y));
             }
             if (left >= Rows::kN) {
-                store_words(p, y);
+                // the weight's gradient is large and read by nobody here (64 rows x 2048 x
+                // 128,256 bf16: 129 us for it, with ordinary stores 217)
+                if (COLS_B && OUT == Out::kStore)
+                    stream_words(p, y);
+                else
+                    store_words(p, y);
             } else {
 #pragma unroll
                 for (int e = 0; e < Rows::kN; ++e)
@@ -366,28 +373,38 @@ constexpr int kPieceTokens = 1 << 18;
 // hidden behind another block's work where units have several.  Splits write and
 // read their sums.  Against all choices of side and splits, timed at nine shapes of
 // 8 to 8,192 rows in both types, it picks one within 5 % of the fastest.
+//
+// fp32 products of at most 32 rows j may take tiles of 64 x 32: each part of A is
+// split for fewer columns that nobody asked for (8 x 4096 x 128,256 forward: 455 us, in 64 x 64 ones 637).
+constexpr int kNarrow = 32;
+
 struct Plan {
     int side, splits, stages;  // stages of a split; no split is empty
 };
 
-Plan plan_product(int64_t i, int64_t j, int64_t stages, int most_splits, bool bf16, int out_bytes)
+Plan plan_product(int64_t i, int64_t j, int64_t stages, int most_splits, bool bf16, int out_bytes, bool narrow)
 {
     struct Side {
-        int side, per_unit, around;  // around: stages that a tile's start and end cost
+        int side, other, per_unit, around;  // around: stages that a tile's start and end cost
         double us[2];
     };
-    constexpr Side kSides[] = {{256, 1, 3, {1.72, 5.2}}, {128, 2, 5, {1.03, 3.1}}, {64, 4, 5, {0.80, 2.3}}};
+    constexpr Side kSides[] = {{256, 256, 1, 3, {1.72, 5.2}},
+                               {128, 128, 2, 5, {1.03, 3.1}},
+                               {64, 64, 4, 5, {0.80, 2.3}},
+                               {kNarrow, 64, 6, 5, {0, 2.3}}};
     constexpr int kUnits = 256;
     constexpr double kBytesPerUs = 19500;  // of a unit
     Plan best{64, 1, (int)stages};
     double least = 1e30;
     for (const Side &s : kSides) {
-        const int64_t tiles = ((i + s.side - 1) / s.side) * ((j + s.side - 1) / s.side);
+        if (s.side == kNarrow && (!narrow || bf16 || j > kNarrow))
+            continue;
+        const int64_t tiles = ((i + s.other - 1) / s.other) * ((j + s.side - 1) / s.side);
         for (int64_t want = 1; want <= most_splits; ++want) {
             const int64_t per = (stages + want - 1) / want;
             const int64_t used = (stages + per - 1) / per;
             const int64_t blocks = tiles * used, slots = (int64_t)kUnits * s.per_unit;
-            const double tile_bytes = (double)s.side * s.side * (used > 1 ? 4 : out_bytes);
+            const double tile_bytes = (double)s.side * s.other * (used > 1 ? 4 : out_bytes);
             const auto round = [&](int64_t per_unit) {
                 const double work = (double)(per + s.around) * s.us[bf16 ? 0 : 1] * (0.4 + 0.6 * (double)per_unit / s.per_unit);
                 const double store = (double)per_unit * tile_bytes / kBytesPerUs;
@@ -421,7 +438,8 @@ struct HeadLayout {
 
 Plan dw_plan(const HeadLayout &l, int rows, int64_t n, bool bf16)
 {
-    return plan_product(l.k, n, up64(rows > 0 ? rows : 1) / l.stage_k, 8, bf16, bf16 ? 2 : 4);
+    const int64_t stages = rows > 0 ? (rows + l.stage_k - 1) / l.stage_k : 1;
+    return plan_product(l.k, n, stages, 8, bf16, bf16 ? 2 : 4, false);
 }
 
 HeadLayout head_layout(int rows, int hidden, int V, int dtype)
@@ -456,7 +474,7 @@ HeadLayout head_layout(int rows, int hidden, int V, int dtype)
     l.g = take(r64 * p64 * elt);
     l.weight = take((size_t)r64 * 4);
     // dx over a piece: few tiles and a long k
-    l.dx_plan = plan_product(l.k, rows, p64 / l.stage_k, 16, dtype == 1, 4);
+    l.dx_plan = plan_product(l.k, rows, p64 / l.stage_k, 16, dtype == 1, 4, true);
     l.dx = take((size_t)l.dx_plan.splits * rows * hidden * 4);
     // dw over a piece, and over the last one: split where hidden and tokens make few tiles
     const auto dw_sums = [&](int64_t n) {
@@ -503,15 +521,24 @@ hipError_t operand(const void *p, int64_t ld, int dtype, int rows, int hidden, c
             return e_;                 \
     } while (0)
 
-template <typename F>
+template <int BM, int BN, int WN>
+struct Tile {
+    static constexpr int kM = BM, kN = BN, kWn = WN;
+    static constexpr int kThreads = 2 * WN * kWave;
+};
+
+// f with the tile of a plan's side; NARROW: whether that may be the 64 x 32 one.
+template <bool NARROW, typename F>
 hipError_t with_tile(int side, F &&f)
 {
     if (side == 256)
-        f(std::integral_constant<int, 256>{}, std::integral_constant<int, 4>{});
+        f(Tile<256, 256, 4>{});
     else if (side == 128)
-        f(std::integral_constant<int, 128>{}, std::integral_constant<int, 2>{});
-    else
-        f(std::integral_constant<int, 64>{}, std::integral_constant<int, 2>{});
+        f(Tile<128, 128, 2>{});
+    else if (side == 64)
+        f(Tile<64, 64, 2>{});
+    else if constexpr (NARROW)
+        f(Tile<64, kNarrow, 1>{});
     return last_launch();
 }
 
@@ -524,10 +551,18 @@ GemmOperand by_columns(const GemmOperand &o, int64_t k)
 template <typename E, bool COLS_B, typename T, Out OUT>
 hipError_t product(const GemmShape &g, const Plan &plan, T *out, int out_rows, int cols, int64_t split_stride, hipStream_t s)
 {
-    return with_tile(plan.side, [&](auto side, auto wn) {
-        constexpr int B = decltype(side)::value, WN = decltype(wn)::value;
-        const int ti = (cols + B - 1) / B, tj = (out_rows + B - 1) / B;
-        product_kernel<E, B, B, 2, WN, COLS_B, T, OUT><<<dim3(ti * tj, plan.splits), 2 * WN * kWave, 0, s>>>(
+    return with_tile<!COLS_B && sizeof(E) == 4>(plan.side, [&](auto tile) {
+        using X = decltype(tile);
+        const int ti = (cols + X::kM - 1) / X::kM, tj = (out_rows + X::kN - 1) / X::kN;
+        const dim3 grid(ti * tj, plan.splits);
+        if constexpr (COLS_B && OUT == Out::kStore && X::kM == 128) {
+            if (plan.stages == 1) {
+                product_kernel<E, X::kM, X::kN, 2, X::kWn, COLS_B, T, OUT, 1><<<grid, X::kThreads, 0, s>>>(
+                    g, out, out_rows, cols, split_stride, plan.stages, ti, tj);
+                return;
+            }
+        }
+        product_kernel<E, X::kM, X::kN, 2, X::kWn, COLS_B, T, OUT, 2><<<grid, X::kThreads, 0, s>>>(
             g, out, out_rows, cols, split_stride, plan.stages, ti, tj);
     });
 }
@@ -559,7 +594,7 @@ hipError_t backward(const HeadArgs &a, const float *lse, const float *grad_loss,
                     hipStream_t s)
 {
     const HeadLayout l = head_layout(a.rows, a.hidden, a.V, a.dtype);
-    const int64_t r64 = up64(a.rows);
+    const int rows_k = (a.rows + l.stage_k - 1) / l.stage_k * l.stage_k;
     float *weight = reinterpret_cast<float *>(ws + l.weight), *dx = reinterpret_cast<float *>(ws + l.dx);
     T *g_piece = reinterpret_cast<T *>(ws + l.g);
     constexpr bool kBf16 = sizeof(T) == 2;
@@ -576,11 +611,11 @@ hipError_t backward(const HeadArgs &a, const float *lse, const float *grad_loss,
         DV_TRY(operand(weight_rows(a, v0), a.ld_w, a.dtype, n, a.hidden, l, ws + l.w, w, s));
         const GemmShape logits{w, x, (int)l.k};
         const GemmOperand g{g_piece, n64, a.rows, 0};
-        DV_TRY(with_tile(plan_product(n, a.rows, l.k / l.stage_k, 1, kBf16, 0).side, [&](auto side, auto wn) {
-            constexpr int B = decltype(side)::value, WN = decltype(wn)::value;
-            const int ti = (n + B - 1) / B, tj = (a.rows + B - 1) / B;
-            grad_kernel<T, B, B, 2, WN><<<ti * tj, 2 * WN * kWave, 0, s>>>(logits, v0, a.V, a.rows, a.masks, a.targets, lse,
-                                                                          weight, g_piece, n64, ti, tj);
+        DV_TRY(with_tile<!kBf16>(plan_product(n, a.rows, l.k / l.stage_k, 1, kBf16, 0, true).side, [&](auto tile) {
+            using X = decltype(tile);
+            const int ti = (n + X::kM - 1) / X::kM, tj = (a.rows + X::kN - 1) / X::kN;
+            grad_kernel<T, X::kM, X::kN, 2, X::kWn><<<ti * tj, X::kThreads, 0, s>>>(
+                logits, v0, a.V, a.rows, a.masks, a.targets, lse, weight, g_piece, n64, ti, tj);
         }));
         if (grad_x) {
             const GemmShape shape{by_columns(w, l.k), g, (int)n64};
@@ -601,8 +636,8 @@ hipError_t backward(const HeadArgs &a, const float *lse, const float *grad_loss,
         }
         if (grad_weight) {
             GemmOperand g_t = by_columns(g, n64);
-            g_t.k_rows = (int)r64;
-            const GemmShape shape{by_columns(x, l.k), g_t, (int)r64};
+            g_t.k_rows = rows_k;
+            const GemmShape shape{by_columns(x, l.k), g_t, rows_k};
             const Plan plan = dw_plan(l, a.rows, n, kBf16);
             T *out = grad_weight + (int64_t)v0 * a.hidden;
             if (plan.splits == 1) {
@@ -643,7 +678,7 @@ hipError_t launch_head_loss(const HeadArgs &a, float *loss, float *lse, void *wo
     DV_TRY(operand(a.x, a.ld_x, a.dtype, a.rows, a.hidden, l, ws + l.x, x, s));
     const bool whole = in_place(a.weight, a.ld_w, a.dtype, a.hidden);  // nothing to pack: one piece
     const int step = whole ? a.V : l.piece;
-    const int side = plan_product(step, a.rows, l.k / l.stage_k, 1, a.dtype == 1, 0).side;
+    const int side = plan_product(step, a.rows, l.k / l.stage_k, 1, a.dtype == 1, 0, true).side;
     for (int v0 = 0; v0 < a.V; v0 += step) {
         const int n = a.V - v0 < step ? a.V - v0 : step;
         GemmOperand w;
@@ -651,16 +686,17 @@ hipError_t launch_head_loss(const HeadArgs &a, float *loss, float *lse, void *wo
         const GemmShape g{w, x, (int)l.k};
         const auto run = [&](auto zero) {
             using E = decltype(zero);
-            return with_tile(side, [&](auto sd, auto wn) {
-                constexpr int B = decltype(sd)::value, WN = decltype(wn)::value;
-                const int ti = (n + B - 1) / B, tj = (a.rows + B - 1) / B;
-                stats_kernel<E, B, B, 2, WN><<<ti * tj, 2 * WN * kWave, 0, s>>>(g, v0, a.V, a.rows, a.masks, a.targets,
-                                                                                parts, target_logit, ti, tj);
+            return with_tile<sizeof(E) == 4>(side, [&](auto tile) {
+                using X = decltype(tile);
+                const int ti = (n + X::kM - 1) / X::kM, tj = (a.rows + X::kN - 1) / X::kN;
+                stats_kernel<E, X::kM, X::kN, 2, X::kWn><<<ti * tj, X::kThreads, 0, s>>>(
+                    g, v0, a.V, a.rows, a.masks, a.targets, parts, target_logit, ti, tj);
             });
         };
         DV_TRY(a.dtype == 1 ? run((__bf16)0.f) : run(0.f));
     }
-    const int nparts = (a.V + side - 1) / side * 2;
+    const int tile_tokens = side == kNarrow ? 64 : side;
+    const int nparts = (a.V + tile_tokens - 1) / tile_tokens * 2;
     // a thread's share of the parts: about 16, more of them only for many rows
     int slices = 16;
     while (slices < (a.rows < 64 ? 256 : 64) && slices * 16 < nparts)

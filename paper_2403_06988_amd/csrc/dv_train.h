@@ -114,6 +114,11 @@ typedef __attribute__((ext_vector_type(4))) uint32_t Words;
 typedef __attribute__((ext_vector_type(4), aligned(2))) uint32_t AnyWords;
 __device__ __forceinline__ Words load_words(const void *p) { return *static_cast<const AnyWords *>(p); }
 __device__ __forceinline__ void store_words(void *p, Words w) { *static_cast<AnyWords *>(p) = w; }
+// the same, past the caches: for what this call does not read again
+__device__ __forceinline__ void stream_words(void *p, Words w)
+{
+    __builtin_nontemporal_store(static_cast<AnyWords>(w), static_cast<AnyWords *>(p));
+}
 // Element i of 16 bytes of T.
 template <typename T>
 __device__ __forceinline__ T element(const Words &w, int i)
