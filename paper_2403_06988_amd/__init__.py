@@ -470,37 +470,42 @@ def _code(dtype) -> int:
 def _matrix(t, name, dev, dtype=None):
     """Checks of a [rows][n] array with unit stride along its rows; returns its
     row stride (at least n)."""
-    if dtype is not None and t.dtype != dtype:
+    if dtype is not None and t.dtype is not dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
     if not t.is_cuda or t.device != dev:
         raise ValueError(f"{name} must be a device tensor on {dev}")
     if t.dim() != 2:
         raise ValueError(f"{name} must have two dimensions")
     rows, n = t.shape
-    if rows and n > 1 and t.stride(1) != 1:
+    step, unit = t.stride()
+    if rows and n > 1 and unit != 1:
         raise ValueError(f"{name} must have unit stride along its rows")
-    if rows > 1 and t.stride(0) < n:
+    if rows <= 1:
+        return n
+    if step < n:
         raise ValueError(f"the rows of {name} must not overlap")
-    return t.stride(0) if rows > 1 else n
+    return step
 
 
 def _vector(t, name, n, dtype, dev):
-    _want(t, name, dtype, dev)
+    if t.dtype is not dtype or t.device != dev or not t.is_contiguous():
+        _want(t, name, dtype, dev)
     if t.dim() != 1 or t.shape[0] != n:
         raise ValueError(f"{name} must be [{n}]")
 
 
 def _mask_args(allow, states, rows, V, dev):
     """(allow pointer, number of states, states pointer) of a call's mask."""
-    if (allow is None) != (states is None):
-        raise ValueError("allow and states must be given together")
-    if allow is None:
+    if allow is None and states is None:
         return None, 0, None
-    _want(allow, "allow", torch.int32, dev)
+    if allow is None or states is None:
+        raise ValueError("allow and states must be given together")
+    if allow.dtype is not torch.int32 or allow.device != dev or not allow.is_contiguous():
+        _want(allow, "allow", torch.int32, dev)
     if allow.dim() != 2 or allow.shape[1] != (V + 31) // 32:
         raise ValueError("allow must be [S][ceil(V/32)]")
     _vector(states, "states", rows, torch.int32, dev)
-    return _ptr(allow), allow.shape[0], _ptr(states)
+    return allow.data_ptr(), allow.shape[0], states.data_ptr()
 
 
 def _result(t, name, shape, dtype, dev):
@@ -508,13 +513,15 @@ def _result(t, name, shape, dtype, dev):
     if t is None:
         return torch.empty(shape, dtype=dtype, device=dev)
     _want(t, name, dtype, dev)
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
     return t
 
 
 def _scratch(workspace, need, dev):
-    return _workspace(workspace, need, dev, lambda: torch.empty(max(need, 1), dtype=torch.uint8, device=dev))
+    if workspace is None:
+        return torch.empty(max(need, 1), dtype=torch.uint8, device=dev), need
+    return _workspace(workspace, need, dev, None)
 
 
 def _head_args(x, weight, targets, allow, states):
