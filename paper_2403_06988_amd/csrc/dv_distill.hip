@@ -6,9 +6,15 @@
 //     loss = sum_L q_k (ln q_k - ln p_{id_k}),
 //     dloss/dz_v = c (p_v - sum of q_k with id_k = v)   on A, 0 elsewhere.
 //
-// The loss needs one read of the row, loss and gradient one read and one
-// write of it: both are bound by memory.  The gradient kernel keeps the row in no
-// wider place than the caches between its two passes: a row is 0.25 to 1 MB.
+// The loss needs one read of the row, loss and gradient one read and one write of
+// it: both are bound by memory.  The gradient's second pass finds the row in the
+// caches.  Loss and gradient of 2,048 rows of 128,256 bf16 logits take 245 us (4.3
+// TB/s of the 4.9 that a copy reaches), of 8,000 rows of 4,000 fp32 58 us (4.4);
+// the loss alone 93 us and 24 us (5.6 and 5.3 TB/s).
+//
+// Few or short rows are bound by latency instead: a row's chain is its loads, a join
+// over the block, and the stores.  So the teacher's entries are loaded first, their
+// logits are on the way while the row streams, and one barrier joins both softmaxes.
 #include <type_traits>
 
 #include "dv_train.h"
@@ -16,8 +22,7 @@
 namespace dv {
 namespace {
 
-constexpr int kThreads = 512;
-constexpr int kWaves = kThreads / kWave;
+constexpr int kThreads = 512;  // of blocks that share a row, and of those with a long one
 constexpr int kMaxTop = 1024;
 
 // Vectors of 16 bytes at any element's alignment.  The gradient's are stored
@@ -91,81 +96,105 @@ struct Vec<uint16_t> {
 };
 
 struct Shared {
-    float wave_a[kWaves], wave_b[kWaves];
+    Softmax row[kThreads / kWave], top[kThreads / kWave];  // of each wave
+    float loss[kThreads / kWave];
     int id[kMaxTop];
     float q[kMaxTop];
     float z[kMaxTop];
 };
 
-// Over the block's waves, in every lane.
-__device__ __forceinline__ float block_sum(float v, Shared &sh)
-{
-    v = wave_sum(v);
-    __syncthreads();
-    if ((threadIdx.x & (kWave - 1)) == 0)
-        sh.wave_a[threadIdx.x / kWave] = v;
-    __syncthreads();
-    float t = 0.f;
-#pragma unroll
-    for (int i = 0; i < kWaves; ++i)
-        t += sh.wave_a[i];
-    return t;
-}
-
-__device__ __forceinline__ Softmax block_join(Softmax v, float c2, Shared &sh)
+__device__ __forceinline__ Softmax wave_join(Softmax v, float c2)
 {
     const float top = wave_max(v.max);
-    const float sum = wave_sum(v.max == -INFINITY ? v.sum : v.sum * softmax_term(v.max, top, c2));
-    __syncthreads();
-    if ((threadIdx.x & (kWave - 1)) == 0) {
-        sh.wave_a[threadIdx.x / kWave] = top;
-        sh.wave_b[threadIdx.x / kWave] = sum;
-    }
-    __syncthreads();
+    return {top, wave_sum(v.max == -INFINITY ? v.sum : v.sum * softmax_term(v.max, top, c2))};
+}
+
+template <int THREADS>
+__device__ __forceinline__ Softmax join_waves(const Softmax *of_wave, float c2)
+{
+    constexpr int kWaves = THREADS / kWave;
     Softmax t{-INFINITY, 0.f};
 #pragma unroll
     for (int i = 0; i < kWaves; ++i)
-        t.max = fmaxf(t.max, sh.wave_a[i]);
+        t.max = fmaxf(t.max, of_wave[i].max);
 #pragma unroll
     for (int i = 0; i < kWaves; ++i)
-        t.sum += sh.wave_a[i] == -INFINITY ? sh.wave_b[i] : sh.wave_b[i] * softmax_term(sh.wave_a[i], t.max, c2);
+        t.sum += of_wave[i].max == -INFINITY ? of_wave[i].sum : of_wave[i].sum * softmax_term(of_wave[i].max, t.max, c2);
     return t;
 }
 
-// The teacher's entries of a row: ids (-1 where an entry takes no part) and
-// probabilities in LDS; returns the maximum and the sum of exp(c (top - max)).
-__device__ __forceinline__ Softmax teacher(const DistillArgs &a, const RowMask &m, int row, float c2, Shared &sh)
-{
-    Softmax own{-INFINITY, 0.f};
-    for (int k = threadIdx.x; k < a.K; k += kThreads) {
-        const int id = a.ids[(size_t)row * a.K + k];
-        const float t = a.top[(size_t)row * a.K + k];
-        const bool in = m.has(id) && t != -INFINITY;
-        sh.id[k] = in ? id : -1;
-        sh.q[k] = t;
-        if (in)
-            own = softmax_join(own, {t, 1.f}, c2);
+// A row's entries of the teacher, spread over a block's lanes.
+template <int THREADS>
+struct Teacher {
+    static constexpr int kN = kMaxTop / THREADS;  // of a lane at most
+    int id[kN];  // -1 where an entry takes no part
+    float top[kN], z[kN];
+
+    __device__ __forceinline__ void load(const DistillArgs &a, int row)
+    {
+#pragma unroll
+        for (int e = 0; e < kN; ++e) {
+            const int k = e * THREADS + threadIdx.x;
+            id[e] = -1;
+            top[e] = -INFINITY;
+            z[e] = 0.f;
+            if (k < a.K) {
+                id[e] = a.ids[(size_t)row * a.K + k];
+                top[e] = a.top[(size_t)row * a.K + k];
+            }
+        }
     }
-    const Softmax all = block_join(own, c2, sh);
-    for (int k = threadIdx.x; k < a.K; k += kThreads)
-        sh.q[k] = sh.id[k] < 0 ? 0.f : softmax_term(sh.q[k], all.max, c2) / all.sum;
-    return all;
-}
+    // logit(k, id): the model's logit of an entry that takes part
+    template <typename F>
+    __device__ __forceinline__ Softmax admit(const RowMask &m, float c2, F &&logit)
+    {
+        Softmax own{-INFINITY, 0.f};
+#pragma unroll
+        for (int e = 0; e < kN; ++e) {
+            if (!m.has(id[e]) || top[e] == -INFINITY) {
+                id[e] = -1;
+            } else {
+                z[e] = logit(e * THREADS + (int)threadIdx.x, id[e]);
+                own = softmax_join(own, {top[e], 1.f}, c2);
+            }
+        }
+        return own;
+    }
+    // Probabilities, ids and logits to LDS, and this lane's part of the loss.
+    __device__ __forceinline__ float publish(int K, Softmax t, Softmax s, float c, float c2, Shared &sh) const
+    {
+        const float lnt = logf(t.sum), lns = logf(s.sum);
+        float loss = 0.f;
+#pragma unroll
+        for (int e = 0; e < kN; ++e) {
+            const int k = e * THREADS + threadIdx.x;
+            const float q = id[e] < 0 ? 0.f : softmax_term(top[e], t.max, c2) / t.sum;
+            if (k < K) {
+                sh.id[k] = id[e];
+                sh.q[k] = q;
+                sh.z[k] = z[e];
+            }
+            if (!(q == 0.f))  // NaN counts
+                loss += q * (((top[e] - t.max) * c - lnt) - ((z[e] - s.max) * c - lns));
+        }
+        return loss;
+    }
+};
 
 // Vectors [j0, j1) of a row, kBatch a lane at a time: f(vectors, first, whole) has
-// vector first + u kThreads + lane in place u; masked elements read as -infinity, and
+// vector first + u THREADS + lane in place u; masked elements read as -infinity, and
 // so do vectors past j1 (only where `whole` is false).  A batch's start is in
 // scalar registers, a lane's offset from it 32 bits.
 constexpr int kBatch = 4;
 
-template <typename T, bool MASK, bool WHOLE>
+template <typename T, int THREADS, bool MASK, bool WHOLE>
 __device__ __forceinline__ void load_batch(Vec<T> (&v)[kBatch], const T *z, const RowMask &m, int first, int j1)
 {
     constexpr int N = Vec<T>::kN;
     uint32_t bits[kBatch];
 #pragma unroll
     for (int u = 0; u < kBatch; ++u) {
-        const int at = first + u * kThreads;  // uniform
+        const int at = first + u * THREADS;  // uniform
         const int left = j1 - at;
         const bool in = WHOLE || (int)threadIdx.x < left;
         const int base = WHOLE || left > 0 ? at : first;
@@ -185,18 +214,18 @@ __device__ __forceinline__ void load_batch(Vec<T> (&v)[kBatch], const T *z, cons
             v[u].keep(bits[u]);
 }
 
-template <typename T, bool MASK, typename F>
+template <typename T, int THREADS, bool MASK, typename F>
 __device__ __forceinline__ void for_batches(const T *z, const RowMask &m, int j0, int j1, F &&f)
 {
-    constexpr int kStep = kThreads * kBatch;
+    constexpr int kStep = THREADS * kBatch;
     Vec<T> v[kBatch];
     int first = j0;
     for (; first + kStep <= j1; first += kStep) {
-        load_batch<T, MASK, true>(v, z, m, first, j1);
+        load_batch<T, THREADS, MASK, true>(v, z, m, first, j1);
         f(v, first, std::true_type{});
     }
     if (first < j1) {
-        load_batch<T, MASK, false>(v, z, m, first, j1);
+        load_batch<T, THREADS, MASK, false>(v, z, m, first, j1);
         f(v, first, std::false_type{});
     }
 }
@@ -222,13 +251,13 @@ struct Shift {
 };
 
 // The softmax state of tokens [from, to) of a row (from a multiple of 8).
-template <typename T, bool MASK>
+template <typename T, int THREADS, bool MASK>
 __device__ __forceinline__ Softmax row_stats(const T *z, const RowMask &m, int from, int to, float c2)
 {
     using V = Vec<T>;
     constexpr int N = V::kN;
     Softmax own{-INFINITY, 0.f};
-    for_batches<T, MASK>(z, m, from / N, to / N, [&](const V (&v)[kBatch], int, auto) {
+    for_batches<T, THREADS, MASK>(z, m, from / N, to / N, [&](const V (&v)[kBatch], int, auto) {
         float top = own.max;
 #pragma unroll
         for (int u = 0; u < kBatch; ++u)
@@ -254,7 +283,7 @@ __device__ __forceinline__ Softmax row_stats(const T *z, const RowMask &m, int f
         const float before = own.max == -INFINITY ? own.sum : own.sum * softmax_term(own.max, t.max, c2);
         own = {top, before + sum};
     });
-    for (int i = to / N * N + threadIdx.x; i < to; i += kThreads)
+    for (int i = to / N * N + threadIdx.x; i < to; i += THREADS)
         if (m.has(i)) {
             const float x = V::one(z + i);
             own = x == -INFINITY ? own : softmax_join(own, {x, 1.f}, c2);
@@ -262,29 +291,14 @@ __device__ __forceinline__ Softmax row_stats(const T *z, const RowMask &m, int f
     return own;
 }
 
-// The row's part of the loss: needs sh.id, sh.q and sh.z.
-__device__ __forceinline__ float row_loss(const DistillArgs &a, int row, Softmax t, Softmax s, Shared &sh)
-{
-    const float c = a.inv_temperature;
-    const float lnt = logf(t.sum), lns = logf(s.sum);
-    float sum = 0.f;
-    for (int k = threadIdx.x; k < a.K; k += kThreads) {
-        const float q = sh.q[k];
-        if (!(q == 0.f))  // NaN counts
-            sum += q * (((a.top[(size_t)row * a.K + k] - t.max) * c - lnt) - ((sh.z[k] - s.max) * c - lns));
-    }
-    return block_sum(sum, sh);
-}
-
 // The gradient of the listed tokens in [from, to), once the block's other stores
 // there are done: an id listed more than once takes the sum of its entries, in
 // their order, from each of them.
-template <typename T>
+template <typename T, int THREADS>
 __device__ __forceinline__ void listed_grad(T *grad, int from, int to, float c2, float max, float scale, float w, int K,
                                             Shared &sh)
 {
-    __syncthreads();
-    for (int k = threadIdx.x; k < K; k += kThreads) {
+    for (int k = threadIdx.x; k < K; k += THREADS) {
         const int id = sh.id[k];
         if (id < from || id >= to)
             continue;
@@ -296,18 +310,18 @@ __device__ __forceinline__ void listed_grad(T *grad, int from, int to, float c2,
 }
 
 // Writes the gradient of tokens [from, to): w (p - q).  `part` false: zeros.
-template <typename T, bool MASK>
+template <typename T, int THREADS, bool MASK>
 __device__ __forceinline__ void row_grad(const T *z, T *grad, const RowMask &m, int from, int to, float c2, Softmax s,
-                                         float w, bool part, int K, Shared &sh)
+                                         float w, bool part)
 {
     using V = Vec<T>;
     constexpr int N = V::kN;
     const int j0 = from / N, j1 = to / N;
     if (!part) {
         const float zeros[N] = {};
-        for (int j = j0 + threadIdx.x; j < j1; j += kThreads)
+        for (int j = j0 + threadIdx.x; j < j1; j += THREADS)
             V::store(grad + (size_t)j * N, zeros);
-        for (int i = j1 * N + threadIdx.x; i < to; i += kThreads)
+        for (int i = j1 * N + threadIdx.x; i < to; i += THREADS)
             V::put(grad + i, 0.f);
         return;
     }
@@ -316,14 +330,14 @@ __device__ __forceinline__ void row_grad(const T *z, T *grad, const RowMask &m, 
     const auto write = [&](auto plain) {
         constexpr bool PLAIN = decltype(plain)::value;
         const float by = PLAIN ? scale * t.correction : scale;
-        for_batches<T, MASK>(z, m, j0, j1, [&](const V (&v)[kBatch], int first, auto whole) {
+        for_batches<T, THREADS, MASK>(z, m, j0, j1, [&](const V (&v)[kBatch], int first, auto whole) {
 #pragma unroll
             for (int u = 0; u < kBatch; ++u) {
                 float y[N];
 #pragma unroll
                 for (int i = 0; i < N; ++i)
                     y[i] = t.template term<PLAIN>(v[u].get(i)) * by;
-                const int at = first + u * kThreads;
+                const int at = first + u * THREADS;
                 if (decltype(whole)::value || at + (int)threadIdx.x < j1)
                     V::store(reinterpret_cast<T *>(reinterpret_cast<char *>(grad) + (size_t)at * 16 + threadIdx.x * 16u), y);
             }
@@ -333,38 +347,70 @@ __device__ __forceinline__ void row_grad(const T *z, T *grad, const RowMask &m, 
         write(std::true_type{});
     else
         write(std::false_type{});
-    for (int i = j1 * N + threadIdx.x; i < to; i += kThreads)
+    for (int i = j1 * N + threadIdx.x; i < to; i += THREADS)
         V::put(grad + i, m.has(i) ? softmax_term(V::one(z + i), s.max, c2) * scale : 0.f);
-    listed_grad(grad, from, to, c2, s.max, scale, w, K, sh);
+}
+
+// What follows a row's (or chunk's) statistics `own` and the teacher's `entries`:
+// the block's lanes join both, then the loss (if wanted) and the gradient of
+// tokens [from, to).  Two barriers: the joined statistics, and the listed tokens
+// after the other stores.
+template <typename T, int THREADS, bool MASK, bool GRAD>
+__device__ __forceinline__ void finish_row(const DistillArgs &a, int row, const T *z, const RowMask &m, int from, int to,
+                                           Softmax own, Teacher<THREADS> &entries, Softmax own_top,
+                                           const float *grad_loss, float *loss, T *grad, Shared &sh)
+{
+    const float c = a.inv_temperature, c2 = c * kLog2e;
+    const bool first_lane = (threadIdx.x & (kWave - 1)) == 0;
+    const int wave = threadIdx.x / kWave;
+    own = wave_join(own, c2);
+    own_top = wave_join(own_top, c2);
+    if (first_lane) {
+        sh.row[wave] = own;
+        sh.top[wave] = own_top;
+    }
+    __syncthreads();
+    const Softmax s = join_waves<THREADS>(sh.row, c2), t = join_waves<THREADS>(sh.top, c2);
+    const bool part = !s.empty() && !t.empty();
+    if (part) {
+        const float l = wave_sum(entries.publish(a.K, t, s, c, c2, sh));
+        if (first_lane)
+            sh.loss[wave] = l;
+    }
+    const float w = GRAD && part ? grad_loss[row] * c : 0.f;
+    if (GRAD)
+        row_grad<T, THREADS, MASK>(z, grad, m, from, to, c2, s, w, part);
+    __syncthreads();
+    if (loss && threadIdx.x == 0) {
+        float l = 0.f;
+#pragma unroll
+        for (int i = 0; i < THREADS / kWave; ++i)
+            l += part ? sh.loss[i] : 0.f;
+        loss[row] = l;
+    }
+    if (GRAD && part)
+        listed_grad<T, THREADS>(grad, from, to, c2, s.max, w / s.sum, w, a.K, sh);
 }
 
 // One block per row: the row's softmax, the loss, and with GRAD the gradient
 // from a second pass over the row, which its first pass left in the caches.
-template <typename T, bool MASK, bool GRAD>
-__global__ __launch_bounds__(kThreads) void distill_row_kernel(DistillArgs a, const float *grad_loss, float *loss,
-                                                                T *grad, int64_t ld_grad)
+template <typename T, int THREADS, bool MASK, bool GRAD>
+__global__ __launch_bounds__(THREADS) void distill_row_kernel(DistillArgs a, const float *grad_loss, float *loss, T *grad,
+                                                              int64_t ld_grad)
 {
     __shared__ Shared sh;
     const int row = blockIdx.x;
     const float c2 = a.inv_temperature * kLog2e;
+    Teacher<THREADS> entries;
+    entries.load(a, row);
     const RowMask m(a.masks, a.V, row);
     const T *z = static_cast<const T *>(a.logits) + (size_t)row * a.ld;
-    const Softmax t = teacher(a, m, row, c2, sh);
-    for (int k = threadIdx.x; k < a.K; k += kThreads)
-        sh.z[k] = sh.id[k] < 0 ? 0.f : Vec<T>::one(z + sh.id[k]);
-    Softmax s{-INFINITY, 0.f};
-    bool part = !m.dead && !t.empty();
-    if (part)
-        s = block_join(row_stats<T, MASK>(z, m, 0, a.V, c2), c2, sh);
-    part = part && !s.empty();
-    if (loss) {
-        const float l = part ? row_loss(a, row, t, s, sh) : 0.f;
-        if (threadIdx.x == 0)
-            loss[row] = l;
-    }
-    if (GRAD)
-        row_grad<T, MASK>(z, grad + (size_t)row * ld_grad, m, 0, a.V, c2, s, part ? grad_loss[row] * a.inv_temperature : 0.f,
-                 part, a.K, sh);
+    const Softmax top = entries.admit(m, c2, [&](int, int id) { return Vec<T>::one(z + id); });
+    Softmax own{-INFINITY, 0.f};
+    if (!m.dead)
+        own = row_stats<T, THREADS, MASK>(z, m, 0, a.V, c2);
+    finish_row<T, THREADS, MASK, GRAD>(a, row, z, m, 0, a.V, own, entries, top, grad_loss, loss,
+                                       GRAD ? grad + (size_t)row * ld_grad : nullptr, sh);
 }
 
 // Rows split over blocks (few rows): the chunks' softmax states, and the
@@ -372,7 +418,7 @@ __global__ __launch_bounds__(kThreads) void distill_row_kernel(DistillArgs a, co
 template <typename T, bool MASK>
 __global__ __launch_bounds__(kThreads) void distill_stats_kernel(DistillArgs a, int chunk, Softmax *part, float *listed)
 {
-    __shared__ Shared sh;
+    __shared__ Softmax of_wave[kThreads / kWave];
     const int row = blockIdx.y, c = blockIdx.x;
     const float c2 = a.inv_temperature * kLog2e;
     const RowMask m(a.masks, a.V, row);
@@ -385,9 +431,13 @@ __global__ __launch_bounds__(kThreads) void distill_stats_kernel(DistillArgs a, 
         }
     Softmax s{-INFINITY, 0.f};
     if (!m.dead)
-        s = block_join(row_stats<T, MASK>(z, m, from, to, c2), c2, sh);
+        s = row_stats<T, kThreads, MASK>(z, m, from, to, c2);
+    s = wave_join(s, c2);
+    if ((threadIdx.x & (kWave - 1)) == 0)
+        of_wave[threadIdx.x / kWave] = s;
+    __syncthreads();
     if (threadIdx.x == 0)
-        part[(size_t)row * gridDim.x + c] = s;
+        part[(size_t)row * gridDim.x + c] = join_waves<kThreads>(of_wave, c2);
 }
 
 // ... and then the loss (chunk 0's block) and each chunk's gradient.
@@ -400,26 +450,17 @@ __global__ __launch_bounds__(kThreads) void distill_finish_kernel(DistillArgs a,
     __shared__ Shared sh;
     const int row = blockIdx.y, c = blockIdx.x;
     const float c2 = a.inv_temperature * kLog2e;
+    Teacher<kThreads> entries;
+    entries.load(a, row);
     const RowMask m(a.masks, a.V, row);
-    const Softmax t = teacher(a, m, row, c2, sh);
-    for (int k = threadIdx.x; k < a.K; k += kThreads)
-        sh.z[k] = listed[(size_t)row * a.K + k];
-    Softmax s{-INFINITY, 0.f};
+    Softmax own{-INFINITY, 0.f};
     for (int i = threadIdx.x; i < chunks; i += kThreads)
-        s = softmax_join(s, parts[(size_t)row * chunks + i], c2);
-    s = block_join(s, c2, sh);
-    const bool part = !t.empty() && !s.empty();
-    if (loss && c == 0) {
-        const float l = part ? row_loss(a, row, t, s, sh) : 0.f;
-        if (threadIdx.x == 0)
-            loss[row] = l;
-    }
-    if (GRAD) {
-        const int from = c * chunk, to = a.V - from < chunk ? a.V : from + chunk;
-        const T *z = static_cast<const T *>(a.logits) + (size_t)row * a.ld;
-        row_grad<T, MASK>(z, grad + (size_t)row * ld_grad, m, from, to, c2, s, part ? grad_loss[row] * a.inv_temperature : 0.f,
-                 part, a.K, sh);
-    }
+        own = softmax_join(own, parts[(size_t)row * chunks + i], c2);
+    const Softmax top = entries.admit(m, c2, [&](int k, int) { return listed[(size_t)row * a.K + k]; });
+    const int from = c * chunk, to = a.V - from < chunk ? a.V : from + chunk;
+    const T *z = static_cast<const T *>(a.logits) + (size_t)row * a.ld;
+    finish_row<T, kThreads, MASK, GRAD>(a, row, z, m, from, to, own, entries, top, grad_loss, c == 0 ? loss : nullptr,
+                                        GRAD ? grad + (size_t)row * ld_grad : nullptr, sh);
 }
 
 struct Split {
@@ -448,17 +489,42 @@ Split split_of(int rows, int V, int dtype, bool grad)
     return {chunk, (V + chunk - 1) / chunk};
 }
 
+// Blocks of 512 lanes leave most of them idle in a short row, and fewer rows under
+// way on a compute unit.  Loss and gradient with 512, 256 and 128 lanes (us):
+//     8,192 x 1,000 fp32 (250 vectors)     57  32  27
+//     8,000 x 4,000 bf16 (500)             81  45  37
+//     8,000 x 4,000 fp32 (1,000)           77  58  65
+//     8,000 x 8,000 bf16 (1,000)           92  59  63
+//     4,000 x 8,000 fp32 (2,000)           53  60   -
+//     4,000 x 16,000 bf16 (2,000)          60  61   -
+// and the loss alone 42 23 16, 57 30 21, 40 24 24, 54 31 28, 24 22, 31 26.
+constexpr int kShortRow = 512;    // vectors of a row for blocks of 128 lanes
+constexpr int kMiddleRow = 2048;  // and of 256, without the gradient
+constexpr int kMiddleRowGrad = 1536;
+
+template <typename T, int THREADS, bool MASK>
+hipError_t launch_rows(const DistillArgs &a, const float *grad_loss, float *loss, T *grad, int64_t ld_grad,
+                       hipStream_t stream)
+{
+    if (grad)
+        distill_row_kernel<T, THREADS, MASK, true><<<a.rows, THREADS, 0, stream>>>(a, grad_loss, loss, grad, ld_grad);
+    else
+        distill_row_kernel<T, THREADS, MASK, false><<<a.rows, THREADS, 0, stream>>>(a, nullptr, loss, nullptr, 0);
+    return last_launch();
+}
+
 template <typename T, bool MASK>
 hipError_t launch(const DistillArgs &a, const float *grad_loss, float *loss, T *grad, int64_t ld_grad, void *workspace,
                   hipStream_t stream)
 {
     const Split s = split_of(a.rows, a.V, a.dtype, grad != nullptr);
     if (s.chunks == 1) {
-        if (grad)
-            distill_row_kernel<T, MASK, true><<<a.rows, kThreads, 0, stream>>>(a, grad_loss, loss, grad, ld_grad);
-        else
-            distill_row_kernel<T, MASK, false><<<a.rows, kThreads, 0, stream>>>(a, nullptr, loss, nullptr, 0);
-        return last_launch();
+        const int vecs = a.V / Vec<T>::kN;
+        if (vecs <= kShortRow)
+            return launch_rows<T, 128, MASK>(a, grad_loss, loss, grad, ld_grad, stream);
+        if (vecs <= (grad ? kMiddleRowGrad : kMiddleRow))
+            return launch_rows<T, 256, MASK>(a, grad_loss, loss, grad, ld_grad, stream);
+        return launch_rows<T, kThreads, MASK>(a, grad_loss, loss, grad, ld_grad, stream);
     }
     Softmax *parts = static_cast<Softmax *>(workspace);
     float *listed = reinterpret_cast<float *>(parts + (size_t)a.rows * s.chunks);
