@@ -9,7 +9,8 @@
 Arguments and results are those of the package's calls of the same names;
 gradients reach tables, weights, hidden states and logits.  Each works out its
 gradient when the backward pass asks for it, from the inputs (and the head loss's
-logarithms of sums): no logits and no probabilities are kept.  A program that knows
+logarithms of sums): no logits and no probabilities are kept.  A gradient of
+gradients raises.  A program that knows
 its rows' weights beforehand calls the ``_backward`` functions itself:
 ``distill_loss_backward`` gives loss and gradient in one pass over the logits, and
 ``embed_backward`` with ``accumulate`` adds to a shared table's gradient in place.
@@ -17,6 +18,7 @@ its rows' weights beforehand calls the ``_backward`` functions itself:
 from __future__ import annotations
 
 import torch
+from torch.autograd.function import once_differentiable
 
 import paper_2403_06988_amd as dv
 
@@ -31,6 +33,7 @@ class _Embed(torch.autograd.Function):
         return dv.embed(weight, ids, scale)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, grad_out):
         (ids,) = ctx.saved_tensors
         return dv.embed_backward(grad_out.contiguous(), ids, ctx.num_tokens, ctx.scale), None, None
@@ -44,6 +47,7 @@ class _HeadLoss(torch.autograd.Function):
         return loss
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, grad_loss):
         x, weight, targets, allow, states, lse = ctx.saved_tensors
         want_x, want_weight = ctx.needs_input_grad[:2]
@@ -60,6 +64,7 @@ class _DistillLoss(torch.autograd.Function):
         return dv.distill_loss(logits, teacher_ids, teacher_logits, inv_temperature, allow, states)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, grad_loss):
         logits, teacher_ids, teacher_logits, allow, states = ctx.saved_tensors
         _, grad = dv.distill_loss_backward(logits, teacher_ids, teacher_logits, grad_loss.contiguous(),
