@@ -508,19 +508,31 @@ def _mask_args(allow, states, rows, V, dev):
     return allow.data_ptr(), allow.shape[0], states.data_ptr()
 
 
-def _result(t, name, shape, dtype, dev):
+def _new(shape, dtype, dev, stream):
+    """A new array from the memory of the stream that the call runs on: that of
+    another stream may still be in use there, or be given out again before this
+    one has finished with it."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=dev)
+    if not hasattr(stream, "cuda_stream"):
+        stream = torch.cuda.ExternalStream(int(stream), device=dev)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=dev)
+
+
+def _result(t, name, shape, dtype, dev, stream):
     """A caller-supplied contiguous output (or a new one)."""
     if t is None:
-        return torch.empty(shape, dtype=dtype, device=dev)
+        return _new(shape, dtype, dev, stream)
     _want(t, name, dtype, dev)
     if t.shape != shape:
         raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
     return t
 
 
-def _scratch(workspace, need, dev):
+def _scratch(workspace, need, dev, stream):
     if workspace is None:
-        return torch.empty(max(need, 1), dtype=torch.uint8, device=dev), need
+        return _new(max(need, 1), torch.uint8, dev, stream), need
     return _workspace(workspace, need, dev, None)
 
 
@@ -546,9 +558,9 @@ def head_loss(x, weight, targets, allow=None, states=None, loss=None, lse=None, 
     with states [N] int32: the tokens each row's state allows; without them
     every token.  Returns (loss [N], lse [N]) fp32."""
     dev, args, (N, D, V, dt) = _head_args(x, weight, targets, allow, states)
-    loss = _result(loss, "loss", (N,), torch.float32, dev)
-    lse = _result(lse, "lse", (N,), torch.float32, dev)
-    workspace, nbytes = _scratch(workspace, int(lib.dv_head_loss_workspace_bytes(N, D, V, dt)), dev)
+    loss = _result(loss, "loss", (N,), torch.float32, dev, stream)
+    lse = _result(lse, "lse", (N,), torch.float32, dev, stream)
+    workspace, nbytes = _scratch(workspace, int(lib.dv_head_loss_workspace_bytes(N, D, V, dt)), dev, stream)
     st = lib.dv_head_loss(*args, _ptr(loss), _ptr(lse), _ptr(workspace), nbytes, _stream(stream, dev))
     _check(st, "dv_head_loss")
     return loss, lse
@@ -564,9 +576,9 @@ def head_loss_backward(x, weight, targets, lse, grad_loss, allow=None, states=No
     _vector(grad_loss, "grad_loss", N, torch.float32, dev)
     if not (want_x or want_weight):
         return None, None
-    grad_x = _result(grad_x, "grad_x", (N, D), x.dtype, dev) if want_x else None
-    grad_weight = _result(grad_weight, "grad_weight", (V, D), x.dtype, dev) if want_weight else None
-    workspace, nbytes = _scratch(workspace, int(lib.dv_head_loss_backward_workspace_bytes(N, D, V, dt)), dev)
+    grad_x = _result(grad_x, "grad_x", (N, D), x.dtype, dev, stream) if want_x else None
+    grad_weight = _result(grad_weight, "grad_weight", (V, D), x.dtype, dev, stream) if want_weight else None
+    workspace, nbytes = _scratch(workspace, int(lib.dv_head_loss_backward_workspace_bytes(N, D, V, dt)), dev, stream)
     st = lib.dv_head_loss_backward(*args, _ptr(lse), _ptr(grad_loss), _ptr(grad_x), _ptr(grad_weight), _ptr(workspace),
                                    nbytes, _stream(stream, dev))
     _check(st, "dv_head_loss_backward")
@@ -596,8 +608,8 @@ def distill_loss(logits, teacher_ids, teacher_logits, inv_temperature=1.0, allow
     fp32, any row stride), both at temperature 1 / inv_temperature.  Returns
     loss [N] fp32 (0 for rows with nothing listed or nothing allowed)."""
     dev, args, (N, V, K) = _distill_args(logits, teacher_ids, teacher_logits, inv_temperature, allow, states)
-    loss = _result(loss, "loss", (N,), torch.float32, dev)
-    workspace, nbytes = _scratch(workspace, distill_loss_workspace_bytes(N, V, K), dev)
+    loss = _result(loss, "loss", (N,), torch.float32, dev, stream)
+    workspace, nbytes = _scratch(workspace, distill_loss_workspace_bytes(N, V, K), dev, stream)
     st = lib.dv_distill_loss(*args, _ptr(loss), _ptr(workspace), nbytes, _stream(stream, dev))
     _check(st, "dv_distill_loss")
     return loss
@@ -610,13 +622,13 @@ def distill_loss_backward(logits, teacher_ids, teacher_logits, grad_loss, inv_te
     be a [N][V] array of any row stride, or the logits themselves."""
     dev, args, (N, V, K) = _distill_args(logits, teacher_ids, teacher_logits, inv_temperature, allow, states)
     _vector(grad_loss, "grad_loss", N, torch.float32, dev)
-    loss = _result(loss, "loss", (N,), torch.float32, dev)
+    loss = _result(loss, "loss", (N,), torch.float32, dev, stream)
     if grad is None:
-        grad = torch.empty((N, V), dtype=logits.dtype, device=dev)
+        grad = _new((N, V), logits.dtype, dev, stream)
     ld_grad = _matrix(grad, "grad", dev, logits.dtype)
     if tuple(grad.shape) != (N, V):
         raise ValueError(f"grad must be [{N}][{V}]")
-    workspace, nbytes = _scratch(workspace, distill_loss_workspace_bytes(N, V, K), dev)
+    workspace, nbytes = _scratch(workspace, distill_loss_workspace_bytes(N, V, K), dev, stream)
     st = lib.dv_distill_loss_backward(*args, _ptr(grad_loss), _ptr(loss), _ptr(grad), ld_grad, _ptr(workspace), nbytes,
                                       _stream(stream, dev))
     _check(st, "dv_distill_loss_backward")
@@ -632,7 +644,7 @@ def embed(weight, ids, scale=1.0, out=None, stream=None):
     V, D = weight.shape
     N = ids.shape[0]
     _vector(ids, "ids", N, torch.int32, dev)
-    out = _result(out, "out", (N, D), weight.dtype, dev)
+    out = _result(out, "out", (N, D), weight.dtype, dev, stream)
     st = lib.dv_embed(_ptr(weight), ld, dt, V, D, _ptr(ids), N, float(scale), _ptr(out), _stream(stream, dev))
     _check(st, "dv_embed")
     return out
@@ -650,8 +662,8 @@ def embed_backward(grad_out, ids, num_tokens, scale=1.0, grad_weight=None, accum
     _vector(ids, "ids", N, torch.int32, dev)
     if accumulate and grad_weight is None:
         raise ValueError("accumulate adds to a given grad_weight")
-    grad_weight = _result(grad_weight, "grad_weight", (num_tokens, D), grad_out.dtype, dev)
-    workspace, nbytes = _scratch(workspace, embed_backward_workspace_bytes(N, D, num_tokens), dev)
+    grad_weight = _result(grad_weight, "grad_weight", (num_tokens, D), grad_out.dtype, dev, stream)
+    workspace, nbytes = _scratch(workspace, embed_backward_workspace_bytes(N, D, num_tokens), dev, stream)
     st = lib.dv_embed_backward(_ptr(grad_out), ld, dt, N, D, _ptr(ids), num_tokens, float(scale), int(bool(accumulate)),
                                _ptr(grad_weight), _ptr(workspace), nbytes, _stream(stream, dev))
     _check(st, "dv_embed_backward")
