@@ -174,8 +174,11 @@ struct Teacher {
                 sh.q[k] = q;
                 sh.z[k] = z[e];
             }
-            if (!(q == 0.f))  // NaN counts
-                loss += q * (((top[e] - t.max) * c - lnt) - ((z[e] - s.max) * c - lns));
+            if (!(q == 0.f)) {  // NaN counts
+                // q c (z - max): c (z - max) of a logit near the type's lowest may pass its range
+                const float below = z[e] - s.max;
+                loss += q * (((top[e] - t.max) * c - lnt) + lns) - (below == -INFINITY ? below : q * c * below);
+            }
         }
         return loss;
     }
