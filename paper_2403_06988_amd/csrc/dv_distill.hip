@@ -8,8 +8,8 @@
 //
 // The loss needs one read of the row, loss and gradient one read and one write of
 // it: both are bound by memory.  The gradient's second pass finds the row in the
-// caches.  Loss and gradient of 2,048 rows of 128,256 bf16 logits take 245 us (4.3
-// TB/s of the 4.9 that a copy reaches), of 8,000 rows of 4,000 fp32 58 us (4.4);
+// caches, or in the block's registers.  Loss and gradient of 2,048 rows of 128,256 bf16 logits take 245 us (4.3
+// TB/s of the 4.9 that a copy reaches), of 8,000 rows of 4,000 fp32 50 us (5.1);
 // the loss alone 93 us and 24 us (5.6 and 5.3 TB/s).
 //
 // Few or short rows are bound by latency instead: a row's chain is its loads, a join
@@ -95,9 +95,10 @@ struct Vec<uint16_t> {
     static __device__ __forceinline__ void put(uint16_t *p, float y) { *p = narrow(y); }
 };
 
+constexpr int kMostThreads = 1024;  // of a block that holds a row
 struct Shared {
-    Softmax row[kThreads / kWave], top[kThreads / kWave];  // of each wave
-    float loss[kThreads / kWave];
+    Softmax row[kMostThreads / kWave], top[kMostThreads / kWave];  // of each wave
+    float loss[kMostThreads / kWave];
     int id[kMaxTop];
     float q[kMaxTop];
     float z[kMaxTop];
@@ -356,12 +357,12 @@ __device__ __forceinline__ void row_grad(const T *z, T *grad, const RowMask &m, 
 
 // What follows a row's (or chunk's) statistics `own` and the teacher's `entries`:
 // the block's lanes join both, then the loss (if wanted) and the gradient of
-// tokens [from, to).  Two barriers: the joined statistics, and the listed tokens
-// after the other stores.
-template <typename T, int THREADS, bool MASK, bool GRAD>
-__device__ __forceinline__ void finish_row(const DistillArgs &a, int row, const T *z, const RowMask &m, int from, int to,
-                                           Softmax own, Teacher<THREADS> &entries, Softmax own_top,
-                                           const float *grad_loss, float *loss, T *grad, Shared &sh)
+// tokens [from, to): write(softmax, weight, part), then the listed tokens.  Two
+// barriers: the joined statistics, and the listed tokens after the other stores.
+template <typename T, int THREADS, bool GRAD, typename F>
+__device__ __forceinline__ void finish_row(const DistillArgs &a, int row, int from, int to, Softmax own,
+                                           Teacher<THREADS> &entries, Softmax own_top, const float *grad_loss, float *loss,
+                                           T *grad, Shared &sh, F &&write)
 {
     const float c = a.inv_temperature, c2 = c * kLog2e;
     const bool first_lane = (threadIdx.x & (kWave - 1)) == 0;
@@ -382,7 +383,7 @@ __device__ __forceinline__ void finish_row(const DistillArgs &a, int row, const 
     }
     const float w = GRAD && part ? grad_loss[row] * c : 0.f;
     if (GRAD)
-        row_grad<T, THREADS, MASK>(z, grad, m, from, to, c2, s, w, part);
+        write(s, w, part);
     __syncthreads();
     if (loss && threadIdx.x == 0) {
         float l = 0.f;
@@ -412,8 +413,115 @@ __global__ __launch_bounds__(THREADS) void distill_row_kernel(DistillArgs a, con
     Softmax own{-INFINITY, 0.f};
     if (!m.dead)
         own = row_stats<T, THREADS, MASK>(z, m, 0, a.V, c2);
-    finish_row<T, THREADS, MASK, GRAD>(a, row, z, m, 0, a.V, own, entries, top, grad_loss, loss,
-                                       GRAD ? grad + (size_t)row * ld_grad : nullptr, sh);
+    T *const out = GRAD ? grad + (size_t)row * ld_grad : nullptr;
+    finish_row<T, THREADS, GRAD>(a, row, 0, a.V, own, entries, top, grad_loss, loss, out, sh,
+                                 [&](Softmax s, float w, bool part) {
+                                     row_grad<T, THREADS, MASK>(z, out, m, 0, a.V, c2, s, w, part);
+                                 });
+}
+
+// Loss and gradient with the row held in the block's registers, VECS vectors a lane
+// (at most THREADS VECS in all): it is read once, and every load is on its way
+// before the first is used.
+template <typename T, int THREADS, int VECS, bool MASK>
+__global__ __launch_bounds__(THREADS, 4) void distill_held_kernel(DistillArgs a, const float *grad_loss, float *loss, T *grad,
+                                                               int64_t ld_grad)
+{
+    using V = Vec<T>;
+    constexpr int N = V::kN;
+    __shared__ Shared sh;
+    const int row = blockIdx.x;
+    const float c2 = a.inv_temperature * kLog2e;
+    Teacher<THREADS> entries;
+    entries.load(a, row);
+    const RowMask m(a.masks, a.V, row);
+    const T *z = static_cast<const T *>(a.logits) + (size_t)row * a.ld;
+    T *const out = grad + (size_t)row * ld_grad;
+    const int vecs = a.V / N;
+    V v[VECS];
+    uint32_t bits[VECS];
+    const uint8_t *bytes = reinterpret_cast<const uint8_t *>(m.words);
+#pragma unroll
+    for (int u = 0; u < VECS; ++u) {
+        const int left = vecs - u * THREADS;  // uniform
+        bits[u] = 0;
+        if (left > 0 && !m.dead) {
+            const bool in = (int)threadIdx.x < left;
+            const uint32_t lane = in ? threadIdx.x : 0;
+            v[u] = V::load(reinterpret_cast<const T *>(reinterpret_cast<const char *>(z) + (size_t)(u * THREADS) * 16 + lane * 16u));
+            bits[u] = in ? 0xFFu : 0u;
+            if (MASK) {
+                const uint8_t *at = bytes + (size_t)(u * THREADS) / (8 / N);
+                bits[u] &= N == 8 ? at[lane] : (uint32_t)at[lane >> 1] >> ((lane & 1) * 4);
+            }
+        }
+    }
+    const Softmax top = entries.admit(m, c2, [&](int, int id) { return V::one(z + id); });
+    float most = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < VECS; ++u) {
+        v[u].keep(bits[u]);
+#pragma unroll
+        for (int i = 0; i < N; i += 2)
+            most = fmaxf(fmaxf(most, v[u].get(i)), v[u].get(i + 1));
+    }
+    // the compiler would keep the widened elements from one pass to the next
+    const auto narrow_again = [&] {
+#pragma unroll
+        for (int u = 0; u < VECS; ++u)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                asm("" : "+v"(v[u].x[i]));
+    };
+    narrow_again();
+    const Shift t(most, c2);
+    float sum = 0.f;
+    if (__all(t.plain)) {
+#pragma unroll
+        for (int u = 0; u < VECS; ++u)
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                sum += t.template term<true>(v[u].get(i));
+        sum *= t.correction;
+    } else {
+#pragma unroll
+        for (int u = 0; u < VECS; ++u)
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                sum += t.template term<false>(v[u].get(i));
+    }
+    Softmax own{most, sum};
+    const int rest = vecs * N + (int)threadIdx.x;  // of the row's end, an element a lane
+    const bool has_rest = rest < a.V && m.has(rest);
+    const float x_rest = has_rest ? V::one(z + rest) : -INFINITY;
+    if (has_rest && x_rest != -INFINITY)
+        own = softmax_join(own, {x_rest, 1.f}, c2);
+    finish_row<T, THREADS, true>(a, row, 0, a.V, own, entries, top, grad_loss, loss, out, sh,
+                                 [&](Softmax s, float w, bool part) {
+        narrow_again();
+        const Shift t(s.max, c2);
+        const float scale = part ? w / s.sum : 0.f;
+        const auto write = [&](auto plain) {
+            constexpr bool PLAIN = decltype(plain)::value;
+            const float by = PLAIN ? scale * t.correction : scale;
+#pragma unroll
+            for (int u = 0; u < VECS; ++u) {
+                const int j = u * THREADS + (int)threadIdx.x;
+                float y[N];
+#pragma unroll
+                for (int i = 0; i < N; ++i)
+                    y[i] = part ? t.template term<PLAIN>(v[u].get(i)) * by : 0.f;
+                if (j < vecs)
+                    V::store(reinterpret_cast<T *>(reinterpret_cast<char *>(out) + (size_t)(u * THREADS) * 16 + threadIdx.x * 16u), y);
+            }
+        };
+        if (t.plain)
+            write(std::true_type{});
+        else
+            write(std::false_type{});
+        if (rest < a.V)
+            V::put(out + rest, part && has_rest ? softmax_term(x_rest, s.max, c2) * scale : 0.f);
+    });
 }
 
 // Rows split over blocks (few rows): the chunks' softmax states, and the
@@ -462,8 +570,11 @@ __global__ __launch_bounds__(kThreads) void distill_finish_kernel(DistillArgs a,
     const Softmax top = entries.admit(m, c2, [&](int k, int) { return listed[(size_t)row * a.K + k]; });
     const int from = c * chunk, to = a.V - from < chunk ? a.V : from + chunk;
     const T *z = static_cast<const T *>(a.logits) + (size_t)row * a.ld;
-    finish_row<T, kThreads, MASK, GRAD>(a, row, z, m, from, to, own, entries, top, grad_loss, c == 0 ? loss : nullptr,
-                                        GRAD ? grad + (size_t)row * ld_grad : nullptr, sh);
+    T *const out = GRAD ? grad + (size_t)row * ld_grad : nullptr;
+    finish_row<T, kThreads, GRAD>(a, row, from, to, own, entries, top, grad_loss, c == 0 ? loss : nullptr, out, sh,
+                                  [&](Softmax s, float w, bool part) {
+                                      row_grad<T, kThreads, MASK>(z, out, m, from, to, c2, s, w, part);
+                                  });
 }
 
 struct Split {
@@ -505,6 +616,44 @@ constexpr int kShortRow = 512;    // vectors of a row for blocks of 128 lanes
 constexpr int kMiddleRow = 2048;  // and of 256, without the gradient
 constexpr int kMiddleRowGrad = 1536;
 
+// The lanes of a block that holds a row of `vecs` vectors of n elements, or 0 for the
+// two passes.  Logits that fit the L2s (32 MB) are read twice at little cost; past
+// them holding pays (loss and gradient, two passes and held, us):
+//     8,192 x 1,000 fp32 (128 lanes x 4 vectors)   28  27     4,000 x 16,000 fp32 (512 x 8)  110  89
+//     8,000 x 4,000 bf16 (128 x 4)                 38  36     2,000 x 32,003 bf16 (512 x 8)   69  62
+//     8,000 x 4,000 fp32 (256 x 4)                 53  50     2,000 x 32,000 fp32 (512 x 16) 116  90
+//     4,000 x 8,000 fp32 (256 x 8)                 52  47     1,500 x 50,257 bf16 (512 x 16)  83  71
+//     4,000 x 16,000 bf16 (256 x 8)                61  52     1,000 x 65,000 fp32 (1024 x 16) 122 107
+// and below 400 x 32,000 bf16 16.0 16.8, 250 x 60,000 bf16 18.3 19.3.  Blocks of 16 vectors a lane
+// fill a compute unit by two (512 lanes) or alone (1,024): the last round of them must
+// not be nearly empty (520 x 50,257 fp32: 57.5 and 59.3).  Alone, bf16 rows' exponentials
+// are not hidden behind another block's loads (2,048 x 128,256: 243 and 263): two passes.
+constexpr int64_t kL2Bytes = (int64_t)32 << 20;
+
+int held_lanes(int64_t rows, int vecs, int n)
+{
+    if (rows * vecs * 16 < kL2Bytes || vecs > (n == 4 ? 16384 : 8192))
+        return 0;
+    if (vecs <= 512)
+        return 128;
+    if (vecs <= 2048)
+        return 256;
+    if (vecs <= 4096)
+        return 512;
+    const int lanes = vecs <= 8192 ? 512 : 1024;
+    const int64_t slots = vecs <= 8192 ? 512 : 256;
+    const int64_t rounds = (rows + slots - 1) / slots;
+    return rounds * slots * 10 <= rows * 13 ? lanes : 0;
+}
+
+template <typename T, int THREADS, int VECS, bool MASK>
+hipError_t launch_held(const DistillArgs &a, const float *grad_loss, float *loss, T *grad, int64_t ld_grad,
+                       hipStream_t stream)
+{
+    distill_held_kernel<T, THREADS, VECS, MASK><<<a.rows, THREADS, 0, stream>>>(a, grad_loss, loss, grad, ld_grad);
+    return last_launch();
+}
+
 template <typename T, int THREADS, bool MASK>
 hipError_t launch_rows(const DistillArgs &a, const float *grad_loss, float *loss, T *grad, int64_t ld_grad,
                        hipStream_t stream)
@@ -523,6 +672,20 @@ hipError_t launch(const DistillArgs &a, const float *grad_loss, float *loss, T *
     const Split s = split_of(a.rows, a.V, a.dtype, grad != nullptr);
     if (s.chunks == 1) {
         const int vecs = a.V / Vec<T>::kN;
+        const int held = grad ? held_lanes(a.rows, vecs, Vec<T>::kN) : 0;
+        if (held == 128)
+            return launch_held<T, 128, 4, MASK>(a, grad_loss, loss, grad, ld_grad, stream);
+        if (held == 256 && vecs <= 1024)
+            return launch_held<T, 256, 4, MASK>(a, grad_loss, loss, grad, ld_grad, stream);
+        if (held == 256)
+            return launch_held<T, 256, 8, MASK>(a, grad_loss, loss, grad, ld_grad, stream);
+        if (held == 512 && vecs <= 4096)
+            return launch_held<T, 512, 8, MASK>(a, grad_loss, loss, grad, ld_grad, stream);
+        if (held == 512)
+            return launch_held<T, 512, 16, MASK>(a, grad_loss, loss, grad, ld_grad, stream);
+        if constexpr (Vec<T>::kN == 4)
+            if (held)
+                return launch_held<T, 1024, 16, MASK>(a, grad_loss, loss, grad, ld_grad, stream);
         if (vecs <= kShortRow)
             return launch_rows<T, 128, MASK>(a, grad_loss, loss, grad, ld_grad, stream);
         if (vecs <= (grad ? kMiddleRowGrad : kMiddleRow))
