@@ -178,8 +178,8 @@ __device__ __forceinline__ void scan_counts(int (*counts)[kBins], int *sums, boo
 }
 
 // Block 0 sorts up to kSortKeys rows in LDS; with `fill` the other blocks
-// write zeros over the table at the same time (the sums then overwrite the
-// rows of the tokens that occur).
+// write zeros over the table (or its first rows) at the same time (the sums then
+// overwrite the rows of the tokens that occur).
 struct SortShared {
     int key[kSortKeys];
     int row[kSortKeys];
@@ -187,24 +187,22 @@ struct SortShared {
     int sums[kBins];
 };
 
-__device__ __forceinline__ void fill_zeros(char *p, size_t bytes, size_t block, size_t blocks, int threads)
+// Zeros over [p, p + bytes) by `threads` threads, of which this is number `thread`.
+__device__ __forceinline__ void fill_zeros(char *p, size_t bytes, size_t thread, size_t threads)
 {
-    // the table is contiguous: its ends byte pair by byte pair, the rest in 16 bytes
+    // the ends byte pair by byte pair, the rest in 16 bytes
     const size_t head = (16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15;
     const size_t h = head < bytes ? head : bytes;
     const size_t vecs = (bytes - h) / 16;
     const size_t tail = (bytes - h) - vecs * 16;
     uint4 *q = reinterpret_cast<uint4 *>(p + h);
-    const size_t stride = blocks * threads;
-    for (size_t i = block * threads + threadIdx.x; i < vecs; i += stride)
+    for (size_t i = thread; i < vecs; i += threads)
         q[i] = make_uint4(0, 0, 0, 0);
-    if (block == 0) {
-        uint16_t *a = reinterpret_cast<uint16_t *>(p), *b = reinterpret_cast<uint16_t *>(p + h + vecs * 16);
-        for (size_t i = threadIdx.x; i < h / 2; i += threads)
-            a[i] = 0;
-        for (size_t i = threadIdx.x; i < tail / 2; i += threads)
-            b[i] = 0;
-    }
+    uint16_t *a = reinterpret_cast<uint16_t *>(p), *b = reinterpret_cast<uint16_t *>(p + h + vecs * 16);
+    if (thread < h / 2)  // less than 8 of each
+        a[thread] = 0;
+    if (thread < tail / 2)
+        b[thread] = 0;
 }
 
 __global__ __launch_bounds__(kSortThreads) void sort_block_kernel(const int32_t *ids, int rows, int V, int digits,
@@ -212,7 +210,8 @@ __global__ __launch_bounds__(kSortThreads) void sort_block_kernel(const int32_t 
 {
     __shared__ SortShared sh;
     if (blockIdx.x) {
-        fill_zeros(fill, fill_bytes, blockIdx.x - 1, gridDim.x - 1, kSortThreads);
+        fill_zeros(fill, fill_bytes, (size_t)(blockIdx.x - 1) * kSortThreads + threadIdx.x,
+                   (size_t)(gridDim.x - 1) * kSortThreads);
         return;
     }
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
@@ -259,7 +258,8 @@ __global__ __launch_bounds__(kSortThreads) void sort_count_kernel(const int32_t 
                                                                    int blocks)
 {
     if ((int)blockIdx.x >= blocks) {
-        fill_zeros(fill, fill_bytes, blockIdx.x - blocks, gridDim.x - blocks, kSortThreads);
+        fill_zeros(fill, fill_bytes, (size_t)(blockIdx.x - blocks) * kSortThreads + threadIdx.x,
+                   (size_t)(gridDim.x - blocks) * kSortThreads);
         return;
     }
     __shared__ int count[kBins];
@@ -358,15 +358,54 @@ __device__ __forceinline__ void emit(T *grad, const float (&acc)[Pack<T>::kN], i
     y.store(grad, n);
 }
 
+// Zeros over the rows of tokens from `first` to V that no key names: a wave looks
+// `group` tokens up at once, and fills each run of them that does not occur.
+template <typename T>
+__device__ __forceinline__ void fill_absent(T *grad, int D, const int *keys, int rows, int first, int V, int group,
+                                            int64_t wave, int64_t waves)
+{
+    const int lane = threadIdx.x & (kWave - 1);
+    for (int64_t from = first + wave * group; from < V; from += waves * group) {
+        const int64_t v = from + lane;
+        bool absent = lane < group && v < V;
+        int lo = 0, hi = rows;  // the first key that is not below v
+        while (lo < hi) {
+            const int mid = (lo + hi) >> 1;
+            if (keys[mid] < v)
+                lo = mid + 1;
+            else
+                hi = mid;
+        }
+        if (lo < rows && keys[lo] == v)
+            absent = false;
+        uint64_t todo = __ballot(absent);
+        while (todo) {
+            const int at = __builtin_ctzll(todo);
+            const uint64_t up = ~(todo >> at);
+            const int n = up ? __builtin_ctzll(up) : kWave;
+            fill_zeros(reinterpret_cast<char *>(grad + (from + at) * D), (size_t)n * D * sizeof(T), lane, kWave);
+            todo = at + n < kWave ? todo >> (at + n) << (at + n) : 0;
+        }
+    }
+}
+
+// Blocks past the chunks' fill the rows from `fill_from` on, `fill_group` at a time.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void sum_chunks_kernel(const T *grad_out, int64_t ld, int D, const int *keys,
-                                                               const int *order, int rows, int V, int chunk,
+                                                               const int *order, int rows, int V, int chunk, int chunks,
                                                                float scale, bool accumulate, T *grad, float *parts,
-                                                               int part_ld)
+                                                               int part_ld, int fill_from, int fill_group)
 {
     constexpr int N = Pack<T>::kN;
     constexpr int U = 8;  // rows on their way at once
     const int c = blockIdx.x;
+    if (c >= chunks) {
+        const int waves = blockDim.x / kWave;
+        const int64_t block = (int64_t)(c - chunks) * gridDim.y + blockIdx.y;
+        fill_absent(grad, D, keys, rows, fill_from, V, fill_group, block * waves + threadIdx.x / kWave,
+                    (int64_t)(gridDim.x - chunks) * gridDim.y * waves);
+        return;
+    }
     const int64_t from = (int64_t)c * chunk;
     const int64_t to = from + chunk < rows ? from + chunk : rows;
     const int col = (blockIdx.y * blockDim.x + threadIdx.x) * N;
@@ -560,9 +599,11 @@ hipError_t embed(const void *weight, int64_t ld, int V, int D, const int32_t *id
     return embed_with<T, 1>(w, ld, V, D, ids, rows, scale, o, stream);
 }
 
+constexpr size_t kFillBytes = 32 << 10;  // of the rows that a wave looks up at once
+
 template <typename T>
 hipError_t sums(const void *grad_out, int64_t ld, int D, const int *keys, const int *order, int rows, int V, float scale,
-                bool accumulate, void *grad_weight, float *parts, hipStream_t stream)
+                bool accumulate, void *grad_weight, float *parts, int fill_from, hipStream_t stream)
 {
     const T *g = static_cast<const T *>(grad_out);
     T *w = static_cast<T *>(grad_weight);
@@ -573,14 +614,34 @@ hipError_t sums(const void *grad_out, int64_t ld, int D, const int *keys, const 
         threads *= 2;
     const dim3 grid(chunks, (vecs + threads - 1) / threads);
     const int part_ld = part_stride(D);
-    sum_chunks_kernel<T><<<grid, threads, 0, stream>>>(g, ld, D, keys, order, rows, V, chunk, scale, accumulate, w, parts,
-                                                       part_ld);
+    int group = kWave;
+    while (group > 1 && (size_t)group * D * sizeof(T) > kFillBytes)
+        group /= 2;
+    const int64_t fill_waves = ((int64_t)V - fill_from + group - 1) / group;
+    const int64_t per_x = (int64_t)(threads / kWave) * grid.y;
+    const dim3 with_fill((unsigned)(chunks + (fill_waves + per_x - 1) / per_x), grid.y);
+    sum_chunks_kernel<T><<<with_fill, threads, 0, stream>>>(g, ld, D, keys, order, rows, V, chunk, chunks, scale, accumulate,
+                                                            w, parts, part_ld, fill_from, group);
     hipError_t e = last_launch();
     if (e != hipSuccess || chunks == 1)
         return e;
     sum_parts_kernel<T><<<grid, threads, 0, stream>>>(D, keys, rows, V, chunk, chunks, scale, accumulate, w, parts,
                                                       part_ld);
     return last_launch();
+}
+
+// The rows of the table that are filled while the sort runs: as many as its time allows
+// (8 us and 2 more for 1,000 rows, at 7 GB/ms), where the rest can be filled while the
+// sums run, which leave the memory idle.  All of them and this rule (us): 64 rows x 2048 x
+// 128,256 bf16 112 and 95, 1,000 x 4096 x 128,256 203 and 195, 8,192 x 2048 x 128,256 122 and
+// 113, 4,000 x 1024 x 256,000 fp32 202 and 191.  Rows under 2 KiB leave short runs (8,192 x
+// 512 x 256,000 bf16: 56 and 59), and more than kSortKeys rows sort in several launches.
+int64_t early_rows(int rows, int V, size_t row_bytes)
+{
+    if (rows == 0 || rows > kSortKeys || row_bytes < 2048)
+        return V;
+    const int64_t early = (int64_t)((((size_t)48 << 20) + (size_t)rows * (16 << 10)) / row_bytes);
+    return early < V ? early : V;
 }
 
 }  // namespace
@@ -612,7 +673,10 @@ hipError_t launch_embed_backward(const void *grad_out, int64_t ld, int dtype, in
     int *hist = reinterpret_cast<int *>(ws + l.hist);
     float *parts = reinterpret_cast<float *>(ws + l.parts);
     const int elt = dtype == 1 ? 2 : 4;
-    const size_t table = accumulate ? 0 : (size_t)V * (size_t)hidden * elt;
+    const size_t row_bytes = (size_t)hidden * elt;
+    const int64_t early = early_rows(rows, V, row_bytes);
+    const size_t table = accumulate ? 0 : (size_t)early * row_bytes;
+    const int fill_from = accumulate ? V : (int)early;
     char *fill = static_cast<char *>(grad_weight);
     const size_t per_block = (size_t)kSortThreads * 16 * 4;
     size_t fill_blocks = (table + per_block - 1) / per_block;
@@ -644,9 +708,9 @@ hipError_t launch_embed_backward(const void *grad_out, int64_t ld, int dtype, in
     if (rows == 0)
         return hipSuccess;
     return dtype == 1 ? sums<uint16_t>(grad_out, ld, hidden, keys[at], order[at], rows, V, scale, accumulate, grad_weight,
-                                       parts, stream)
+                                       parts, fill_from, stream)
                       : sums<float>(grad_out, ld, hidden, keys[at], order[at], rows, V, scale, accumulate, grad_weight,
-                                    parts, stream);
+                                    parts, fill_from, stream);
 }
 
 }  // namespace dv
