@@ -282,6 +282,14 @@ struct Gemm {
                      : "memory");
     }
 
+    // Tiles of few fragments have registers to spare and are those of few rows, whose
+    // results stand for themselves: their sums run in kChains accumulators, joined at the
+    // end.  bf16: each half of a stage of each parity its own, a quarter of the additions one
+    // after the other.  fp32: the leading products of each parity, and the five small ones, which
+    // then round nothing of the large sum.
+    static constexpr bool kSplitSums = kTm * kTn <= 4;
+    static constexpr int kChains = !kSplitSums ? 1 : sizeof(E) == 2 ? 4 : 3;
+
     // acc += the tile at i0 of A and j0 of B.  Lane l of a wave ends with
     // acc[ti][tj][e] = C[i0 + wm BM/WM + 16 ti + 4 (l / 16) + e][j0 + wn BN/WN + 16 tj + l mod 16].
     // `from`, `stages` (at least 1): this block's part of the stages of k.
@@ -350,12 +358,13 @@ struct Gemm {
             wait_loads<0>();
         }
         barrier();
+        f32x4 more[kChains > 1 ? kChains - 1 : 1][kTm][kTn] = {};  // the chains beside acc
         if constexpr (sizeof(E) == 2) {
             Fragments f0, f1;
             read(f0, lds, a0, b0);
-            for (int s = 0; s < stages; ++s) {
+            const auto work = [&](int s, f32x4 (&first)[kTm][kTn], f32x4 (&second)[kTm][kTn]) {
                 read(f1, lds + (s & 1) * kStageBytes, a1, b1);
-                multiply(acc, f0);
+                multiply(first, f0);
                 if (s + 1 < stages) {
                     wait_loads<0>();
                     barrier();
@@ -363,10 +372,20 @@ struct Gemm {
                         load(s & 1);
                     read(f0, lds + ((s + 1) & 1) * kStageBytes, a0, b0);
                 }
-                multiply(acc, f1);
+                multiply(second, f1);
+            };
+            if constexpr (kSplitSums) {
+                for (int s = 0; s < stages; s += 2) {
+                    work(s, acc, more[0]);
+                    if (s + 1 < stages)
+                        work(s + 1, more[1], more[2]);
+                }
+            } else {
+                for (int s = 0; s < stages; ++s)
+                    work(s, acc, acc);
             }
         } else {
-            for (int s = 0; s < stages; ++s) {
+            const auto work = [&](int s, f32x4 (&large)[kTm][kTn], f32x4 (&small)[kTm][kTn]) {
                 const char *tile = lds + (s & 1) * kStageBytes;
                 float x[8];
                 SplitFragment b[kTn];
@@ -390,9 +409,11 @@ struct Gemm {
 #pragma unroll
                     for (int p = 0; p < 6; ++p)
 #pragma unroll
-                        for (int j = 0; j < kTn; ++j)
-                            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.part[kPairs[p][0]], b[j].part[kPairs[p][1]],
-                                                                                acc[i][j], 0, 0, 0);
+                        for (int j = 0; j < kTn; ++j) {
+                            f32x4 &sum = p < 5 ? small[i][j] : large[i][j];
+                            sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.part[kPairs[p][0]], b[j].part[kPairs[p][1]], sum, 0,
+                                                                          0, 0);
+                        }
                 }
                 if (s + 1 < stages) {
                     wait_loads<0>();
@@ -400,7 +421,28 @@ struct Gemm {
                     if (s + 2 < stages)
                         load(s & 1);
                 }
+            };
+            if constexpr (kSplitSums) {
+                for (int s = 0; s < stages; s += 2) {
+                    work(s, acc, more[0]);
+                    if (s + 1 < stages)
+                        work(s + 1, more[1], more[0]);
+                }
+            } else {
+                for (int s = 0; s < stages; ++s)
+                    work(s, acc, acc);
             }
+        }
+        if constexpr (kSplitSums) {
+#pragma unroll
+            for (int i = 0; i < kTm; ++i)
+#pragma unroll
+                for (int j = 0; j < kTn; ++j) {
+                    if constexpr (sizeof(E) == 2)
+                        acc[i][j] = (acc[i][j] + more[0][i][j]) + (more[1][i][j] + more[2][i][j]);
+                    else
+                        acc[i][j] = (acc[i][j] + more[1][i][j]) + more[0][i][j];
+                }
         }
     }
 };
