@@ -8,8 +8,8 @@
 //
 // The logits (4 N V bytes) never reach memory.  Forward: a tile of logits stays
 // in the registers of the product that made it and leaves as each row's
-// maximum and sum of exponentials over the tile; a second kernel joins the
-// tiles.  Backward: a piece of the vocabulary at a time, the same product again,
+// maximum and sum of exponentials over the tile, the target's apart; a second kernel
+// joins the tiles.  Backward: a piece of the vocabulary at a time, the same product again,
 // its tiles leaving as G in bf16, and from the piece's G the two other products.
 // Four products of 2 N D V operations against six N D V that cannot be avoided:
 // the price of not keeping the logits.
@@ -89,8 +89,8 @@ struct RowStage {
 
 // --------------------------------------------------------------- the logits
 
-// Per row and tile: maximum and sum of exponentials of the allowed logits;
-// the target's logit.  i runs over the piece's tokens, j over rows.
+// Per row and tile: maximum and sum of exponentials of the allowed logits but the
+// target's; the target's logit.  i runs over the piece's tokens, j over rows.
 template <typename E, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__(WM *WN *kWave, 2) void stats_kernel(GemmShape g, int v0, int V, int rows, Masks masks,
                                                                  const int32_t *targets, Softmax *parts,
@@ -113,10 +113,11 @@ __global__ __launch_bounds__(WM *WN *kWave, 2) void stats_kernel(GemmShape g, in
         const int n = tj * BN + wn * (BN / WN) + b * 16 + (lane & 15);
         const bool live = n < rows;
         const RowMask m(masks, V, live ? n : 0);
+        const int t = live ? targets[n] - vw : -1;
         uint32_t word[kWords];
 #pragma unroll
         for (int i = 0; i < kWords; ++i)
-            word[i] = m.word((vw >> 5) + i) >> (quarter * 4);
+            word[i] = (m.word((vw >> 5) + i) & ~(t >> 5 == i ? 1u << (t & 31) : 0u)) >> (quarter * 4);
         float top = -INFINITY;
 #pragma unroll
         for (int a = 0; a < G::kTm; ++a)
@@ -139,7 +140,6 @@ __global__ __launch_bounds__(WM *WN *kWave, 2) void stats_kernel(GemmShape g, in
             }
         sum += __shfl_xor(sum, 16);
         sum += __shfl_xor(sum, 32);
-        const int t = live ? targets[n] - vw : -1;
         if (live && quarter == 0)
             parts[(size_t)(vw / (BM / WM)) * rows + n] = {top, sum};
         const bool here = (uint32_t)t < (uint32_t)(BM / WM) && ((t >> 2) & 3) == quarter;
@@ -182,9 +182,23 @@ __global__ __launch_bounds__(256) void finish_kernel(const Softmax *parts, int n
     s = sh[threadIdx.x];
     const int t = targets[n];
     const RowMask m(masks, V, n);
-    const float lns = s.empty() ? 0.f : logf(s.sum);
-    lse[n] = s.empty() ? -INFINITY : s.max + lns;
-    loss[n] = m.has(t) ? (s.max - target_logit[n]) + lns : 0.f;
+    // s holds every allowed token but the target.  Where the target is the largest, the
+    // loss is ln(1 + the others' share of it), to the last bits also where that is small.
+    if (!m.has(t)) {
+        lse[n] = s.empty() ? -INFINITY : s.max + logf(s.sum);
+        loss[n] = 0.f;
+        return;
+    }
+    const float z = target_logit[n];
+    if (z >= s.max) {
+        const float l = log1pf(s.empty() ? 0.f : s.sum * softmax_term(s.max, z, kLog2e)) + (z - z);  // NaN if z is infinite
+        lse[n] = z + l;
+        loss[n] = l;
+    } else {
+        const float lns = logf(s.sum + softmax_term(z, s.max, kLog2e));
+        lse[n] = s.max + lns;
+        loss[n] = (s.max - z) + lns;
+    }
 }
 
 // The weight of each row's gradient: grad_loss where the target is allowed, else 0.
