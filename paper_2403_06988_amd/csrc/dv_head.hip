@@ -91,6 +91,9 @@ struct RowStage {
 
 // Per row and tile: maximum and sum of exponentials of the allowed logits but the
 // target's; the target's logit.  i runs over the piece's tokens, j over rows.
+// Bound by the matrix instructions: 8,192 x 4,096 x 128,256 bf16 in 6.3 ms, 1.36 PFLOP/s
+// (a library product that stores the logits: 5.9 ms); 1 x 1,024 x 32,000 in 13.0 us, by the
+// weights' 65 MB; fp32 1,024 x 512 x 32,000 in 200 us, 168 TFLOP/s (a library product 249).
 template <typename E, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__(WM *WN *kWave, 2) void stats_kernel(GemmShape g, int v0, int V, int rows, Masks masks,
                                                                  const int32_t *targets, Softmax *parts,
@@ -211,7 +214,7 @@ __global__ void weights_kernel(int rows, int V, Masks masks, const int32_t *targ
 
 // A piece of G in the operands' type: [rows][ld] with the piece's tokens along a
 // row, zeros up to the next multiple of 64 of them, and up to the next whole stage
-// of rows.
+// of rows.  8,192 x 4,096 x 16,128 tokens bf16: 859 us, 1.26 PFLOP/s with 264 MB of stores.
 template <typename E, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__(WM *WN *kWave, 2) void grad_kernel(GemmShape g, int v0, int V, int rows, Masks masks,
                                                                 const int32_t *targets, const float *lse,
@@ -271,7 +274,8 @@ enum class Out { kStore, kPartial, kPartialAdd };
 
 // C[j][i] of a product as `out_rows` rows of `cols` elements: in T, or in fp32
 // as (or on top of) the partial sums of this block's share of k.  A is stored by
-// columns, B by columns with COLS_B.  One buffer where k is one stage: three
+// columns, B by columns with COLS_B.  8,192 x 4,096 x 16,128 bf16: 765 us either way, 1.41
+// PFLOP/s, bound by the matrix instructions.  One buffer where k is one stage: three
 // blocks a compute unit instead of two (64 rows x 2048 x 128,256 bf16: 103 us and 128).
 template <typename E, int BM, int BN, int WM, int WN, bool COLS_B, typename T, Out OUT, int BUFFERS>
 __global__ __launch_bounds__(WM *WN *kWave, 2) void product_kernel(GemmShape g, T *out, int out_rows, int cols,
