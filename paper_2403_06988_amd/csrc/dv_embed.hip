@@ -132,21 +132,24 @@ __device__ __forceinline__ int sort_key(int id, int V) { return (uint32_t)id < (
 // kBins words of the wave) holds the wave's running counts.
 __device__ __forceinline__ int wave_rank(int digit, bool live, int *counts)
 {
-    uint64_t same = __ballot(live);
+    // lanes of the same digit, as 32-bit halves: a bit's ballot, or its complement where
+    // this lane's bit is clear (the sort is bound by its one compute unit's vector issue)
+    const uint64_t alive = __ballot(live);
+    uint32_t lo = (uint32_t)alive, hi = (uint32_t)(alive >> 32);
 #pragma unroll
     for (int b = 0; b < kDigitBits; ++b) {
-        const bool bit = digit >> b & 1;
-        const uint64_t with = __ballot(bit);
-        same &= bit ? with : ~with;
+        const int mine = (int)((uint32_t)digit << (31 - b)) >> 31;  // -1 or 0
+        const uint64_t with = __ballot(mine != 0);
+        lo &= ~((uint32_t)with ^ (uint32_t)mine);
+        hi &= ~((uint32_t)(with >> 32) ^ (uint32_t)mine);
     }
-    const int lane = threadIdx.x & (kWave - 1);
-    const int before = __popcll(same & ((1ull << lane) - 1ull));
+    const int before = (int)__builtin_amdgcn_mbcnt_hi(hi, __builtin_amdgcn_mbcnt_lo(lo, 0));
     int base = 0;
     if (live)
         base = counts[digit];
     wave_lds_sync();
     if (live && before == 0)
-        counts[digit] = base + __popcll(same);
+        counts[digit] = base + __popc(lo) + __popc(hi);
     wave_lds_sync();
     return base + before;
 }
