@@ -95,7 +95,7 @@ struct Vec<uint16_t> {
     static __device__ __forceinline__ void put(uint16_t *p, float y) { *p = narrow(y); }
 };
 
-constexpr int kMostThreads = 1024;  // of a block that holds a row
+constexpr int kMostThreads = 1024;  // of a block that holds a long row, or has a unit to itself
 struct Shared {
     Softmax row[kMostThreads / kWave], top[kMostThreads / kWave];  // of each wave
     float loss[kMostThreads / kWave];
@@ -654,12 +654,27 @@ hipError_t launch_held(const DistillArgs &a, const float *grad_loss, float *loss
     return last_launch();
 }
 
+// The second pass over rows past the L2s finds them in the memory-side cache (256 MB) if the
+// rows under way fit there.  Four blocks a compute unit of rows over 200 KB do not: LDS
+// that a block asks for and does not use leaves room for two, or for one of twice the
+// lanes (loss and gradient with four, two, one, and one of 1,024 lanes, us):
+//     1,000 x 150,000 bf16 147 143 158   -     1,000 x 256,000 bf16 276 256 251 243
+//     1,000 x 200,000 bf16 201 196 201   -     2,000 x 256,000 bf16 560 506 494 479
+//     1,000 x 100,000 fp32 205 192 192   -       600 x 128,256 fp32 161 162 149 144
+//     2,000 x  80,000 fp32 312 304 299   -     1,000 x 256,000 fp32 599 601 502 487
+// (2,048 x 128,256 bf16, three instead of four: 243 242.)
+constexpr size_t kRowsUnderWay = (size_t)208 << 20;
+constexpr unsigned kRoomForTwo = 50 << 10, kRoomForOne = 100 << 10;  // of 160 KB; a block uses 13
+
+bool too_many(int64_t blocks_per_unit, size_t row_bytes) { return blocks_per_unit * 256 * row_bytes > kRowsUnderWay; }
+
 template <typename T, int THREADS, bool MASK>
 hipError_t launch_rows(const DistillArgs &a, const float *grad_loss, float *loss, T *grad, int64_t ld_grad,
-                       hipStream_t stream)
+                       hipStream_t stream, unsigned idle_lds = 0)
 {
     if (grad)
-        distill_row_kernel<T, THREADS, MASK, true><<<a.rows, THREADS, 0, stream>>>(a, grad_loss, loss, grad, ld_grad);
+        distill_row_kernel<T, THREADS, MASK, true>
+            <<<a.rows, THREADS, idle_lds, stream>>>(a, grad_loss, loss, grad, ld_grad);
     else
         distill_row_kernel<T, THREADS, MASK, false><<<a.rows, THREADS, 0, stream>>>(a, nullptr, loss, nullptr, 0);
     return last_launch();
@@ -690,7 +705,14 @@ hipError_t launch(const DistillArgs &a, const float *grad_loss, float *loss, T *
             return launch_rows<T, 128, MASK>(a, grad_loss, loss, grad, ld_grad, stream);
         if (vecs <= (grad ? kMiddleRowGrad : kMiddleRow))
             return launch_rows<T, 256, MASK>(a, grad_loss, loss, grad, ld_grad, stream);
-        return launch_rows<T, kThreads, MASK>(a, grad_loss, loss, grad, ld_grad, stream);
+        const size_t row_bytes = (size_t)a.V * sizeof(T);
+        if (grad && too_many(2, row_bytes)) {
+            distill_row_kernel<T, kMostThreads, MASK, true>
+                <<<a.rows, kMostThreads, kRoomForOne, stream>>>(a, grad_loss, loss, grad, ld_grad);
+            return last_launch();
+        }
+        return launch_rows<T, kThreads, MASK>(a, grad_loss, loss, grad, ld_grad, stream,
+                                              too_many(3, row_bytes) ? kRoomForTwo : 0);
     }
     Softmax *parts = static_cast<Softmax *>(workspace);
     float *listed = reinterpret_cast<float *>(parts + (size_t)a.rows * s.chunks);
