@@ -637,7 +637,7 @@ hipError_t sums(const void *grad_out, int64_t ld, int D, const int *keys, const 
 }
 
 // The rows of the table that are filled while the sort runs: as many as its time allows
-// (8 us and 2 more for 1,000 rows, at 7 GB/ms), where the rest can be filled while the
+// (about 8 us and 1.3 more for 1,000 rows, at 7 GB/ms), where the rest can be filled while the
 // sums run, which leave the memory idle.  All of them and this rule (us): 64 rows x 2048 x
 // 128,256 bf16 112 and 95, 1,000 x 4096 x 128,256 203 and 195, 8,192 x 2048 x 128,256 122 and
 // 113, 4,000 x 1024 x 256,000 fp32 202 and 191.  Rows under 2 KiB leave short runs (8,192 x
