@@ -236,8 +236,9 @@ __device__ __forceinline__ void for_batches(const T *z, const RowMask &m, int j0
 
 // exp(c (x - max)) as exp2(x c2 - shift), shift = max c2 rounded: one operation and
 // one rounding; `correction` is the factor 2^(shift - max c2) that the rounding of
-// the shift leaves.  Only where max c2 is of ordinary size: else (a row of
-// nothing but the type's lowest value, say) differences are scaled.
+// the shift leaves: an exponential of its own, once a batch, because at logits of 500,000
+// its first-order form 1 - d ln 2 is off by 2.4e-4.  Only where max c2 is of ordinary size:
+// else (a row of nothing but the type's lowest value, say) differences are scaled.
 struct Shift {
     float max, c2, shift, correction;
     bool plain;
@@ -245,7 +246,7 @@ struct Shift {
     {
         shift = max * c2;
         plain = fabsf(shift) < 1048576.f;
-        correction = plain ? 1.f - __builtin_fmaf(max, c2, -shift) * 0.69314718f : 1.f;
+        correction = plain ? exp2_fast(-__builtin_fmaf(max, c2, -shift)) : 1.f;
     }
     template <bool PLAIN>
     __device__ __forceinline__ float term(float x) const

@@ -7,6 +7,7 @@ import pytest
 import torch
 
 from tests.train_common import check, distill_reference, masks, pack_mask, row_mask
+from tests.train_common import U, UB
 
 pytestmark = pytest.mark.gpu
 DEV = torch.device("cuda:0")
@@ -177,3 +178,64 @@ def test_refusals(dv):
                 lambda: dv.distill_loss_backward(wide[:, :100], ids, top, g, grad=wide[:, 1:101])):
         with pytest.raises(dv.DvError):
             bad()
+
+
+def far_reference(z, ids, top, c, g):
+    """distill_reference for unmasked rows at once, with bounds that do not grow
+    with the tokens: a sum of terms of one sign is off by as many U of itself as its
+    chain is long, at most 64 or V / 512 terms of a lane and fewer than 64 joins."""
+    N, V = z.shape
+    z64, t64 = z.double(), top.double()
+    zc, tc = c * (z64 - z64.max(1, keepdim=True).values), c * (t64 - t64.max(1, keepdim=True).values)
+    lnp = zc - torch.logsumexp(zc, 1, keepdim=True)
+    lnq = tc - torch.logsumexp(tc, 1, keepdim=True)
+    q, at = lnq.exp(), ids.long()
+    span = lnq - lnp.gather(1, at)
+    loss = (q * span).sum(1)
+    # exp's argument (two roundings) and its own, the sums, the logarithms
+    rel = U * (max(64, V / 512) + 64 + 8 * (zc.clamp(min=-120).abs() + math.log(V) + 4))
+    loss_tol = (q * (rel.gather(1, at) + U * (64 + 8 * (tc.abs() + lnq.abs() + span.abs())))).sum(1)
+    Q = torch.zeros_like(z64).scatter_add_(1, at, q)
+    w = g.double()[:, None] * c
+    y = w * (lnp.exp() - Q)
+    store = UB if z.dtype == torch.bfloat16 else 2 * U
+    tol = (w.abs() * (lnp.exp() * rel + Q * U * (96 + 16 * tc.abs().max())) + store * y.abs()) * 1.01 + 1e-37
+    return loss, loss_tol, y, tol
+
+
+# a block a row, rows split over blocks, rows held in registers
+@pytest.mark.parametrize("N,V,dtype", [(6, 700, torch.float32), (6, 5000, torch.bfloat16), (7, 50000, torch.float32),
+                                       (8500, 1001, torch.float32), (2200, 8191, torch.bfloat16), (170, 40000, torch.float32)])
+@pytest.mark.parametrize("c", [1.0, 0.75])
+def test_logits_far_from_zero(dv, N, V, dtype, c):
+    """Rows whose logits lie about 1e4, 1e5 and 6e5 from zero, on both sides of
+    it: a softmax knows differences only, which are exact there."""
+    print(f"distill far N={N} V={V} {dtype} c={c}", flush=True)
+    rng = np.random.default_rng(N + V)
+    ulp = 2.0 ** 12 if dtype == torch.bfloat16 else 2.0 ** -4
+    c2 = np.float32(c) * np.float32(1.4426950408889634)
+
+    def rounding(m):  # of the largest logit's exponent of two, in units of e
+        m = m.astype(np.float32)
+        return (m.astype(np.float64) * np.float64(c2) - np.float64(m * c2)) * math.log(2)
+
+    # of 64 values near each distance the one whose exponent rounds most
+    some = np.array([1e4, 1e5, 6e5])[np.arange(N) % 3][:, None] * rng.uniform(0.9, 1.1, (N, 64))
+    some = np.round(some / ulp) * ulp
+    some[1::2] *= -1
+    some = torch.from_numpy(some).to(dtype).double().numpy()
+    far = some[np.arange(N), np.abs(rounding(some)).argmax(1)]
+    step = rng.integers(0, 200, (N, V)) * (ulp if dtype == torch.bfloat16 else 0.125)
+    step[:, ::2] = 0  # half of the tokens at the maximum
+    z = torch.from_numpy(far[:, None] - step).to(dtype)
+    assert dtype == torch.bfloat16 or bool((z.double() == torch.from_numpy(far[:, None] - step)).all())
+    ids = torch.from_numpy(np.stack([rng.permutation(V)[:6] // 2 * 2 for _ in range(N)]).astype(np.int32))
+    top = torch.from_numpy(rng.normal(size=(N, 6))).float()
+    g = torch.from_numpy(rng.normal(size=N)).float()
+    loss, loss_tol, grad, grad_tol = far_reference(z, ids, top, c, g)
+    # what a first-order factor for that rounding would leave out passes the bound
+    assert (rounding(far) ** 2 / 2 > 2 * loss_tol.numpy()).any()
+    alone, got, got_grad = run(dv, z, ids, top, c, None, None, g)
+    check(alone, loss, loss_tol, "loss alone")
+    check(got, loss, loss_tol, "loss")
+    check(got_grad, grad, grad_tol, "grad")
