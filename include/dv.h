@@ -521,7 +521,8 @@ DV_API size_t dv_distill_loss_workspace_bytes(int32_t rows, int32_t num_tokens, 
  *
  * logits [rows][ld_logits] of `dtype`; teacher_ids [rows][num_top] int32 (ids
  * outside [0, V) take no part), teacher_logits [rows][num_top] fp32; loss
- * [rows] fp32.  inv_temperature finite and > 0.
+ * [rows] fp32.  inv_temperature > 0 and at most 2.3e38 (its product
+ * with log2(e), in fp32, has to be finite).
  * rows = 0 is valid and enqueues nothing.
  * Errors as dv_head_loss.
  */

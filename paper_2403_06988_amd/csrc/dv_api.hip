@@ -672,6 +672,9 @@ size_t dv_distill_loss_workspace_bytes(int32_t rows, int32_t num_tokens, int32_t
 
 namespace {
 
+// The kernels take powers of two: inv_temperature log2(e) has to be finite.
+constexpr float kMaxInvTemperature = 2.3e38f;
+
 // Both distillation calls; `grad_wanted`: the backward one.
 dv_status distill_common(const char *name, bool grad_wanted, const void *logits, int64_t ld_logits, int32_t dtype,
                          int32_t rows, int32_t num_tokens, const int32_t *teacher_ids, const float *teacher_logits,
@@ -685,8 +688,9 @@ dv_status distill_common(const char *name, bool grad_wanted, const void *logits,
     DV_CHECK(train_sizes(name, {rows, num_tokens, dtype}));
     if (num_top < 1 || num_top > DV_MAX_TOP)
         return fail(DV_ERR_SHAPE, "%s: num_top=%d outside [1, %d]", name, num_top, DV_MAX_TOP);
-    if (!(inv_temperature > 0.0f && inv_temperature <= 3.0e38f))
-        return fail(DV_ERR_SHAPE, "%s: inv_temperature=%g must be finite and > 0", name, (double)inv_temperature);
+    if (!(inv_temperature > 0.0f && inv_temperature <= kMaxInvTemperature))
+        return fail(DV_ERR_SHAPE, "%s: inv_temperature=%g must be > 0 and at most %g", name, (double)inv_temperature,
+                    (double)kMaxInvTemperature);
     DV_CHECK(row_stride(name, "ld_logits", ld_logits, num_tokens));
     if (grad_wanted)
         DV_CHECK(row_stride(name, "ld_grad", ld_grad, num_tokens));

@@ -239,3 +239,17 @@ def test_logits_far_from_zero(dv, N, V, dtype, c):
     check(alone, loss, loss_tol, "loss alone")
     check(got, loss, loss_tol, "loss")
     check(got_grad, grad, grad_tol, "grad")
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("N,V", [(4, 300), (2, 90000), (8500, 2001)])  # a block a row, split rows, held rows
+def test_largest_inverse_temperature(dv, dtype, N, V):
+    """Both softmaxes are one token each there: where it is the same one, nothing is left."""
+    rng = np.random.default_rng(V)
+    z = torch.from_numpy(rng.integers(-50, 50, (N, V))).to(dtype)
+    best = torch.from_numpy(rng.integers(0, V, N))
+    z[torch.arange(N), best] = 64.0
+    ids = torch.stack([best, (best + 1) % V], 1).int()
+    top = torch.tensor([[2.0, 1.0]]).repeat(N, 1)
+    alone, loss, grad = run(dv, z, ids, top, 2.3e38, None, None, torch.full((N,), 0.5))
+    assert not alone.any() and not loss.any() and not grad.any()

@@ -165,3 +165,11 @@ def test_binding_refuses_host_tensors():
                 lambda: dv.distill_loss(x, torch.zeros((2, 3), dtype=torch.int32), torch.zeros((2, 3)))):
         with pytest.raises((TypeError, ValueError)):
             bad()
+
+
+@pytest.mark.parametrize("call", [distill, distill_back])
+def test_inverse_temperature_whose_exponent_is_not_finite(call):
+    """The kernels scale by c log2(e) in fp32, infinite from 2.36e38 on."""
+    assert call(c=2.4e38) == call(c=3.0e38) == call(c=3.4e38) == SHAPE
+    assert b"inv_temperature" in lib.dv_last_error()
+    assert call(c=2.3e38, ws=None) == WORKSPACE  # passes; the next check does not
