@@ -442,10 +442,20 @@ DV_API dv_status dv_spec_verify(const int32_t *next_state, const uint32_t *allow
  */
 
 /*
- * dv_head_loss_workspace_bytes -- device workspace of dv_head_loss.  Returns 0
- * when an argument is outside its limit.
+ * dv_head_loss_workspace_bytes -- device workspace of dv_head_loss, for
+ * operands of any stride and alignment.  Returns 0 when an argument is outside
+ * its limit.
+ *
+ * Operands are multiplied where they lie if hidden is a multiple of 64, their
+ * rows start on 16-byte boundaries and are at most 2^20 elements apart; else
+ * copies take their place: of x whole, of the weights a piece at a time (2^27 + 2^19
+ * rows elements, or 8,192 tokens if those are more).  dv_head_loss_workspace_bytes_for
+ * is the workspace of a call with these operands, without copies of what needs
+ * none; the pointers are not dereferenced.
  */
 DV_API size_t dv_head_loss_workspace_bytes(int32_t rows, int32_t hidden, int32_t num_tokens, int32_t dtype);
+DV_API size_t dv_head_loss_workspace_bytes_for(const void *x, int64_t ld_x, const void *weight, int64_t ld_weight,
+                                               int32_t dtype, int32_t rows, int32_t hidden, int32_t num_tokens);
 
 /*
  * dv_head_loss -- softmax cross entropy over the allowed tokens, from hidden
@@ -472,11 +482,16 @@ DV_API dv_status dv_head_loss(const void *x, int64_t ld_x, const void *weight, i
 
 /*
  * dv_head_loss_backward_workspace_bytes -- device workspace of
- * dv_head_loss_backward (a piece of the vocabulary at a time: it grows with
- * rows and hidden, and with num_tokens only up to one piece).  Returns 0 when
- * an argument is outside its limit.
+ * dv_head_loss_backward, for operands of any stride and alignment: what
+ * dv_head_loss copies, G of a piece of the vocabulary (2^27 elements, or 4,096
+ * tokens if those are more) and the gradients' partial sums.  Returns 0 when an
+ * argument is outside its limit.  dv_head_loss_backward_workspace_bytes_for: of
+ * a call with these operands.
  */
 DV_API size_t dv_head_loss_backward_workspace_bytes(int32_t rows, int32_t hidden, int32_t num_tokens, int32_t dtype);
+DV_API size_t dv_head_loss_backward_workspace_bytes_for(const void *x, int64_t ld_x, const void *weight, int64_t ld_weight,
+                                                        int32_t dtype, int32_t rows, int32_t hidden,
+                                                        int32_t num_tokens);
 
 /*
  * dv_head_loss_backward -- the gradients of sum_n grad_loss[n] loss[n].

@@ -27,8 +27,8 @@ import torch
 __all__ = ["align", "validate_vocab", "masked_step", "masked_step_noalloc", "masked_sample", "spec_walk", "spec_verify", "align_workspace_bytes",
            "masked_step_workspace_bytes", "masked_sample_workspace_bytes", "spec_verify_workspace_bytes",
            "step_workspace", "sample_workspace", "spec_workspace", "head_loss", "head_loss_backward",
-           "head_loss_workspace_bytes", "head_loss_backward_workspace_bytes", "distill_loss", "distill_loss_backward",
-           "distill_loss_workspace_bytes", "embed", "embed_backward", "embed_backward_workspace_bytes", "DvError", "DEAD",
+           "head_loss_workspace_bytes", "head_loss_workspace_bytes_for", "head_loss_backward_workspace_bytes",
+           "head_loss_backward_workspace_bytes_for", "distill_loss", "distill_loss_backward", "distill_loss_workspace_bytes", "embed", "embed_backward", "embed_backward_workspace_bytes", "DvError", "DEAD",
            "library_path", "lib"]
 
 DEAD = -1
@@ -92,10 +92,14 @@ def _load():
     mask = [vp, i32, vp]
     lib.dv_head_loss_workspace_bytes.restype = sz
     lib.dv_head_loss_workspace_bytes.argtypes = [i32, i32, i32, i32]
+    lib.dv_head_loss_workspace_bytes_for.restype = sz
+    lib.dv_head_loss_workspace_bytes_for.argtypes = [vp, i64, vp, i64, i32, i32, i32, i32]
     lib.dv_head_loss.restype = ctypes.c_int
     lib.dv_head_loss.argtypes = [vp, i64, vp, i64, i32, i32, i32, i32, vp, *mask, vp, vp, vp, sz, vp]
     lib.dv_head_loss_backward_workspace_bytes.restype = sz
     lib.dv_head_loss_backward_workspace_bytes.argtypes = [i32, i32, i32, i32]
+    lib.dv_head_loss_backward_workspace_bytes_for.restype = sz
+    lib.dv_head_loss_backward_workspace_bytes_for.argtypes = [vp, i64, vp, i64, i32, i32, i32, i32]
     lib.dv_head_loss_backward.restype = ctypes.c_int
     lib.dv_head_loss_backward.argtypes = [vp, i64, vp, i64, i32, i32, i32, i32, vp, *mask, vp, vp, vp, vp, vp, sz, vp]
     lib.dv_distill_loss_workspace_bytes.restype = sz
@@ -444,11 +448,21 @@ def spec_verify(next_state, allow, states, proposals, logits, token=None, accept
 # ------------------------------------------------------------------ training
 
 def head_loss_workspace_bytes(rows: int, hidden: int, num_tokens: int, dtype) -> int:
+    """Of ``head_loss`` for operands of any strides and alignment; for those at
+    hand ``head_loss_workspace_bytes_for``, which may be far less."""
     return int(lib.dv_head_loss_workspace_bytes(rows, hidden, num_tokens, _code(dtype)))
 
 
 def head_loss_backward_workspace_bytes(rows: int, hidden: int, num_tokens: int, dtype) -> int:
     return int(lib.dv_head_loss_backward_workspace_bytes(rows, hidden, num_tokens, _code(dtype)))
+
+
+def head_loss_workspace_bytes_for(x, weight) -> int:
+    return int(lib.dv_head_loss_workspace_bytes_for(*_head_operands(x, weight)[1]))
+
+
+def head_loss_backward_workspace_bytes_for(x, weight) -> int:
+    return int(lib.dv_head_loss_backward_workspace_bytes_for(*_head_operands(x, weight)[1]))
 
 
 def distill_loss_workspace_bytes(rows: int, num_tokens: int, num_top: int) -> int:
@@ -536,16 +550,21 @@ def _scratch(workspace, need, dev, stream):
     return _workspace(workspace, need, dev, None)
 
 
-def _head_args(x, weight, targets, allow, states):
+def _head_operands(x, weight):
     dev = weight.device
     ld_x, ld_w = _matrix(x, "x", dev), _matrix(weight, "weight", dev, x.dtype)
     dt = _code(x.dtype)
     (N, D), V = x.shape, weight.shape[0]
     if weight.shape[1] != D:
         raise ValueError(f"weight must be [V][{D}]")
+    return dev, (_ptr(x), ld_x, _ptr(weight), ld_w, dt, N, D, V)
+
+
+def _head_args(x, weight, targets, allow, states):
+    dev, operands = _head_operands(x, weight)
+    N, V = operands[5], operands[7]
     _vector(targets, "targets", N, torch.int32, dev)
-    mask = _mask_args(allow, states, N, V, dev)
-    return dev, (_ptr(x), ld_x, _ptr(weight), ld_w, dt, N, D, V, _ptr(targets), *mask), (N, D, V, dt)
+    return dev, operands, (_ptr(targets), *_mask_args(allow, states, N, V, dev))
 
 
 def head_loss(x, weight, targets, allow=None, states=None, loss=None, lse=None, workspace=None, stream=None):
@@ -557,11 +576,12 @@ def head_loss(x, weight, targets, allow=None, states=None, loss=None, lse=None, 
     takes no part (loss 0).  allow [S][ceil(V/32)] int32 (as from ``align``)
     with states [N] int32: the tokens each row's state allows; without them
     every token.  Returns (loss [N], lse [N]) fp32."""
-    dev, args, (N, D, V, dt) = _head_args(x, weight, targets, allow, states)
+    dev, operands, rest = _head_args(x, weight, targets, allow, states)
+    N = operands[5]
     loss = _result(loss, "loss", (N,), torch.float32, dev, stream)
     lse = _result(lse, "lse", (N,), torch.float32, dev, stream)
-    workspace, nbytes = _scratch(workspace, int(lib.dv_head_loss_workspace_bytes(N, D, V, dt)), dev, stream)
-    st = lib.dv_head_loss(*args, _ptr(loss), _ptr(lse), _ptr(workspace), nbytes, _stream(stream, dev))
+    workspace, nbytes = _scratch(workspace, int(lib.dv_head_loss_workspace_bytes_for(*operands)), dev, stream)
+    st = lib.dv_head_loss(*operands, *rest, _ptr(loss), _ptr(lse), _ptr(workspace), nbytes, _stream(stream, dev))
     _check(st, "dv_head_loss")
     return loss, lse
 
@@ -571,16 +591,17 @@ def head_loss_backward(x, weight, targets, lse, grad_loss, allow=None, states=No
     """Gradients of sum(grad_loss * loss) of ``head_loss``; lse [N] as it
     returned it.  Returns (grad_x [N][D], grad_weight [V][D]) in the inputs'
     dtype; ``want_x`` / ``want_weight`` false: None in its place, not computed."""
-    dev, args, (N, D, V, dt) = _head_args(x, weight, targets, allow, states)
+    dev, operands, rest = _head_args(x, weight, targets, allow, states)
+    N, D, V = operands[5:]
     _vector(lse, "lse", N, torch.float32, dev)
     _vector(grad_loss, "grad_loss", N, torch.float32, dev)
     if not (want_x or want_weight):
         return None, None
     grad_x = _result(grad_x, "grad_x", (N, D), x.dtype, dev, stream) if want_x else None
     grad_weight = _result(grad_weight, "grad_weight", (V, D), x.dtype, dev, stream) if want_weight else None
-    workspace, nbytes = _scratch(workspace, int(lib.dv_head_loss_backward_workspace_bytes(N, D, V, dt)), dev, stream)
-    st = lib.dv_head_loss_backward(*args, _ptr(lse), _ptr(grad_loss), _ptr(grad_x), _ptr(grad_weight), _ptr(workspace),
-                                   nbytes, _stream(stream, dev))
+    workspace, nbytes = _scratch(workspace, int(lib.dv_head_loss_backward_workspace_bytes_for(*operands)), dev, stream)
+    st = lib.dv_head_loss_backward(*operands, *rest, _ptr(lse), _ptr(grad_loss), _ptr(grad_x), _ptr(grad_weight),
+                                   _ptr(workspace), nbytes, _stream(stream, dev))
     _check(st, "dv_head_loss_backward")
     return grad_x, grad_weight
 

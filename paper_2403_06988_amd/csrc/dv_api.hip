@@ -598,6 +598,14 @@ size_t dv_head_loss_workspace_bytes(int32_t rows, int32_t hidden, int32_t num_to
     return head_sizes_ok(rows, hidden, num_tokens, dtype) ? dv::head_workspace_bytes(rows, hidden, num_tokens, dtype) : 0;
 }
 
+size_t dv_head_loss_workspace_bytes_for(const void *x, int64_t ld_x, const void *weight, int64_t ld_weight, int32_t dtype,
+                                        int32_t rows, int32_t hidden, int32_t num_tokens)
+{
+    if (!head_sizes_ok(rows, hidden, num_tokens, dtype))
+        return 0;
+    return dv::head_workspace_bytes({x, ld_x, weight, ld_weight, dtype, rows, hidden, num_tokens, nullptr, {}});
+}
+
 dv_status dv_head_loss(const void *x, int64_t ld_x, const void *weight, int64_t ld_weight, int32_t dtype, int32_t rows,
                        int32_t hidden, int32_t num_tokens, const int32_t *targets, const uint32_t *allow,
                        int32_t num_states, const int32_t *states, float *loss, float *lse, void *workspace,
@@ -611,14 +619,14 @@ dv_status dv_head_loss(const void *x, int64_t ld_x, const void *weight, int64_t 
         return DV_OK;
     if (!loss || !lse)
         return fail(DV_ERR_INVALID_ARG, "%s: loss and lse must be non-NULL when rows > 0", name);
-    const size_t elt = element_size(dtype), need = dv::head_workspace_bytes(rows, hidden, num_tokens, dtype);
+    const dv::HeadArgs a{x, ld_x, weight, ld_weight, dtype, rows, hidden, num_tokens, targets, {allow, states, num_states}};
+    const size_t elt = element_size(dtype), need = dv::head_workspace_bytes(a);
     DV_CHECK(workspace_args(name, workspace, workspace_bytes, need));
     const Range outs[] = {range_of(loss, (size_t)rows * 4), range_of(lse, (size_t)rows * 4), range_of(workspace, need)};
     const Range ins[] = {rows_range(x, rows, hidden, ld_x, elt), rows_range(weight, num_tokens, hidden, ld_weight, elt),
                          range_of(targets, (size_t)rows * 4), allow_range(allow, num_states, num_tokens),
                          range_of(states, states ? (size_t)rows * 4 : 0)};
     DV_CHECK(no_overlap(name, outs, ins));
-    const dv::HeadArgs a{x, ld_x, weight, ld_weight, dtype, rows, hidden, num_tokens, targets, {allow, states, num_states}};
     return hip_status(dv::launch_head_loss(a, loss, lse, workspace, static_cast<hipStream_t>(stream)),
                       "dv_head_loss launch");
 }
@@ -628,6 +636,14 @@ size_t dv_head_loss_backward_workspace_bytes(int32_t rows, int32_t hidden, int32
     return head_sizes_ok(rows, hidden, num_tokens, dtype)
                ? dv::head_backward_workspace_bytes(rows, hidden, num_tokens, dtype)
                : 0;
+}
+
+size_t dv_head_loss_backward_workspace_bytes_for(const void *x, int64_t ld_x, const void *weight, int64_t ld_weight,
+                                                 int32_t dtype, int32_t rows, int32_t hidden, int32_t num_tokens)
+{
+    if (!head_sizes_ok(rows, hidden, num_tokens, dtype))
+        return 0;
+    return dv::head_backward_workspace_bytes({x, ld_x, weight, ld_weight, dtype, rows, hidden, num_tokens, nullptr, {}});
 }
 
 dv_status dv_head_loss_backward(const void *x, int64_t ld_x, const void *weight, int64_t ld_weight, int32_t dtype,
@@ -647,7 +663,8 @@ dv_status dv_head_loss_backward(const void *x, int64_t ld_x, const void *weight,
     const size_t elt = element_size(dtype);
     DV_CHECK(aligned(name, "grad_x", grad_x, elt));
     DV_CHECK(aligned(name, "grad_weight", grad_weight, elt));
-    const size_t need = dv::head_backward_workspace_bytes(rows, hidden, num_tokens, dtype);
+    const dv::HeadArgs a{x, ld_x, weight, ld_weight, dtype, rows, hidden, num_tokens, targets, {allow, states, num_states}};
+    const size_t need = dv::head_backward_workspace_bytes(a);
     DV_CHECK(workspace_args(name, workspace, workspace_bytes, need));
     const Range outs[] = {rows_range(grad_x, rows, hidden, hidden, elt),
                           rows_range(grad_weight, num_tokens, hidden, hidden, elt), range_of(workspace, need)};
@@ -656,7 +673,6 @@ dv_status dv_head_loss_backward(const void *x, int64_t ld_x, const void *weight,
                          range_of(states, states ? (size_t)rows * 4 : 0), range_of(lse, (size_t)rows * 4),
                          range_of(grad_loss, (size_t)rows * 4)};
     DV_CHECK(no_overlap(name, outs, ins));
-    const dv::HeadArgs a{x, ld_x, weight, ld_weight, dtype, rows, hidden, num_tokens, targets, {allow, states, num_states}};
     return hip_status(dv::launch_head_loss_backward(a, lse, grad_loss, grad_x, grad_weight, workspace,
                                                     static_cast<hipStream_t>(stream)),
                       "dv_head_loss_backward launch");

@@ -380,6 +380,7 @@ __global__ void zero_kernel(T *p, int64_t n)
 
 constexpr int64_t kPieceElements = (int64_t)1 << 27;
 constexpr int kPieceTokens = 1 << 18;
+constexpr int64_t kPackedPerRow = (int64_t)1 << 19;
 
 // The tile side and the splits of k for a product of `i` x `j` over `stages` of
 // k (64 of bf16, 32 of fp32), by the time that each choice would take.  Up to
@@ -443,15 +444,94 @@ Plan plan_product(int64_t i, int64_t j, int64_t stages, int most_splits, bool bf
 
 int64_t up64(int64_t n) { return (n + 63) / 64 * 64; }
 
+// Which operands are used where they lie, the others packed: rows of whole stages from
+// 16-byte boundaries, not too far apart for the loads' 32-bit offsets.
+struct InPlace {
+    bool x, w;
+};
+
+bool in_place(const void *p, int64_t ld, int dtype, int hidden)
+{
+    return hidden % 64 == 0 && ld % (dtype == 1 ? 8 : 4) == 0 && reinterpret_cast<uintptr_t>(p) % 16 == 0 &&
+           ld <= ((int64_t)1 << 20);
+}
+
+InPlace in_place(const HeadArgs &a)
+{
+    return {in_place(a.x, a.ld_x, a.dtype, a.hidden), in_place(a.weight, a.ld_w, a.dtype, a.hidden)};
+}
+
+// The workspace: packed operands where they are not in place, and what the call itself needs.
 struct HeadLayout {
+    InPlace here;
     int64_t k;        // hidden size as the products see it
     int stage_k;
     int piece;        // tokens of a piece, a multiple of 256 (or all)
     int pieces;
+    size_t x, w;
+    size_t bytes;
+
+    size_t take(size_t n)
+    {
+        const size_t at = bytes;
+        bytes += align_up(n, 256);
+        return at;
+    }
+};
+
+// A piece has at most kPieceElements of G, and of packed weights that many and more with the
+// rows, whose products lose by a cut (backward of 500 rows x 2048 x 128,256 bf16 in one piece
+// and two: 1024 and 1136 us; of 8 x 4096 x 128,256 in one and four: 1115 and 1044); or the least
+// number of tokens that keeps the products' tiles busy.
+HeadLayout head_layout(int rows, int hidden, int V, int dtype, InPlace here)
+{
+    HeadLayout l{};
+    const size_t elt = dtype == 1 ? 2 : 4;
+    l.here = here;
+    l.k = up64(hidden);
+    l.stage_k = 128 / (int)elt;
+    const int64_t r64 = up64(rows > 0 ? rows : 1);
+    const auto tokens = [](int64_t elements, int64_t least) {
+        const int64_t n = elements / 256 * 256;
+        return n < least ? least : n > kPieceTokens ? kPieceTokens : n;
+    };
+    int64_t piece = tokens(kPieceElements / r64, 4096);
+    if (!here.w) {
+        const int64_t packed = tokens((kPieceElements + rows * kPackedPerRow) / l.k, 8192);
+        piece = packed < piece ? packed : piece;
+    }
+    l.pieces = (int)((V + piece - 1) / piece);
+    // pieces of about the same size
+    piece = ((V + l.pieces - 1) / l.pieces + 255) / 256 * 256;
+    l.piece = (int)(piece < V ? piece : V);
+    l.pieces = (int)((V + l.piece - 1) / l.piece);
+    l.x = l.take(here.x ? 0 : r64 * l.k * elt);
+    l.w = l.take(here.w ? 0 : up64(l.piece) * l.k * elt);
+    return l;
+}
+
+struct ForwardLayout : HeadLayout {
+    int step;    // tokens of a launch: all, or a packed piece
+    int side;
+    int nparts;  // softmax states of a row
+    size_t parts, target_logit;
+};
+
+ForwardLayout forward_layout(int rows, int hidden, int V, int dtype, InPlace here)
+{
+    ForwardLayout l{head_layout(rows, hidden, V, dtype, here)};
+    l.step = here.w ? V : l.piece;
+    l.side = plan_product(l.step, rows, l.k / l.stage_k, 1, dtype == 1, 0, true).side;
+    const int tile_tokens = l.side == kNarrow ? 64 : l.side;
+    l.nparts = (V + tile_tokens - 1) / tile_tokens * 2;
+    l.parts = l.take((size_t)l.nparts * rows * sizeof(Softmax));
+    l.target_logit = l.take((size_t)rows * 4);
+    return l;
+}
+
+struct BackwardLayout : HeadLayout {
     Plan dx_plan;
-    size_t x, w, parts, target_logit;  // forward
-    size_t g, weight, dx, dw;          // backward
-    size_t forward_bytes, backward_bytes;
+    size_t g, weight, dx, dw;
 };
 
 Plan dw_plan(const HeadLayout &l, int rows, int64_t n, bool bf16)
@@ -460,74 +540,42 @@ Plan dw_plan(const HeadLayout &l, int rows, int64_t n, bool bf16)
     return plan_product(l.k, n, stages, 8, bf16, bf16 ? 2 : 4, false);
 }
 
-HeadLayout head_layout(int rows, int hidden, int V, int dtype)
+BackwardLayout backward_layout(int rows, int hidden, int V, int dtype, InPlace here)
 {
-    HeadLayout l{};
-    const size_t elt = dtype == 1 ? 2 : 4;
-    l.k = up64(hidden);
-    l.stage_k = 128 / (int)elt;
-    const int64_t r64 = up64(rows > 0 ? rows : 1);
-    int64_t piece = kPieceElements / r64 / 256 * 256;
-    piece = piece < 4096 ? 4096 : piece;
-    piece = piece > kPieceTokens ? kPieceTokens : piece;
-    l.pieces = (int)((V + piece - 1) / piece);
-    // pieces of about the same size
-    piece = ((V + l.pieces - 1) / l.pieces + 255) / 256 * 256;
-    l.piece = (int)(piece < V ? piece : V);
-    l.pieces = (int)((V + l.piece - 1) / l.piece);
-    const int64_t p64 = up64(l.piece);
-    size_t at = 0;
-    const auto take = [&](size_t bytes) {
-        const size_t here = at;
-        at += align_up(bytes, 256);
-        return here;
-    };
-    l.x = take(r64 * l.k * elt);
-    l.w = take(p64 * l.k * elt);
-    const size_t shared = at;
-    l.parts = take(((size_t)V / 32 + 8) * r64 * sizeof(Softmax));
-    l.target_logit = take((size_t)r64 * 4);
-    l.forward_bytes = at;
-    at = shared;
-    l.g = take(r64 * p64 * elt);
-    l.weight = take((size_t)r64 * 4);
+    BackwardLayout l{head_layout(rows, hidden, V, dtype, here)};
+    const int64_t r64 = up64(rows > 0 ? rows : 1), p64 = up64(l.piece);
+    l.g = l.take(r64 * p64 * (dtype == 1 ? 2 : 4));
+    l.weight = l.take((size_t)r64 * 4);
     // dx over a piece: few tiles and a long k
     l.dx_plan = plan_product(l.k, rows, p64 / l.stage_k, 16, dtype == 1, 4, true);
-    l.dx = take((size_t)l.dx_plan.splits * rows * hidden * 4);
+    l.dx = l.take((size_t)l.dx_plan.splits * rows * hidden * 4);
     // dw over a piece, and over the last one: split where hidden and tokens make few tiles
     const auto dw_sums = [&](int64_t n) {
         const Plan p = dw_plan(l, rows, n, dtype == 1);
         return p.splits > 1 ? (size_t)p.splits * n * hidden * 4 : 0;
     };
     const size_t whole = dw_sums(l.piece), last = dw_sums(V - (int64_t)(l.pieces - 1) * l.piece);
-    l.dw = take(whole > last ? whole : last);
-    l.backward_bytes = at;
+    l.dw = l.take(whole > last ? whole : last);
     return l;
 }
 
 // An operand as the products need it: in place, or packed into `buffer`.
-bool in_place(const void *p, int64_t ld, int dtype, int hidden)
-{
-    return hidden % 64 == 0 && ld % (dtype == 1 ? 8 : 4) == 0 && reinterpret_cast<uintptr_t>(p) % 16 == 0 &&
-           ld <= ((int64_t)1 << 20);
-}
-
-hipError_t operand(const void *p, int64_t ld, int dtype, int rows, int hidden, const HeadLayout &l, void *buffer,
+hipError_t operand(const void *p, int64_t ld, int dtype, int rows, int hidden, bool here, int64_t k, void *buffer,
                    GemmOperand &out, hipStream_t s)
 {
-    if (in_place(p, ld, dtype, hidden)) {
+    if (here) {
         out = {p, ld, rows, 0};
         return hipSuccess;
     }
-    out = {buffer, l.k, rows, 0};
-    const int64_t vecs = (int64_t)rows * (l.k / (dtype == 1 ? 8 : 4));
+    out = {buffer, k, rows, 0};
+    const int64_t vecs = (int64_t)rows * (k / (dtype == 1 ? 8 : 4));
     const int64_t blocks = (vecs + 255) / 256;
     const unsigned grid = (unsigned)(blocks < 8192 ? blocks : 8192);
     if (dtype == 1)
-        pack_kernel<uint16_t><<<grid, 256, 0, s>>>(static_cast<const uint16_t *>(p), ld, rows, hidden, (int)l.k,
+        pack_kernel<uint16_t><<<grid, 256, 0, s>>>(static_cast<const uint16_t *>(p), ld, rows, hidden, (int)k,
                                                    static_cast<uint16_t *>(buffer));
     else
-        pack_kernel<float><<<grid, 256, 0, s>>>(static_cast<const float *>(p), ld, rows, hidden, (int)l.k,
+        pack_kernel<float><<<grid, 256, 0, s>>>(static_cast<const float *>(p), ld, rows, hidden, (int)k,
                                                 static_cast<float *>(buffer));
     return last_launch();
 }
@@ -611,13 +659,13 @@ template <typename T>
 hipError_t backward(const HeadArgs &a, const float *lse, const float *grad_loss, T *grad_x, T *grad_weight, char *ws,
                     hipStream_t s)
 {
-    const HeadLayout l = head_layout(a.rows, a.hidden, a.V, a.dtype);
+    const BackwardLayout l = backward_layout(a.rows, a.hidden, a.V, a.dtype, in_place(a));
     const int rows_k = (a.rows + l.stage_k - 1) / l.stage_k * l.stage_k;
     float *weight = reinterpret_cast<float *>(ws + l.weight), *dx = reinterpret_cast<float *>(ws + l.dx);
     T *g_piece = reinterpret_cast<T *>(ws + l.g);
     constexpr bool kBf16 = sizeof(T) == 2;
     GemmOperand x;
-    DV_TRY(operand(a.x, a.ld_x, a.dtype, a.rows, a.hidden, l, ws + l.x, x, s));
+    DV_TRY(operand(a.x, a.ld_x, a.dtype, a.rows, a.hidden, l.here.x, l.k, ws + l.x, x, s));
     weights_kernel<<<(a.rows + 255) / 256, 256, 0, s>>>(a.rows, a.V, a.masks, a.targets, grad_loss, weight);
     DV_TRY(last_launch());
     int splits = 1;
@@ -626,7 +674,7 @@ hipError_t backward(const HeadArgs &a, const float *lse, const float *grad_loss,
         const int n = a.V - v0 < l.piece ? a.V - v0 : l.piece;
         const int64_t n64 = up64(n);
         GemmOperand w;
-        DV_TRY(operand(weight_rows(a, v0), a.ld_w, a.dtype, n, a.hidden, l, ws + l.w, w, s));
+        DV_TRY(operand(weight_rows(a, v0), a.ld_w, a.dtype, n, a.hidden, l.here.w, l.k, ws + l.w, w, s));
         const GemmShape logits{w, x, (int)l.k};
         const GemmOperand g{g_piece, n64, a.rows, 0};
         DV_TRY(with_tile<!kBf16>(plan_product(n, a.rows, l.k / l.stage_k, 1, kBf16, 0, true).side, [&](auto tile) {
@@ -676,35 +724,53 @@ hipError_t backward(const HeadArgs &a, const float *lse, const float *grad_loss,
 
 }  // namespace
 
+size_t head_workspace_bytes(const HeadArgs &a)
+{
+    return forward_layout(a.rows, a.hidden, a.V, a.dtype, in_place(a)).bytes;
+}
+
+size_t head_backward_workspace_bytes(const HeadArgs &a)
+{
+    return backward_layout(a.rows, a.hidden, a.V, a.dtype, in_place(a)).bytes;
+}
+
+// For operands of any stride and alignment.
 size_t head_workspace_bytes(int rows, int hidden, int V, int dtype)
 {
-    return head_layout(rows, hidden, V, dtype).forward_bytes;
+    size_t most = 0;
+    for (const InPlace here : {InPlace{false, false}, InPlace{false, true}}) {
+        const size_t n = forward_layout(rows, hidden, V, dtype, here).bytes;
+        most = n > most ? n : most;
+    }
+    return most;
 }
 
 size_t head_backward_workspace_bytes(int rows, int hidden, int V, int dtype)
 {
-    return head_layout(rows, hidden, V, dtype).backward_bytes;
+    size_t most = 0;
+    for (const InPlace here : {InPlace{false, false}, InPlace{false, true}}) {
+        const size_t n = backward_layout(rows, hidden, V, dtype, here).bytes;
+        most = n > most ? n : most;
+    }
+    return most;
 }
 
 hipError_t launch_head_loss(const HeadArgs &a, float *loss, float *lse, void *workspace, hipStream_t s)
 {
-    const HeadLayout l = head_layout(a.rows, a.hidden, a.V, a.dtype);
+    const ForwardLayout l = forward_layout(a.rows, a.hidden, a.V, a.dtype, in_place(a));
     char *ws = static_cast<char *>(workspace);
     Softmax *parts = reinterpret_cast<Softmax *>(ws + l.parts);
     float *target_logit = reinterpret_cast<float *>(ws + l.target_logit);
     GemmOperand x;
-    DV_TRY(operand(a.x, a.ld_x, a.dtype, a.rows, a.hidden, l, ws + l.x, x, s));
-    const bool whole = in_place(a.weight, a.ld_w, a.dtype, a.hidden);  // nothing to pack: one piece
-    const int step = whole ? a.V : l.piece;
-    const int side = plan_product(step, a.rows, l.k / l.stage_k, 1, a.dtype == 1, 0, true).side;
-    for (int v0 = 0; v0 < a.V; v0 += step) {
-        const int n = a.V - v0 < step ? a.V - v0 : step;
+    DV_TRY(operand(a.x, a.ld_x, a.dtype, a.rows, a.hidden, l.here.x, l.k, ws + l.x, x, s));
+    for (int v0 = 0; v0 < a.V; v0 += l.step) {
+        const int n = a.V - v0 < l.step ? a.V - v0 : l.step;
         GemmOperand w;
-        DV_TRY(operand(weight_rows(a, v0), a.ld_w, a.dtype, n, a.hidden, l, ws + l.w, w, s));
+        DV_TRY(operand(weight_rows(a, v0), a.ld_w, a.dtype, n, a.hidden, l.here.w, l.k, ws + l.w, w, s));
         const GemmShape g{w, x, (int)l.k};
         const auto run = [&](auto zero) {
             using E = decltype(zero);
-            return with_tile<sizeof(E) == 4>(side, [&](auto tile) {
+            return with_tile<sizeof(E) == 4>(l.side, [&](auto tile) {
                 using X = decltype(tile);
                 const int ti = (n + X::kM - 1) / X::kM, tj = (a.rows + X::kN - 1) / X::kN;
                 stats_kernel<E, X::kM, X::kN, 2, X::kWn><<<ti * tj, X::kThreads, 0, s>>>(
@@ -713,14 +779,12 @@ hipError_t launch_head_loss(const HeadArgs &a, float *loss, float *lse, void *wo
         };
         DV_TRY(a.dtype == 1 ? run((__bf16)0.f) : run(0.f));
     }
-    const int tile_tokens = side == kNarrow ? 64 : side;
-    const int nparts = (a.V + tile_tokens - 1) / tile_tokens * 2;
     // a thread's share of the parts: about 16, more of them only for many rows
     int slices = 16;
-    while (slices < (a.rows < 64 ? 256 : 64) && slices * 16 < nparts)
+    while (slices < (a.rows < 64 ? 256 : 64) && slices * 16 < l.nparts)
         slices *= 2;
     const int per_block = 256 / slices;
-    finish_kernel<<<(a.rows + per_block - 1) / per_block, 256, 0, s>>>(parts, nparts, a.rows, a.V, a.masks, a.targets,
+    finish_kernel<<<(a.rows + per_block - 1) / per_block, 256, 0, s>>>(parts, l.nparts, a.rows, a.V, a.masks, a.targets,
                                                                       target_logit, loss, lse, slices);
     return last_launch();
 }

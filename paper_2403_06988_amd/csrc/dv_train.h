@@ -144,8 +144,11 @@ struct HeadArgs {
     const int32_t *targets;
     Masks masks;
 };
+// For a call's own operands (x, weight, their strides, type and sizes), and for any operands.
+size_t head_workspace_bytes(const HeadArgs &a);
 size_t head_workspace_bytes(int rows, int hidden, int V, int dtype);
 hipError_t launch_head_loss(const HeadArgs &a, float *loss, float *lse, void *workspace, hipStream_t stream);
+size_t head_backward_workspace_bytes(const HeadArgs &a);
 size_t head_backward_workspace_bytes(int rows, int hidden, int V, int dtype);
 hipError_t launch_head_loss_backward(const HeadArgs &a, const float *lse, const float *grad_loss, void *grad_x,
                                      void *grad_weight, void *workspace, hipStream_t stream);

@@ -261,3 +261,35 @@ def test_refusals(dv):
             bad()
     with pytest.raises(dv.DvError):  # an output over an input
         dv.head_loss_backward(x, w, t, torch.zeros(4, device=DEV), torch.zeros(4, device=DEV), grad_x=x)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_few_rows_beside_a_large_table_take_little_memory(dv, dtype):
+    """Operands in place: no room for a copy of them; in a wider buffer: a piece's."""
+    N, D, V = 2, 1024, 200000
+    wide = torch.empty((V, D + 1), dtype=dtype, device=DEV).normal_()
+    table = wide[:, :D].contiguous()
+    x = torch.randn((N, D), device=DEV).to(dtype)
+    t = torch.tensor([0, V - 1], dtype=torch.int32, device=DEV)
+    gl = torch.ones(N, device=DEV)
+    gx, gw = torch.empty_like(x), torch.empty_like(table)
+
+    def most(w):
+        torch.cuda.synchronize()
+        torch.cuda.empty_cache()
+        torch.cuda.reset_peak_memory_stats()
+        before = torch.cuda.memory_allocated()
+        loss, lse = dv.head_loss(x, w, t)
+        dv.head_loss_backward(x, w, t, lse, gl, grad_x=gx, grad_weight=gw)
+        torch.cuda.synchronize()
+        return torch.cuda.max_memory_allocated() - before, loss, lse, gx.clone(), gw.clone()
+
+    aligned, packed = most(table), most(wide[:, :D])
+    g = 64 * (V + 64) * table.element_size()  # a piece of G for 64 rows
+    assert aligned[0] < g + (8 << 20)
+    assert packed[0] < g + (8 << 20) + ((1 << 27) + (N << 19)) * table.element_size()
+    assert dv.head_loss_workspace_bytes_for(x, table) < dv.head_loss_workspace_bytes_for(x, wide[:, :D])
+    assert dv.head_loss_workspace_bytes_for(x, wide[:, :D]) <= dv.head_loss_workspace_bytes(N, D, V, dtype)
+    assert dv.head_loss_backward_workspace_bytes_for(x, table) < dv.head_loss_backward_workspace_bytes(N, D, V, dtype)
+    for a, b in zip(aligned[1:3], packed[1:3]):
+        assert torch.equal(a, b)  # the same tiles' sums

@@ -173,3 +173,37 @@ def test_inverse_temperature_whose_exponent_is_not_finite(call):
     assert call(c=2.4e38) == call(c=3.0e38) == call(c=3.4e38) == SHAPE
     assert b"inv_temperature" in lib.dv_last_error()
     assert call(c=2.3e38, ws=None) == WORKSPACE  # passes; the next check does not
+
+
+def test_head_workspaces_hold_no_copy_that_is_not_made():
+    """A call's own query: nothing for operands that are used where they lie.  Any
+    operands' query: at most 2^27 elements of packed weights, and 2^19 a row."""
+    MB = 1 << 20
+    for dt, elt in ((1, 2), (0, 4)):
+        for rows in (1, 8, 64):
+            for D, V in ((4096, 128256), (4096, 256000), (1024, 1000000)):
+                at = lambda q, x=P, ld_x=D, w=P + 64 * GB, ld_w=D: q(x, ld_x, w, ld_w, dt, rows, D, V)  # noqa: E731
+                copies = ((1 << 27) + (rows << 19)) * elt + 64 * D * elt
+                states, g = (V // 32 + 8) * rows * 8 + MB, min(V + 64, 1 << 18) * 64 * elt + 64 * D * 16 * 4 + MB
+                own, back = lib.dv_head_loss_workspace_bytes_for, lib.dv_head_loss_backward_workspace_bytes_for
+                assert 0 < at(own) <= states and 0 < at(back) <= g
+                assert at(own, w=P + 64 * GB + 16) == at(own)
+                for kw in (dict(w=P + 64 * GB + 2 * elt), dict(ld_w=D + 1), dict(x=P + elt), dict(ld_x=D + 1), dict(ld_w=(1 << 20) + 64)):
+                    assert at(own) < at(own, **kw) <= states + copies, kw
+                    assert at(back) < at(back, **kw) <= g + copies, kw
+                    assert at(own, **kw) <= lib.dv_head_loss_workspace_bytes(rows, D, V, dt) <= states + copies
+                    assert at(back, **kw) <= lib.dv_head_loss_backward_workspace_bytes(rows, D, V, dt) <= g + copies
+    # the states of 128-token tiles, not of 32-token ones
+    assert own(P, 4096, P + 64 * GB, 4096, 1, 8192, 4096, 256000) < 8192 * (256000 // 128 + 2) * 8 + MB
+    for bad in ((-1, 64, 100), (8, 0, 100), (8, 64, 0), (8, 70000, 100)):
+        assert own(P, 1 << 17, P, 1 << 17, 1, *bad) == back(P, 1 << 17, P, 1 << 17, 1, *bad) == 0
+
+
+def test_a_workspace_of_the_calls_own_size_is_taken():
+    """Aligned operands pass with their own size; the same size with a stride that needs copies does not."""
+    need = lib.dv_head_loss_workspace_bytes_for(P, 64, P + GB, 64, 1, 8, 64, 1000)
+    assert head(nb=need - 1) == WORKSPACE and head(nb=need, loss=P + 16) == ALIAS
+    assert head(nb=need, ldw=65) == head(nb=need, x=P + 2) == WORKSPACE
+    need = lib.dv_head_loss_backward_workspace_bytes_for(P, 64, P + GB, 64, 1, 8, 64, 1000)
+    assert head_back(nb=need - 1) == WORKSPACE and head_back(nb=need, gx=P) == ALIAS
+    assert head_back(nb=need, ldw=65) == head_back(nb=need, x=P + 2) == WORKSPACE
