@@ -93,6 +93,24 @@ DVPROBE_API int32_t dvprobe_step_floor(int32_t mode, const void *logits, int32_t
 DVPROBE_API int32_t dvprobe_step_shape(int32_t batch, int32_t num_tokens, int32_t dtype, int32_t *chunk_vectors,
                                        int32_t *chunks, int32_t *lanes);
 
+/* How dv_head_loss and its backward pass cut their work (host only, no HIP
+ * call): `loss_tokens` of the vocabulary a launch of the loss, in tiles of
+ * `loss_side`; the backward pass `pieces` of `piece_tokens`, the last one of
+ * `last_piece_tokens`, with each product's tile side (32: 64 tokens x 32 rows) and the
+ * number of parts that its sum is split into.  Pairs: of a whole piece and of the last. */
+struct dvprobe_head_plan {
+    int32_t loss_tokens, loss_side;
+    int32_t pieces, piece_tokens, last_piece_tokens;
+    int32_t logits_side[2];
+    int32_t grad_x_side, grad_x_splits;
+    int32_t grad_weight_side[2], grad_weight_splits[2];
+};
+
+/* x_in_place, weight_in_place: whether the operand is multiplied where it lies
+ * (dv_head_loss_workspace_bytes).  Returns 0, or 1 for a bad argument. */
+DVPROBE_API int32_t dvprobe_head_plan(int32_t rows, int32_t hidden, int32_t num_tokens, int32_t dtype,
+                                      int32_t x_in_place, int32_t weight_in_place, struct dvprobe_head_plan *plan);
+
 #ifdef __cplusplus
 }
 #endif

@@ -5,6 +5,7 @@
 // rates next to what the same memory path reaches on its own.  Measurement
 // code: not part of libdv.so.
 #include "../../include/dv_probes.h"
+#include "dv_head_plan.h"
 #include "dv_internal.h"
 
 namespace dv {
@@ -420,6 +421,33 @@ int32_t dvprobe_step_shape(int32_t batch, int32_t num_tokens, int32_t dtype, int
     *chunk_vectors = g.chunk_vec;
     *chunks = g.nchunks;
     *lanes = g.threads;
+    return 0;
+}
+
+int32_t dvprobe_head_plan(int32_t rows, int32_t hidden, int32_t num_tokens, int32_t dtype, int32_t x_in_place,
+                          int32_t weight_in_place, struct dvprobe_head_plan *plan)
+{
+    if (!plan || rows < 1 || hidden < 1 || num_tokens < 1 || (dtype != 0 && dtype != 1))
+        return 1;
+    const dv::InPlace here{x_in_place != 0, weight_in_place != 0};
+    const bool bf16 = dtype == 1;
+    const dv::ForwardLayout f = dv::forward_layout(rows, hidden, num_tokens, dtype, here);
+    const dv::BackwardLayout b = dv::backward_layout(rows, hidden, num_tokens, dtype, here);
+    const int32_t last = num_tokens - (b.pieces - 1) * b.piece;
+    const dv::Plan dw = dv::dw_plan(b, rows, b.piece, bf16), dw_last = dv::dw_plan(b, rows, last, bf16);
+    plan->loss_tokens = f.step;
+    plan->loss_side = f.side;
+    plan->pieces = b.pieces;
+    plan->piece_tokens = b.piece;
+    plan->last_piece_tokens = last;
+    plan->logits_side[0] = dv::logits_side(b, rows, b.piece, bf16);
+    plan->logits_side[1] = dv::logits_side(b, rows, last, bf16);
+    plan->grad_x_side = b.dx_plan.side;
+    plan->grad_x_splits = b.dx_plan.splits;
+    plan->grad_weight_side[0] = dw.side;
+    plan->grad_weight_side[1] = dw_last.side;
+    plan->grad_weight_splits[0] = dw.splits;
+    plan->grad_weight_splits[1] = dw_last.splits;
     return 0;
 }
 

@@ -1,7 +1,9 @@
 """dv_head_loss and its backward pass against their 64-bit forms, element by
 element within derived bounds; gradients also against differences of the
 loss; edges of masks, targets, strides and sizes; refusals."""
+import ctypes
 import math
+import os
 
 import numpy as np
 import pytest
@@ -11,6 +13,7 @@ from tests.train_common import check, head_reference, masks, pack_mask, row_mask
 
 pytestmark = pytest.mark.gpu
 DEV = torch.device("cuda:0")
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
 @pytest.fixture(scope="module")
@@ -293,3 +296,121 @@ def test_few_rows_beside_a_large_table_take_little_memory(dv, dtype):
     assert dv.head_loss_backward_workspace_bytes_for(x, table) < dv.head_loss_backward_workspace_bytes(N, D, V, dtype)
     for a, b in zip(aligned[1:3], packed[1:3]):
         assert torch.equal(a, b)  # the same tiles' sums
+
+
+# ------------------------------------------------ every tile, split and piece
+
+class Plan(ctypes.Structure):
+    """struct dvprobe_head_plan"""
+    _fields_ = [(n, ctypes.c_int32) for n in ("loss_tokens", "loss_side", "pieces", "piece_tokens", "last_piece_tokens")] + [
+        ("logits_side", ctypes.c_int32 * 2), ("grad_x_side", ctypes.c_int32), ("grad_x_splits", ctypes.c_int32),
+        ("grad_weight_side", ctypes.c_int32 * 2), ("grad_weight_splits", ctypes.c_int32 * 2)]
+
+
+def plan_of(N, D, V, dtype, in_place):
+    lib = ctypes.CDLL(os.path.join(ROOT, "paper_2403_06988_amd", "libdv_probes.so"))
+    p = Plan()
+    assert lib.dvprobe_head_plan(N, D, V, 1 if dtype == torch.bfloat16 else 0, in_place, in_place, ctypes.byref(p)) == 0
+    return p
+
+
+def make_on_device(seed, N, D, V, dtype, few, pad):
+    """Masks from nothing over `few` tokens in a thousand to everything, dead rows, padding.
+    Most rows' losses have no weight, and many rows few allowed tokens: a misplaced
+    row or token then is no small part of the sums that it misses or spoils."""
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    x = on_device(torch.randn((N, D), generator=g, device=DEV).to(dtype), pad)
+    w = on_device((torch.randn((V, D), generator=g, device=DEV) * (3.0 / math.sqrt(D))).to(dtype), pad)
+    shares = torch.tensor([0.0, few / 1000, few / 1000, 0.3, 1.0], device=DEV)
+    may = torch.rand((5, V), generator=g, device=DEV) < shares[:, None]
+    states = torch.randint(-1, 6, (N,), generator=g, device=DEV, dtype=torch.int32)
+    states[-1] = 1
+    alive = (states >= 0) & (states < 5)
+    mask = may[states.clamp(0, 4).long()] & alive[:, None]
+    score = torch.rand((N, V), generator=g, device=DEV).masked_fill_(~mask, -1.0)
+    t = score.argmax(1).int()  # an allowed token of each row that has one
+    del score
+    at = torch.arange(N, device=DEV)
+    t[at % 11 == 3] = torch.tensor([-1, V, -2147483648], dtype=torch.int32, device=DEV)[at[at % 11 == 3] % 3]
+    gl = torch.randn(N, generator=g, device=DEV)
+    gl[(at % 29 != 0) & (at < N - 3)] = 0
+    return x, w, t, may, states, mask, gl
+
+
+def check_on_device(dv, x, w, t, may, states, mask, gl):
+    kw = dict(allow=pack_mask(may.cpu()).to(DEV), states=states)
+    loss, lse = dv.head_loss(x, w, t, **kw)
+    gx, gw = dv.head_loss_backward(x, w, t, lse, gl, **kw)
+    with torch.device(DEV):
+        ref = {k: v.cpu() for k, v in head_reference(x, w, t, mask, gl).items()}
+    check(lse, ref["lse"], ref["lse_tol"], "lse")
+    check(loss, ref["loss"], ref["loss_tol"], "loss")
+    check(gx, ref["grad_x"], ref["grad_x_tol"], "grad_x")
+    check(gw, ref["grad_weight"], ref["grad_weight_tol"], "grad_weight")
+
+
+BF, F = torch.bfloat16, torch.float32
+# rows, hidden, tokens, row stride beyond hidden; then what the case is there for: the side of
+# grad_x's tiles, whether its sum is split, several pieces; the same of grad_weight's
+PLANS = [
+    (BF, 2100, 2001, 501, 0, (128, False, False), (64, False)), (BF, 4000, 99, 17003, 0, (128, True, False), (128, True)),
+    (BF, 20000, 250, 9001, 0, (128, False, True), (128, True)), (BF, 2100, 2001, 9001, 0, (256, True, False), (128, False)),
+    (BF, 2100, 2048, 9001, 0, (256, True, False), (128, False)), (BF, 9000, 1499, 2003, 0, (256, False, False), (128, True)),
+    (BF, 9000, 501, 17001, 0, (256, True, True), (256, True)), (BF, 9000, 1499, 17001, 0, (256, False, True), (256, False)),
+    (BF, 9000, 1536, 17001, 0, (256, False, True), (256, False)), (BF, 300, 250, 50257, 3, (64, True, False), (256, False)),
+    (BF, 6000, 99, 9001, 0, (64, True, False), (128, True)), (BF, 40, 99, 33001, 0, (64, True, False), (128, False)),
+    (F, 2100, 2001, 501, 0, (128, False, False), (64, True)), (F, 9000, 99, 2003, 0, (128, True, False), (64, True)),
+    (F, 2100, 4001, 501, 0, (256, False, False), (128, True)), (F, 700, 4001, 2003, 0, (256, True, False), (128, False)),
+    (F, 700, 4096, 2003, 0, (256, True, False), (128, False)), (F, 9000, 249, 17001, 0, (256, True, True), (256, True)),
+    (F, 9000, 1499, 17001, 0, (256, False, True), (256, True)), (F, 9000, 1536, 17001, 0, (256, False, True), (256, True)),
+    (F, 40, 250, 33001, 3, (64, True, False), (256, False)), (F, 1100, 250, 17001, 0, (128, True, False), (256, True)),
+    (F, 1500, 99, 9001, 0, (64, True, False), (128, True)), (F, 40, 99, 33001, 0, (64, True, False), (128, False)),
+]
+
+
+@pytest.mark.parametrize("dtype,N,D,V,pad,grad_x,grad_weight", PLANS)
+def test_every_tile_and_split_of_the_gradients(dv, dtype, N, D, V, pad, grad_x, grad_weight):
+    print(f"head plan N={N} D={D} V={V} {dtype}", flush=True)
+    p = plan_of(N, D, V, dtype, D % 64 == 0 and pad == 0)
+    assert (p.grad_x_side, p.grad_x_splits > 1, p.pieces > 1) == grad_x
+    assert (p.grad_weight_side[0], p.grad_weight_splits[0] > 1) == grad_weight
+    check_on_device(dv, *make_on_device(N + D, N, D, V, dtype, 3, pad))
+
+
+@pytest.mark.parametrize("dtype,N,D,V,pad", [
+    (BF, 9, 65, 262501, 0), (F, 9, 65, 262501, 0),        # pieces of 2^18 tokens at most
+    (BF, 9, 4100, 70001, 0), (F, 9, 4096, 70001, 1),      # of 2^27 packed elements
+    (BF, 4200, 33, 33003, 0), (F, 4200, 64, 33003, 3),    # of 2^27 logits
+])
+def test_several_packed_pieces(dv, dtype, N, D, V, pad):
+    """Weights that are copied a piece at a time, in the loss too: each piece's
+    place among masks, targets and partial results."""
+    print(f"head packed pieces N={N} D={D} V={V} {dtype}", flush=True)
+    p = plan_of(N, D, V, dtype, False)
+    assert p.pieces > 1 and p.loss_tokens == p.piece_tokens and p.last_piece_tokens < p.piece_tokens
+    x, w, t, may, states, mask, gl = make_on_device(D, N, D, V, dtype, 3, pad)
+    # targets on both sides of each piece's end, and at the vocabulary's ends
+    ends = [0, V - 1] + [v for i in range(1, p.pieces) for v in (i * p.piece_tokens - 1, i * p.piece_tokens)]
+    assert len(ends) < N
+    may[1:, ends] = True
+    states[:len(ends)] = torch.arange(len(ends), dtype=torch.int32, device=DEV) % 4 + 1
+    t[:len(ends)] = torch.tensor(ends, dtype=torch.int32, device=DEV)
+    states[-2], states[-1] = 0, -1
+    gl[:len(ends)] = 1.0
+    mask = may[states.clamp(0, 4).long()] & ((states >= 0) & (states < 5))[:, None]
+    check_on_device(dv, x, w, t, may, states, mask, gl)
+
+
+def test_plans_of_the_measured_range():
+    """The query itself: sides and pieces as the kernels have them, refusals."""
+    for dtype in (BF, F):
+        for N, D, V in ((1, 1024, 32000), (8192, 4096, 128256), (1999, 1000, 32003), (1 << 20, 64, 5000)):
+            p = plan_of(N, D, V, dtype, False)
+            assert p.loss_side in (32, 64, 128, 256) and p.grad_x_side in (32, 64, 128, 256)
+            assert set(p.grad_weight_side) | set(p.logits_side) <= {32, 64, 128, 256}
+            assert (p.pieces - 1) * p.piece_tokens + p.last_piece_tokens == V and 0 < p.last_piece_tokens <= p.piece_tokens
+            assert plan_of(N, D, V, dtype, True).loss_tokens == V
+    lib = ctypes.CDLL(os.path.join(ROOT, "paper_2403_06988_amd", "libdv_probes.so"))
+    assert lib.dvprobe_head_plan(0, 8, 8, 1, 1, 1, ctypes.byref(Plan())) == 1
+    assert lib.dvprobe_head_plan(8, 8, 8, 2, 1, 1, ctypes.byref(Plan())) == 1
+    assert lib.dvprobe_head_plan(8, 8, 8, 1, 1, 1, None) == 1
