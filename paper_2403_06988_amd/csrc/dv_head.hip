@@ -343,30 +343,30 @@ __global__ __launch_bounds__(WM *WN *kWave, 2) void product_kernel(GemmShape g, 
     }
 }
 
-// The sum of the splits' parts, n elements each (a lane four of them), in T.
+// The sum of the splits' parts, n elements each (a lane four of them at a time), in T.
 template <typename T>
 __global__ __launch_bounds__(256) void join_splits_kernel(const float *parts, int splits, int64_t n, T *out)
 {
-    const int64_t i = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) * 4;
-    if (i >= n)
-        return;
-    const int left = (int)(n - i < 4 ? n - i : 4);
-    f32x4 s = {};
-    for (int k = 0; k < splits; ++k) {
-        f32x4 x = {};
+    const int64_t first = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) * 4;
+    for (int64_t i = first; i < n; i += (int64_t)gridDim.x * blockDim.x * 4) {
+        const int left = (int)(n - i < 4 ? n - i : 4);
+        f32x4 s = {};
+        for (int k = 0; k < splits; ++k) {
+            f32x4 x = {};
+            if (left == 4)
+                x = __builtin_bit_cast(f32x4, load_words(parts + k * n + i));
+            else
+                for (int e = 0; e < left; ++e)
+                    x[e] = parts[k * n + i + e];
+            s += x;
+        }
+        const T y[4] = {(T)s[0], (T)s[1], (T)s[2], (T)s[3]};
         if (left == 4)
-            x = __builtin_bit_cast(f32x4, load_words(parts + k * n + i));
+            __builtin_memcpy(out + i, y, sizeof y);
         else
             for (int e = 0; e < left; ++e)
-                x[e] = parts[k * n + i + e];
-        s += x;
+                out[i + e] = y[e];
     }
-    const T y[4] = {(T)s[0], (T)s[1], (T)s[2], (T)s[3]};
-    if (left == 4)
-        __builtin_memcpy(out + i, y, sizeof y);
-    else
-        for (int e = 0; e < left; ++e)
-            out[i + e] = y[e];
 }
 
 template <typename T>
@@ -465,7 +465,8 @@ hipError_t zero(T *p, int64_t n, hipStream_t s)
 template <typename T>
 hipError_t join_splits(const float *parts, int splits, int64_t n, T *out, hipStream_t s)
 {
-    join_splits_kernel<T><<<(unsigned)((n + 1023) / 1024), 256, 0, s>>>(parts, splits, n, out);
+    const int64_t blocks = (n + 1023) / 1024, most = (int64_t)1 << 23;  // a grid has fewer than 2^32 threads
+    join_splits_kernel<T><<<(unsigned)(blocks < most ? blocks : most), 256, 0, s>>>(parts, splits, n, out);
     return last_launch();
 }
 

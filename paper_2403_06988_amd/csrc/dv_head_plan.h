@@ -144,8 +144,16 @@ inline int logits_side(const HeadLayout &l, int rows, int64_t n, bool bf16)
     return plan_product(n, rows, l.k / l.stage_k, 1, bf16, 0, true).side;
 }
 
+// Tokens of one launch of the loss at most: tiles of any side, 512 threads each, stay below
+// the 2^32 threads of a grid.
+inline int64_t launch_tokens(int rows)
+{
+    constexpr int64_t kMostTiles = (int64_t)1 << 22;
+    return kMostTiles / (((int64_t)rows + 63) / 64) * 64 / 256 * 256;
+}
+
 struct ForwardLayout : HeadLayout {
-    int step;    // tokens of a launch: all, or a packed piece
+    int step;    // tokens of a launch
     int side;
     int nparts;  // softmax states of a row
     size_t parts, target_logit;
@@ -155,6 +163,8 @@ inline ForwardLayout forward_layout(int rows, int hidden, int V, int dtype, InPl
 {
     ForwardLayout l{head_layout(rows, hidden, V, dtype, here)};
     l.step = here.w ? V : l.piece;
+    if (rows > 0 && l.step > launch_tokens(rows))
+        l.step = (int)launch_tokens(rows);
     l.side = logits_side(l, rows, l.step, dtype == 1);
     const int tile_tokens = l.side == kNarrow ? 64 : l.side;
     l.nparts = (V + tile_tokens - 1) / tile_tokens * 2;

@@ -174,3 +174,25 @@ def test_a_step_on_another_stream(dv):
     side.synchronize()
     for k, v in out.items():
         assert torch.equal(v, want[k]), k
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_head_loss_in_several_launches(dv, dtype):
+    """More tiles than one grid is given: the vocabulary in several launches, the weights in place."""
+    N, D, V = 290001, 64, 70001
+    from tests.test_gpu_head_loss import plan_of
+    step = plan_of(N, D, V, dtype, True).loss_tokens
+    assert step < V
+    print(f"head N={N} D={D} V={V} {dtype} in launches of {step}", flush=True)
+    g = gen(6)
+    w = (torch.randn((V, D), generator=g, device=DEV) * 0.4).to(dtype)
+    x = torch.randn((N, D), generator=g, device=DEV).to(dtype)
+    t = torch.randint(0, V, (N,), generator=g, device=DEV, dtype=torch.int32)
+    pick = torch.arange(0, N, 1999, device=DEV)
+    pick[-1] = N - 1
+    t[pick[:4]] = torch.tensor([0, step - 1, step, V - 1], dtype=torch.int32, device=DEV)
+    loss, lse = dv.head_loss(x, w, t)
+    with torch.device(DEV):
+        ref = head_reference(x[pick], w, t[pick], torch.ones((len(pick), V), dtype=torch.bool))
+    for got, name in ((loss, "loss"), (lse, "lse")):
+        check(got[pick], ref[name].cpu(), ref[name + "_tol"].cpu(), name)

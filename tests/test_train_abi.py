@@ -207,3 +207,26 @@ def test_a_workspace_of_the_calls_own_size_is_taken():
     need = lib.dv_head_loss_backward_workspace_bytes_for(P, 64, P + GB, 64, 1, 8, 64, 1000)
     assert head_back(nb=need - 1) == WORKSPACE and head_back(nb=need, gx=P) == ALIAS
     assert head_back(nb=need, ldw=65) == head_back(nb=need, x=P + 2) == WORKSPACE
+
+
+def test_head_launches_stay_within_the_grid():
+    """A launch has fewer than 2^32 threads, whatever the limits allow."""
+    from tests.test_gpu_head_loss import plan_of
+    import torch
+    threads = {256: 512, 128: 256, 64: 256, 32: 128}
+
+    def launch(i, j, side):
+        other = 64 if side == 32 else side
+        return -(-i // other) * -(-j // side) * threads[side]
+
+    for dtype in (torch.bfloat16, torch.float32):
+        for N in (1, 33, 8192, 100000, 300000, 1 << 20):
+            for V in (1, 1000, 128256, 600000, 5000000, 1 << 24):
+                for D in (1, 64, 4096, 65536):
+                    for here in (False, True):
+                        p = plan_of(N, D, V, dtype, here)
+                        assert p.loss_tokens == V or p.loss_tokens % 256 == 0
+                        k = (D + 63) // 64 * 64
+                        for n in (launch(p.loss_tokens, N, p.loss_side), launch(p.piece_tokens, N, p.logits_side[0]),
+                                  launch(k, N, p.grad_x_side), launch(k, p.piece_tokens, p.grad_weight_side[0])):
+                            assert n < 1 << 32, (N, V, D, here)
