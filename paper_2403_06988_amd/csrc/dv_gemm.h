@@ -269,8 +269,8 @@ struct Gemm {
     // 16 bytes a lane from base + offset to LDS, lane after lane from `dst` on.
     // In assembly, because the compiler takes any later transposing read for a
     // read of what is on its way and waits for it; it writes no register, and
-    // the waits and the barrier of `run` order it.  (m0 is never held over a
-    // statement: the compiler sets it where it needs it.)
+    // the waits and the barrier of `run` order it.  m0, which it sets, is named as
+    // written: the compiler keeps nothing there across it.
     static __device__ __forceinline__ void load_to_lds(const char *base, int offset, uint32_t dst)
     {
         typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
@@ -279,7 +279,7 @@ struct Gemm {
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
                      :
                      : "s"(dst), "v"(offset), "s"(rsrc)
-                     : "memory");
+                     : "memory", "m0");
     }
 
     // Tiles of few fragments have registers to spare and are those of few rows, whose
