@@ -468,7 +468,10 @@ DV_API size_t dv_head_loss_workspace_bytes_for(const void *x, int64_t ld_x, cons
  *
  * x [rows][ld_x], weight [V][ld_weight] of `dtype`; targets [rows] int32.
  * fp32 operands are multiplied as sums of three bf16 parts each: the products
- * of parts below 2^-22 of the whole are left out.
+ * of parts below 2^-22 of the whole are left out.  They must be finite and at
+ * most 2^127 (1.7e38) in magnitude: an fp32 element beyond, infinities among
+ * them, makes NaN of its row's logits (of x) or its token's (of weight), and of
+ * no other.  bf16 operands take infinities as they are.
  * loss, lse [rows] fp32.
  * rows = 0 is valid and enqueues nothing.
  * Errors: DV_ERR_INVALID_ARG (NULL, misaligned elements, or only one of allow

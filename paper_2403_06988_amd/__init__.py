@@ -570,7 +570,8 @@ def _head_args(x, weight, targets, allow, states):
 def head_loss(x, weight, targets, allow=None, states=None, loss=None, lse=None, workspace=None, stream=None):
     """Softmax cross entropy over the allowed tokens, from hidden states
     x [N][D] and head weights weight [V][D] (bf16 or fp32, any row stride),
-    without keeping the logits.
+    without keeping the logits.  An fp32 element that is infinite or beyond 2^127
+    makes NaN of its own row's or token's logits.
 
     targets [N] int32; a row whose target is outside [0, V) or not allowed
     takes no part (loss 0).  allow [S][ceil(V/32)] int32 (as from ``align``)

@@ -414,3 +414,30 @@ def test_plans_of_the_measured_range():
     assert lib.dvprobe_head_plan(0, 8, 8, 1, 1, 1, ctypes.byref(Plan())) == 1
     assert lib.dvprobe_head_plan(8, 8, 8, 2, 1, 1, ctypes.byref(Plan())) == 1
     assert lib.dvprobe_head_plan(8, 8, 8, 1, 1, 1, None) == 1
+
+
+@pytest.mark.parametrize("value", [math.inf, -math.inf, 3.4e38])
+@pytest.mark.parametrize("N", [40, 1200])
+def test_fp32_elements_beyond_the_range_stay_in_their_row(dv, value, N):
+    """Infinite or nearly so: NaN for the row (or the rows that allow the token), and not a bit elsewhere."""
+    D, V = 100, 700
+    x, w, t, may, states, mask, g = make(71, N, D, V, F, 3, shares=(0.5, 1.0, 0.3))
+    kw = dict(allow=pack_mask(may).to(DEV), states=states.to(DEV))
+    t = t.to(DEV)
+    clean = dv.head_loss(x.to(DEV), w.to(DEV), t, **kw)
+    bad = x.clone()
+    at = int(torch.nonzero((clean[0].cpu() != 0))[3, 0])
+    bad[at, 17] = value
+    got = dv.head_loss(bad.to(DEV), w.to(DEV), t, **kw)
+    rest = torch.arange(N, device=DEV) != at
+    for a, b in zip(got, clean):
+        assert bool(torch.isnan(a[at])) and torch.equal(a[rest], b[rest])
+    v = int(torch.nonzero(~may[0] & ~may[2])[0, 0])
+    bad = w.clone()
+    bad[v, 99] = value
+    got = dv.head_loss(x.to(DEV), bad.to(DEV), t, **kw)
+    sees = mask[:, v].to(DEV)
+    assert sees.any() and not sees.all()
+    assert bool(torch.isnan(got[1][sees]).all())
+    for a, b in zip(got, clean):
+        assert torch.equal(a[~sees], b[~sees])
