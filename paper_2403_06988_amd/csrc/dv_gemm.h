@@ -276,10 +276,13 @@ struct Gemm {
         typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
         const uint64_t p = reinterpret_cast<uint64_t>(base);
         const u32x4 rsrc = {(uint32_t)p, (uint32_t)(p >> 32) & 0xFFFFu, 0x7FFFFFFFu, 0x00027000u};
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"  // m0 is reserved: not preserved, as meant
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
                      :
                      : "s"(dst), "v"(offset), "s"(rsrc)
                      : "memory", "m0");
+#pragma clang diagnostic pop
     }
 
     // Tiles of few fragments have registers to spare and are those of few rows, whose
