@@ -486,8 +486,8 @@ DV_API dv_status dv_head_loss(const void *x, int64_t ld_x, const void *weight, i
 /*
  * dv_head_loss_backward_workspace_bytes -- device workspace of
  * dv_head_loss_backward, for operands of any stride and alignment: what
- * dv_head_loss copies, G of a piece of the vocabulary (2^27 elements, or 4,096
- * tokens if those are more) and the gradients' partial sums.  Returns 0 when an
+ * dv_head_loss copies, G of a piece of the vocabulary (2^27 elements of 4 bytes, or
+ * 4,096 tokens if those are more) and the gradients' partial sums.  Returns 0 when an
  * argument is outside its limit.  dv_head_loss_backward_workspace_bytes_for: of
  * a call with these operands.
  */
@@ -506,8 +506,8 @@ DV_API size_t dv_head_loss_backward_workspace_bytes_for(const void *x, int64_t l
  * both contiguous, of `dtype`; either may be NULL and is then not computed.
  * lse [rows] fp32 as dv_head_loss wrote it for the same inputs; grad_loss
  * [rows] fp32.  The logits are computed again a piece at a time.  For bf16
- * inputs G is rounded to bf16 on its way into the two products (a relative
- * error of 2^-8 of each term, of the size of the outputs' own rounding).
+ * inputs G goes into the two products as the sum of two bf16 parts (a relative
+ * error below 2^-16 of each term): what the outputs lose is their own rounding.
  * x and weight must be finite.
  * rows = 0 is valid: grad_weight is filled with zeros.
  * Errors as dv_head_loss.

@@ -1,7 +1,7 @@
 // Tiled matrix product C[i][j] = sum_k A(i, k) B(j, k) of bf16 or fp32 operands with
 // fp32 sums, the core of the head loss (dv_head.hip).  Each operand is stored with
 // k along its rows ("rows": i by k) or with k from row to row ("columns": k by i);
-// row starts are on 16-byte boundaries.
+// row starts are on 16-byte boundaries.  B may be a bf16 operand in two parts.
 #pragma once
 
 #include "dv_internal.h"
@@ -25,8 +25,13 @@ struct GemmOperand {
 
 struct GemmShape {
     GemmOperand a, b;
-    int k;  // whole stages: a multiple of 64 (bf16) or 32 (fp32)
+    int k;  // whole stages: a multiple of 64 (bf16) or 32 (fp32); two parts: of both together
 };
+
+// The place of column c in a row of an operand in two bf16 parts, the sum of which is the
+// operand: 32 columns of the first part, the same 32 of the second, and so on.
+constexpr int kPartColumns = 32;
+__host__ __device__ constexpr int64_t part_column(int64_t c) { return (c / kPartColumns * 2) * kPartColumns + c % kPartColumns; }
 
 // The waves of a block split its BM x BN tile into WM x WN parts; COLS_A and
 // COLS_B say which operands are stored by columns.
@@ -49,6 +54,10 @@ struct GemmShape {
 // apart, which groups of 1024 / (4 BM) rows, 64 bytes more than their size apart,
 // keep in distinct banks.
 //
+// B in two parts (bf16; A by columns): a stage holds 32 k of A, and of B those 32 of the
+// first part, then of the second: one half of its k each, both multiplied by the same
+// fragments of A.  By rows that is how B lies; by columns a lane loads its row's parts.
+//
 // bf16: while the matrix instructions work on one half of a stage's k in
 // registers, its other half (then the next stage's first) goes from LDS to
 // registers, and the stage after it from memory to LDS.  One barrier a stage: past
@@ -67,12 +76,17 @@ struct GemmStage {
     static constexpr int kK = 128 / (int)sizeof(E);  // k of a stage
 };
 
-// One side's tile in LDS: B rows or columns, of which a wave takes F fragments.
-template <typename E, int B, bool COLS>
+// One side's tile in LDS: B rows or columns, of which a wave takes F fragments.  HALF: 32 k
+// of an operand by columns, for both halves of a stage; PARTS: an operand in two parts.
+template <typename E, int B, bool COLS, bool HALF = false, bool PARTS = false>
 struct GemmSide {
     static constexpr bool kBf16 = sizeof(E) == 2;
     static constexpr int kStageK = GemmStage<E>::kK;
-    static constexpr int kGroups = B / 8;
+    static constexpr int kGroups = HALF ? B / 16 : B / 8;
+    // of a stage, by columns: rows of k in memory
+    static constexpr int kStageRows = HALF || PARTS ? kStageK / 2 : kStageK;
+    static_assert(!HALF || (COLS && kBf16), "half a stage is of bf16 by columns");
+    static_assert(!PARTS || (kBf16 && !HALF), "parts are bf16");
     static constexpr int kPitch = !COLS ? 1024 : kBf16 ? 1024 + 32 : 1024 + 64;
     static constexpr int kBytes = kGroups * kPitch;
     static constexpr int kRowBytes = B * (int)sizeof(E);      // by columns: of a row of k
@@ -81,10 +95,17 @@ struct GemmSide {
 
     // By columns, the row of k at place `slot` of a group.  bf16: bits 0, 1, 3
     // of r (and of 4, 5 what the place does not take) make the group.  fp32: bits
-    // 3, 4 (and of 0 to 2 what the place does not take).
+    // 3, 4 (and of 0 to 2 what the place does not take).  Half a stage of 64 columns has four
+    // groups: bit 3 makes the place's first bit, half of the banks apart.
     static __device__ __forceinline__ int row_of(int group, int slot)
     {
-        if constexpr (kBf16) {
+        if constexpr (HALF) {
+            if (kRowsPerGroup == 8)
+                return (group & 3) | (slot & 1) << 3 | (slot >> 1 & 1) << 2 | (slot >> 2 & 1) << 4;
+            int r = (group & 3) | (group >> 2 & 1) << 3 | (slot & 1) << 2;
+            r |= (kRowsPerGroup == 2 ? group >> 3 & 1 : slot >> 1 & 1) << 4;
+            return r;
+        } else if constexpr (kBf16) {
             int r = (group & 3) | (group >> 2 & 1) << 3 | (slot & 1) << 2;
             if (kRowsPerGroup == 2)
                 r |= (group >> 3 & 1) << 4 | (group >> 4 & 1) << 5;
@@ -107,8 +128,12 @@ struct GemmSide {
             constexpr int kPieces = kRowBytes / 16;
             int r = row_of(group, lane / kPieces);
             int c = (lane % kPieces) * (16 / kElt);
-            r = r < k_left ? r : k_left - 1;
             c = c < o.n - i0 ? c : o.n - 16 / kElt - i0;
+            if constexpr (PARTS) {
+                c = (int)part_column(c) + r / kStageRows * kPartColumns;
+                r %= kStageRows;
+            }
+            r = r < k_left ? r : k_left - 1;
             return r * (int)(o.ld * kElt) + c * kElt;
         } else {
             int r = group * 8 + (lane >> 3);
@@ -126,7 +151,12 @@ struct GemmSide {
     static __device__ __forceinline__ int place(int lane, int h)
     {
         const int r = lane & 15, b = lane >> 4;
-        if constexpr (COLS && kBf16) {
+        if constexpr (HALF) {
+            if (kRowsPerGroup == 8)
+                return (r >> 2) * kPitch + (lane & 3) * 8 + (b & 1) * kRowBytes + (b >> 1) * 4 * kRowBytes;
+            const int group = r >> 2 | (b & 1) << 2;
+            return group * kPitch + (lane & 3) * 8 + (b >> 1) * (kRowsPerGroup == 2 ? 8 * kPitch : 2 * kRowBytes);
+        } else if constexpr (COLS && kBf16) {
             const int group = r >> 2 | (b & 1) << 2;
             int at = group * kPitch + (lane & 3) * 8;
             if (kRowsPerGroup == 2)
@@ -155,8 +185,9 @@ struct GemmSide {
                 s16x4 half[2];
                 bf16x8 v;
             } f;
+            constexpr int kNext = HALF && kRowsPerGroup == 8 ? 2 * kRowBytes : kRowBytes;  // bit 2 of k
             f.half[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Ptr)(tile + at + i * kFragmentStep));
-            f.half[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Ptr)(tile + at + i * kFragmentStep + kRowBytes));
+            f.half[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Ptr)(tile + at + i * kFragmentStep + kNext));
             return f.v;
         } else {
             return *reinterpret_cast<const bf16x8 *>(tile + at + i * kFragmentStep);
@@ -200,10 +231,10 @@ struct SplitFragment {
     }
 };
 
-template <typename E, int BM, int BN, int WM, int WN, bool COLS_A = false, bool COLS_B = false>
+template <typename E, int BM, int BN, int WM, int WN, bool COLS_A = false, bool COLS_B = false, bool PARTS = false>
 struct Gemm {
-    using A = GemmSide<E, BM, COLS_A>;
-    using B = GemmSide<E, BN, COLS_B>;
+    using A = GemmSide<E, BM, COLS_A, PARTS>;
+    using B = GemmSide<E, BN, COLS_B, false, PARTS>;
     static constexpr int kStageK = GemmStage<E>::kK;
     static constexpr int kWaves = WM * WN;
     static constexpr int kTm = BM / WM / 16;  // 16-row fragments of a wave
@@ -220,18 +251,21 @@ struct Gemm {
         bf16x8 a[kTm], b[kTn];
     };
 
+    template <bool BOTH = true>
     static __device__ __forceinline__ void read(Fragments &f, const char *stage, int at_a, int at_b)
     {
 #pragma unroll
         for (int i = 0; i < kTn; ++i)
             f.b[i] = B::fragment(stage + A::kBytes, at_b, i);
+        if constexpr (BOTH)
 #pragma unroll
-        for (int i = 0; i < kTm; ++i)
-            f.a[i] = A::fragment(stage, at_a, i);
+            for (int i = 0; i < kTm; ++i)
+                f.a[i] = A::fragment(stage, at_a, i);
     }
 
-    // acc += a b^T, with the LDS reads issued just before dealt out between
-    // the matrix instructions.
+    // acc += a b^T, with the LDS reads issued just before (of both sides, or of B)
+    // dealt out between the matrix instructions.
+    template <bool BOTH = true>
     static __device__ __forceinline__ void multiply(f32x4 (&acc)[kTm][kTn], const Fragments &f)
     {
 #pragma unroll
@@ -239,7 +273,7 @@ struct Gemm {
 #pragma unroll
             for (int j = 0; j < kTn; ++j)
                 acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.a[i], f.b[j], acc[i][j], 0, 0, 0);
-        constexpr int kReads = kTm * (COLS_A ? 2 : 1) + kTn * (COLS_B ? 2 : 1);
+        constexpr int kReads = (BOTH ? kTm * (COLS_A ? 2 : 1) : 0) + kTn * (COLS_B ? 2 : 1);
         static_assert(kReads <= 2 * kTm * kTn, "at least one matrix instruction to two reads");
         constexpr int kPer = kReads > kTm * kTn ? 2 : 1;
 #pragma unroll
@@ -310,14 +344,15 @@ struct Gemm {
             constexpr bool kMixed = A::kGroups % kLoads != 0;
             return group + (kMixed ? i : 0) < A::kGroups;
         };
-        const auto start = [&](const GemmOperand &o, bool cols, int first) {
-            return reinterpret_cast<const char *>(static_cast<const E *>(o.p) + (cols ? first : first * o.ld));
+        const auto start = [&](const GemmOperand &o, bool cols, bool parts, int first) {
+            return reinterpret_cast<const char *>(static_cast<const E *>(o.p) +
+                                                  (!cols ? first * o.ld : parts ? part_column(first) : first));
         };
-        const auto step = [&](const GemmOperand &o, bool cols) {
-            return (cols ? kStageK * o.ld : kStageK) * (int64_t)sizeof(E);
+        const auto step = [&](const GemmOperand &o, bool cols, int rows) {
+            return (cols ? rows * o.ld : kStageK) * (int64_t)sizeof(E);
         };
-        const char *const start_a = start(g.a, COLS_A, i0), *const start_b = start(g.b, COLS_B, j0);
-        const int64_t step_a = step(g.a, COLS_A), step_b = step(g.b, COLS_B);
+        const char *const start_a = start(g.a, COLS_A, false, i0), *const start_b = start(g.b, COLS_B, PARTS, j0);
+        const int64_t step_a = step(g.a, COLS_A, A::kStageRows), step_b = step(g.b, COLS_B, B::kStageRows);
         int voff[kLoads];
         const auto place_loads = [&](int left_a, int left_b) {
 #pragma unroll
@@ -325,19 +360,19 @@ struct Gemm {
                 voff[i] = side_a(i) ? A::source(g.a, i0, group + i, lane, left_a)
                                     : B::source(g.b, j0, group + i - A::kGroups, lane, left_b);
         };
-        place_loads(kStageK, kStageK);
+        place_loads(A::kStageRows, B::kStageRows);
         int stage = from;
 
         const auto load = [&](int slot) {
             // rows of k that do not exist, by columns: the last one again
-            const auto left = [&](const GemmOperand &o, bool cols) {
-                return cols ? o.k_rows - stage * kStageK : kStageK;
+            const auto left = [&](const GemmOperand &o, bool cols, int rows) {
+                return cols ? o.k_rows - stage * rows : rows;
             };
             const auto place = [&](const char *start, int64_t step, const GemmOperand &o, int left) {
                 return left > 0 ? start + stage * step : start + (int64_t)(o.k_rows - 1) * o.ld * (int64_t)sizeof(E);
             };
-            const int left_a = left(g.a, COLS_A), left_b = left(g.b, COLS_B);
-            if (left_a < kStageK || left_b < kStageK)
+            const int left_a = left(g.a, COLS_A, A::kStageRows), left_b = left(g.b, COLS_B, B::kStageRows);
+            if (left_a < A::kStageRows || left_b < B::kStageRows)
                 place_loads(left_a > 0 ? left_a : 1, left_b > 0 ? left_b : 1);
             const char *const qa = place(start_a, step_a, g.a, left_a), *const qb = place(start_b, step_b, g.b, left_b);
             const uint32_t dst = (uint32_t)(uintptr_t)(Lds)(lds + slot * kStageBytes);
@@ -366,8 +401,12 @@ struct Gemm {
             Fragments f0, f1;
             read(f0, lds, a0, b0);
             const auto work = [&](int s, f32x4 (&first)[kTm][kTn], f32x4 (&second)[kTm][kTn]) {
-                read(f1, lds + (s & 1) * kStageBytes, a1, b1);
-                multiply(first, f0);
+                read<!PARTS>(f1, lds + (s & 1) * kStageBytes, a1, b1);
+                if constexpr (PARTS)
+#pragma unroll
+                    for (int i = 0; i < kTm; ++i)
+                        f1.a[i] = f0.a[i];
+                multiply<!PARTS>(first, f0);
                 if (s + 1 < stages) {
                     wait_loads<0>();
                     barrier();

@@ -10,9 +10,14 @@
 // in the registers of the product that made it and leaves as each row's
 // maximum and sum of exponentials over the tile, the target's apart; a second kernel
 // joins the tiles.  Backward: a piece of the vocabulary at a time, the same product again,
-// its tiles leaving as G in bf16, and from the piece's G the two other products.
+// its tiles leaving as G, and from the piece's G the two other products.
 // Four products of 2 N D V operations against six N D V that cannot be avoided:
 // the price of not keeping the logits.
+//
+// For bf16 operands G leaves as two bf16 parts, 16 bits together, and each of the two
+// products runs over both (8,192 x 4,096 x 128,256, loss and gradients: 36.5 ms, with G rounded
+// to one part 26.0).  One part costs an error of the size of the results' own rounding: gradients
+// off by 0.0024 to 0.0027 of their norm, where that rounding alone makes 0.0017.
 //
 // All products are the one of dv_gemm.h, which takes operands with k along their
 // rows or from row to row: x, w and G are used as they lie.
@@ -86,6 +91,13 @@ struct RowStage {
         wave_lds_sync();
     }
 };
+
+// Parts of an element of G in the operands' type.
+template <typename E>
+constexpr int parts_of()
+{
+    return sizeof(E) == 2 ? 2 : 1;
+}
 
 // --------------------------------------------------------------- the logits
 
@@ -212,13 +224,13 @@ __global__ void weights_kernel(int rows, int V, Masks masks, const int32_t *targ
         weight[n] = RowMask(masks, V, n).has(targets[n]) ? grad_loss[n] : 0.f;
 }
 
-// A piece of G in the operands' type: [rows][ld] with the piece's tokens along a
-// row, zeros up to the next multiple of 64 of them, and up to the next whole stage
-// of rows.  8,192 x 4,096 x 16,128 tokens bf16: 859 us, 1.26 PFLOP/s with 264 MB of stores.
+// A piece of G: rows of `cols` tokens in fp32, or in two bf16 parts (part_column), zeros from
+// the piece's end up to the next multiple of 64 tokens and from the last row up to the next
+// whole stage of rows.  8,192 x 4,096 x 16,128 tokens bf16: 907 us, 1.19 PFLOP/s with 528 MB of stores.
 template <typename E, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__(WM *WN *kWave, 2) void grad_kernel(GemmShape g, int v0, int V, int rows, Masks masks,
                                                                 const int32_t *targets, const float *lse,
-                                                                const float *weight, E *out, int64_t ld, int tiles_i,
+                                                                const float *weight, E *out, int cols, int tiles_i,
                                                                 int tiles_j)
 {
     using G = Gemm<E, BM, BN, WM, WN>;
@@ -233,7 +245,8 @@ __global__ __launch_bounds__(WM *WN *kWave, 2) void grad_kernel(GemmShape g, int
     const int lw = ti * BM + wm * (BM / WM);  // the wave's first token in the piece
     const int vw = v0 + lw;
     const int quarter = lane >> 4;
-    const int rows_k = (rows + G::kStageK - 1) / G::kStageK * G::kStageK;
+    constexpr int kParts = parts_of<E>();
+    const int rows_k = gradient_rows(rows);
     using Rows = RowStage<E, BM / WM>;
     static_assert(WM * WN * Rows::kBytes <= G::kLdsBytes, "every wave has its rows");
     char *mine = lds + wave * Rows::kBytes;
@@ -252,19 +265,32 @@ __global__ __launch_bounds__(WM *WN *kWave, 2) void grad_kernel(GemmShape g, int
 #pragma unroll
         for (int a = 0; a < G::kTm; ++a) {
             const uint32_t bits = m.word((vw >> 5) + (a >> 1)) >> (quarter * 4 + (a & 1) * 16);
-            E y[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 float p = (bits >> e & 1u) && w != 0.f ? softmax_term(acc[a][b][e], base, kLog2e) : 0.f;
                 p -= t == a * 16 + quarter * 4 + e ? 1.f : 0.f;
-                y[e] = (E)(p * w);
+                acc[a][b][e] = p * w;
             }
-            Rows::put(mine, lane, a, y);
         }
-        Rows::each(mine, lane, [&](int row, int col, Words y) {
-            if (lw + col < ld)  // 64 divides ld
-                store_words(out + (int64_t)(n0 + row) * ld + lw + col, y);
-        });
+#pragma unroll
+        for (int part = 0; part < kParts; ++part) {
+#pragma unroll
+            for (int a = 0; a < G::kTm; ++a) {
+                E y[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    y[e] = (E)acc[a][b][e];
+                    acc[a][b][e] -= (float)y[e];  // the rest
+                }
+                Rows::put(mine, lane, a, y);
+            }
+            Rows::each(mine, lane, [&](int row, int col, Words y) {
+                if (lw + col >= cols)  // 64 divides cols
+                    return;
+                E *to = out + (int64_t)(n0 + row) * kParts * cols;
+                store_words(to + (kParts == 2 ? part_column(lw + col) + part * kPartColumns : lw + col), y);
+            });
+        }
     }
 }
 
@@ -274,16 +300,16 @@ enum class Out { kStore, kPartial, kPartialAdd };
 
 // C[j][i] of a product as `out_rows` rows of `cols` elements: in T, or in fp32
 // as (or on top of) the partial sums of this block's share of k.  A is stored by
-// columns, B by columns with COLS_B.  8,192 x 4,096 x 16,128 bf16: 765 us either way, 1.41
-// PFLOP/s, bound by the matrix instructions.  One buffer where k is one stage: three
-// blocks a compute unit instead of two (64 rows x 2048 x 128,256 bf16: 103 us and 128).
-template <typename E, int BM, int BN, int WM, int WN, bool COLS_B, typename T, Out OUT, int BUFFERS>
+// columns, B (G, in two parts if bf16) by columns with COLS_B.  8,192 x 4,096 x 16,128
+// tokens bf16: dx 1.39 ms, dw 1.47 over both parts, 1.56 and 1.47 PFLOP/s, bound by the matrix
+// instructions.
+template <typename E, int BM, int BN, int WM, int WN, bool COLS_B, typename T, Out OUT>
 __global__ __launch_bounds__(WM *WN *kWave, 2) void product_kernel(GemmShape g, T *out, int out_rows, int cols,
                                                                    int64_t split_stride, int split_stages, int tiles_i,
                                                                    int tiles_j)
 {
-    using G = Gemm<E, BM, BN, WM, WN, true, COLS_B>;
-    __shared__ __attribute__((aligned(1024))) char lds[BUFFERS * G::kStageBytes];
+    using G = Gemm<E, BM, BN, WM, WN, true, COLS_B, parts_of<E>() == 2>;
+    __shared__ __attribute__((aligned(1024))) char lds[G::kLdsBytes];
     int ti, tj;
     tile_of_block(blockIdx.x, tiles_i, tiles_j, ti, tj);
     const int total = g.k / G::kStageK;
@@ -295,7 +321,7 @@ __global__ __launch_bounds__(WM *WN *kWave, 2) void product_kernel(GemmShape g, 
     const int wm = wave / WN, wn = wave % WN;
     out += blockIdx.y * split_stride;
     using Rows = RowStage<T, BM / WM>;
-    static_assert(WM * WN * Rows::kBytes <= BUFFERS * G::kStageBytes, "every wave has its rows");
+    static_assert(WM * WN * Rows::kBytes <= G::kLdsBytes, "every wave has its rows");
     char *mine = lds + wave * Rows::kBytes;
     G::barrier();  // the last stage is read
     const int c0 = ti * BM + wm * (BM / WM);
@@ -328,7 +354,7 @@ __global__ __launch_bounds__(WM *WN *kWave, 2) void product_kernel(GemmShape g, 
             }
             if (left >= Rows::kN) {
                 // the weight's gradient is large and read by nobody here (64 rows x 2048 x
-                // 128,256 bf16: 129 us for it, with ordinary stores 217)
+                // 128,256 bf16: 123 us for it; in one part 129, with ordinary stores 217)
                 if (COLS_B && OUT == Out::kStore)
                     stream_words(p, y);
                 else
@@ -440,14 +466,7 @@ hipError_t product(const GemmShape &g, const Plan &plan, T *out, int out_rows, i
         using X = decltype(tile);
         const int ti = (cols + X::kM - 1) / X::kM, tj = (out_rows + X::kN - 1) / X::kN;
         const dim3 grid(ti * tj, plan.splits);
-        if constexpr (COLS_B && OUT == Out::kStore && X::kM == 128) {
-            if (plan.stages == 1) {
-                product_kernel<E, X::kM, X::kN, 2, X::kWn, COLS_B, T, OUT, 1><<<grid, X::kThreads, 0, s>>>(
-                    g, out, out_rows, cols, split_stride, plan.stages, ti, tj);
-                return;
-            }
-        }
-        product_kernel<E, X::kM, X::kN, 2, X::kWn, COLS_B, T, OUT, 2><<<grid, X::kThreads, 0, s>>>(
+        product_kernel<E, X::kM, X::kN, 2, X::kWn, COLS_B, T, OUT><<<grid, X::kThreads, 0, s>>>(
             g, out, out_rows, cols, split_stride, plan.stages, ti, tj);
     });
 }
@@ -480,7 +499,8 @@ hipError_t backward(const HeadArgs &a, const float *lse, const float *grad_loss,
                     hipStream_t s)
 {
     const BackwardLayout l = backward_layout(a.rows, a.hidden, a.V, a.dtype, in_place(a));
-    const int rows_k = (a.rows + l.stage_k - 1) / l.stage_k * l.stage_k;
+    constexpr int kParts = parts_of<T>();
+    const int rows_k = gradient_rows(a.rows);
     float *weight = reinterpret_cast<float *>(ws + l.weight), *dx = reinterpret_cast<float *>(ws + l.dx);
     T *g_piece = reinterpret_cast<T *>(ws + l.g);
     constexpr bool kBf16 = sizeof(T) == 2;
@@ -496,15 +516,15 @@ hipError_t backward(const HeadArgs &a, const float *lse, const float *grad_loss,
         GemmOperand w;
         DV_TRY(operand(weight_rows(a, v0), a.ld_w, a.dtype, n, a.hidden, l.here.w, l.k, ws + l.w, w, s));
         const GemmShape logits{w, x, (int)l.k};
-        const GemmOperand g{g_piece, n64, a.rows, 0};
+        const GemmOperand g{g_piece, kParts * n64, a.rows, 0};
         DV_TRY(with_tile<!kBf16>(logits_side(l, a.rows, n, kBf16), [&](auto tile) {
             using X = decltype(tile);
             const int ti = (n + X::kM - 1) / X::kM, tj = (a.rows + X::kN - 1) / X::kN;
             grad_kernel<T, X::kM, X::kN, 2, X::kWn><<<ti * tj, X::kThreads, 0, s>>>(
-                logits, v0, a.V, a.rows, a.masks, a.targets, lse, weight, g_piece, n64, ti, tj);
+                logits, v0, a.V, a.rows, a.masks, a.targets, lse, weight, g_piece, (int)n64, ti, tj);
         }));
         if (grad_x) {
-            const GemmShape shape{by_columns(w, l.k), g, (int)n64};
+            const GemmShape shape{by_columns(w, l.k), g, (int)(kParts * n64)};
             const int64_t stride = (int64_t)a.rows * a.hidden;
             if (piece == 0) {
                 splits = l.dx_plan.splits;
@@ -514,7 +534,7 @@ hipError_t backward(const HeadArgs &a, const float *lse, const float *grad_loss,
                     DV_TRY((product<T, false, float, Out::kPartial>(shape, l.dx_plan, dx, a.rows, a.hidden, stride, s)));
             } else {
                 // the last piece's k is no longer than the first one's: its splits are no more
-                const int stages = (int)(n64 / l.stage_k);
+                const int stages = (int)(n64 / kGradientStage);
                 Plan plan = l.dx_plan;
                 plan.splits = (stages + plan.stages - 1) / plan.stages;
                 DV_TRY((product<T, false, float, Out::kPartialAdd>(shape, plan, dx, a.rows, a.hidden, stride, s)));
@@ -523,7 +543,7 @@ hipError_t backward(const HeadArgs &a, const float *lse, const float *grad_loss,
         if (grad_weight) {
             GemmOperand g_t = by_columns(g, n64);
             g_t.k_rows = rows_k;
-            const GemmShape shape{by_columns(x, l.k), g_t, rows_k};
+            const GemmShape shape{by_columns(x, l.k), g_t, kParts * rows_k};
             const Plan plan = dw_plan(l, a.rows, n, kBf16);
             T *out = grad_weight + (int64_t)v0 * a.hidden;
             if (plan.splits == 1) {

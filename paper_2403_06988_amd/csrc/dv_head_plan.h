@@ -173,6 +173,11 @@ inline ForwardLayout forward_layout(int rows, int hidden, int V, int dtype, InPl
     return l;
 }
 
+// A stage of the gradients' products takes 32 rows or tokens of G: in fp32, or in two bf16
+// parts (a stage of 64 k).
+constexpr int kGradientStage = 32;
+__host__ __device__ constexpr int gradient_rows(int rows) { return (rows + kGradientStage - 1) / kGradientStage * kGradientStage; }
+
 struct BackwardLayout : HeadLayout {
     Plan dx_plan;
     size_t g, weight, dx, dw;
@@ -180,18 +185,18 @@ struct BackwardLayout : HeadLayout {
 
 inline Plan dw_plan(const HeadLayout &l, int rows, int64_t n, bool bf16)
 {
-    const int64_t stages = rows > 0 ? (rows + l.stage_k - 1) / l.stage_k : 1;
+    const int64_t stages = rows > 0 ? gradient_rows(rows) / kGradientStage : 1;
     return plan_product(l.k, n, stages, 8, bf16, bf16 ? 2 : 4, false);
 }
 
 inline BackwardLayout backward_layout(int rows, int hidden, int V, int dtype, InPlace here)
 {
     BackwardLayout l{head_layout(rows, hidden, V, dtype, here)};
-    const int64_t r64 = up64(rows > 0 ? rows : 1), p64 = up64(l.piece);
-    l.g = l.take(r64 * p64 * (dtype == 1 ? 2 : 4));
-    l.weight = l.take((size_t)r64 * 4);
+    const int64_t p64 = up64(l.piece);
+    l.g = l.take((size_t)gradient_rows(rows) * p64 * 4);  // an fp32 element or both parts
+    l.weight = l.take((size_t)rows * 4);
     // dx over a piece: few tiles and a long k
-    l.dx_plan = plan_product(l.k, rows, p64 / l.stage_k, 16, dtype == 1, 4, true);
+    l.dx_plan = plan_product(l.k, rows, p64 / kGradientStage, 16, dtype == 1, 4, true);
     l.dx = l.take((size_t)l.dx_plan.splits * rows * hidden * 4);
     // dw over a piece, and over the last one: split where hidden and tokens make few tiles
     const auto dw_sums = [&](int64_t n) {

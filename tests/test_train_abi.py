@@ -184,7 +184,7 @@ def test_head_workspaces_hold_no_copy_that_is_not_made():
             for D, V in ((4096, 128256), (4096, 256000), (1024, 1000000)):
                 at = lambda q, x=P, ld_x=D, w=P + 64 * GB, ld_w=D: q(x, ld_x, w, ld_w, dt, rows, D, V)  # noqa: E731
                 copies = ((1 << 27) + (rows << 19)) * elt + 64 * D * elt
-                states, g = (V // 32 + 8) * rows * 8 + MB, min(V + 64, 1 << 18) * 64 * elt + 64 * D * 16 * 4 + MB
+                states, g = (V // 32 + 8) * rows * 8 + MB, min(V + 64, 1 << 18) * 64 * 4 + 64 * D * 16 * 4 + MB
                 own, back = lib.dv_head_loss_workspace_bytes_for, lib.dv_head_loss_backward_workspace_bytes_for
                 assert 0 < at(own) <= states and 0 < at(back) <= g
                 assert at(own, w=P + 64 * GB + 16) == at(own)
