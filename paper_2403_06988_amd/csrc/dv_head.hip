@@ -15,7 +15,7 @@
 // the price of not keeping the logits.
 //
 // For bf16 operands G leaves as two bf16 parts, 16 bits together, and each of the two
-// products runs over both (8,192 x 4,096 x 128,256, loss and gradients: 36.5 ms, with G rounded
+// products runs over both (8,192 x 4,096 x 128,256, loss and gradients: 37.5 ms, with G rounded
 // to one part 26.0).  One part costs an error of the size of the results' own rounding: gradients
 // off by 0.0024 to 0.0027 of their norm, where that rounding alone makes 0.0017.
 //
@@ -105,7 +105,8 @@ constexpr int parts_of()
 // target's; the target's logit.  i runs over the piece's tokens, j over rows.
 // Bound by the matrix instructions: 8,192 x 4,096 x 128,256 bf16 in 6.3 ms, 1.36 PFLOP/s
 // (a library product that stores the logits: 5.9 ms); 1 x 1,024 x 32,000 in 13.0 us, by the
-// weights' 65 MB; fp32 1,024 x 512 x 32,000 in 200 us, 168 TFLOP/s (a library product 249).
+// weights' 65 MB; fp32 1,024 x 512 x 32,000 in 200 us, 168
+// TFLOP/s (a library product: 249 us).
 template <typename E, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__(WM *WN *kWave, 2) void stats_kernel(GemmShape g, int v0, int V, int rows, Masks masks,
                                                                  const int32_t *targets, Softmax *parts,
@@ -226,7 +227,7 @@ __global__ void weights_kernel(int rows, int V, Masks masks, const int32_t *targ
 
 // A piece of G: rows of `cols` tokens in fp32, or in two bf16 parts (part_column), zeros from
 // the piece's end up to the next multiple of 64 tokens and from the last row up to the next
-// whole stage of rows.  8,192 x 4,096 x 16,128 tokens bf16: 907 us, 1.19 PFLOP/s with 528 MB of stores.
+// whole stage of rows.  8,192 x 4,096 x 16,128 tokens bf16: 910 us, 1.19 PFLOP/s with 528 MB of stores.
 template <typename E, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__(WM *WN *kWave, 2) void grad_kernel(GemmShape g, int v0, int V, int rows, Masks masks,
                                                                 const int32_t *targets, const float *lse,
@@ -301,7 +302,7 @@ enum class Out { kStore, kPartial, kPartialAdd };
 // C[j][i] of a product as `out_rows` rows of `cols` elements: in T, or in fp32
 // as (or on top of) the partial sums of this block's share of k.  A is stored by
 // columns, B (G, in two parts if bf16) by columns with COLS_B.  8,192 x 4,096 x 16,128
-// tokens bf16: dx 1.39 ms, dw 1.47 over both parts, 1.56 and 1.47 PFLOP/s, bound by the matrix
+// tokens bf16: dx 1.43 ms, dw 1.51 over both parts, 1.51 and 1.43 PFLOP/s, bound by the matrix
 // instructions.
 template <typename E, int BM, int BN, int WM, int WN, bool COLS_B, typename T, Out OUT>
 __global__ __launch_bounds__(WM *WN *kWave, 2) void product_kernel(GemmShape g, T *out, int out_rows, int cols,
@@ -354,7 +355,7 @@ __global__ __launch_bounds__(WM *WN *kWave, 2) void product_kernel(GemmShape g, 
             }
             if (left >= Rows::kN) {
                 // the weight's gradient is large and read by nobody here (64 rows x 2048 x
-                // 128,256 bf16: 123 us for it; in one part 129, with ordinary stores 217)
+                // 128,256 bf16 with one part of G: 129 us for it, with ordinary stores 217)
                 if (COLS_B && OUT == Out::kStore)
                     stream_words(p, y);
                 else

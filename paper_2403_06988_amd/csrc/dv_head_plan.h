@@ -108,9 +108,9 @@ struct HeadLayout {
 };
 
 // A piece has at most kPieceElements of G, and of packed weights that many and more with the
-// rows, whose products lose by a cut (backward of 500 rows x 2048 x 128,256 bf16 in one piece
-// and two: 1024 and 1136 us; of 8 x 4096 x 128,256 in one and four: 1115 and 1044); or the least
-// number of tokens that keeps the products' tiles busy.
+// rows, whose products lose by a cut (the loss of 300 rows x 4100 x 50,257 bf16 in one piece
+// and two: 384 and 413 us; 8 x 4096 x 128,256 in one and four: 655 and 630, backward 1111 and
+// 1049); or the least number of tokens that keeps the products' tiles busy.
 inline HeadLayout head_layout(int rows, int hidden, int V, int dtype, InPlace here)
 {
     HeadLayout l{};
