@@ -664,7 +664,7 @@ def embed(weight, ids, scale=1.0, out=None, stream=None):
     ld = _matrix(weight, "weight", dev)
     dt = _code(weight.dtype)
     V, D = weight.shape
-    N = ids.shape[0]
+    N = ids.numel()
     _vector(ids, "ids", N, torch.int32, dev)
     out = _result(out, "out", (N, D), weight.dtype, dev, stream)
     st = lib.dv_embed(_ptr(weight), ld, dt, V, D, _ptr(ids), N, float(scale), _ptr(out), _stream(stream, dev))

@@ -131,3 +131,12 @@ def test_refusals(dv):
                 lambda: dv.embed_backward(w[:4], ids, 10, grad_weight=w)):
         with pytest.raises(dv.DvError):
             bad()
+
+
+def test_ids_that_are_no_vector_are_refused(dv):
+    w = torch.zeros((10, 8), device=DEV)
+    for ids in (torch.tensor(3, dtype=torch.int32, device=DEV), torch.zeros((2, 2), dtype=torch.int32, device=DEV)):
+        with pytest.raises(ValueError):
+            dv.embed(w, ids)
+        with pytest.raises(ValueError):
+            dv.embed_backward(w[:2], ids, 10)
