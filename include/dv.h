@@ -28,6 +28,10 @@
  *   dv_distill_loss, softmax cross entropy over the allowed tokens from hidden
  *   dv_embed and    states and head weights, divergence from a teacher's top
  *   their _backward logits, and the embedding, each with its gradients.
+ *   dv_rms_norm,    from a model's last hidden states to the logits that the
+ *   dv_quantize_f8, steps above read: the last norm with the residual's
+ *   dv_product_f8,  addition, the head's product in 8 bits (both with their
+ *   dv_adjust_logits  gradients), and penalties, biases and the grammar's mask.
  *
  * Conventions shared by every call:
  *   - Every array argument is a DEVICE pointer (hipMalloc'd or a torch CUDA
@@ -72,6 +76,10 @@ extern "C" {
 #define DV_NOALLOC_MAX_BATCH 65536 /* batch of dv_masked_step_noalloc          */
 #define DV_MAX_HIDDEN 65536        /* hidden      in [1, DV_MAX_HIDDEN]  */
 #define DV_MAX_TOP    1024         /* num_top     in [1, DV_MAX_TOP]     */
+#define DV_MAX_DEPTH  4194304      /* depth       in [128, DV_MAX_DEPTH] */
+#define DV_MAX_BIAS   1024         /* num_bias    in [0, DV_MAX_BIAS]    */
+#define DV_MAX_HISTORY 1048575     /* max_history in [0, DV_MAX_HISTORY] */
+#define DV_SCALE_BLOCK 128         /* columns, or rows and columns, of an 8-bit operand's scale */
 
 typedef enum dv_status {
     DV_OK = 0,
@@ -598,6 +606,143 @@ DV_API dv_status dv_embed_backward(const void *grad_out, int64_t ld_grad_out, in
                                    int32_t hidden, const int32_t *ids, int32_t num_tokens, float scale,
                                    int32_t accumulate, void *grad_weight, void *workspace, size_t workspace_bytes,
                                    void *stream);
+
+/*
+ * From the last layer to the logits
+ * ---------------------------------
+ * The calls below lead from a model's last hidden states to the logits that the
+ * steps above decode from (and, with their gradients, from the head loss back to
+ * the last layer).  Conventions are those of the training calls: rows of any
+ * stride and alignment where a stride is an argument, sums in fp32, each result
+ * rounded once, the same call the same bits, no atomics in memory.
+ *
+ * 8-bit operands.  An e4m3 matrix (the OCP format: largest 448, no infinities,
+ * NaN 0x7F) of n rows over k columns is stored as rows of K bytes, K the next
+ * multiple of 128 of k, zeros beyond k, with fp32 scales:
+ *   by rows    one for each row and 128 columns, stored [K/128][n];
+ *   by tiles   one for each 128 rows and 128 columns, stored [ceil(n/128)][K/128].
+ * A block of values x is quantized as
+ *     scale = max(largest |x| of the block, 2^-100) / 448   (in fp32)
+ *     q     = the e4m3 value nearest to the fp32 quotient x / scale, ties to even;
+ * a block that holds an infinity or a NaN becomes NaN, its scale too.
+ */
+
+/*
+ * dv_rms_norm -- root-mean-square norm with the residual's addition.
+ *
+ * For every row, with D = hidden:
+ *     h    = x + residual, rounded to the type (h = x where residual is NULL)
+ *     rstd = 1 / sqrt(sum_d h_d^2 / D + eps)
+ *     y_d  = h_d rstd weight_d
+ *
+ * x, residual [rows][ld_*], weight [D] of `dtype`.  Outputs, each NULL if not
+ * wanted, contiguous: total [rows][D] = h of `dtype`; out [rows][D] = y of
+ * `dtype`; rstd [rows] fp32; q and scales (both or none) = y as an 8-bit operand by
+ * rows, quantized from fp32.  q 8-byte aligned.  total may be the residual or x
+ * itself (the same address, row stride D).  At least one of out and q is wanted.
+ * eps >= 0 and finite.  A row of zeros with eps = 0 gives NaN.
+ * rows = 0 is valid and enqueues nothing.
+ * Errors as dv_head_loss (no workspace).
+ */
+DV_API dv_status dv_rms_norm(const void *x, int64_t ld_x, const void *residual, int64_t ld_residual, const void *weight,
+                             int32_t dtype, int32_t rows, int32_t hidden, float eps, void *total, void *out, float *rstd,
+                             void *q, float *scales, void *stream);
+
+/*
+ * dv_rms_norm_backward_workspace_bytes -- device workspace of
+ * dv_rms_norm_backward; for one hidden it never falls as rows grow.  Returns 0
+ * when an argument is outside its limit.
+ */
+DV_API size_t dv_rms_norm_backward_workspace_bytes(int32_t rows, int32_t hidden);
+
+/*
+ * dv_rms_norm_backward -- gradients of sum(grad_out y) + sum(grad_total h).
+ *
+ *     grad_x      = rstd g - h rstd^3 / D (sum_d g_d h_d) + grad_total,  g = grad_out weight
+ *                   [rows][D]: the gradient of x, and of the residual
+ *     grad_weight = sum over rows of grad_out h rstd   [D]
+ * both contiguous, of `dtype`; either may be NULL and is then not computed.
+ * total [rows][ld_total]: h as dv_rms_norm wrote it (x where there was no
+ * residual), rstd as it wrote it; grad_total [rows][ld_grad_total] or NULL
+ * (zeros): what reaches h past the norm.
+ * rows = 0 is valid: grad_weight is filled with zeros.
+ * Errors as dv_head_loss.
+ */
+DV_API dv_status dv_rms_norm_backward(const void *grad_out, int64_t ld_grad_out, const void *total, int64_t ld_total,
+                                      const void *weight, const float *rstd, const void *grad_total,
+                                      int64_t ld_grad_total, int32_t dtype, int32_t rows, int32_t hidden, void *grad_x,
+                                      void *grad_weight, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * dv_quantize_f8 -- a matrix as an 8-bit operand: as it lies, transposed, or both.
+ *
+ * x [rows][ld_x] of `dtype`, `cols` columns.  tile = 1: by rows; tile = 128: by
+ * tiles.  q [rows][up(cols)] with scales; t_q [cols][up(rows)] with t_scales is
+ * the operand of the transposed matrix (by rows: blocks of 128 rows of a column);
+ * up(): the next multiple of 128.  One of the pairs may be NULL.  q and t_q 16-byte aligned.
+ * rows in [0, DV_MAX_TOKENS], cols in [1, DV_MAX_TOKENS], fewer than 2^24 tiles
+ * of 128 x 128.  rows = 0 is valid and enqueues nothing.
+ * Errors as dv_head_loss (no workspace; DV_ERR_SHAPE for another tile).
+ */
+DV_API dv_status dv_quantize_f8(const void *x, int64_t ld_x, int32_t dtype, int32_t rows, int32_t cols, int32_t tile,
+                                void *q, float *scales, void *t_q, float *t_scales, void *stream);
+
+/*
+ * dv_product_f8_workspace_bytes -- device workspace of dv_product_f8 (sums of
+ * parts of a long depth).  Returns 0 when an argument is outside its limit, and
+ * may return 0 otherwise: then none is needed.
+ */
+DV_API size_t dv_product_f8_workspace_bytes(int32_t rows, int32_t cols, int32_t depth);
+
+/*
+ * dv_product_f8 -- the matrix product of two 8-bit operands:
+ *     out[m][n] = sum over blocks kb of a_scales(kb, m) b_scales(kb, n)
+ *                 * (sum over the block's 128 k of a[m][k] b[n][k]).
+ *
+ * a [rows][ld_a] with scales by rows; b [cols][ld_b] with scales by rows (tile =
+ * 1) or by tiles (tile = 128); depth: a multiple of 128.  Row starts on 16-byte
+ * boundaries (ld_* multiples of 16, at least depth and at most DV_MAX_DEPTH).
+ * out [rows][ld_out] of `dtype`.  A head's logits: a the hidden states, b the
+ * weights by tiles.  Gradients of out = x w^T: of x, a = the gradient's q, b = w's
+ * t_q by tiles; of w, a = the gradient's t_q, b = x's t_q by rows.
+ * rows = 0 is valid and enqueues nothing; rows * cols < 2^36.
+ * Errors as dv_head_loss.
+ */
+DV_API dv_status dv_product_f8(const void *a, int64_t ld_a, const float *a_scales, const void *b, int64_t ld_b,
+                               const float *b_scales, int32_t tile, int32_t rows, int32_t cols, int32_t depth,
+                               int32_t dtype, void *out, int64_t ld_out, void *workspace, size_t workspace_bytes,
+                               void *stream);
+
+/*
+ * dv_adjust_logits -- logits with each sequence's penalties, biases and mask.
+ *
+ * Row n's history is history[n*ld_history ..] of lengths[n] tokens (clamped to
+ * [0, max_history]), the first prompt_lengths[n] of them its prompt (NULL: none),
+ * the others its output; ids outside [0, V) take no part.  For a token v with
+ * logit z, in fp32:
+ *     v in the history:        z = z / repetition[n] if z > 0, else z * repetition[n]
+ *     v c > 0 times in the output:  z = z - c frequency[n] - presence[n]
+ *     then                     z = z + the sum of bias[n][i] over the i, in their
+ *                              order, with bias_ids[n][i] = v
+ *     v not allowed:           z = -infinity, whatever it was
+ * rounded once to the type; a token that nothing names keeps its logit's bits.
+ *
+ * logits [rows][ld_logits], out [rows][ld_out] of `dtype`; out may be the logits
+ * themselves (the same address and stride): then, without a mask, only the tokens
+ * that something names are read and written.  history [rows][ld_history] int32
+ * (NULL with max_history 0), lengths, prompt_lengths [rows] int32, repetition (> 0),
+ * presence, frequency [rows] fp32, each NULL for none; bias_ids [rows][num_bias]
+ * int32 and bias [rows][num_bias] fp32, contiguous; allow, num_states, states as
+ * for the training calls (NULL: every token is allowed).
+ * rows * ceil(V / 8192) < 2^24.  rows = 0 is valid and enqueues nothing.
+ * Errors as dv_head_loss (no workspace).
+ */
+DV_API dv_status dv_adjust_logits(const void *logits, int64_t ld_logits, int32_t dtype, int32_t rows, int32_t num_tokens,
+                                  const int32_t *history, int64_t ld_history, int32_t max_history, const int32_t *lengths,
+                                  const int32_t *prompt_lengths, const float *repetition, const float *presence,
+                                  const float *frequency, const int32_t *bias_ids, const float *bias, int32_t num_bias,
+                                  const uint32_t *allow, int32_t num_states, const int32_t *states, void *out,
+                                  int64_t ld_out, void *stream);
 
 /* Static, human-readable name of a status code ("DV_OK", ...). */
 DV_API const char *dv_status_string(int32_t status);

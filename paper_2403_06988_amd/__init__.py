@@ -16,6 +16,11 @@ Algorithm 2, walked to full depth as in Sec. 3.5) for a byte-level DFA;
 For training under the same constraint (a proposer for the speculation, or a
 model): ``head_loss``, ``distill_loss`` and ``embed`` with their ``_backward``
 calls; the ``autograd`` module has them as differentiable functions.
+
+From a model's last hidden states to the logits of a step: ``rms_norm`` and
+``rms_norm_f8`` (with the residual's addition), ``quantize_f8`` and
+``product_f8`` (the head's product in 8 bits) and ``adjust_logits`` (penalties,
+biases and the grammar's mask).
 """
 from __future__ import annotations
 
@@ -28,7 +33,9 @@ __all__ = ["align", "validate_vocab", "masked_step", "masked_step_noalloc", "mas
            "masked_step_workspace_bytes", "masked_sample_workspace_bytes", "spec_verify_workspace_bytes",
            "step_workspace", "sample_workspace", "spec_workspace", "head_loss", "head_loss_backward",
            "head_loss_workspace_bytes", "head_loss_workspace_bytes_for", "head_loss_backward_workspace_bytes",
-           "head_loss_backward_workspace_bytes_for", "distill_loss", "distill_loss_backward", "distill_loss_workspace_bytes", "embed", "embed_backward", "embed_backward_workspace_bytes", "DvError", "DEAD",
+           "head_loss_backward_workspace_bytes_for", "distill_loss", "distill_loss_backward", "distill_loss_workspace_bytes", "embed", "embed_backward", "embed_backward_workspace_bytes",
+           "rms_norm", "rms_norm_f8", "rms_norm_backward", "rms_norm_backward_workspace_bytes", "quantize_f8",
+           "product_f8", "product_f8_workspace_bytes", "adjust_logits", "DvError", "DEAD",
            "library_path", "lib"]
 
 DEAD = -1
@@ -114,6 +121,20 @@ def _load():
     lib.dv_embed_backward_workspace_bytes.argtypes = [i32, i32, i32]
     lib.dv_embed_backward.restype = ctypes.c_int
     lib.dv_embed_backward.argtypes = [vp, i64, i32, i32, i32, vp, i32, f32, i32, vp, vp, sz, vp]
+    lib.dv_rms_norm.restype = ctypes.c_int
+    lib.dv_rms_norm.argtypes = [vp, i64, vp, i64, vp, i32, i32, i32, f32, vp, vp, vp, vp, vp, vp]
+    lib.dv_rms_norm_backward_workspace_bytes.restype = sz
+    lib.dv_rms_norm_backward_workspace_bytes.argtypes = [i32, i32]
+    lib.dv_rms_norm_backward.restype = ctypes.c_int
+    lib.dv_rms_norm_backward.argtypes = [vp, i64, vp, i64, vp, vp, vp, i64, i32, i32, i32, vp, vp, vp, sz, vp]
+    lib.dv_quantize_f8.restype = ctypes.c_int
+    lib.dv_quantize_f8.argtypes = [vp, i64, i32, i32, i32, i32, vp, vp, vp, vp, vp]
+    lib.dv_product_f8_workspace_bytes.restype = sz
+    lib.dv_product_f8_workspace_bytes.argtypes = [i32, i32, i32]
+    lib.dv_product_f8.restype = ctypes.c_int
+    lib.dv_product_f8.argtypes = [vp, i64, vp, vp, i64, vp, i32, i32, i32, i32, i32, vp, i64, vp, sz, vp]
+    lib.dv_adjust_logits.restype = ctypes.c_int
+    lib.dv_adjust_logits.argtypes = [vp, i64, i32, i32, i32, vp, i64, i32, vp, vp, vp, vp, vp, vp, vp, i32, *mask, vp, i64, vp]
     return lib
 
 
@@ -690,3 +711,226 @@ def embed_backward(grad_out, ids, num_tokens, scale=1.0, grad_weight=None, accum
                                _ptr(grad_weight), _ptr(workspace), nbytes, _stream(stream, dev))
     _check(st, "dv_embed_backward")
     return grad_weight
+
+
+# -------------------------------------------- from the last layer to the logits
+
+def rms_norm_backward_workspace_bytes(rows: int, hidden: int) -> int:
+    return int(lib.dv_rms_norm_backward_workspace_bytes(rows, hidden))
+
+
+def product_f8_workspace_bytes(rows: int, cols: int, depth: int) -> int:
+    return int(lib.dv_product_f8_workspace_bytes(rows, cols, depth))
+
+
+F8 = torch.float8_e4m3fn
+SCALE_BLOCK = 128   # columns, or rows and columns, of an 8-bit operand's scale
+
+
+def _run(call, what, dev, stream, *args):
+    """A call on its tensors' device, whichever is the current one."""
+    if torch.cuda.current_device() == dev.index:
+        st = call(*args, _stream(stream, dev))
+    else:
+        with torch.cuda.device(dev):
+            st = call(*args, _stream(stream, dev))
+    _check(st, what)
+
+
+def _blocks(n: int) -> int:
+    return (n + SCALE_BLOCK - 1) // SCALE_BLOCK
+
+
+def _norm_args(x, weight, residual, total):
+    dev = x.device
+    ld = _matrix(x, "x", dev)
+    dt = _code(x.dtype)
+    N, D = x.shape
+    _vector(weight, "weight", D, x.dtype, dev)
+    ld_res = D
+    if residual is not None:
+        ld_res = _matrix(residual, "residual", dev, x.dtype)
+        if residual.shape != x.shape:
+            raise ValueError(f"residual must be [{N}][{D}]")
+    elif total is not None:
+        raise ValueError("total is the sum with a residual")
+    return dev, (_ptr(x), ld, _ptr(residual), ld_res, _ptr(weight), dt, N, D), (N, D)
+
+
+def rms_norm(x, weight, eps=1e-6, residual=None, out=None, total=None, rstd=None, want_rstd=False, stream=None):
+    """Root-mean-square norm of hidden states x [N][D] (bf16 or fp32, any row
+    stride) with weight [D], of x + residual where a residual [N][D] is given.
+
+    Returns (out [N][D], total, rstd): total = x + residual [N][D] (None without
+    a residual; it may be given as the residual or x itself, then overwritten),
+    rstd [N] fp32 with ``want_rstd`` (for ``rms_norm_backward``), else None."""
+    dev, args, (N, D) = _norm_args(x, weight, residual, total)
+    out = _result(out, "out", (N, D), x.dtype, dev, stream)
+    if residual is not None:
+        total = _result(total, "total", (N, D), x.dtype, dev, stream)
+    if want_rstd or rstd is not None:
+        rstd = _result(rstd, "rstd", (N,), torch.float32, dev, stream)
+    _run(lib.dv_rms_norm, "dv_rms_norm", dev, stream, *args, float(eps), _ptr(total), _ptr(out), _ptr(rstd), None, None)
+    return out, total, rstd
+
+
+def rms_norm_f8(x, weight, eps=1e-6, residual=None, q=None, scales=None, total=None, stream=None):
+    """``rms_norm`` with its result as an 8-bit operand of ``product_f8``.
+
+    Returns (q [N][K] float8_e4m3fn, K the next multiple of 128 of D, zeros
+    beyond D; scales [K/128][N] fp32; total)."""
+    dev, args, (N, D) = _norm_args(x, weight, residual, total)
+    kb = _blocks(D)
+    q = _result(q, "q", (N, kb * SCALE_BLOCK), F8, dev, stream)
+    scales = _result(scales, "scales", (kb, N), torch.float32, dev, stream)
+    if residual is not None:
+        total = _result(total, "total", (N, D), x.dtype, dev, stream)
+    _run(lib.dv_rms_norm, "dv_rms_norm", dev, stream, *args, float(eps), _ptr(total), None, None, _ptr(q), _ptr(scales))
+    return q, scales, total
+
+
+def rms_norm_backward(grad_out, total, weight, rstd, grad_total=None, grad_x=None, grad_weight=None, want_x=True,
+                      want_weight=True, workspace=None, stream=None):
+    """Gradients of ``rms_norm``: (grad_x [N][D], which is also the residual's,
+    and grad_weight [D]).  total [N][D] as it was returned (x where there was no
+    residual), rstd [N] too; grad_total [N][D]: the gradient that reaches total
+    past the norm.  ``want_x`` / ``want_weight`` false: None in its place."""
+    dev = total.device
+    ld = _matrix(total, "total", dev)
+    dt = _code(total.dtype)
+    N, D = total.shape
+    ld_g = _matrix(grad_out, "grad_out", dev, total.dtype)
+    _vector(weight, "weight", D, total.dtype, dev)
+    _vector(rstd, "rstd", N, torch.float32, dev)
+    ld_gt = D
+    if grad_total is not None:
+        ld_gt = _matrix(grad_total, "grad_total", dev, total.dtype)
+    if grad_out.shape != total.shape or (grad_total is not None and grad_total.shape != total.shape):
+        raise ValueError(f"grad_out and grad_total must be [{N}][{D}]")
+    if not (want_x or want_weight):
+        return None, None
+    grad_x = _result(grad_x, "grad_x", (N, D), total.dtype, dev, stream) if want_x else None
+    grad_weight = _result(grad_weight, "grad_weight", (D,), total.dtype, dev, stream) if want_weight else None
+    workspace, nbytes = _scratch(workspace, rms_norm_backward_workspace_bytes(N, D), dev, stream)
+    _run(lib.dv_rms_norm_backward, "dv_rms_norm_backward", dev, stream, _ptr(grad_out), ld_g, _ptr(total), ld,
+         _ptr(weight), _ptr(rstd), _ptr(grad_total), ld_gt, dt, N, D, _ptr(grad_x), _ptr(grad_weight), _ptr(workspace), nbytes)
+    return grad_x, grad_weight
+
+
+def _scale_shape(n: int, k: int, tile: int):
+    """Of the scales of n rows over k columns (as the operand lies)."""
+    return (_blocks(k), n) if tile == 1 else (_blocks(n), _blocks(k))
+
+
+def quantize_f8(x, tile=1, want_rows=True, want_columns=False, q=None, scales=None, t_q=None, t_scales=None, stream=None):
+    """x [N][K] (bf16 or fp32, any row stride) as an 8-bit operand of
+    ``product_f8``: with a scale for every 128 columns of a row (``tile`` 1) or for
+    every 128 x 128 (``tile`` 128).
+
+    Returns (q, scales, t_q, t_scales): q [N][up(K)] float8_e4m3fn (up(): the next
+    multiple of 128) with scales [up(K)/128][N], or [up(N)/128][up(K)/128] by
+    tiles; t_q [K][up(N)] and t_scales, the same of the transposed matrix, with
+    ``want_columns``.  None where not wanted."""
+    dev = x.device
+    ld = _matrix(x, "x", dev)
+    dt = _code(x.dtype)
+    N, K = x.shape
+    if not (want_rows or want_columns):
+        return None, None, None, None
+    if want_rows:
+        q = _result(q, "q", (N, _blocks(K) * SCALE_BLOCK), F8, dev, stream)
+        scales = _result(scales, "scales", _scale_shape(N, K, tile), torch.float32, dev, stream)
+    else:
+        q = scales = None
+    if want_columns:
+        t_q = _result(t_q, "t_q", (K, _blocks(N) * SCALE_BLOCK), F8, dev, stream)
+        t_scales = _result(t_scales, "t_scales", _scale_shape(K, N, tile), torch.float32, dev, stream)
+    else:
+        t_q = t_scales = None
+    _run(lib.dv_quantize_f8, "dv_quantize_f8", dev, stream, _ptr(x), ld, dt, N, K, int(tile), _ptr(q), _ptr(scales),
+         _ptr(t_q), _ptr(t_scales))
+    return q, scales, t_q, t_scales
+
+
+def product_f8(a, a_scales, b, b_scales, tile=128, dtype=torch.bfloat16, out=None, workspace=None, stream=None):
+    """a b^T of two 8-bit operands: a [M][K] with scales by rows [K/128][M], b
+    [N][K] with scales by tiles ([ceil(N/128)][K/128], ``tile`` 128) or by rows
+    ([K/128][N], ``tile`` 1), as ``quantize_f8`` and ``rms_norm_f8`` give them (K a
+    multiple of 128, float8_e4m3fn, row starts on 16-byte boundaries).  Returns
+    out [M][N] in ``dtype`` (float32 or bfloat16); a given ``out`` may have any
+    row stride, and its type is the result's."""
+    dev = b.device
+    ld_a, ld_b = _matrix(a, "a", dev, F8), _matrix(b, "b", dev, F8)
+    (M, K), N = a.shape, b.shape[0]
+    if b.shape[1] != K:
+        raise ValueError(f"b must be [N][{K}]")
+    for t, name, shape in ((a_scales, "a_scales", _scale_shape(M, K, 1)), (b_scales, "b_scales", _scale_shape(N, K, tile))):
+        _want(t, name, torch.float32, dev)
+        if tuple(t.shape) != shape:
+            raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
+    if out is None:
+        _code(dtype)
+        out = _new((M, N), dtype, dev, stream)
+    ld_out = _matrix(out, "out", dev)
+    if tuple(out.shape) != (M, N):
+        raise ValueError(f"out must be [{M}][{N}]")
+    need = product_f8_workspace_bytes(M, N, K)
+    workspace, nbytes = _scratch(workspace, need, dev, stream) if need else (None, 0)
+    _run(lib.dv_product_f8, "dv_product_f8", dev, stream, _ptr(a), ld_a, _ptr(a_scales), _ptr(b), ld_b, _ptr(b_scales),
+         int(tile), M, N, K, _code(out.dtype), _ptr(out), ld_out, _ptr(workspace), nbytes)
+    return out
+
+
+def adjust_logits(logits, history=None, lengths=None, prompt_lengths=None, repetition=None, presence=None, frequency=None,
+                  bias_ids=None, bias=None, allow=None, states=None, out=None, stream=None):
+    """Logits [B][V] (bf16 or fp32, any row stride) with each sequence's
+    penalties, biases and grammar mask applied, in a new array or ``out``.
+
+    history [B][H] int32 of which lengths [B] int32 hold tokens, the first
+    prompt_lengths [B] (None: none) of them the prompt; repetition, presence,
+    frequency [B] fp32 (None: no such penalty): tokens of the history have their
+    logits divided by the repetition penalty (multiplied where they are not
+    positive), then tokens that stand c > 0 times in the output lose
+    c * frequency + presence.  bias_ids [B][n] int32 and bias [B][n] fp32 are added
+    (ids outside [0, V) are unused entries); tokens that allow [S][ceil(V/32)]
+    does not allow in states [B] become -infinity.  ``out`` may be the logits
+    themselves: without a mask only the tokens that something names are touched."""
+    dev = logits.device
+    ld = _matrix(logits, "logits", dev)
+    dt = _code(logits.dtype)
+    B, V = logits.shape
+    H = ld_h = 0
+    if history is not None:
+        ld_h = _matrix(history, "history", dev, torch.int32)
+        H = history.shape[1]
+        if history.shape[0] != B:
+            raise ValueError(f"history must be [{B}][H]")
+        if lengths is None:
+            raise ValueError("history and lengths must be given together")
+        _vector(lengths, "lengths", B, torch.int32, dev)
+        if prompt_lengths is not None:
+            _vector(prompt_lengths, "prompt_lengths", B, torch.int32, dev)
+        for t, name in ((repetition, "repetition"), (presence, "presence"), (frequency, "frequency")):
+            if t is not None:
+                _vector(t, name, B, torch.float32, dev)
+    elif any(t is not None for t in (lengths, prompt_lengths, repetition, presence, frequency)):
+        raise ValueError("penalties need a history")
+    n = 0
+    if (bias_ids is None) != (bias is None):
+        raise ValueError("bias_ids and bias must be given together")
+    if bias_ids is not None:
+        _want(bias_ids, "bias_ids", torch.int32, dev)
+        _want(bias, "bias", torch.float32, dev)
+        if bias_ids.dim() != 2 or bias_ids.shape[0] != B or bias_ids.shape != bias.shape:
+            raise ValueError(f"bias_ids and bias must both be [{B}][n]")
+        n = bias_ids.shape[1]
+    mask = _mask_args(allow, states, B, V, dev)
+    if out is None:
+        out = _new((B, V), logits.dtype, dev, stream)
+    ld_out = _matrix(out, "out", dev, logits.dtype)
+    if tuple(out.shape) != (B, V):
+        raise ValueError(f"out must be [{B}][{V}]")
+    _run(lib.dv_adjust_logits, "dv_adjust_logits", dev, stream, _ptr(logits), ld, dt, B, V, _ptr(history), ld_h, H,
+         _ptr(lengths), _ptr(prompt_lengths), _ptr(repetition), _ptr(presence), _ptr(frequency), _ptr(bias_ids), _ptr(bias), n, *mask,
+         _ptr(out), ld_out)
+    return out

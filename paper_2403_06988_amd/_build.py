@@ -11,7 +11,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 SOURCES = ["dv_api.hip", "dv_align.hip", "dv_step.hip", "dv_spec.hip", "dv_sample.hip",
-           "dv_head.hip", "dv_distill.hip", "dv_embed.hip"]
+           "dv_head.hip", "dv_distill.hip", "dv_embed.hip",
+           "dv_norm.hip", "dv_quantize.hip", "dv_product.hip", "dv_adjust.hip"]
 PROBE_SOURCES = ["dv_probes.hip"]
 LIB = os.path.join(HERE, "libdv.so")
 PROBE_LIB = os.path.join(HERE, "libdv_probes.so")

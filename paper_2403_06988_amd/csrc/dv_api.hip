@@ -9,6 +9,7 @@
 
 #include "../../include/dv.h"
 #include "dv_internal.h"
+#include "dv_logits.h"
 #include "dv_sample.h"
 #include "dv_train.h"
 
@@ -826,6 +827,256 @@ dv_status dv_embed_backward(const void *grad_out, int64_t ld_grad_out, int32_t d
                                                 accumulate != 0, grad_weight, workspace,
                                                 static_cast<hipStream_t>(stream)),
                       "dv_embed_backward launch");
+}
+
+namespace {
+
+dv_status rows_args(const char *name, int32_t rows, int32_t hidden, int32_t dtype)
+{
+    DV_CHECK(train_sizes(name, {rows, 1, dtype}));
+    return hidden_size(name, hidden);
+}
+
+}  // namespace
+
+dv_status dv_rms_norm(const void *x, int64_t ld_x, const void *residual, int64_t ld_residual, const void *weight,
+                      int32_t dtype, int32_t rows, int32_t hidden, float eps, void *total, void *out, float *rstd, void *q,
+                      float *scales, void *stream)
+{
+    g_error[0] = '\0';
+    const char *name = "dv_rms_norm";
+    if (!weight || (rows > 0 && !x))
+        return fail(DV_ERR_INVALID_ARG, "%s: weight must be non-NULL, x when rows > 0", name);
+    if (!q != !scales)
+        return fail(DV_ERR_INVALID_ARG, "%s: q and scales must be given together", name);
+    DV_CHECK(rows_args(name, rows, hidden, dtype));
+    DV_CHECK(row_stride(name, "ld_x", ld_x, hidden));
+    if (residual)
+        DV_CHECK(row_stride(name, "ld_residual", ld_residual, hidden));
+    if (!(eps >= 0.f && eps <= 3.0e38f))
+        return fail(DV_ERR_SHAPE, "%s: eps=%g must be >= 0 and finite", name, (double)eps);
+    const size_t elt = element_size(dtype);
+    DV_CHECK(aligned(name, "x", x, elt));
+    DV_CHECK(aligned(name, "residual", residual, elt));
+    DV_CHECK(aligned(name, "weight", weight, elt));
+    DV_CHECK(aligned(name, "total", total, elt));
+    DV_CHECK(aligned(name, "out", out, elt));
+    DV_CHECK(aligned(name, "q", q, 8));
+    if (rows == 0)
+        return DV_OK;
+    if (!out && !q)
+        return fail(DV_ERR_INVALID_ARG, "%s: out or q must be non-NULL when rows > 0", name);
+    const size_t depth = (size_t)dv::up_block(hidden), n = (size_t)rows;
+    const bool over_x = total && total == x && (ld_x == hidden || rows == 1);
+    const bool over_residual = total && total == residual && (ld_residual == hidden || rows == 1);
+    const Range none = range_of(nullptr, 0), r_total = rows_range(total, rows, hidden, hidden, elt);
+    const Range outs[] = {rows_range(out, rows, hidden, hidden, elt), range_of(rstd, rstd ? n * 4 : 0),
+                          range_of(q, q ? n * depth : 0), range_of(scales, scales ? depth / 128 * n * 4 : 0), r_total};
+    const Range r_x = rows_range(x, rows, hidden, ld_x, elt), r_res = rows_range(residual, rows, hidden, ld_residual, elt);
+    const Range ins[] = {range_of(weight, (size_t)hidden * elt)};
+    DV_CHECK(no_overlap(name, outs, ins));
+    for (const Range &o : outs) {
+        const bool is_total = &o == &outs[4];
+        if (overlap(o, is_total && over_x ? none : r_x) || overlap(o, is_total && over_residual ? none : r_res))
+            return fail(DV_ERR_ALIAS, "%s: an output overlaps an input", name);
+    }
+    const dv::NormArgs a{x,    ld_x, residual, ld_residual, weight, dtype, rows, hidden, eps, total, out, rstd,
+                         static_cast<uint8_t *>(q), scales};
+    return hip_status(dv::launch_rms_norm(a, static_cast<hipStream_t>(stream)), "dv_rms_norm launch");
+}
+
+size_t dv_rms_norm_backward_workspace_bytes(int32_t rows, int32_t hidden)
+{
+    return head_sizes_ok(rows, hidden, 1, DV_F32) ? dv::rms_norm_backward_workspace_bytes(rows, hidden) : 0;
+}
+
+dv_status dv_rms_norm_backward(const void *grad_out, int64_t ld_grad_out, const void *total, int64_t ld_total,
+                               const void *weight, const float *rstd, const void *grad_total, int64_t ld_grad_total,
+                               int32_t dtype, int32_t rows, int32_t hidden, void *grad_x, void *grad_weight,
+                               void *workspace, size_t workspace_bytes, void *stream)
+{
+    g_error[0] = '\0';
+    const char *name = "dv_rms_norm_backward";
+    if (!weight || (rows > 0 && (!grad_out || !total || !rstd)))
+        return fail(DV_ERR_INVALID_ARG, "%s: weight must be non-NULL, grad_out, total and rstd when rows > 0", name);
+    DV_CHECK(rows_args(name, rows, hidden, dtype));
+    DV_CHECK(row_stride(name, "ld_grad_out", ld_grad_out, hidden));
+    DV_CHECK(row_stride(name, "ld_total", ld_total, hidden));
+    if (grad_total)
+        DV_CHECK(row_stride(name, "ld_grad_total", ld_grad_total, hidden));
+    if (!grad_weight && (rows == 0 || !grad_x))
+        return rows == 0 ? DV_OK : fail(DV_ERR_INVALID_ARG, "%s: grad_x or grad_weight must be non-NULL", name);
+    const size_t elt = element_size(dtype);
+    DV_CHECK(aligned(name, "grad_out", grad_out, elt));
+    DV_CHECK(aligned(name, "total", total, elt));
+    DV_CHECK(aligned(name, "weight", weight, elt));
+    DV_CHECK(aligned(name, "grad_total", grad_total, elt));
+    DV_CHECK(aligned(name, "grad_x", grad_x, elt));
+    DV_CHECK(aligned(name, "grad_weight", grad_weight, elt));
+    const size_t need = dv::rms_norm_backward_workspace_bytes(rows, hidden);
+    DV_CHECK(workspace_args(name, workspace, workspace_bytes, need));
+    const Range outs[] = {rows_range(grad_x, rows, hidden, hidden, elt),
+                          range_of(grad_weight, grad_weight ? (size_t)hidden * elt : 0), range_of(workspace, need)};
+    const Range ins[] = {rows_range(grad_out, rows, hidden, ld_grad_out, elt), rows_range(total, rows, hidden, ld_total, elt),
+                         range_of(weight, (size_t)hidden * elt), range_of(rstd, (size_t)rows * 4),
+                         rows_range(grad_total, rows, hidden, ld_grad_total, elt)};
+    DV_CHECK(no_overlap(name, outs, ins));
+    const dv::NormGradArgs a{grad_out, ld_grad_out, total, ld_total, weight, rstd, grad_total, ld_grad_total,
+                             dtype,    rows,        hidden, rows > 0 ? grad_x : nullptr, grad_weight};
+    return hip_status(dv::launch_rms_norm_backward(a, workspace, static_cast<hipStream_t>(stream)),
+                      "dv_rms_norm_backward launch");
+}
+
+namespace {
+
+// By rows or by tiles.
+dv_status tile_arg(const char *name, int32_t tile)
+{
+    if (tile != 1 && tile != DV_SCALE_BLOCK)
+        return fail(DV_ERR_SHAPE, "%s: tile=%d must be 1 or %d", name, tile, DV_SCALE_BLOCK);
+    return DV_OK;
+}
+
+// Bytes of the scales of an 8-bit operand.
+size_t scale_bytes(int64_t n, int64_t depth, int32_t tile)
+{
+    return (size_t)(tile == 1 ? n : dv::up_block(n) / DV_SCALE_BLOCK) * (size_t)(depth / DV_SCALE_BLOCK) * 4;
+}
+
+}  // namespace
+
+dv_status dv_quantize_f8(const void *x, int64_t ld_x, int32_t dtype, int32_t rows, int32_t cols, int32_t tile, void *q,
+                         float *scales, void *t_q, float *t_scales, void *stream)
+{
+    g_error[0] = '\0';
+    const char *name = "dv_quantize_f8";
+    if (rows > 0 && !x)
+        return fail(DV_ERR_INVALID_ARG, "%s: x must be non-NULL when rows > 0", name);
+    if (!q != !scales || !t_q != !t_scales)
+        return fail(DV_ERR_INVALID_ARG, "%s: q and scales, t_q and t_scales must be given together", name);
+    DV_CHECK(train_sizes(name, {0, cols, dtype}));
+    if (rows < 0 || rows > DV_MAX_TOKENS)
+        return fail(DV_ERR_SHAPE, "%s: rows=%d outside [0, %d]", name, rows, DV_MAX_TOKENS);
+    DV_CHECK(tile_arg(name, tile));
+    DV_CHECK(row_stride(name, "ld_x", ld_x, cols));
+    const int64_t depth = dv::up_block(cols), t_depth = dv::up_block(rows);
+    if ((depth / 128) * (t_depth / 128) >= (int64_t)1 << 24)
+        return fail(DV_ERR_SHAPE, "%s: %d x %d has 2^24 tiles or more", name, rows, cols);
+    DV_CHECK(aligned(name, "x", x, element_size(dtype)));
+    DV_CHECK(aligned(name, "q", q, 16));
+    DV_CHECK(aligned(name, "t_q", t_q, 16));
+    if (rows == 0)
+        return DV_OK;
+    if (!q && !t_q)
+        return fail(DV_ERR_INVALID_ARG, "%s: q or t_q must be non-NULL when rows > 0", name);
+    const Range outs[] = {range_of(q, q ? (size_t)rows * (size_t)depth : 0), range_of(scales, scales ? scale_bytes(rows, depth, tile) : 0),
+                          range_of(t_q, t_q ? (size_t)cols * (size_t)t_depth : 0),
+                          range_of(t_scales, t_scales ? scale_bytes(cols, t_depth, tile) : 0)};
+    const Range ins[] = {rows_range(x, rows, cols, ld_x, element_size(dtype))};
+    DV_CHECK(no_overlap(name, outs, ins));
+    const dv::QuantizeArgs a{x, ld_x, dtype, rows, cols, tile != 1, static_cast<uint8_t *>(q), scales,
+                             static_cast<uint8_t *>(t_q), t_scales};
+    return hip_status(dv::launch_quantize_f8(a, static_cast<hipStream_t>(stream)), "dv_quantize_f8 launch");
+}
+
+namespace {
+
+bool product_sizes_ok(int32_t rows, int32_t cols, int32_t depth)
+{
+    return rows >= 0 && rows <= DV_MAX_TOKENS && cols >= 1 && cols <= DV_MAX_TOKENS && depth >= DV_SCALE_BLOCK &&
+           depth <= DV_MAX_DEPTH && depth % DV_SCALE_BLOCK == 0 && (int64_t)rows * cols < (int64_t)1 << 36;
+}
+
+}  // namespace
+
+size_t dv_product_f8_workspace_bytes(int32_t rows, int32_t cols, int32_t depth)
+{
+    return product_sizes_ok(rows, cols, depth) ? dv::product_f8_workspace_bytes(rows, cols, depth) : 0;
+}
+
+dv_status dv_product_f8(const void *a, int64_t ld_a, const float *a_scales, const void *b, int64_t ld_b,
+                        const float *b_scales, int32_t tile, int32_t rows, int32_t cols, int32_t depth, int32_t dtype,
+                        void *out, int64_t ld_out, void *workspace, size_t workspace_bytes, void *stream)
+{
+    g_error[0] = '\0';
+    const char *name = "dv_product_f8";
+    if (!b || !b_scales || (rows > 0 && (!a || !a_scales || !out)))
+        return fail(DV_ERR_INVALID_ARG, "%s: b and b_scales must be non-NULL, a, a_scales and out when rows > 0", name);
+    DV_CHECK(train_sizes(name, {0, 1, dtype}));
+    DV_CHECK(tile_arg(name, tile));
+    if (!product_sizes_ok(rows, cols, depth))
+        return fail(DV_ERR_SHAPE, "%s: rows=%d in [0, %d], cols=%d in [1, %d], fewer than 2^36 results, depth=%d a multiple of 128 in [128, %d]",
+                    name, rows, DV_MAX_TOKENS, cols, DV_MAX_TOKENS, depth, DV_MAX_DEPTH);
+    DV_CHECK(row_stride(name, "ld_a", ld_a, depth));
+    DV_CHECK(row_stride(name, "ld_b", ld_b, depth));
+    if (ld_a % 16 || ld_b % 16 || ld_a > DV_MAX_DEPTH || ld_b > DV_MAX_DEPTH)
+        return fail(DV_ERR_SHAPE, "%s: ld_a=%lld and ld_b=%lld must be multiples of 16 and at most %d", name, (long long)ld_a,
+                    (long long)ld_b, DV_MAX_DEPTH);
+    DV_CHECK(row_stride(name, "ld_out", ld_out, cols));
+    const size_t elt = element_size(dtype);
+    DV_CHECK(aligned(name, "a", a, 16));
+    DV_CHECK(aligned(name, "b", b, 16));
+    DV_CHECK(aligned(name, "out", out, elt));
+    if (rows == 0)
+        return DV_OK;
+    const size_t need = dv::product_f8_workspace_bytes(rows, cols, depth);
+    if (need)
+        DV_CHECK(workspace_args(name, workspace, workspace_bytes, need));
+    const Range outs[] = {rows_range(out, rows, cols, ld_out, elt), range_of(workspace, need)};
+    const Range ins[] = {rows_range(a, rows, depth, ld_a, 1), rows_range(b, cols, depth, ld_b, 1),
+                         range_of(a_scales, scale_bytes(rows, depth, 1)), range_of(b_scales, scale_bytes(cols, depth, tile))};
+    DV_CHECK(no_overlap(name, outs, ins));
+    const dv::ProductArgs p{static_cast<const uint8_t *>(a), ld_a, a_scales, static_cast<const uint8_t *>(b), ld_b, b_scales,
+                            tile != 1, rows, cols, depth, dtype, out, ld_out};
+    return hip_status(dv::launch_product_f8(p, workspace, static_cast<hipStream_t>(stream)), "dv_product_f8 launch");
+}
+
+dv_status dv_adjust_logits(const void *logits, int64_t ld_logits, int32_t dtype, int32_t rows, int32_t num_tokens,
+                           const int32_t *history, int64_t ld_history, int32_t max_history, const int32_t *lengths,
+                           const int32_t *prompt_lengths, const float *repetition, const float *presence,
+                           const float *frequency, const int32_t *bias_ids, const float *bias, int32_t num_bias,
+                           const uint32_t *allow, int32_t num_states, const int32_t *states, void *out, int64_t ld_out,
+                           void *stream)
+{
+    g_error[0] = '\0';
+    const char *name = "dv_adjust_logits";
+    if (rows > 0 && (!logits || !out))
+        return fail(DV_ERR_INVALID_ARG, "%s: logits and out must be non-NULL when rows > 0", name);
+    DV_CHECK(train_sizes(name, {rows, num_tokens, dtype}));
+    if (max_history < 0 || max_history > DV_MAX_HISTORY)
+        return fail(DV_ERR_SHAPE, "%s: max_history=%d outside [0, %d]", name, max_history, DV_MAX_HISTORY);
+    if (num_bias < 0 || num_bias > DV_MAX_BIAS)
+        return fail(DV_ERR_SHAPE, "%s: num_bias=%d outside [0, %d]", name, num_bias, DV_MAX_BIAS);
+    if (rows > 0 && max_history > 0 && (!history || !lengths))
+        return fail(DV_ERR_INVALID_ARG, "%s: history and lengths must be non-NULL with max_history > 0", name);
+    if (rows > 0 && num_bias > 0 && (!bias_ids || !bias))
+        return fail(DV_ERR_INVALID_ARG, "%s: bias_ids and bias must be non-NULL with num_bias > 0", name);
+    if (max_history > 0)
+        DV_CHECK(row_stride(name, "ld_history", ld_history, max_history));
+    DV_CHECK(row_stride(name, "ld_logits", ld_logits, num_tokens));
+    DV_CHECK(row_stride(name, "ld_out", ld_out, num_tokens));
+    if ((int64_t)rows * (((int64_t)num_tokens + 8191) / 8192) >= (int64_t)1 << 24)
+        return fail(DV_ERR_SHAPE, "%s: %d rows of %d tokens are too many", name, rows, num_tokens);
+    DV_CHECK(mask_args(name, allow, num_states, states, rows));
+    const size_t elt = element_size(dtype), n = (size_t)rows;
+    DV_CHECK(aligned(name, "logits", logits, elt));
+    DV_CHECK(aligned(name, "out", out, elt));
+    if (rows == 0)
+        return DV_OK;
+    const bool in_place = out == logits && (ld_out == ld_logits || rows == 1);
+    const Range outs[] = {rows_range(out, rows, num_tokens, ld_out, elt)};
+    const Range ins[] = {in_place ? range_of(nullptr, 0) : rows_range(logits, rows, num_tokens, ld_logits, elt),
+                         max_history ? rows_range(history, rows, max_history, ld_history, 4) : range_of(nullptr, 0),
+                         range_of(lengths, max_history ? n * 4 : 0), range_of(prompt_lengths, prompt_lengths ? n * 4 : 0),
+                         range_of(repetition, repetition ? n * 4 : 0), range_of(presence, presence ? n * 4 : 0),
+                         range_of(frequency, frequency ? n * 4 : 0), range_of(bias_ids, n * (size_t)num_bias * 4),
+                         range_of(bias, n * (size_t)num_bias * 4), allow_range(allow, num_states, num_tokens),
+                         range_of(states, states ? n * 4 : 0)};
+    DV_CHECK(no_overlap(name, outs, ins));
+    const dv::AdjustArgs a{logits,     ld_logits,  dtype,     rows,     num_tokens, max_history ? history : nullptr,
+                           ld_history, max_history, lengths,  prompt_lengths, repetition, presence,
+                           frequency,  bias_ids,   bias,      num_bias, {allow, states, num_states}, out, ld_out};
+    return hip_status(dv::launch_adjust_logits(a, static_cast<hipStream_t>(stream)), "dv_adjust_logits launch");
 }
 
 }  // extern "C"

@@ -1,0 +1,335 @@
+// Root-mean-square norm with the residual's addition, and its gradients.
+//
+//     h = x + residual, rounded to the inputs' type (what the next layer adds to)
+//     r = 1 / sqrt(mean of h^2 + eps),   y = h r w
+//     u = h r,   dh = r (g w - u / D  sum of (g w u)) + dtotal,   dw = sum over rows of g u
+//
+// y leaves in the inputs' type, or in e4m3 with a scale for every 128 columns, which is
+// how the 8-bit head product reads it.
+//
+// Memory-bound: each row is read once and held in registers, 8 columns a lane and
+// vector, by one wave (up to 1,024 columns) or one block.
+#include "dv_logits.h"
+
+namespace dv {
+namespace {
+
+// Sum over the threads of a row: a wave, or a block through LDS.  `sums` is free again
+// for what comes after the block's next barrier.
+template <int THREADS>
+__device__ __forceinline__ float row_sum(float v, float *sums)
+{
+    v = wave_sum(v);
+    if constexpr (THREADS > kWave) {
+        constexpr int kWaves = THREADS / kWave;
+        if ((threadIdx.x & (kWave - 1)) == 0)
+            sums[threadIdx.x / kWave] = v;
+        __syncthreads();
+        v = 0.f;
+#pragma unroll
+        for (int i = 0; i < kWaves; ++i)
+            v += sums[i];
+    }
+    return v;
+}
+
+// The bits of the largest magnitude over the threads of a row, likewise.
+template <int THREADS>
+__device__ __forceinline__ uint32_t row_largest(uint32_t v, float *sums)
+{
+    v = wave_reduce<true>(v);
+    if constexpr (THREADS > kWave) {
+        if ((threadIdx.x & (kWave - 1)) == 0)
+            sums[threadIdx.x / kWave] = __uint_as_float(v);
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < THREADS / kWave; ++i)
+            v = larger(v, __float_as_uint(sums[i]));
+    }
+    return v;
+}
+
+// THREADS take a row, NV vectors of 8 columns each; blocks hold max(THREADS, 256) threads.
+template <typename T, int THREADS, int NV>
+__global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void norm_kernel(const T *x, int64_t ld_x, const T *residual,
+                                                                             int64_t ld_residual, const T *weight,
+                                                                             int rows, int hidden, float eps, T *total,
+                                                                             T *out, float *rstd, uint8_t *q, float *scales)
+{
+    constexpr int kRows = THREADS < 256 ? 256 / THREADS : 1;  // of a block
+    __shared__ float sums[3][kRows == 1 ? THREADS / kWave : 1];
+    const int t = threadIdx.x % THREADS;
+    const int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / THREADS;
+    if (kRows > 1 && row >= rows)  // whole waves
+        return;
+    float h[NV][8];
+    float sum = 0.f;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+        const int c = (v * THREADS + t) * 8;
+        load8(h[v], x + row * ld_x, c, hidden);
+        if (residual) {
+            float y[8];
+            load8(y, residual + row * ld_residual, c, hidden);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                h[v][e] += y[e];
+                if constexpr (sizeof(T) == 2)
+                    h[v][e] = widen(narrow(h[v][e]));
+            }
+        }
+        if (total)
+            store8(total + row * hidden, c, hidden, h[v]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            sum = __builtin_fmaf(h[v][e], h[v][e], sum);
+    }
+    sum = row_sum<THREADS>(sum, sums[0]);
+    float mean = sum / (float)hidden + eps, unit = 1.f;
+    if (!(mean >= 0x1p-90f && sum <= 0x1p120f)) {
+        // squares out of range: the same of h times a power of two, if the row is finite
+        uint32_t m = 0;
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                m = larger(m, magnitude(h[v][e]));
+        m = row_largest<THREADS>(m, sums[1]);
+        if (m && m < 0x7F800000u) {
+            const int up = 127 - (int)(m >> 23);
+            unit = __builtin_ldexpf(1.f, up < 100 ? up : 100);
+            sum = 0.f;
+#pragma unroll
+            for (int v = 0; v < NV; ++v)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    h[v][e] *= unit;
+                    sum = __builtin_fmaf(h[v][e], h[v][e], sum);
+                }
+            sum = row_sum<THREADS>(sum, sums[2]);
+            mean = sum / (float)hidden + eps * unit * unit;
+        }
+    }
+    const float r = 1.f / sqrtf(mean);
+    if (rstd && t == 0)
+        rstd[row] = r * unit;
+    const int64_t depth = up_block(hidden);
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+        const int c = (v * THREADS + t) * 8;
+        float w[8];
+        load8(w, weight, c, hidden);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            h[v][e] = h[v][e] * r * w[e];
+        if (out)
+            store8(out + row * hidden, c, hidden, h[v]);
+        if (q) {  // 16 lanes hold a block; lanes past the depth take part with zeros
+            uint32_t m = 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                m = larger(m, magnitude(h[v][e]));
+            const BlockScale s(largest16(m));
+            if (c < depth) {
+                *reinterpret_cast<uint2 *>(q + row * depth + c) = quantize8(h[v], s);
+                if ((t & 15) == 0)
+                    scales[(int64_t)(c / kScaleBlock) * rows + row] = s.scale;
+            }
+        }
+    }
+}
+
+// Blocks take every gridDim.x-th row.  HELD: a row's h and g stay in registers, else
+// (the longest rows) they are read again.  Each block's share of dw goes to `partial`
+// [gridDim.x][hidden].
+template <typename T, int THREADS, int NV, bool HELD>
+__global__ __launch_bounds__(THREADS) void norm_grad_kernel(const T *grad_out, int64_t ld_g, const T *total, int64_t ld_h,
+                                                            const T *weight, const float *rstd, const T *grad_total,
+                                                            int64_t ld_gt, int rows, int hidden, T *grad_x, float *partial)
+{
+    __shared__ float sums[2][THREADS / kWave];
+    float dw[NV][8];
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            dw[v][e] = 0.f;
+    int half = 0;
+    for (int64_t row = blockIdx.x; row < rows; row += gridDim.x) {
+        const T *gr = grad_out + row * ld_g, *hr = total + row * ld_h;
+        const float r = rstd[row];
+        float h[HELD ? NV : 1][8], g[HELD ? NV : 1][8];
+        float sum = 0.f;
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const int at = HELD ? v : 0;
+            const int c = (v * THREADS + threadIdx.x) * 8;
+            load8(h[at], hr, c, hidden);
+            load8(g[at], gr, c, hidden);
+            float w[8];
+            load8(w, weight, c, hidden);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                h[at][e] *= r;
+                dw[v][e] = __builtin_fmaf(g[at][e], h[at][e], dw[v][e]);
+                g[at][e] *= w[e];
+                sum = __builtin_fmaf(g[at][e], h[at][e], sum);
+            }
+        }
+        if (!grad_x)
+            continue;
+        sum = row_sum<THREADS>(sum, sums[half]);
+        half ^= 1;  // the next row's sums meet elsewhere: its barrier comes after everyone has read these
+        const float k = sum / (float)hidden;
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const int at = HELD ? v : 0;
+            const int c = (v * THREADS + threadIdx.x) * 8;
+            if constexpr (!HELD) {
+                load8(h[at], hr, c, hidden);
+                load8(g[at], gr, c, hidden);
+                float w[8];
+                load8(w, weight, c, hidden);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    h[at][e] *= r;
+                    g[at][e] *= w[e];
+                }
+            }
+            float d[8];
+            if (grad_total) {
+                load8(d, grad_total + row * ld_gt, c, hidden);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    d[e] = 0.f;
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                d[e] = __builtin_fmaf(r, g[at][e] - h[at][e] * k, d[e]);
+            store8(grad_x + row * hidden, c, hidden, d);
+        }
+    }
+    if (partial)
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+            store8(partial + (int64_t)blockIdx.x * hidden, (v * THREADS + threadIdx.x) * 8, hidden, dw[v]);
+}
+
+// dw: the blocks' shares added, 64 columns a block, 16 waves a share of the rows each.
+template <typename T>
+__global__ __launch_bounds__(1024) void norm_weight_kernel(const float *partial, int parts, int hidden, T *grad_weight)
+{
+    __shared__ float sh[16][kWave];
+    const int lane = threadIdx.x & (kWave - 1), slice = threadIdx.x / kWave;
+    const int c = blockIdx.x * kWave + lane;
+    float s = 0.f;
+    if (c < hidden)
+        for (int p = slice; p < parts; p += 16)
+            s += partial[(int64_t)p * hidden + c];
+    sh[slice][lane] = s;
+    __syncthreads();
+    if (slice || c >= hidden)
+        return;
+    s = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+        s += sh[i][lane];
+    if constexpr (sizeof(T) == 2)
+        grad_weight[c] = narrow(s);
+    else
+        grad_weight[c] = s;
+}
+
+template <typename T>
+hipError_t launch_norm(const NormArgs &a, hipStream_t stream)
+{
+    const auto go = [&](auto kernel, int threads) {
+        const int per_block = threads < 256 ? 256 / threads : 1;
+        const unsigned grid = (unsigned)((a.rows + per_block - 1) / per_block);
+        kernel<<<grid, threads < 256 ? 256 : threads, 0, stream>>>(
+            static_cast<const T *>(a.x), a.ld_x, static_cast<const T *>(a.residual), a.ld_residual,
+            static_cast<const T *>(a.weight), a.rows, a.hidden, a.eps, static_cast<T *>(a.total), static_cast<T *>(a.out),
+            a.rstd, a.q, a.scales);
+    };
+    const int64_t depth = up_block(a.hidden);
+    if (depth <= 512)
+        go(norm_kernel<T, 64, 1>, 64);
+    else if (depth <= 1024)
+        go(norm_kernel<T, 64, 2>, 64);
+    else if (depth <= 2048)
+        go(norm_kernel<T, 256, 1>, 256);
+    else if (depth <= 4096)
+        go(norm_kernel<T, 256, 2>, 256);
+    else if (depth <= 8192)
+        go(norm_kernel<T, 256, 4>, 256);
+    else if (depth <= 16384)
+        go(norm_kernel<T, 1024, 2>, 1024);
+    else if (depth <= 32768)
+        go(norm_kernel<T, 1024, 4>, 1024);
+    else
+        go(norm_kernel<T, 1024, 8>, 1024);
+    return last_launch();
+}
+
+// Blocks of the backward pass: each leaves a share of dw, so no more than fill the card.
+int grad_blocks(int rows, int hidden)
+{
+    const int most = hidden <= 8192 ? 1024 : 256;
+    return rows < most ? rows : most;
+}
+
+template <typename T>
+hipError_t launch_grad(const NormGradArgs &a, float *partial, hipStream_t stream)
+{
+    const int blocks = grad_blocks(a.rows, a.hidden);
+    const auto go = [&](auto kernel, int threads) {
+        kernel<<<(unsigned)blocks, threads, 0, stream>>>(
+            static_cast<const T *>(a.grad_out), a.ld_grad_out, static_cast<const T *>(a.total), a.ld_total,
+            static_cast<const T *>(a.weight), a.rstd, static_cast<const T *>(a.grad_total), a.ld_grad_total, a.rows,
+            a.hidden, static_cast<T *>(a.grad_x), a.grad_weight ? partial : nullptr);
+    };
+    if (a.rows > 0) {
+        if (a.hidden <= 512)
+            go(norm_grad_kernel<T, 64, 1, true>, 64);
+        else if (a.hidden <= 1024)
+            go(norm_grad_kernel<T, 128, 1, true>, 128);
+        else if (a.hidden <= 2048)
+            go(norm_grad_kernel<T, 256, 1, true>, 256);
+        else if (a.hidden <= 4096)
+            go(norm_grad_kernel<T, 256, 2, true>, 256);
+        else if (a.hidden <= 8192)
+            go(norm_grad_kernel<T, 512, 2, true>, 512);
+        else if (a.hidden <= 16384)
+            go(norm_grad_kernel<T, 1024, 2, true>, 1024);
+        else if (a.hidden <= 32768)
+            go(norm_grad_kernel<T, 1024, 4, false>, 1024);
+        else
+            go(norm_grad_kernel<T, 1024, 8, false>, 1024);
+    }
+    if (a.grad_weight)
+        norm_weight_kernel<T><<<(unsigned)((a.hidden + kWave - 1) / kWave), 1024, 0, stream>>>(
+            partial, blocks, a.hidden, static_cast<T *>(a.grad_weight));
+    return last_launch();
+}
+
+}  // namespace
+
+hipError_t launch_rms_norm(const NormArgs &a, hipStream_t stream)
+{
+    return a.dtype == 1 ? launch_norm<uint16_t>(a, stream) : launch_norm<float>(a, stream);
+}
+
+size_t rms_norm_backward_workspace_bytes(int rows, int hidden)
+{
+    const int blocks = grad_blocks(rows, hidden);
+    return align_up((size_t)(blocks > 0 ? blocks : 1) * (size_t)hidden * 4, 256);
+}
+
+hipError_t launch_rms_norm_backward(const NormGradArgs &a, void *workspace, hipStream_t stream)
+{
+    float *partial = static_cast<float *>(workspace);
+    return a.dtype == 1 ? launch_grad<uint16_t>(a, partial, stream) : launch_grad<float>(a, partial, stream);
+}
+
+}  // namespace dv

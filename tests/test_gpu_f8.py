@@ -1,0 +1,164 @@
+"""8-bit operands: quantization bit for bit against its definition, products
+against the sums in 64 bits."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from tests.logits_common import B, product_reference, quantize, up
+from tests.train_common import check
+
+pytestmark = pytest.mark.gpu
+DEV = torch.device("cuda:0")
+BF, F32 = torch.bfloat16, torch.float32
+
+
+@pytest.fixture(scope="module")
+def dv():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import paper_2403_06988_amd as dv_mod
+    return dv_mod
+
+
+def same(q, want):
+    return torch.equal(q.cpu().view(torch.uint8), want.view(torch.uint8))
+
+
+def nan_equal(a, b):
+    a = a.cpu()
+    return a.shape == b.shape and bool(((a == b) | (torch.isnan(a) & torch.isnan(b))).all())
+
+
+def source(rng, N, K, dtype, pad=0, shift=0):
+    t = torch.from_numpy(rng.normal(size=(N, K)) * np.exp(rng.normal(size=(N, 1)) * 3)).to(dtype)
+    buf = torch.full((N * (K + pad) + shift + 8,), math.nan, dtype=dtype, device=DEV)
+    view = buf[shift:shift + N * (K + pad)].view(N, K + pad)[:, :K]
+    view.copy_(t)
+    return view, t
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("tile", [1, 128])
+@pytest.mark.parametrize("N,K,pad,shift", [(1, 1, 0, 0), (1, 128, 0, 0), (128, 1, 3, 1), (127, 129, 1, 1), (257, 100, 4, 0),
+                                           (64, 1024, 0, 0), (1000, 515, 5, 3), (3, 4099, 0, 1)])
+def test_quantize_is_its_definition(dv, N, K, pad, shift, tile, dtype):
+    rng = np.random.default_rng(N * 5003 + K + tile)
+    x, t = source(rng, N, K, dtype, pad, shift)
+    want, want_s = quantize(t, tile)
+    want_t, want_ts = quantize(t.t().contiguous(), tile)
+    q, s, tq, ts = dv.quantize_f8(x, tile=tile, want_columns=True)
+    assert q.shape == (N, up(K)) and tq.shape == (K, up(N))
+    assert torch.equal(s.cpu(), want_s) and torch.equal(ts.cpu(), want_ts)
+    assert same(q, want) and same(tq, want_t)
+    q2, s2, none, none2 = dv.quantize_f8(x, tile=tile)
+    assert none is None and none2 is None and same(q2, want) and torch.equal(s2, s)
+    none, none2, tq2, ts2 = dv.quantize_f8(x, tile=tile, want_rows=False, want_columns=True)
+    assert none is None and none2 is None and same(tq2, want_t) and torch.equal(ts2, ts)
+
+
+@pytest.mark.parametrize("tile", [1, 128])
+def test_quantize_borders(dv, tile):
+    """Every bf16 mantissa against block maxima of every mantissa: quotients on and next to the borders."""
+    m = 1 + torch.arange(128).float() / 128
+    t = torch.zeros((128, 128 * 3))
+    t[:, :128] = m[None, :] / 2
+    t[:, 0] = m                                 # a row's largest
+    t[:, 128:256] = m[None, :] * 2.0 ** -torch.arange(128)[:, None].float().remainder(12)
+    t[:, 256:] = -m[:, None] * (1 - 2.0 ** -8 * torch.arange(128)[None, :].float())
+    for dtype in (BF, F32):
+        q, s, tq, ts = dv.quantize_f8(t.to(dtype).to(DEV), tile=tile, want_columns=True)
+        want, want_s = quantize(t.to(dtype), tile)
+        want_t, want_ts = quantize(t.to(dtype).t().contiguous(), tile)
+        assert torch.equal(s.cpu(), want_s) and same(q, want)
+        assert torch.equal(ts.cpu(), want_ts) and same(tq, want_t)
+
+
+@pytest.mark.parametrize("tile", [1, 128])
+def test_quantize_special_values(dv, tile):
+    t = torch.from_numpy(np.random.default_rng(2).normal(size=(300, 300))).float()
+    t[0, :128] = 0
+    t[1] = 1e-38                                # far below 2^-100
+    t[2, 7] = math.inf
+    t[3, 200] = math.nan
+    t[4, 131] = -math.inf
+    t[5] = t[5].clamp(-3, 3) * 1e38
+    t[128:256, 128:256] = 0
+    t[128:256, :128] *= 2.0 ** -120
+    q, s, tq, ts = dv.quantize_f8(t.to(DEV), tile=tile, want_columns=True)
+    want, want_s = quantize(t, tile)
+    want_t, want_ts = quantize(t.t().contiguous(), tile)
+    assert nan_equal(s, want_s) and same(q, want)
+    assert nan_equal(ts, want_ts) and same(tq, want_t)
+
+
+def operands(rng, M, N, K, tile):
+    def one(n, t):
+        x = torch.from_numpy(rng.normal(size=(n, K)) * np.exp(rng.normal(size=(n, 1))))
+        return quantize(x.float(), t)
+    return (*one(M, 1), *one(N, tile))
+
+
+SHAPES = [(1, 1, 128), (1, 129, 256), (2, 16, 128), (16, 128, 384), (17, 130, 1024), (33, 1000, 640), (64, 257, 2048),
+          (65, 500, 128), (100, 1, 256), (129, 127, 384), (200, 300, 1152), (257, 513, 256), (300, 64, 4224), (1, 5000, 4096),
+          (3, 20000, 1024), (520, 1030, 512)]
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("tile", [1, 128])
+@pytest.mark.parametrize("M,N,K", SHAPES)
+def test_product(dv, M, N, K, tile, dtype):
+    a, sa, b, sb = operands(np.random.default_rng(M * 31 + N * 7 + K), M, N, K, tile)
+    want, tol = product_reference(a, sa, b, sb, tile, dtype)
+    to = lambda t: t.to(DEV)  # noqa: E731
+    out = dv.product_f8(to(a), to(sa), to(b), to(sb), tile=tile, dtype=dtype)
+    check(out, want, tol, "product")
+    # the same bits again, and in a wider buffer whose other elements stay
+    wide = torch.full((M, N + 5), 3.0, dtype=dtype, device=DEV)
+    dv.product_f8(to(a), to(sa), to(b), to(sb), tile=tile, out=wide[:, 2:N + 2])
+    assert torch.equal(wide[:, 2:N + 2], out)
+    assert (wide[:, :2] == 3).all() and (wide[:, N + 2:] == 3).all()
+
+
+def test_product_of_wider_rows(dv):
+    """Rows 16-byte apart beyond the depth; the bytes between belong to others (NaN here)."""
+    rng = np.random.default_rng(4)
+    M, N, K = 70, 200, 256
+    a, sa, b, sb = operands(rng, M, N, K, 128)
+    want = dv.product_f8(a.to(DEV), sa.to(DEV), b.to(DEV), sb.to(DEV))
+    wa = torch.full((M, K + 16), 0x7F, dtype=torch.uint8, device=DEV).view(dv.F8)
+    wb = torch.full((N, K + 48), 0x7F, dtype=torch.uint8, device=DEV).view(dv.F8)
+    wa.view(torch.uint8)[:, :K] = a.view(torch.uint8).to(DEV)
+    wb.view(torch.uint8)[:, :K] = b.view(torch.uint8).to(DEV)
+    assert torch.equal(dv.product_f8(wa[:, :K], sa.to(DEV), wb[:, :K], sb.to(DEV)), want)
+
+
+def test_product_special_values(dv):
+    """NaN of a row or a tile stays there; scales of any size; a row of zeros."""
+    rng = np.random.default_rng(9)
+    for M in (5, 40, 150):
+        a, sa, b, sb = operands(rng, M, 300, 256, 128)
+        qa = a.view(torch.uint8).clone()
+        qa[1, 3] = 0x7F
+        qa[2] = 0
+        sa[1, 3] = 1e-30
+        sa[0, 4] = 1e30
+        sb[1, 1] = math.nan                        # n in [128, 256), k in [128, 256)
+        a = qa.view(torch.float8_e4m3fn)
+        out = dv.product_f8(a.to(DEV), sa.to(DEV), b.to(DEV), sb.to(DEV), dtype=F32).cpu()
+        assert torch.isnan(out[1]).all() and torch.isnan(out[:, 128:256]).all()
+        assert (out[2, :128] == 0).all() and (out[2, 256:] == 0).all()
+        want, tol = product_reference(a, sa, b, sb, 128, F32)
+        keep = [m for m in range(M) if m != 1]
+        for cols in (slice(0, 128), slice(256, 300)):
+            check(out[keep][:, cols], want[keep][:, cols], tol[keep][:, cols], f"beside NaN, M {M}")
+
+
+def test_no_rows(dv):
+    b, sb = quantize(torch.randn(100, 128), 128)
+    a = torch.empty((0, 128), dtype=dv.F8, device=DEV)
+    out = dv.product_f8(a, torch.empty((1, 0), device=DEV), b.to(DEV), sb.to(DEV))
+    assert out.shape == (0, 100)
+    q, s, tq, ts = dv.quantize_f8(torch.empty((0, 100), device=DEV), want_columns=True)
+    assert q.shape == (0, 128) and s.shape == (1, 0) and tq.shape == (100, 0) and ts.shape == (0, 100)
