@@ -4,7 +4,7 @@
 // row starts are on 16-byte boundaries.  B may be a bf16 operand in two parts.
 #pragma once
 
-#include "dv_internal.h"
+#include "dv_train.h"
 
 namespace dv {
 
@@ -486,6 +486,38 @@ struct Gemm {
                         acc[i][j] = (acc[i][j] + more[1][i][j]) + more[0][i][j];
                 }
         }
+    }
+};
+
+// A wave's results on their way out: 16 rows (index j of the product, one a lane of
+// each 16) of COLS columns (index i, four a lane) go through LDS, so that they
+// leave as 16-byte pieces of whole lines (8-byte stores of 16 rows at a time,
+// straight from the registers, wrote 1 GB at 1.3 TB/s).
+template <typename T, int COLS>
+struct RowStage {
+    static constexpr int kPitch = COLS * (int)sizeof(T) + 16;
+    static constexpr int kBytes = 16 * kPitch;
+    static constexpr int kN = 16 / (int)sizeof(T);        // elements of a piece
+    static constexpr int kLanesPerRow = COLS / kN;
+    static constexpr int kRowsAtOnce = kWave / kLanesPerRow;
+    static_assert(kLanesPerRow <= kWave && kWave % kLanesPerRow == 0, "whole rows at once");
+
+    // four elements of fragment a, from lane `lane`
+    static __device__ __forceinline__ void put(char *lds, int lane, int a, const T (&y)[4])
+    {
+        __builtin_memcpy(lds + (lane & 15) * kPitch + (a * 16 + (lane >> 4) * 4) * (int)sizeof(T), y, sizeof y);
+    }
+    // f(row of the 16, first column, piece) for each of this lane's pieces
+    template <typename F>
+    static __device__ __forceinline__ void each(const char *lds, int lane, F &&f)
+    {
+        wave_lds_sync();
+#pragma unroll
+        for (int r = 0; r < 16; r += kRowsAtOnce) {
+            const int row = r + lane / kLanesPerRow, piece = lane % kLanesPerRow;
+            f(row, piece * kN, *reinterpret_cast<const Words *>(lds + row * kPitch + piece * 16));
+        }
+        wave_lds_sync();
     }
 };
 

@@ -19,13 +19,6 @@ namespace dv {
 namespace {
 
 typedef __attribute__((ext_vector_type(8))) int i32x8;
-typedef __attribute__((ext_vector_type(4))) int i32x4;
-
-__device__ __forceinline__ f32x4 mfma8(i32x8 a, i32x8 b)
-{
-    const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, zero, 0, 0, 0, 0, 0, 0);
-}
 
 struct ProductShape {
     GemmOperand b, a;  // in units of two bytes, as dv_gemm.h takes them
@@ -34,17 +27,59 @@ struct ProductShape {
     int blocks;        // of 128 k
 };
 
-template <int BM, int BN, int WM, int WN, bool TILES>
+// A lane's 32 e4m3 values of a fragment (16 rows of 128 k), as the 8-bit matrix instruction
+// takes them, or (EXACT) as bf16, which holds each of them.
+template <bool EXACT>
+struct Fragment8 {
+    i32x8 v;
+    __device__ __forceinline__ void set(i32x8 x) { v = x; }
+    static __device__ __forceinline__ f32x4 multiply(const Fragment8 &a, const Fragment8 &b)
+    {
+        return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a.v, b.v, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);
+    }
+};
+template <>
+struct Fragment8<true> {
+    bf16x8 part[4];
+    __device__ __forceinline__ void set(i32x8 x)
+    {
+        typedef __attribute__((ext_vector_type(2))) __bf16 Pair;
+#pragma unroll
+        for (int w = 0; w < 8; ++w) {
+            const Pair lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((unsigned)x[w], 1.f, false);
+            const Pair hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((unsigned)x[w], 1.f, true);
+            part[w / 2][w % 2 * 4] = lo[0];
+            part[w / 2][w % 2 * 4 + 1] = lo[1];
+            part[w / 2][w % 2 * 4 + 2] = hi[0];
+            part[w / 2][w % 2 * 4 + 3] = hi[1];
+        }
+    }
+    static __device__ __forceinline__ f32x4 multiply(const Fragment8 &a, const Fragment8 &b)
+    {
+        f32x4 p = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int h = 0; h < 4; ++h)
+            p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.part[h], b.part[h], p, 0, 0, 0);
+        return p;
+    }
+};
+
+template <int BM, int BN, int WM, int WN, bool TILES, bool EXACT>
 struct Product8 {
     using G = Gemm<__bf16, BM, BN, WM, WN>;
     using A = typename G::A;
     using B = typename G::B;
-    static constexpr int kTm = G::kTm, kTn = G::kTn, kLoads = G::kLoads;
-    static constexpr int kLdsBytes = G::kLdsBytes;
+    using Fragment = Fragment8<EXACT>;
+    static constexpr int kTm = G::kTm, kTn = G::kTn, kLoads = G::kLoads, kWaves = G::kWaves;
+    // by rows, b's scales of a stage stand in LDS behind the operands
+    static constexpr int kScaleBytes = TILES ? 0 : BM * 4;
+    static constexpr int kStageBytes = G::kStageBytes + kScaleBytes;
+    static constexpr int kLdsBytes = 2 * kStageBytes;
     static_assert(!TILES || BM / WM <= kScaleBlock, "one scale of b a wave");
+    static_assert(TILES || BM / kWave <= kWaves, "a wave loads 64 scales at most");
 
     template <typename S>
-    static __device__ __forceinline__ i32x8 fragment(const char *tile, int at0, int at1, int i)
+    static __device__ __forceinline__ i32x8 raw(const char *tile, int at0, int at1, int i)
     {
         union {
             bf16x8 half[2];
@@ -55,6 +90,7 @@ struct Product8 {
         return f.v;
     }
 
+    // acc += the tile at i0 of b and j0 of a, over `stages` blocks of 128 k from `from` on.
     static __device__ __forceinline__ void run(f32x4 (&acc)[kTm][kTn], const ProductShape &g, int i0, int j0, int from,
                                                int stages, char *lds)
     {
@@ -72,10 +108,15 @@ struct Product8 {
 #pragma unroll
         for (int i = 0; i < kLoads; ++i)
             voff[i] = side_a(i) ? A::source(g.b, i0, group + i, lane, 0) : B::source(g.a, j0, group + i - A::kGroups, lane, 0);
+        const bool loads_scales = !TILES && wave < BM / kWave;
+        const int scale_at = i0 + wave * kWave + lane < g.cols ? i0 + wave * kWave + lane : g.cols - 1;
         int stage = from;
         const auto load = [&](int slot) {
-            const uint32_t dst = (uint32_t)(uintptr_t)(typename G::Lds)(lds + slot * G::kStageBytes);
-            const int64_t at = (int64_t)stage * 128;
+            const uint32_t dst = (uint32_t)(uintptr_t)(typename G::Lds)(lds + slot * kStageBytes);
+            const int64_t at = (int64_t)stage * kScaleBlock;
+            if constexpr (!TILES)
+                if (loads_scales)
+                    load_word_to_lds(g.sb + (int64_t)stage * g.cols, scale_at * 4, dst + G::kStageBytes + wave * kWave * 4);
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) {
                 const int p = group + i;
@@ -87,73 +128,109 @@ struct Product8 {
         const int at_a = wm * (A::kFragmentStep * kTm), at_b = wn * (B::kFragmentStep * kTn);
         const int a0 = at_a + A::place(lane, 0), a1 = at_a + A::place(lane, 1);
         const int b0 = at_b + B::place(lane, 0), b1 = at_b + B::place(lane, 1);
+        const int at_scales = G::kStageBytes + (wm * (BM / WM) + (lane >> 4) * 4) * 4;
 
-        // the scales' places: columns past the end read the last one
-        int jcol[kTn];
+        // the scales of a: rows past the end read the last one
+        int at_sa[kTn];
 #pragma unroll
         for (int j = 0; j < kTn; ++j) {
             const int c = j0 + wn * (BN / WN) + j * 16 + (lane & 15);
-            jcol[j] = c < g.rows ? c : g.rows - 1;
+            at_sa[j] = c < g.rows ? c : g.rows - 1;
         }
         const int iw = i0 + wm * (BM / WM);
         const float *sb_tile = g.sb + (int64_t)((iw < g.cols ? iw : g.cols - 1) / kScaleBlock) * g.blocks;
+        float scale[kTn], next_scale[kTn], next_sb = 1.f;
+        const auto load_scales = [&](int kb) {
+            const float *p = g.sa + (int64_t)kb * g.rows;
+#pragma unroll
+            for (int j = 0; j < kTn; ++j)
+                next_scale[j] = p[at_sa[j]];
+            if constexpr (TILES)
+                next_sb = sb_tile[kb];
+        };
 
+        load_scales(from);
         load(0);
         if (stages > 1)
             load(1);
+        if (stages > 1 && TILES)
+            G::template wait_loads<kLoads>();
+        else
+            G::template wait_loads<0>();
+        G::barrier();
+        Fragment fa, fb[kTn];
+        f32x4 p[2];
+        i32x8 next = raw<A>(lds, a0, a1, 0);
+#pragma unroll
+        for (int j = 0; j < kTn; ++j)
+            fb[j].set(raw<B>(lds + A::kBytes, b0, b1, j));
         for (int s = 0; s < stages; ++s) {
-            const int kb = from + s;
-            float sa[kTn];
+            const char *tile = lds + (s & 1) * kStageBytes;
+            f32x4 sb[2];
+            // a finished product, under its scales
+            const auto add = [&](int i, int j) {
+                const f32x4 x = p[(i * kTn + j) & 1];
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    acc[i][j][e] = __builtin_fmaf(TILES ? x[e] : x[e] * sb[i & 1][e], scale[j], acc[i][j][e]);
+                // here, not where the compiler would sink it to: that takes registers for every product
+                asm volatile("" : "+v"(acc[i][j]));
+            };
 #pragma unroll
             for (int j = 0; j < kTn; ++j)
-                sa[j] = g.sa[(int64_t)kb * g.rows + jcol[j]];
-            if constexpr (TILES) {
-                const float sb = sb_tile[kb];
-#pragma unroll
-                for (int j = 0; j < kTn; ++j)
-                    sa[j] *= sb;
-            }
+                scale[j] = TILES ? next_scale[j] * next_sb : next_scale[j];
             if (s + 1 < stages)
-                G::template wait_loads<kLoads>();
-            else
-                G::template wait_loads<0>();
-            G::barrier();
-            const char *tile = lds + (s & 1) * G::kStageBytes;
-            i32x8 fb[kTn];
-#pragma unroll
-            for (int j = 0; j < kTn; ++j)
-                fb[j] = fragment<B>(tile + A::kBytes, b0, b1, j);
+                load_scales(from + s + 1);
 #pragma unroll
             for (int i = 0; i < kTm; ++i) {
-                const i32x8 fa = fragment<A>(tile, a0, a1, i);
-                f32x4 sb = {1.f, 1.f, 1.f, 1.f};
+                fa.set(next);
                 if constexpr (!TILES)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int c = iw + i * 16 + (lane >> 4) * 4 + e;
-                        sb[e] = g.sb[(int64_t)kb * g.cols + (c < g.cols ? c : g.cols - 1)];
-                    }
+                    sb[i & 1] = *reinterpret_cast<const f32x4 *>(tile + at_scales + i * 64);
+                if (i + 1 < kTm) {
+                    next = raw<A>(tile, a0, a1, i + 1);
+                } else if (s + 1 < stages) {
+                    G::template wait_loads<0>();  // and this wave's reads of the stage
+                    G::barrier();
+                    if (s + 2 < stages)
+                        load(s & 1);
+                    next = raw<A>(lds + ((s + 1) & 1) * kStageBytes, a0, a1, 0);
+                }
+                // a product at a time, the one before it added while it runs
 #pragma unroll
                 for (int j = 0; j < kTn; ++j) {
-                    const f32x4 p = mfma8(fa, fb[j]);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        acc[i][j][e] = __builtin_fmaf(TILES ? p[e] : p[e] * sb[e], sa[j], acc[i][j][e]);
+                    p[(i * kTn + j) & 1] = Fragment::multiply(fa, fb[j]);
+                    if (i + j)
+                        add(j ? i : i - 1, j ? j - 1 : kTn - 1);
+                    __builtin_amdgcn_sched_barrier(0);
+                    if (i + 1 == kTm && s + 1 < stages)
+                        fb[j].set(raw<B>(lds + ((s + 1) & 1) * kStageBytes + A::kBytes, b0, b1, j));
                 }
             }
-            __builtin_amdgcn_s_waitcnt(0xC07F);  // this wave's reads from LDS are done
-            G::barrier();                        // and every wave's are
-            if (s + 2 < stages)
-                load(s & 1);
+            add(kTm - 1, kTn - 1);
         }
+    }
+
+    // 4 bytes a lane from base + offset to LDS, as Gemm::load_to_lds
+    static __device__ __forceinline__ void load_word_to_lds(const float *base, int offset, uint32_t dst)
+    {
+        typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+        const uint64_t p = reinterpret_cast<uint64_t>(base);
+        const u32x4 rsrc = {(uint32_t)p, (uint32_t)(p >> 32) & 0xFFFFu, 0x7FFFFFFFu, 0x00027000u};
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"  // m0 is reserved: not preserved, as meant
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds"
+                     :
+                     : "s"(dst), "v"(offset), "s"(rsrc)
+                     : "memory", "m0");
+#pragma clang diagnostic pop
     }
 };
 
-template <typename T, int BM, int BN, int WM, int WN, bool TILES>
+template <typename T, int BM, int BN, int WM, int WN, bool TILES, bool EXACT>
 __global__ __launch_bounds__(WM *WN *kWave, 2) void product8_kernel(ProductShape g, T *out, int64_t ld, int64_t split_stride,
                                                                     int split_stages, int tiles_i, int tiles_j)
 {
-    using P = Product8<BM, BN, WM, WN, TILES>;
+    using P = Product8<BM, BN, WM, WN, TILES, EXACT>;
     __shared__ __attribute__((aligned(1024))) char lds[P::kLdsBytes];
     int ti, tj;
     tile_of_block(blockIdx.x, tiles_i, tiles_j, ti, tj);
@@ -164,19 +241,38 @@ __global__ __launch_bounds__(WM *WN *kWave, 2) void product8_kernel(ProductShape
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
     const int wm = wave / WN, wn = wave % WN;
     out += blockIdx.y * split_stride;
+    // results leave through LDS in whole lines, 16 rows of them a time
+    using Rows = RowStage<T, BM / WM>;
+    static_assert(WM * WN * Rows::kBytes <= P::kLdsBytes, "every wave has its rows");
+    char *mine = lds + wave * Rows::kBytes;
+    __builtin_amdgcn_s_waitcnt(0xC07F);
+    P::G::barrier();  // the last stage is read
+    const int c0 = ti * BM + wm * (BM / WM);
 #pragma unroll
     for (int j = 0; j < P::kTn; ++j) {
-        const int r = tj * BN + wn * (BN / WN) + j * 16 + (lane & 15);
-        if (r >= g.rows)
-            continue;
+        const int r0 = tj * BN + wn * (BN / WN) + j * 16;
+        if (r0 >= g.rows)
+            break;
 #pragma unroll
-        for (int i = 0; i < P::kTm; ++i)
+        for (int i = 0; i < P::kTm; ++i) {
+            T y[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int c = ti * BM + wm * (BM / WM) + i * 16 + (lane >> 4) * 4 + e;
-                if (c < g.cols)
-                    out[r * ld + c] = (T)acc[i][j][e];
+            for (int e = 0; e < 4; ++e)
+                y[e] = (T)acc[i][j][e];
+            Rows::put(mine, lane, i, y);
+        }
+        Rows::each(mine, lane, [&](int row, int col, Words y) {
+            T *to = out + (int64_t)(r0 + row) * ld + c0 + col;
+            const int left = r0 + row < g.rows ? g.cols - c0 - col : 0;
+            if (left >= Rows::kN) {
+                store_words(to, y);
+            } else {
+#pragma unroll
+                for (int e = 0; e < Rows::kN; ++e)
+                    if (e < left)
+                        to[e] = element<T>(y, e);
             }
+        });
     }
 }
 
@@ -188,17 +284,26 @@ hipError_t launch_product_f8(const ProductArgs &a, void *, hipStream_t stream)
 {
     const ProductShape g{{a.b, a.ld_b / 2, a.cols, 0}, {a.a, a.ld_a / 2, a.rows, 0}, a.a_scales, a.b_scales,
                          a.rows, a.cols, a.depth / kScaleBlock};
-    const auto go = [&](auto tiles, auto zero) {
+    const auto go = [&](auto kernel, auto zero, int side_i, int side_j, int threads) {
         using T = decltype(zero);
-        constexpr int kSide = 128;
-        const int ti = (a.cols + kSide - 1) / kSide, tj = (a.rows + kSide - 1) / kSide;
-        product8_kernel<T, kSide, kSide, 2, 2, decltype(tiles)::value>
-            <<<dim3((unsigned)(ti * tj)), 256, 0, stream>>>(g, static_cast<T *>(a.out), a.ld_out, 0, g.blocks, ti, tj);
+        const int ti = (a.cols + side_i - 1) / side_i, tj = (a.rows + side_j - 1) / side_j;
+        kernel<<<dim3((unsigned)(ti * tj)), threads, 0, stream>>>(g, static_cast<T *>(a.out), a.ld_out, 0, g.blocks, ti, tj);
     };
-    if (a.dtype == 1)
-        a.tiles ? go(std::true_type{}, __bf16{}) : go(std::false_type{}, __bf16{});
-    else
-        a.tiles ? go(std::true_type{}, float{}) : go(std::false_type{}, float{});
+    const auto sides = [&](auto tiles, auto zero, auto exact) {
+        using T = decltype(zero);
+        constexpr bool kTiles = decltype(tiles)::value, kExact = decltype(exact)::value;
+        if constexpr (!kExact)
+            if (a.rows > 256)
+                return go(product8_kernel<T, 256, 256, 2, 4, kTiles, kExact>, zero, 256, 256, 512);
+        go(product8_kernel<T, 128, 128, 2, 2, kTiles, kExact>, zero, 128, 128, 256);
+    };
+    const auto types = [&](auto tiles) {
+        if (a.dtype == 1)
+            a.rows > 256 ? sides(tiles, __bf16{}, std::false_type{}) : sides(tiles, __bf16{}, std::true_type{});
+        else
+            sides(tiles, float{}, std::true_type{});
+    };
+    a.tiles ? types(std::true_type{}) : types(std::false_type{});
     return last_launch();
 }
 
