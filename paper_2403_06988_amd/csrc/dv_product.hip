@@ -226,6 +226,190 @@ struct Product8 {
     }
 };
 
+// Few rows of a (at most 16 KN): bound by b, which passes once, from memory to registers.
+//
+// A wave takes 16 n, a block WAVES of them.  D blocks of 128 k of b are on their way to a wave's
+// registers at any time: each is asked for as soon as the one whose place it takes has been
+// multiplied.  a's rows are shared through LDS, C blocks of k at a time in two buffers,
+// as bf16 (turned once a block, not once a wave), with the chunk's scales.  An a row's 16-byte unit u stands
+// at place u ^ (row mod 16): the 16 rows that are read at once meet distinct banks.
+template <typename T, int KN, int WAVES, int C, int D, bool TILES>
+__global__ __launch_bounds__(WAVES *kWave, 4) void stream8_kernel(ProductShape g, T *out, int64_t ld, int64_t split_stride,
+                                                               int split_blocks)
+{
+    static_assert(D % C == 0, "a turn of b's places is whole chunks of a");
+    constexpr int kRows = 16 * KN, kThreads = WAVES * kWave, kCols = WAVES * 16;
+    constexpr int kPitch = C * kScaleBlock * 2, kA = kRows * kPitch;
+    constexpr int kScales = C * (kRows + (TILES ? 0 : kCols));  // of a chunk: a's, then b's by rows
+    constexpr int kBuffer = kA + kScales * 4;
+    constexpr int kPieces = kRows * C * 8;                      // of 16 e4m3 values, in a chunk of a
+    constexpr int kMine = (kPieces + kThreads - 1) / kThreads;
+    constexpr int kMyScales = (kScales + kThreads - 1) / kThreads;
+    constexpr int kOutPitch = kCols * (int)sizeof(T) + 16;
+    constexpr int kOut = kRows * kOutPitch;
+    __shared__ __attribute__((aligned(16))) char lds[2 * kBuffer > kOut ? 2 * kBuffer : kOut];
+    const int lane = threadIdx.x & (kWave - 1);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int n0 = blockIdx.x * kCols, nw = n0 + wave * 16;
+    const int from = blockIdx.y * split_blocks;
+    const int blocks = g.blocks - from < split_blocks ? g.blocks - from : split_blocks;
+    const int n = nw + (lane & 15) < g.cols ? nw + (lane & 15) : g.cols - 1;
+    const char *const b = static_cast<const char *>(g.b.p) + (int64_t)n * g.b.ld * 2 + (int64_t)from * kScaleBlock + (lane >> 4) * 16;
+    const char *const a = static_cast<const char *>(g.a.p) + (int64_t)from * kScaleBlock;
+    const float *const sb_tile = g.sb + (int64_t)((nw < g.cols ? nw : g.cols - 1) / kScaleBlock) * g.blocks + from;
+
+    const auto load_b = [&](int kb) {
+        const char *p = b + (int64_t)kb * kScaleBlock;
+        union {
+            Words half[2];
+            i32x8 v;
+        } f;
+        f.half[0] = *reinterpret_cast<const Words *>(p);
+        f.half[1] = *reinterpret_cast<const Words *>(p + 64);
+        return f.v;
+    };
+    Words pieces[kMine];
+    float scales[kMyScales];
+    const auto load_a = [&](int chunk) {
+        const auto block = [&](int i) { return chunk * C + i < blocks ? chunk * C + i : blocks - 1; };
+#pragma unroll
+        for (int m = 0; m < kMine; ++m) {
+            const int at = m * kThreads + threadIdx.x;
+            if (kPieces % kThreads && at >= kPieces)
+                break;
+            const int row = at / (C * 8), piece = at % (C * 8);
+            pieces[m] = *reinterpret_cast<const Words *>(a + (int64_t)(row < g.rows ? row : g.rows - 1) * g.a.ld * 2 +
+                                                         block(piece / 8) * kScaleBlock + piece % 8 * 16);
+        }
+#pragma unroll
+        for (int m = 0; m < kMyScales; ++m) {
+            const int at = m * kThreads + threadIdx.x;
+            if (at >= kScales)
+                break;
+            if (at < C * kRows) {
+                const int r = at % kRows;
+                scales[m] = g.sa[(int64_t)(from + block(at / kRows)) * g.rows + (r < g.rows ? r : g.rows - 1)];
+            } else {
+                const int c = n0 + (at - C * kRows) % kCols;
+                scales[m] = g.sb[(int64_t)(from + block((at - C * kRows) / kCols)) * g.cols + (c < g.cols ? c : g.cols - 1)];
+            }
+        }
+    };
+    const auto keep_a = [&](char *buffer) {
+        typedef __attribute__((ext_vector_type(2))) __bf16 Pair;
+#pragma unroll
+        for (int m = 0; m < kMine; ++m) {
+            const int at = m * kThreads + threadIdx.x;
+            if (kPieces % kThreads && at >= kPieces)
+                break;
+            const int row = at / (C * 8), piece = at % (C * 8);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                union {
+                    Pair p[4];
+                    Words w;
+                } y;
+#pragma unroll
+                for (int w = 0; w < 2; ++w) {
+                    y.p[2 * w] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(pieces[m][2 * h + w], 1.f, false);
+                    y.p[2 * w + 1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(pieces[m][2 * h + w], 1.f, true);
+                }
+                *reinterpret_cast<Words *>(buffer + row * kPitch + (((piece * 2 + h) ^ (row & 15)) * 16)) = y.w;
+            }
+        }
+#pragma unroll
+        for (int m = 0; m < kMyScales; ++m) {
+            const int at = m * kThreads + threadIdx.x;
+            if (at < kScales)
+                reinterpret_cast<float *>(buffer + kA)[at] = scales[m];
+        }
+    };
+    const auto barrier = [&] {  // LDS is written and read; loads stay on their way
+        __builtin_amdgcn_s_waitcnt(0xC07F);
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+
+    f32x4 acc[KN] = {};
+    i32x8 x[D];
+    load_a(0);
+#pragma unroll
+    for (int i = 0; i < D; ++i)
+        x[i] = load_b(i < blocks ? i : blocks - 1);
+    keep_a(lds);
+    barrier();
+    for (int base = 0; base < blocks; base += D) {
+#pragma unroll
+        for (int i = 0; i < D; ++i) {
+            const int kb = base + i;
+            if (kb >= blocks)
+                break;
+            const int chunk = kb / C;
+            const bool more = (chunk + 1) * C < blocks;
+            if (i % C == 0 && more)
+                load_a(chunk + 1);
+            const char *const buffer = lds + (chunk & 1) * kBuffer;
+            const float *const sc = reinterpret_cast<const float *>(buffer + kA);
+            Fragment8<true> fb;
+            fb.set(x[i]);
+            if (kb + D < blocks)
+                x[i] = load_b(kb + D);
+            const float tile_scale = TILES ? sb_tile[kb] : 1.f;
+            f32x4 sb = {1.f, 1.f, 1.f, 1.f};
+            if constexpr (!TILES)
+                sb = *reinterpret_cast<const f32x4 *>(sc + C * kRows + i % C * kCols + wave * 16 + (lane >> 4) * 4);
+#pragma unroll
+            for (int j = 0; j < KN; ++j) {
+                f32x4 p = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int h = 0; h < 4; ++h) {
+                    const int unit = i % C * 16 + ((lane >> 4) + (h >> 1) * 4) * 2 + (h & 1);
+                    const bf16x8 fa = *reinterpret_cast<const bf16x8 *>(buffer + (j * 16 + (lane & 15)) * kPitch +
+                                                                        ((unit ^ (lane & 15)) * 16));
+                    p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb.part[h], fa, p, 0, 0, 0);
+                }
+                const float sa = sc[i % C * kRows + j * 16 + (lane & 15)] * tile_scale;
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    acc[j][e] = __builtin_fmaf(TILES ? p[e] : p[e] * sb[e], sa, acc[j][e]);
+            }
+            if (i % C == C - 1 && more) {
+                keep_a(lds + ((chunk + 1) & 1) * kBuffer);
+                barrier();
+            }
+        }
+    }
+    barrier();
+    // whole lines of the result's rows leave through LDS
+#pragma unroll
+    for (int j = 0; j < KN; ++j) {
+        T y[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            y[e] = (T)acc[j][e];
+        __builtin_memcpy(lds + (j * 16 + (lane & 15)) * kOutPitch + (wave * 16 + (lane >> 4) * 4) * (int)sizeof(T), y, sizeof y);
+    }
+    __syncthreads();
+    constexpr int kN = 16 / (int)sizeof(T), kPerRow = kCols / kN;
+    out += blockIdx.y * split_stride;
+    for (int at = threadIdx.x; at < kRows * kPerRow; at += kThreads) {
+        const int row = at / kPerRow, col = at % kPerRow * kN;
+        if (row >= g.rows)
+            break;
+        const Words y = *reinterpret_cast<const Words *>(lds + row * kOutPitch + col * (int)sizeof(T));
+        T *to = out + row * ld + n0 + col;
+        const int left = g.cols - n0 - col;
+        if (left >= kN) {
+            store_words(to, y);
+        } else {
+#pragma unroll
+            for (int e = 0; e < kN; ++e)
+                if (e < left)
+                    to[e] = element<T>(y, e);
+        }
+    }
+}
+
 template <typename T, int BM, int BN, int WM, int WN, bool TILES, bool EXACT>
 __global__ __launch_bounds__(WM *WN *kWave, 2) void product8_kernel(ProductShape g, T *out, int64_t ld, int64_t split_stride,
                                                                     int split_stages, int tiles_i, int tiles_j)
@@ -280,18 +464,30 @@ __global__ __launch_bounds__(WM *WN *kWave, 2) void product8_kernel(ProductShape
 
 size_t product_f8_workspace_bytes(int, int, int) { return 0; }
 
-hipError_t launch_product_f8(const ProductArgs &a, void *, hipStream_t stream)
+hipError_t launch_product_f8(const ProductArgs &a, void *, hipStream_t stream_)
 {
     const ProductShape g{{a.b, a.ld_b / 2, a.cols, 0}, {a.a, a.ld_a / 2, a.rows, 0}, a.a_scales, a.b_scales,
                          a.rows, a.cols, a.depth / kScaleBlock};
     const auto go = [&](auto kernel, auto zero, int side_i, int side_j, int threads) {
         using T = decltype(zero);
         const int ti = (a.cols + side_i - 1) / side_i, tj = (a.rows + side_j - 1) / side_j;
-        kernel<<<dim3((unsigned)(ti * tj)), threads, 0, stream>>>(g, static_cast<T *>(a.out), a.ld_out, 0, g.blocks, ti, tj);
+        kernel<<<dim3((unsigned)(ti * tj)), threads, 0, stream_>>>(g, static_cast<T *>(a.out), a.ld_out, 0, g.blocks, ti, tj);
     };
     const auto sides = [&](auto tiles, auto zero, auto exact) {
         using T = decltype(zero);
         constexpr bool kTiles = decltype(tiles)::value, kExact = decltype(exact)::value;
+        const auto stream = [&](auto kernel, int waves) {
+            kernel<<<dim3((unsigned)((a.cols + waves * 16 - 1) / (waves * 16))), waves * kWave, 0, stream_>>>(
+                g, static_cast<T *>(a.out), a.ld_out, 0, g.blocks);
+        };
+        if constexpr (kExact) {
+            if (a.rows <= 16)
+                return stream(stream8_kernel<T, 1, 4, 2, 4, kTiles>, 4);
+            if (a.rows <= 32)
+                return stream(stream8_kernel<T, 2, 4, 2, 4, kTiles>, 4);
+            if (a.rows <= 64)
+                return stream(stream8_kernel<T, 4, 8, 2, 2, kTiles>, 8);
+        }
         if constexpr (!kExact)
             if (a.rows > 256)
                 return go(product8_kernel<T, 256, 256, 2, 4, kTiles, kExact>, zero, 256, 256, 512);
