@@ -734,7 +734,7 @@ DV_API dv_status dv_product_f8(const void *a, int64_t ld_a, const float *a_scale
  * presence, frequency [rows] fp32, each NULL for none; bias_ids [rows][num_bias]
  * int32 and bias [rows][num_bias] fp32, contiguous; allow, num_states, states as
  * for the training calls (NULL: every token is allowed).
- * rows * ceil(V / 8192) < 2^24.  rows = 0 is valid and enqueues nothing.
+ * rows * ceil(V / 4096) < 2^24.  rows = 0 is valid and enqueues nothing.
  * Errors as dv_head_loss (no workspace).
  */
 DV_API dv_status dv_adjust_logits(const void *logits, int64_t ld_logits, int32_t dtype, int32_t rows, int32_t num_tokens,

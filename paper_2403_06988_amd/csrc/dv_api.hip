@@ -1055,7 +1055,7 @@ dv_status dv_adjust_logits(const void *logits, int64_t ld_logits, int32_t dtype,
         DV_CHECK(row_stride(name, "ld_history", ld_history, max_history));
     DV_CHECK(row_stride(name, "ld_logits", ld_logits, num_tokens));
     DV_CHECK(row_stride(name, "ld_out", ld_out, num_tokens));
-    if ((int64_t)rows * (((int64_t)num_tokens + 8191) / 8192) >= (int64_t)1 << 24)
+    if ((int64_t)rows * (((int64_t)num_tokens + 4095) / 4096) >= (int64_t)1 << 24)
         return fail(DV_ERR_SHAPE, "%s: %d rows of %d tokens are too many", name, rows, num_tokens);
     DV_CHECK(mask_args(name, allow, num_states, states, rows));
     const size_t elt = element_size(dtype), n = (size_t)rows;
