@@ -49,14 +49,14 @@ __device__ __forceinline__ uint32_t row_largest(uint32_t v, float *sums)
     return v;
 }
 
-// THREADS take a row, NV vectors of 8 columns each; blocks hold max(THREADS, 256) threads.
+// THREADS take a row, NV vectors of 8 columns each; blocks hold a row, or four of a wave each.
 template <typename T, int THREADS, int NV>
-__global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void norm_kernel(const T *x, int64_t ld_x, const T *residual,
+__global__ __launch_bounds__(THREADS == kWave ? 256 : THREADS) void norm_kernel(const T *x, int64_t ld_x, const T *residual,
                                                                              int64_t ld_residual, const T *weight,
                                                                              int rows, int hidden, float eps, T *total,
                                                                              T *out, float *rstd, uint8_t *q, float *scales)
 {
-    constexpr int kRows = THREADS < 256 ? 256 / THREADS : 1;  // of a block
+    constexpr int kRows = THREADS == kWave ? 256 / THREADS : 1;  // of a block
     __shared__ float sums[3][kRows == 1 ? THREADS / kWave : 1];
     const int t = threadIdx.x % THREADS;
     const int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / THREADS;
@@ -216,38 +216,70 @@ __global__ __launch_bounds__(THREADS) void norm_grad_kernel(const T *grad_out, i
             store8(partial + (int64_t)blockIdx.x * hidden, (v * THREADS + threadIdx.x) * 8, hidden, dw[v]);
 }
 
-// dw: the blocks' shares added, 64 columns a block, 16 waves a share of the rows each.
+// dw: the blocks' shares added.  A block takes 64 columns, 16 lanes a share with 4 of them each
+// (the columns past the end are not there: 16 bytes are read where they lie in the row), its 64
+// groups every 64th share, 8 of them asked for at a time; then the groups' sums, through LDS.
 template <typename T>
 __global__ __launch_bounds__(1024) void norm_weight_kernel(const float *partial, int parts, int hidden, T *grad_weight)
 {
-    __shared__ float sh[16][kWave];
-    const int lane = threadIdx.x & (kWave - 1), slice = threadIdx.x / kWave;
-    const int c = blockIdx.x * kWave + lane;
-    float s = 0.f;
-    if (c < hidden)
-        for (int p = slice; p < parts; p += 16)
-            s += partial[(int64_t)p * hidden + c];
-    sh[slice][lane] = s;
-    __syncthreads();
-    if (slice || c >= hidden)
-        return;
-    s = 0.f;
+    constexpr int kGroups = 64, kColumns = 64, kAtOnce = 8;
+    __shared__ float sh[kGroups][kColumns];
+    const int lane = threadIdx.x % 16, group = threadIdx.x / 16;
+    const int c = blockIdx.x * kColumns + lane * 4;
+    const int left = hidden - c;
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int from = group; from < parts; from += kGroups * kAtOnce) {
+        float x[kAtOnce][4];
 #pragma unroll
-    for (int i = 0; i < 16; ++i)
-        s += sh[i][lane];
-    if constexpr (sizeof(T) == 2)
-        grad_weight[c] = narrow(s);
-    else
-        grad_weight[c] = s;
+        for (int k = 0; k < kAtOnce; ++k) {
+            const int p = from + k * kGroups;
+            const float *row = partial + (int64_t)p * hidden + c;
+            if (p < parts && left >= 4) {
+                const Words w = load_words(row);
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    x[k][e] = __uint_as_float(w[e]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    x[k][e] = p < parts && e < left ? row[e] : 0.f;
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                s[e] += x[k][e];
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        sh[group][lane * 4 + e] = s[e];
+    __syncthreads();
+    // 16 threads a column, 4 groups each, of one wave's quarter
+    const int column = threadIdx.x / 16, part = threadIdx.x % 16;
+    float sum = 0.f;
+#pragma unroll
+    for (int k = 0; k < kGroups / 16; ++k)
+        sum += sh[part * (kGroups / 16) + k][column];
+#pragma unroll
+    for (int d = 8; d; d >>= 1)
+        sum += __shfl_xor(sum, d);
+    const int at = blockIdx.x * kColumns + column;
+    if (part == 0 && at < hidden) {
+        if constexpr (sizeof(T) == 2)
+            grad_weight[at] = narrow(sum);
+        else
+            grad_weight[at] = sum;
+    }
 }
 
 template <typename T>
 hipError_t launch_norm(const NormArgs &a, hipStream_t stream)
 {
     const auto go = [&](auto kernel, int threads) {
-        const int per_block = threads < 256 ? 256 / threads : 1;
+        const int per_block = threads == kWave ? 256 / threads : 1;
         const unsigned grid = (unsigned)((a.rows + per_block - 1) / per_block);
-        kernel<<<grid, threads < 256 ? 256 : threads, 0, stream>>>(
+        kernel<<<grid, threads == kWave ? 256 : threads, 0, stream>>>(
             static_cast<const T *>(a.x), a.ld_x, static_cast<const T *>(a.residual), a.ld_residual,
             static_cast<const T *>(a.weight), a.rows, a.hidden, a.eps, static_cast<T *>(a.total), static_cast<T *>(a.out),
             a.rstd, a.q, a.scales);
@@ -308,7 +340,7 @@ hipError_t launch_grad(const NormGradArgs &a, float *partial, hipStream_t stream
             go(norm_grad_kernel<T, 1024, 8, false>, 1024);
     }
     if (a.grad_weight)
-        norm_weight_kernel<T><<<(unsigned)((a.hidden + kWave - 1) / kWave), 1024, 0, stream>>>(
+        norm_weight_kernel<T><<<(unsigned)((a.hidden + 63) / 64), 1024, 0, stream>>>(
             partial, blocks, a.hidden, static_cast<T *>(a.grad_weight));
     return last_launch();
 }

@@ -71,6 +71,18 @@ struct Product8 {
     using B = typename G::B;
     using Fragment = Fragment8<EXACT>;
     static constexpr int kTm = G::kTm, kTn = G::kTn, kLoads = G::kLoads, kWaves = G::kWaves;
+    // Fragments of b on their way from LDS, and products on their way before one is added under
+    // its scales: 8,192 x 32,000 x 4,096 (8-bit instructions) with 1 and 1 1.13 ms, 2 and 1 1.10,
+    // 2 and 2 1.04.
+    static constexpr int kAhead = EXACT ? 1 : 2, kLag = EXACT ? 1 : 2;
+    // A stage's loads are asked for one after kPerLoad products, the first kEarly of them as soon as
+    // the stage before the last has been read: all of a block's at once hold up every wave (the
+    // same product: 1.10 ms; exact, 4,096 in each direction, all at once 127 us, one a product 126).
+    static constexpr int kPerLoad = EXACT ? 1 : 2;
+    static constexpr int kEarly = kAhead * kTn / kPerLoad < kLoads ? kAhead * kTn / kPerLoad : kLoads;
+    static_assert(kLag < 4 && kTn % kPerLoad == 0, "four products are held");
+    static_assert(kEarly + (kTm - kAhead) * (kTn / kPerLoad) >= kLoads, "every load has its place");
+    static_assert(kTm % 4 == 0 && kTm % kAhead == 0 && kAhead <= 2, "a stage is whole turns of the fragments' and scales' places");
     // by rows, b's scales of a stage stand in LDS behind the operands
     static constexpr int kScaleBytes = TILES ? 0 : BM * 4;
     static constexpr int kStageBytes = G::kStageBytes + kScaleBytes;
@@ -110,20 +122,20 @@ struct Product8 {
             voff[i] = side_a(i) ? A::source(g.b, i0, group + i, lane, 0) : B::source(g.a, j0, group + i - A::kGroups, lane, 0);
         const bool loads_scales = !TILES && wave < BM / kWave;
         const int scale_at = i0 + wave * kWave + lane < g.cols ? i0 + wave * kWave + lane : g.cols - 1;
-        int stage = from;
-        const auto load = [&](int slot) {
-            const uint32_t dst = (uint32_t)(uintptr_t)(typename G::Lds)(lds + slot * kStageBytes);
-            const int64_t at = (int64_t)stage * kScaleBlock;
-            if constexpr (!TILES)
-                if (loads_scales)
-                    load_word_to_lds(g.sb + (int64_t)stage * g.cols, scale_at * 4, dst + G::kStageBytes + wave * kWave * 4);
+        // this wave's loads i0 to i1 of stage s
+        const auto load = [&](int s, int i0, int i1) {
+            const uint32_t dst = (uint32_t)(uintptr_t)(typename G::Lds)(lds + (s & 1) * kStageBytes);
+            const int64_t at = (int64_t)(from + s) * kScaleBlock;
+            if (!TILES && i0 == 0 && loads_scales)
+                load_word_to_lds(g.sb + (int64_t)(from + s) * g.cols, scale_at * 4, dst + G::kStageBytes + wave * kWave * 4);
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) {
+                if (i < i0 || i >= i1)
+                    continue;
                 const int p = group + i;
                 G::load_to_lds((side_a(i) ? start_a : start_b) + at, voff[i],
                                dst + (side_a(i) ? p * A::kPitch : A::kBytes + (p - A::kGroups) * B::kPitch));
             }
-            ++stage;
         };
         const int at_a = wm * (A::kFragmentStep * kTm), at_b = wn * (B::kFragmentStep * kTn);
         const int a0 = at_a + A::place(lane, 0), a1 = at_a + A::place(lane, 1);
@@ -150,29 +162,34 @@ struct Product8 {
         };
 
         load_scales(from);
-        load(0);
-        if (stages > 1)
-            load(1);
-        if (stages > 1 && TILES)
-            G::template wait_loads<kLoads>();
-        else
-            G::template wait_loads<0>();
+        load(0, 0, kLoads);
+        G::template wait_loads<0>();
         G::barrier();
+        if (stages > 1)
+            load(1, 0, kEarly);
         Fragment fa, fb[kTn];
-        f32x4 p[2];
-        i32x8 next = raw<A>(lds, a0, a1, 0);
+        f32x4 p[4];
+        i32x8 next[kAhead];
+        f32x4 sb[4];  // of the row before, this one and those ahead
+        const auto read = [&](const char *tile, int i) {
+            next[i % kAhead] = raw<A>(tile, a0, a1, i);
+            if constexpr (!TILES)
+                sb[i & 3] = *reinterpret_cast<const f32x4 *>(tile + at_scales + i * 64);
+        };
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i)
+            read(lds, i);
 #pragma unroll
         for (int j = 0; j < kTn; ++j)
             fb[j].set(raw<B>(lds + A::kBytes, b0, b1, j));
         for (int s = 0; s < stages; ++s) {
             const char *tile = lds + (s & 1) * kStageBytes;
-            f32x4 sb[2];
             // a finished product, under its scales
             const auto add = [&](int i, int j) {
-                const f32x4 x = p[(i * kTn + j) & 1];
+                const f32x4 x = p[(i * kTn + j) & 3];
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    acc[i][j][e] = __builtin_fmaf(TILES ? x[e] : x[e] * sb[i & 1][e], scale[j], acc[i][j][e]);
+                    acc[i][j][e] = __builtin_fmaf(TILES ? x[e] : x[e] * sb[i & 3][e], scale[j], acc[i][j][e]);
                 // here, not where the compiler would sink it to: that takes registers for every product
                 asm volatile("" : "+v"(acc[i][j]));
             };
@@ -183,30 +200,39 @@ struct Product8 {
                 load_scales(from + s + 1);
 #pragma unroll
             for (int i = 0; i < kTm; ++i) {
-                fa.set(next);
-                if constexpr (!TILES)
-                    sb[i & 1] = *reinterpret_cast<const f32x4 *>(tile + at_scales + i * 64);
-                if (i + 1 < kTm) {
-                    next = raw<A>(tile, a0, a1, i + 1);
+                fa.set(next[i % kAhead]);
+                if (i + kAhead < kTm) {
+                    read(tile, i + kAhead);
                 } else if (s + 1 < stages) {
-                    G::template wait_loads<0>();  // and this wave's reads of the stage
-                    G::barrier();
-                    if (s + 2 < stages)
-                        load(s & 1);
-                    next = raw<A>(lds + ((s + 1) & 1) * kStageBytes, a0, a1, 0);
+                    if (i + kAhead == kTm) {
+                        G::template wait_loads<0>();  // and this wave's reads of the stage
+                        G::barrier();
+                    }
+                    read(lds + ((s + 1) & 1) * kStageBytes, i + kAhead - kTm);
                 }
-                // a product at a time, the one before it added while it runs
+                // a product at a time, one before it added while it runs, and a load asked for
 #pragma unroll
                 for (int j = 0; j < kTn; ++j) {
-                    p[(i * kTn + j) & 1] = Fragment::multiply(fa, fb[j]);
-                    if (i + j)
-                        add(j ? i : i - 1, j ? j - 1 : kTn - 1);
+                    const int at = i * kTn + j;
+                    p[at & 3] = Fragment::multiply(fa, fb[j]);
+                    if (at >= kLag)
+                        add((at - kLag) / kTn, (at - kLag) % kTn);
+                    if (j % kPerLoad == kPerLoad - 1) {
+                        const int early = (i + kAhead - kTm) * (kTn / kPerLoad) + j / kPerLoad;
+                        const int late = kEarly + i * (kTn / kPerLoad) + j / kPerLoad;
+                        if (i + kAhead >= kTm && early < kEarly && s + 2 < stages)
+                            load(s + 2, early, early + 1);
+                        else if (late < kLoads && s + 1 < stages)
+                            load(s + 1, late, late + 1);
+                    }
                     __builtin_amdgcn_sched_barrier(0);
                     if (i + 1 == kTm && s + 1 < stages)
                         fb[j].set(raw<B>(lds + ((s + 1) & 1) * kStageBytes + A::kBytes, b0, b1, j));
                 }
             }
-            add(kTm - 1, kTn - 1);
+#pragma unroll
+            for (int l = kLag; l > 0; --l)
+                add((kTm * kTn - l) / kTn, (kTm * kTn - l) % kTn);
         }
     }
 
@@ -460,47 +486,171 @@ __global__ __launch_bounds__(WM *WN *kWave, 2) void product8_kernel(ProductShape
     }
 }
 
-}  // namespace
+// The sum of the splits' parts [rows][cols], four elements a lane, as rows of the result.
+template <typename T>
+__global__ __launch_bounds__(256) void join8_kernel(const float *parts, int splits, int rows, int cols, T *out, int64_t ld)
+{
+    const int vecs = (cols + 3) / 4;
+    const int64_t total = (int64_t)rows * vecs, step = (int64_t)rows * cols;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+        const int64_t row = i / vecs;
+        const int c = (int)(i - row * vecs) * 4;
+        const float *p = parts + row * cols + c;
+        T *to = out + row * ld + c;
+        f32x4 s = {0.f, 0.f, 0.f, 0.f};
+        if (c + 4 <= cols) {
+            for (int k = 0; k < splits; ++k)
+                s += __builtin_bit_cast(f32x4, load_words(p + k * step));
+            const T y[4] = {(T)s[0], (T)s[1], (T)s[2], (T)s[3]};
+            __builtin_memcpy(to, y, sizeof y);
+        } else {
+            for (int e = 0; c + e < cols; ++e) {
+                float x = 0.f;
+                for (int k = 0; k < splits; ++k)
+                    x += p[k * step + e];
+                to[e] = (T)x;
+            }
+        }
+    }
+}
 
-size_t product_f8_workspace_bytes(int, int, int) { return 0; }
+// ------------------------------------------------------------------- the plan
 
-hipError_t launch_product_f8(const ProductArgs &a, void *, hipStream_t stream_)
+// How a product is cut: the kernel (few rows, or tiles of a side), and the splits of its
+// blocks of 128 k, none of them empty.
+struct Plan8 {
+    bool exact;
+    int side;    // of a tile; 0: the kernel of at most 64 rows
+    int waves;   // of one of its blocks
+    int splits, blocks;
+};
+
+constexpr int kFewRows = 64, kMostSplits = 16;
+
+// Sums through the 8-bit matrix instruction lose what lies 2^16 and more below a block's largest
+// product: 1.4e-5 of a normal block's size, a hundredth of a bf16 result's rounding.  fp32
+// results take the products of the same values as bf16, which lose nothing (half the rate: 4,096 in each direction
+// 126 us against 63), and so do bf16 results of a decode step's at most 256 rows, whose time is mostly b's.
+bool exact_sums(int rows, int dtype) { return dtype == 0 || rows <= 256; }
+
+Plan8 plan_f8(int rows, int cols, int depth, int dtype)
+{
+    const int blocks = depth / kScaleBlock;
+    Plan8 best{exact_sums(rows, dtype), 0, 0, 1, blocks};
+    if (rows <= kFewRows) {
+        best.waves = rows <= 32 ? 4 : 8;
+        const int64_t n = (cols + best.waves * 16 - 1) / (best.waves * 16);
+        int64_t want = n >= 384 ? 1 : 512 / n;
+        want = want < blocks / 4 ? want : blocks / 4;
+        want = want < kMostSplits ? want : kMostSplits;
+        best.blocks = want > 1 ? (int)((blocks + want - 1) / want) : blocks;
+        best.splits = (blocks + best.blocks - 1) / best.blocks;
+        return best;
+    }
+    // By the time that each choice would take: a block of k of all the tiles that a compute unit
+    // holds takes `us`, one tile alone two fifths of that and more; a tile costs `around` blocks
+    // of k to start and end; splits write and read their sums.
+    struct Side {
+        int side, per_unit, around;
+        double us;
+    };
+    constexpr Side kFast[] = {{256, 1, 3, 1.85}, {128, 2, 5, 1.2}}, kExact[] = {{128, 2, 4, 1.85}};
+    constexpr int kUnits = 256;
+    double least = 1e30;
+    const auto consider = [&](const Side &s) {
+        const int64_t tiles = (int64_t)((rows + s.side - 1) / s.side) * ((cols + s.side - 1) / s.side);
+        if (tiles > (int64_t)1 << 22 && s.side < 256 && !best.exact)
+            return;
+        for (int want = 1; want <= kMostSplits && want <= blocks; ++want) {
+            const int per = (blocks + want - 1) / want, used = (blocks + per - 1) / per;
+            const int64_t n = tiles * used, slots = (int64_t)kUnits * s.per_unit, rest = n % slots;
+            const auto round = [&](int64_t per_unit) {
+                return (per + s.around) * s.us * (0.4 + 0.6 * (double)per_unit / s.per_unit);
+            };
+            const double us = (double)(n / slots) * round(s.per_unit) + (rest ? round((rest + kUnits - 1) / kUnits) : 0) +
+                              (used > 1 ? (double)used * rows * cols * 2e-6 + 5 : 0);
+            if (us < least) {
+                least = us;
+                best.side = s.side;
+                best.splits = used;
+                best.blocks = per;
+            }
+        }
+    };
+    if (best.exact)
+        for (const Side &s : kExact)
+            consider(s);
+    else
+        for (const Side &s : kFast)
+            consider(s);
+    return best;
+}
+
+size_t parts_bytes(const Plan8 &p, int rows, int cols)
+{
+    return p.splits > 1 ? align_up((size_t)p.splits * (size_t)rows * (size_t)cols * 4, 256) : 0;
+}
+
+template <typename T>
+hipError_t launch_product(const ProductArgs &a, const Plan8 &plan, void *workspace, hipStream_t stream)
 {
     const ProductShape g{{a.b, a.ld_b / 2, a.cols, 0}, {a.a, a.ld_a / 2, a.rows, 0}, a.a_scales, a.b_scales,
                          a.rows, a.cols, a.depth / kScaleBlock};
-    const auto go = [&](auto kernel, auto zero, int side_i, int side_j, int threads) {
-        using T = decltype(zero);
-        const int ti = (a.cols + side_i - 1) / side_i, tj = (a.rows + side_j - 1) / side_j;
-        kernel<<<dim3((unsigned)(ti * tj)), threads, 0, stream_>>>(g, static_cast<T *>(a.out), a.ld_out, 0, g.blocks, ti, tj);
-    };
-    const auto sides = [&](auto tiles, auto zero, auto exact) {
-        using T = decltype(zero);
-        constexpr bool kTiles = decltype(tiles)::value, kExact = decltype(exact)::value;
-        const auto stream = [&](auto kernel, int waves) {
-            kernel<<<dim3((unsigned)((a.cols + waves * 16 - 1) / (waves * 16))), waves * kWave, 0, stream_>>>(
-                g, static_cast<T *>(a.out), a.ld_out, 0, g.blocks);
+    const unsigned splits = (unsigned)plan.splits;
+    const auto run = [&](auto tiles, auto *out, int64_t ld, int64_t stride) {
+        using O = std::remove_pointer_t<decltype(out)>;
+        constexpr bool kTiles = decltype(tiles)::value;
+        const auto few = [&](auto kernel) {
+            const int n = plan.waves * 16;
+            kernel<<<dim3((unsigned)((a.cols + n - 1) / n), splits), plan.waves * kWave, 0, stream>>>(g, out, ld, stride, plan.blocks);
         };
-        if constexpr (kExact) {
+        const auto tiled = [&](auto kernel, int threads) {
+            const int ti = (a.cols + plan.side - 1) / plan.side, tj = (a.rows + plan.side - 1) / plan.side;
+            kernel<<<dim3((unsigned)(ti * tj), splits), threads, 0, stream>>>(g, out, ld, stride, plan.blocks, ti, tj);
+        };
+        if (!plan.side) {
             if (a.rows <= 16)
-                return stream(stream8_kernel<T, 1, 4, 2, 4, kTiles>, 4);
-            if (a.rows <= 32)
-                return stream(stream8_kernel<T, 2, 4, 2, 4, kTiles>, 4);
-            if (a.rows <= 64)
-                return stream(stream8_kernel<T, 4, 8, 2, 2, kTiles>, 8);
+                few(stream8_kernel<O, 1, 4, 2, 4, kTiles>);
+            else if (a.rows <= 32)
+                few(stream8_kernel<O, 2, 4, 2, 4, kTiles>);
+            else
+                few(stream8_kernel<O, 4, 8, 2, 2, kTiles>);
+        } else if (plan.exact) {
+            tiled(product8_kernel<O, 128, 128, 2, 2, kTiles, true>, 256);
+        } else if (plan.side == 256) {
+            tiled(product8_kernel<O, 256, 256, 2, 4, kTiles, false>, 512);
+        } else {
+            tiled(product8_kernel<O, 128, 128, 2, 2, kTiles, false>, 256);
         }
-        if constexpr (!kExact)
-            if (a.rows > 256)
-                return go(product8_kernel<T, 256, 256, 2, 4, kTiles, kExact>, zero, 256, 256, 512);
-        go(product8_kernel<T, 128, 128, 2, 2, kTiles, kExact>, zero, 128, 128, 256);
     };
-    const auto types = [&](auto tiles) {
-        if (a.dtype == 1)
-            a.rows > 256 ? sides(tiles, __bf16{}, std::false_type{}) : sides(tiles, __bf16{}, std::true_type{});
-        else
-            sides(tiles, float{}, std::true_type{});
+    const auto types = [&](auto *out, int64_t ld, int64_t stride) {
+        a.tiles ? run(std::true_type{}, out, ld, stride) : run(std::false_type{}, out, ld, stride);
     };
-    a.tiles ? types(std::true_type{}) : types(std::false_type{});
+    T *const out = static_cast<T *>(a.out);
+    if (splits == 1) {
+        types(out, a.ld_out, 0);
+    } else {
+        float *const parts = static_cast<float *>(workspace);
+        types(parts, a.cols, (int64_t)a.rows * a.cols);
+        const int64_t blocks = ((int64_t)a.rows * ((a.cols + 3) / 4) + 255) / 256;
+        join8_kernel<<<(unsigned)(blocks < 4096 ? blocks : 4096), 256, 0, stream>>>(parts, plan.splits, a.rows, a.cols, out, a.ld_out);
+    }
     return last_launch();
+}
+
+}  // namespace
+
+size_t product_f8_workspace_bytes(int rows, int cols, int depth)
+{
+    const size_t f32 = parts_bytes(plan_f8(rows, cols, depth, 0), rows, cols);
+    const size_t bf16 = parts_bytes(plan_f8(rows, cols, depth, 1), rows, cols);
+    return f32 > bf16 ? f32 : bf16;
+}
+
+hipError_t launch_product_f8(const ProductArgs &a, void *workspace, hipStream_t stream)
+{
+    const Plan8 plan = plan_f8(a.rows, a.cols, a.depth, a.dtype);
+    return a.dtype == 1 ? launch_product<__bf16>(a, plan, workspace, stream) : launch_product<float>(a, plan, workspace, stream);
 }
 
 }  // namespace dv

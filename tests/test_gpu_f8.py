@@ -162,3 +162,21 @@ def test_no_rows(dv):
     assert out.shape == (0, 100)
     q, s, tq, ts = dv.quantize_f8(torch.empty((0, 100), device=DEV), want_columns=True)
     assert q.shape == (0, 128) and s.shape == (1, 0) and tq.shape == (100, 0) and ts.shape == (0, 100)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("tile", [1, 128])
+@pytest.mark.parametrize("M,N,K", [(1, 200, 8192), (40, 100, 4096), (300, 260, 6016), (70, 130, 12800), (600, 140, 3968), (257, 1, 1280)])
+def test_product_in_parts(dv, M, N, K, tile, dtype):
+    """Few tiles and a long depth: sums of parts of it, joined; a workspace of the call's own size."""
+    a, sa, b, sb = operands(np.random.default_rng(M + K), M, N, K, tile)
+    want, tol = product_reference(a, sa, b, sb, tile, dtype)
+    args = (a.to(DEV), sa.to(DEV), b.to(DEV), sb.to(DEV))
+    need = dv.product_f8_workspace_bytes(M, N, K)
+    assert need > 0
+    ws = torch.full((need + 256,), 0xFF, dtype=torch.uint8, device=DEV)       # NaN where nothing is written
+    wide = torch.full((M, N + 3), 9.0, dtype=dtype, device=DEV)
+    dv.product_f8(*args, tile=tile, out=wide[:, :N], workspace=ws[:need])
+    check(wide[:, :N], want, tol, "product in parts")
+    assert (wide[:, N:] == 9).all() and (ws[need:] == 0xFF).all()
+    assert torch.equal(dv.product_f8(*args, tile=tile, dtype=dtype), wide[:, :N])
