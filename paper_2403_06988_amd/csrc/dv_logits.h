@@ -16,15 +16,15 @@ constexpr int64_t up_block(int64_t n) { return (n + kScaleBlock - 1) / kScaleBlo
 // below 2^-100 count as that, so that a scale and its reciprocal are normal
 // numbers.  An infinity or a NaN in a block makes NaN of all of it.
 struct BlockScale {
-    float scale, inv;
-    bool bad;
+    float scale, inv;  // both NaN where the block is
 
+    BlockScale() = default;
+    __device__ __forceinline__ BlockScale(float scale, float inv) : scale(scale), inv(inv) {}
     // `largest`: the bits of the largest magnitude (as whole numbers they order as the
     // values do, infinity and then NaN above the rest)
     __device__ __forceinline__ explicit BlockScale(uint32_t largest)
     {
-        bad = largest >= 0x7F800000u;
-        scale = bad ? __uint_as_float(0x7FC00000u) : fmaxf(__uint_as_float(largest), 0x1p-100f) / 448.f;
+        scale = largest >= 0x7F800000u ? __uint_as_float(0x7FC00000u) : fmaxf(__uint_as_float(largest), 0x1p-100f) / 448.f;
         inv = 1.f / scale;
     }
     // x / scale correctly rounded: one Newton step on the product with the correctly rounded
@@ -50,13 +50,12 @@ __device__ __forceinline__ uint32_t to_e4m3(float a, float b, float c, float d)
 // Eight values of a block in e4m3.
 __device__ __forceinline__ uint2 quantize8(const float (&x)[8], const BlockScale &s)
 {
-    if (s.bad)
-        return {0x7F7F7F7Fu, 0x7F7F7F7Fu};
     float t[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e)
         t[e] = s.quotient(x[e]);
-    return {to_e4m3(t[0], t[1], t[2], t[3]), to_e4m3(t[4], t[5], t[6], t[7])};
+    const bool bad = s.inv != s.inv;
+    return {bad ? 0x7F7F7F7Fu : to_e4m3(t[0], t[1], t[2], t[3]), bad ? 0x7F7F7F7Fu : to_e4m3(t[4], t[5], t[6], t[7])};
 }
 
 // Largest of 16 lanes' values (lanes 0-15, 16-31, ...), in each of them.
@@ -68,39 +67,48 @@ __device__ __forceinline__ uint32_t largest16(uint32_t v)
     return larger(v, dpp_move<kDppRowMirror>(v));
 }
 
-// Eight consecutive elements of a row of n in fp32, from column c on (zeros past n).
+// Eight consecutive elements of a row of n, from column c on (zeros past n), as they lie:
+// asked for here, turned to fp32 where they are needed, so that several are on their way at once.
 template <typename T>
-__device__ __forceinline__ void load8(float (&x)[8], const T *row, int c, int n)
-{
-    if (c + 8 <= n) {
-        if constexpr (sizeof(T) == 2) {
-            const Words w = load_words(row + c);
+struct Raw8 {
+    Words w[sizeof(T) / 2];
+
+    __device__ __forceinline__ void load(const T *row, int c, int n)
+    {
+        constexpr int kN = 16 / (int)sizeof(T);
+        if (c + 8 <= n) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                x[2 * e] = __uint_as_float(w[e] << 16);
-                x[2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u);
-            }
+            for (int i = 0; i < (int)sizeof(T) / 2; ++i)
+                w[i] = load_words(row + c + i * kN);
         } else {
-            const Words lo = load_words(row + c), hi = load_words(row + c + 4);
+            T t[8];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                x[e] = __uint_as_float(lo[e]);
-                x[4 + e] = __uint_as_float(hi[e]);
-            }
-        }
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            x[e] = 0.f;
-            if (c + e < n) {
-                if constexpr (sizeof(T) == 2)
-                    x[e] = widen(row[c + e]);
-                else
-                    x[e] = row[c + e];
-            }
+            for (int e = 0; e < 8; ++e)
+                t[e] = c + e < n ? row[c + e] : T(0);
+            __builtin_memcpy(w, t, sizeof t);
         }
     }
-}
+    __device__ __forceinline__ void zero()
+    {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i)
+            w[i] = Words{0, 0, 0, 0};
+    }
+    __device__ __forceinline__ void to(float (&x)[8]) const
+    {
+        if constexpr (sizeof(T) == 2) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                x[2 * e] = __uint_as_float(w[0][e] << 16);
+                x[2 * e + 1] = __uint_as_float(w[0][e] & 0xFFFF0000u);
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                x[e] = __uint_as_float(w[e / 4][e % 4]);
+        }
+    }
+};
 
 // The same to memory, rounded once to T (uint16_t: bf16).
 template <typename T>

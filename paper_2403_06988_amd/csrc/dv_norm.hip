@@ -62,15 +62,35 @@ __global__ __launch_bounds__(THREADS == kWave ? 256 : THREADS) void norm_kernel(
     const int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / THREADS;
     if (kRows > 1 && row >= rows)  // whole waves
         return;
+    // all of a row's vectors at once, but for the longest rows, whose registers hold one after the other
+    constexpr int kAtOnce = NV <= 4 ? NV : 1;
+    Raw8<T> raw[kAtOnce], raw_residual[kAtOnce], raw_weight[kAtOnce];
+    const auto load = [&](int v) {
+        const int c = (v * THREADS + t) * 8;
+        raw[v % kAtOnce].load(x + row * ld_x, c, hidden);
+        if (residual)
+            raw_residual[v % kAtOnce].load(residual + row * ld_residual, c, hidden);
+    };
+    const auto load_weight = [&](int v) { raw_weight[v % kAtOnce].load(weight, (v * THREADS + t) * 8, hidden); };
+    if constexpr (kAtOnce == NV) {
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+            load(v);
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+            load_weight(v);
+    }
     float h[NV][8];
     float sum = 0.f;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
         const int c = (v * THREADS + t) * 8;
-        load8(h[v], x + row * ld_x, c, hidden);
+        if constexpr (kAtOnce != NV)
+            load(v);
+        raw[v % kAtOnce].to(h[v]);
         if (residual) {
             float y[8];
-            load8(y, residual + row * ld_residual, c, hidden);
+            raw_residual[v % kAtOnce].to(y);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 h[v][e] += y[e];
@@ -118,7 +138,9 @@ __global__ __launch_bounds__(THREADS == kWave ? 256 : THREADS) void norm_kernel(
     for (int v = 0; v < NV; ++v) {
         const int c = (v * THREADS + t) * 8;
         float w[8];
-        load8(w, weight, c, hidden);
+        if constexpr (kAtOnce != NV)
+            load_weight(v);
+        raw_weight[v % kAtOnce].to(w);
 #pragma unroll
         for (int e = 0; e < 8; ++e)
             h[v][e] = h[v][e] * r * w[e];
@@ -137,6 +159,14 @@ __global__ __launch_bounds__(THREADS == kWave ? 256 : THREADS) void norm_kernel(
             }
         }
     }
+}
+
+template <typename T>
+__device__ __forceinline__ void read8(float (&x)[8], const T *row, int c, int n)
+{
+    Raw8<T> raw;
+    raw.load(row, c, n);
+    raw.to(x);
 }
 
 // Blocks take every gridDim.x-th row.  HELD: a row's h and g stay in registers, else
@@ -158,16 +188,32 @@ __global__ __launch_bounds__(THREADS) void norm_grad_kernel(const T *grad_out, i
     for (int64_t row = blockIdx.x; row < rows; row += gridDim.x) {
         const T *gr = grad_out + row * ld_g, *hr = total + row * ld_h;
         const float r = rstd[row];
+        Raw8<T> raw_h[HELD ? NV : 1], raw_g[HELD ? NV : 1], raw_d[HELD ? NV : 1];
+        if constexpr (HELD) {
+#pragma unroll
+            for (int v = 0; v < NV; ++v) {
+                const int c = (v * THREADS + threadIdx.x) * 8;
+                raw_h[v].load(hr, c, hidden);
+                raw_g[v].load(gr, c, hidden);
+            }
+            if (grad_total && grad_x)
+#pragma unroll
+                for (int v = 0; v < NV; ++v)
+                    raw_d[v].load(grad_total + row * ld_gt, (v * THREADS + threadIdx.x) * 8, hidden);
+        }
         float h[HELD ? NV : 1][8], g[HELD ? NV : 1][8];
         float sum = 0.f;
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             const int at = HELD ? v : 0;
-            const int c = (v * THREADS + threadIdx.x) * 8;
-            load8(h[at], hr, c, hidden);
-            load8(g[at], gr, c, hidden);
+            if constexpr (!HELD) {
+                raw_h[at].load(hr, (v * THREADS + threadIdx.x) * 8, hidden);
+                raw_g[at].load(gr, (v * THREADS + threadIdx.x) * 8, hidden);
+            }
+            raw_h[at].to(h[at]);
+            raw_g[at].to(g[at]);
             float w[8];
-            load8(w, weight, c, hidden);
+            read8(w, weight, (v * THREADS + threadIdx.x) * 8, hidden);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 h[at][e] *= r;
@@ -186,10 +232,10 @@ __global__ __launch_bounds__(THREADS) void norm_grad_kernel(const T *grad_out, i
             const int at = HELD ? v : 0;
             const int c = (v * THREADS + threadIdx.x) * 8;
             if constexpr (!HELD) {
-                load8(h[at], hr, c, hidden);
-                load8(g[at], gr, c, hidden);
+                read8(h[at], hr, c, hidden);
+                read8(g[at], gr, c, hidden);
                 float w[8];
-                load8(w, weight, c, hidden);
+                read8(w, weight, c, hidden);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     h[at][e] *= r;
@@ -198,7 +244,9 @@ __global__ __launch_bounds__(THREADS) void norm_grad_kernel(const T *grad_out, i
             }
             float d[8];
             if (grad_total) {
-                load8(d, grad_total + row * ld_gt, c, hidden);
+                if constexpr (!HELD)
+                    raw_d[at].load(grad_total + row * ld_gt, c, hidden);
+                raw_d[at].to(d);
             } else {
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
