@@ -256,14 +256,18 @@ struct Product8 {
 //
 // A wave takes 16 n, a block WAVES of them.  D blocks of 128 k of b are on their way to a wave's
 // registers at any time: each is asked for as soon as the one whose place it takes has been
-// multiplied.  a's rows are shared through LDS, C blocks of k at a time in two buffers,
-// as bf16 (turned once a block, not once a wave), with the chunk's scales.  An a row's 16-byte unit u stands
+// used.  a's rows are shared through LDS, C blocks of k at a time in two buffers, as
+// bf16 (turned once a block, not once a wave), with the scales; a chunk is asked for two chunks
+// ahead, so that what waits for it leaves the later blocks of b on their way.  An a row's 16-byte unit u stands
 // at place u ^ (row mod 16): the 16 rows that are read at once meet distinct banks.
+//
+// 128,256 x 4,096: 16 rows 101 us (5.3 TB/s; loads alone in this pattern 95), 32 rows 109, 64 rows
+// 124 (4.4 TB/s); 1 x 1,024 x 32,000 9.5 us, most of them the call.
 template <typename T, int KN, int WAVES, int C, int D, bool TILES>
-__global__ __launch_bounds__(WAVES *kWave, 4) void stream8_kernel(ProductShape g, T *out, int64_t ld, int64_t split_stride,
+__global__ __launch_bounds__(WAVES *kWave, KN == 1 ? 4 : 3) void stream8_kernel(ProductShape g, T *out, int64_t ld, int64_t split_stride,
                                                                int split_blocks)
 {
-    static_assert(D % C == 0, "a turn of b's places is whole chunks of a");
+    static_assert(D % (2 * C) == 0, "a turn of b's places is a whole turn of the two chunks that are held");
     constexpr int kRows = 16 * KN, kThreads = WAVES * kWave, kCols = WAVES * 16;
     constexpr int kPitch = C * kScaleBlock * 2, kA = kRows * kPitch;
     constexpr int kScales = C * (kRows + (TILES ? 0 : kCols));  // of a chunk: a's, then b's by rows
@@ -282,7 +286,6 @@ __global__ __launch_bounds__(WAVES *kWave, 4) void stream8_kernel(ProductShape g
     const int n = nw + (lane & 15) < g.cols ? nw + (lane & 15) : g.cols - 1;
     const char *const b = static_cast<const char *>(g.b.p) + (int64_t)n * g.b.ld * 2 + (int64_t)from * kScaleBlock + (lane >> 4) * 16;
     const char *const a = static_cast<const char *>(g.a.p) + (int64_t)from * kScaleBlock;
-    const float *const sb_tile = g.sb + (int64_t)((nw < g.cols ? nw : g.cols - 1) / kScaleBlock) * g.blocks + from;
 
     const auto load_b = [&](int kb) {
         const char *p = b + (int64_t)kb * kScaleBlock;
@@ -294,9 +297,16 @@ __global__ __launch_bounds__(WAVES *kWave, 4) void stream8_kernel(ProductShape g
         f.half[1] = *reinterpret_cast<const Words *>(p + 64);
         return f.v;
     };
-    Words pieces[kMine];
-    float scales[kMyScales];
-    const auto load_a = [&](int chunk) {
+    static_assert(!TILES || kScaleBlock % kCols == 0, "a block of threads lies in one tile of b's scales");
+    struct Held {
+        Words pieces[kMine];
+        float scales[kMyScales], tile_scales[TILES ? kMyScales : 1];
+    };
+    Held held[2];
+    const auto load_a = [&](Held &to, int chunk) {
+        Words (&pieces)[kMine] = to.pieces;
+        float (&scales)[kMyScales] = to.scales;
+        // (b's scales by tiles with a's: one read by itself for each block of k would wait for everything before it)
         const auto block = [&](int i) { return chunk * C + i < blocks ? chunk * C + i : blocks - 1; };
 #pragma unroll
         for (int m = 0; m < kMine; ++m) {
@@ -309,19 +319,21 @@ __global__ __launch_bounds__(WAVES *kWave, 4) void stream8_kernel(ProductShape g
         }
 #pragma unroll
         for (int m = 0; m < kMyScales; ++m) {
-            const int at = m * kThreads + threadIdx.x;
-            if (at >= kScales)
-                break;
-            if (at < C * kRows) {
+            const int at = m * kThreads + (int)threadIdx.x < kScales ? m * kThreads + (int)threadIdx.x : kScales - 1;
+            if (TILES || at < C * kRows) {
                 const int r = at % kRows;
                 scales[m] = g.sa[(int64_t)(from + block(at / kRows)) * g.rows + (r < g.rows ? r : g.rows - 1)];
+                if constexpr (TILES)
+                    to.tile_scales[m] = g.sb[(int64_t)(n0 / kScaleBlock) * g.blocks + from + block(at / kRows)];
             } else {
                 const int c = n0 + (at - C * kRows) % kCols;
                 scales[m] = g.sb[(int64_t)(from + block((at - C * kRows) / kCols)) * g.cols + (c < g.cols ? c : g.cols - 1)];
             }
         }
     };
-    const auto keep_a = [&](char *buffer) {
+    const auto keep_a = [&](const Held &from, char *buffer) {
+        const Words (&pieces)[kMine] = from.pieces;
+        const float (&scales)[kMyScales] = from.scales;
         typedef __attribute__((ext_vector_type(2))) __bf16 Pair;
 #pragma unroll
         for (int m = 0; m < kMine; ++m) {
@@ -347,7 +359,7 @@ __global__ __launch_bounds__(WAVES *kWave, 4) void stream8_kernel(ProductShape g
         for (int m = 0; m < kMyScales; ++m) {
             const int at = m * kThreads + threadIdx.x;
             if (at < kScales)
-                reinterpret_cast<float *>(buffer + kA)[at] = scales[m];
+                reinterpret_cast<float *>(buffer + kA)[at] = TILES ? scales[m] * from.tile_scales[TILES ? m : 0] : scales[m];
         }
     };
     const auto barrier = [&] {  // LDS is written and read; loads stay on their way
@@ -358,29 +370,38 @@ __global__ __launch_bounds__(WAVES *kWave, 4) void stream8_kernel(ProductShape g
 
     f32x4 acc[KN] = {};
     i32x8 x[D];
-    load_a(0);
+    load_a(held[0], 0);
+    if (C < blocks)
+        load_a(held[1], 1);
 #pragma unroll
     for (int i = 0; i < D; ++i)
         x[i] = load_b(i < blocks ? i : blocks - 1);
-    keep_a(lds);
+    keep_a(held[0], lds);
     barrier();
-    for (int base = 0; base < blocks; base += D) {
+    // a lane's units of a fragment of a: h's sixteen bytes of its two pieces
+    int place[4];
+#pragma unroll
+    for (int h = 0; h < 4; ++h)
+        place[h] = (lane & 15) * kPitch + (((((lane >> 4) + (h >> 1) * 4) * 2 + (h & 1)) ^ (lane & 15)) * 16);
+    // D blocks of k from `base` on.  ALL: as many follow, and nothing is conditional (a load that may not
+    // have been asked for makes what waits for an earlier one wait for all: 16 x 128,256 x 4,096 108 us for 101).
+    const auto turn = [&](int base, auto all) {
+        constexpr bool ALL = decltype(all)::value;
 #pragma unroll
         for (int i = 0; i < D; ++i) {
             const int kb = base + i;
-            if (kb >= blocks)
+            if (!ALL && kb >= blocks)
                 break;
-            const int chunk = kb / C;
-            const bool more = (chunk + 1) * C < blocks;
-            if (i % C == 0 && more)
-                load_a(chunk + 1);
-            const char *const buffer = lds + (chunk & 1) * kBuffer;
+            if (i % C == 0 && (ALL || kb + 2 * C < blocks))
+                load_a(held[i / C % 2], kb / C + 2);
+            constexpr int kTurn = D / C;  // chunks: an even number, so that a chunk's buffer is known here
+            static_assert(kTurn % 2 == 0, "two buffers");
+            const char *const buffer = lds + i / C % 2 * kBuffer;
             const float *const sc = reinterpret_cast<const float *>(buffer + kA);
             Fragment8<true> fb;
             fb.set(x[i]);
-            if (kb + D < blocks)
+            if (ALL || kb + D < blocks)
                 x[i] = load_b(kb + D);
-            const float tile_scale = TILES ? sb_tile[kb] : 1.f;
             f32x4 sb = {1.f, 1.f, 1.f, 1.f};
             if constexpr (!TILES)
                 sb = *reinterpret_cast<const f32x4 *>(sc + C * kRows + i % C * kCols + wave * 16 + (lane >> 4) * 4);
@@ -389,22 +410,28 @@ __global__ __launch_bounds__(WAVES *kWave, 4) void stream8_kernel(ProductShape g
                 f32x4 p = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int h = 0; h < 4; ++h) {
-                    const int unit = i % C * 16 + ((lane >> 4) + (h >> 1) * 4) * 2 + (h & 1);
-                    const bf16x8 fa = *reinterpret_cast<const bf16x8 *>(buffer + (j * 16 + (lane & 15)) * kPitch +
-                                                                        ((unit ^ (lane & 15)) * 16));
+                    const bf16x8 fa = *reinterpret_cast<const bf16x8 *>(buffer + j * 16 * kPitch + i % C * 256 + place[h]);
                     p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb.part[h], fa, p, 0, 0, 0);
                 }
-                const float sa = sc[i % C * kRows + j * 16 + (lane & 15)] * tile_scale;
+                const float sa = sc[i % C * kRows + j * 16 + (lane & 15)];
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
                     acc[j][e] = __builtin_fmaf(TILES ? p[e] : p[e] * sb[e], sa, acc[j][e]);
+                if constexpr (KN > 2)
+                    asm volatile("" : "+v"(acc[j]));  // added here, as in Product8
             }
-            if (i % C == C - 1 && more) {
-                keep_a(lds + ((chunk + 1) & 1) * kBuffer);
+            if (i % C == C - 1 && (ALL || kb + 1 < blocks)) {
+                keep_a(held[(i / C + 1) % 2], lds + (i / C + 1) % 2 * kBuffer);
                 barrier();
             }
+            __builtin_amdgcn_sched_barrier(0);  // a block of k after the other: registers
         }
-    }
+    };
+    int base = 0;
+    for (; base + 2 * D <= blocks; base += D)
+        turn(base, std::true_type{});
+    for (; base < blocks; base += D)
+        turn(base, std::false_type{});
     barrier();
     // whole lines of the result's rows leave through LDS
 #pragma unroll
@@ -614,7 +641,7 @@ hipError_t launch_product(const ProductArgs &a, const Plan8 &plan, void *workspa
             else if (a.rows <= 32)
                 few(stream8_kernel<O, 2, 4, 2, 4, kTiles>);
             else
-                few(stream8_kernel<O, 4, 8, 2, 2, kTiles>);
+                few(stream8_kernel<O, 4, 8, 2, 4, kTiles>);
         } else if (plan.exact) {
             tiled(product8_kernel<O, 128, 128, 2, 2, kTiles, true>, 256);
         } else if (plan.side == 256) {
