@@ -137,7 +137,7 @@ def test_product_of_wider_rows(dv):
 def test_product_special_values(dv):
     """NaN of a row or a tile stays there; scales of any size; a row of zeros."""
     rng = np.random.default_rng(9)
-    for M in (5, 40, 150):
+    for M, dtype in ((5, F32), (40, F32), (150, F32), (300, BF)):
         a, sa, b, sb = operands(rng, M, 300, 256, 128)
         qa = a.view(torch.uint8).clone()
         qa[1, 3] = 0x7F
@@ -146,10 +146,10 @@ def test_product_special_values(dv):
         sa[0, 4] = 1e30
         sb[1, 1] = math.nan                        # n in [128, 256), k in [128, 256)
         a = qa.view(torch.float8_e4m3fn)
-        out = dv.product_f8(a.to(DEV), sa.to(DEV), b.to(DEV), sb.to(DEV), dtype=F32).cpu()
+        out = dv.product_f8(a.to(DEV), sa.to(DEV), b.to(DEV), sb.to(DEV), dtype=dtype).cpu()
         assert torch.isnan(out[1]).all() and torch.isnan(out[:, 128:256]).all()
         assert (out[2, :128] == 0).all() and (out[2, 256:] == 0).all()
-        want, tol = product_reference(a, sa, b, sb, 128, F32)
+        want, tol = product_reference(a, sa, b, sb, 128, dtype)
         keep = [m for m in range(M) if m != 1]
         for cols in (slice(0, 128), slice(256, 300)):
             check(out[keep][:, cols], want[keep][:, cols], tol[keep][:, cols], f"beside NaN, M {M}")
@@ -180,3 +180,28 @@ def test_product_in_parts(dv, M, N, K, tile, dtype):
     check(wide[:, :N], want, tol, "product in parts")
     assert (wide[:, N:] == 9).all() and (ws[need:] == 0xFF).all()
     assert torch.equal(dv.product_f8(*args, tile=tile, dtype=dtype), wide[:, :N])
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("M,N,K", [(3, 70, 256), (50, 200, 384), (200, 150, 256), (400, 300, 512)])
+def test_product_of_every_value(dv, M, N, K, dtype):
+    """All e4m3 values alike, subnormal ones and both zeros among them: products 2^35 apart."""
+    rng = np.random.default_rng(M)
+    def one(n):
+        q = rng.integers(0, 256, (n, K)).astype(np.uint8)
+        q[(q & 0x7F) == 0x7F] = 0x80
+        return torch.from_numpy(q).view(torch.float8_e4m3fn)
+    a, b = one(M), one(N)
+    sa = torch.from_numpy(np.exp(rng.normal(size=(K // B, M)))).float()
+    sb = torch.from_numpy(np.exp(rng.normal(size=((N + B - 1) // B, K // B)))).float()
+    want, tol = product_reference(a, sa, b, sb, 128, dtype)
+    check(dv.product_f8(a.to(DEV), sa.to(DEV), b.to(DEV), sb.to(DEV), dtype=dtype), want, tol, "product")
+
+
+def test_product_error_on_normal_values(dv):
+    """Many rows in bf16: what the 8-bit matrix instruction cuts is small beside the rounding
+    (each result's at most 2^-9 + 2^-8 / 4 of it in the mean of squares for normal values)."""
+    a, sa, b, sb = operands(np.random.default_rng(3), 512, 384, 1024, 128)
+    want, _ = product_reference(a, sa, b, sb, 128, BF)
+    off = dv.product_f8(a.to(DEV), sa.to(DEV), b.to(DEV), sb.to(DEV)).cpu().double() - want
+    assert float(off.norm() / want.norm()) < 2.0 ** -9
