@@ -727,9 +727,13 @@ F8 = torch.float8_e4m3fn
 SCALE_BLOCK = 128   # columns, or rows and columns, of an 8-bit operand's scale
 
 
+# the current device without the check that there is one (a tensor is on it)
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
 def _run(call, what, dev, stream, *args):
     """A call on its tensors' device, whichever is the current one."""
-    if torch.cuda.current_device() == dev.index:
+    if _current_device() == dev.index:
         st = call(*args, _stream(stream, dev))
     else:
         with torch.cuda.device(dev):
