@@ -10,6 +10,10 @@
 // often it stands in the output, whether it was seen at all, and the number of its
 // bias.  Where the word is zero a logit leaves as it came.  In place and without a mask only
 // the tokens of the history and of the biases are touched, each by whoever takes its word first.
+//
+// 256 x 128,256 bf16 with histories of up to 2,048, 32 biases and a mask: 36 us (reading and writing
+// all of it once: 26 at a copy's rate); windows of 8,192 tokens (fewer blocks at once) 58 us
+// before the loads came first, of 4,096 45.  A mask alone on 64 x 128,256: 7.1 us.
 #include "../../include/dv.h"
 #include "dv_logits.h"
 

@@ -10,6 +10,9 @@
 // A scale and its reciprocal (two divisions) are worked out once, by one lane of the 16 or one
 // thread of the block, and read by the others.  The transposed tile goes through LDS, 8
 // bytes (8 rows of a column) a thread and column, and leaves in whole lines.
+//
+// Memory-bound: 8,192 x 32,000 bf16 by rows 151 us (5.2 TB/s), transposed 177, both 241 (4.35 TB/s,
+// the quotients of both hold three waves a SIMD); by tiles both 222.
 #include <type_traits>
 
 #include "dv_logits.h"
