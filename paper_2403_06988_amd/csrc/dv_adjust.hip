@@ -14,6 +14,8 @@
 // 256 x 128,256 bf16 with histories of up to 2,048, 32 biases and a mask: 36 us (reading and writing
 // all of it once: 26 at a copy's rate); windows of 8,192 tokens (fewer blocks at once) 58 us
 // before the loads came first, of 4,096 45.  A mask alone on 64 x 128,256: 7.1 us.
+#include <type_traits>
+
 #include "../../include/dv.h"
 #include "dv_logits.h"
 
@@ -64,10 +66,10 @@ __device__ __forceinline__ float adjusted(float z, uint32_t word, const Request 
 // NAMED: the call has histories or biases.  Everything that it reads at known places is asked for
 // at once, before the first of it is needed: a block is mostly one wait for memory.
 // Dynamic LDS: the window's words, then the biases' entries.
-template <typename T, bool SPARSE, bool NAMED>
-__global__ __launch_bounds__(256) void adjust_kernel(AdjustArgs a, int windows)
+template <typename T, int THREADS, bool SPARSE, bool NAMED>
+__global__ __launch_bounds__(THREADS) void adjust_kernel(AdjustArgs a, int windows)
 {
-    constexpr int kN = 16 / (int)sizeof(T), kV = kWindow / 256 / kN;  // logits of a vector, vectors of a thread
+    constexpr int kN = 16 / (int)sizeof(T), kV = kWindow / THREADS / kN;  // logits of a vector, vectors of a thread
     extern __shared__ __attribute__((aligned(16))) uint32_t words[];
     struct Entry {
         int at;        // the token's place in the window (past it: another window's, or none)
@@ -80,7 +82,7 @@ __global__ __launch_bounds__(256) void adjust_kernel(AdjustArgs a, int windows)
     const int n = a.V - v0 < kWindow ? a.V - v0 : kWindow;
     const T *in = static_cast<const T *>(a.logits) + (int64_t)row * a.ld + v0;
     T *out = static_cast<T *>(a.out) + (int64_t)row * a.ld_out + v0;
-    const auto place = [&](int i) { return (i * 256 + (int)threadIdx.x) * kN; };  // of vector i in the window
+    const auto place = [&](int i) { return (i * THREADS + (int)threadIdx.x) * kN; };  // of vector i in the window
 
     constexpr int kAtOnce = 8;
     const int32_t *const history = NAMED && a.history ? a.history + (int64_t)row * a.ld_history : nullptr;
@@ -93,7 +95,7 @@ __global__ __launch_bounds__(256) void adjust_kernel(AdjustArgs a, int windows)
         if (history) {
 #pragma unroll
             for (int k = 0; k < kAtOnce; ++k) {
-                const int i = k * 256 + (int)threadIdx.x;
+                const int i = k * THREADS + (int)threadIdx.x;
                 first_ids[k] = i < a.max_history ? history[i] : -1;
             }
             length = a.lengths[row];
@@ -131,21 +133,21 @@ __global__ __launch_bounds__(256) void adjust_kernel(AdjustArgs a, int windows)
     }
 
     if constexpr (NAMED) {
-        for (int i = threadIdx.x; i < kWindow / 4; i += 256)
+        for (int i = threadIdx.x; i < kWindow / 4; i += THREADS)
             reinterpret_cast<uint4 *>(words)[i] = uint4{0, 0, 0, 0};
-        for (int i = threadIdx.x; i < a.num_bias; i += 256) {
-            const bool first = i < 256;
+        for (int i = threadIdx.x; i < a.num_bias; i += THREADS) {
+            const bool first = i < THREADS;
             entries[i] = {(int)((uint32_t)(first ? my_id : bias_ids[i]) - (uint32_t)v0), first ? my_bias : bias[i], 0};
         }
         __syncthreads();
         if (a.num_bias) {
             // the word's upper bits take the token's first entry
-            for (int i = threadIdx.x; i < a.num_bias; i += 256)
+            for (int i = threadIdx.x; i < a.num_bias; i += THREADS)
                 if ((uint32_t)entries[i].at < (uint32_t)n)
                     atomicMax(&words[entries[i].at], (uint32_t)(DV_MAX_BIAS - i) << kBiasShift);
             __syncthreads();
             int others = 0;
-            for (int i = threadIdx.x; i < a.num_bias; i += 256)
+            for (int i = threadIdx.x; i < a.num_bias; i += THREADS)
                 if ((uint32_t)entries[i].at < (uint32_t)n) {
                     const int first = DV_MAX_BIAS - (int)(words[entries[i].at] >> kBiasShift);
                     if (first != i)
@@ -154,7 +156,7 @@ __global__ __launch_bounds__(256) void adjust_kernel(AdjustArgs a, int windows)
             if (__syncthreads_or(others)) {
                 // a token listed twice: a wave adds up its entries, in their order
                 const int lane = threadIdx.x & (kWave - 1);
-                for (int base = threadIdx.x - lane; base < a.num_bias; base += 256) {
+                for (int base = threadIdx.x - lane; base < a.num_bias; base += THREADS) {
                     uint64_t marked = __ballot(base + lane < a.num_bias && entries[base + lane].again);
                     for (; marked; marked &= marked - 1) {
                         const int i = base + __builtin_ctzll(marked), at = entries[i].at;
@@ -182,17 +184,17 @@ __global__ __launch_bounds__(256) void adjust_kernel(AdjustArgs a, int windows)
             };
 #pragma unroll
             for (int k = 0; k < kAtOnce; ++k)
-                count(k * 256 + (int)threadIdx.x, first_ids[k]);
-            for (int from = kAtOnce * 256; from < length; from += kAtOnce * 256) {
+                count(k * THREADS + (int)threadIdx.x, first_ids[k]);
+            for (int from = kAtOnce * THREADS; from < length; from += kAtOnce * THREADS) {
                 int id[kAtOnce];
 #pragma unroll
                 for (int k = 0; k < kAtOnce; ++k) {
-                    const int i = from + k * 256 + (int)threadIdx.x;
+                    const int i = from + k * THREADS + (int)threadIdx.x;
                     id[k] = i < length ? history[i] : -1;
                 }
 #pragma unroll
                 for (int k = 0; k < kAtOnce; ++k)
-                    count(from + k * 256 + (int)threadIdx.x, id[k]);
+                    count(from + k * THREADS + (int)threadIdx.x, id[k]);
             }
         }
         __syncthreads();
@@ -206,9 +208,9 @@ __global__ __launch_bounds__(256) void adjust_kernel(AdjustArgs a, int windows)
                     out[at] = as_logit<T>(adjusted(as_float(in[at]), word, r, bias_of));
             }
         };
-        for (int i = threadIdx.x; i < length; i += 256)
+        for (int i = threadIdx.x; i < length; i += THREADS)
             touch((uint32_t)history[i] - (uint32_t)v0);
-        for (int i = threadIdx.x; i < a.num_bias; i += 256)
+        for (int i = threadIdx.x; i < a.num_bias; i += THREADS)
             touch((uint32_t)entries[i].at);
     } else {
 #pragma unroll
@@ -259,17 +261,25 @@ hipError_t launch_adjust_logits(const AdjustArgs &a, hipStream_t stream)
     const int windows = (a.V + kWindow - 1) / kWindow;
     const unsigned grid = (unsigned)((int64_t)a.rows * windows);
     const size_t lds = named ? kWindow * 4 + (size_t)a.num_bias * 12 : 0;
-    const auto go = [&](auto kernel) { kernel<<<grid, 256, lds, stream>>>(a, windows); };
-    const auto types = [&](auto zero) {
+    // Blocks of 512 threads where all of them run at once: a history is counted in half the time
+    // (77 x 50,257 fp32, histories of up to 16,384 tokens: 14.0 us, in blocks of 256 17.2; 1 x 32,000 4.8
+    // and 5.9).  Of 256 where they take turns (256 x 128,256 bf16 36 us, in blocks of 512 44).
+    const auto types = [&](auto zero, auto threads) {
         using T = decltype(zero);
+        constexpr int kThreads = decltype(threads)::value;
+        const auto go = [&](auto kernel) { kernel<<<grid, kThreads, lds, stream>>>(a, windows); };
         if (sparse)
-            go(adjust_kernel<T, true, true>);
+            go(adjust_kernel<T, kThreads, true, true>);
         else if (named)
-            go(adjust_kernel<T, false, true>);
-        else
-            go(adjust_kernel<T, false, false>);
+            go(adjust_kernel<T, kThreads, false, true>);
+        else if constexpr (kThreads == 256)
+            go(adjust_kernel<T, kThreads, false, false>);
     };
-    a.dtype == 1 ? types(uint16_t{}) : types(float{});
+    const auto blocks = [&](auto threads) { a.dtype == 1 ? types(uint16_t{}, threads) : types(float{}, threads); };
+    if (named && grid <= 1024)
+        blocks(std::integral_constant<int, 512>{});
+    else
+        blocks(std::integral_constant<int, 256>{});
     return last_launch();
 }
 

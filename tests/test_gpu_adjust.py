@@ -75,7 +75,7 @@ def compare(got, z, want, tol, kept, may):
 
 CASES = [(1, 1, 1, 1, 0), (1, 1000, 0, 0, 3), (3, 31, 5, 2, 2), (5, 8192, 64, 4, 0), (4, 8193, 300, None, 5),
          (7, 20011, None, 33, 0), (6, 50257, 3000, 300, 0), (3, 128256, 700, 8, 4), (2, 16385, 20000, 1024, 3),
-         (9, 4099, None, None, 6)]
+         (9, 4099, None, None, 6), (230, 20011, 50, 9, 4), (260, 16500, 2500, None, 0)]
 
 
 @pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
