@@ -105,6 +105,7 @@ class _LinearF8(torch.autograd.Function):
         q, scales, t_q, t_scales = dv.quantize_f8(x, want_columns=want_weight)
         w_q, w_scales, wt_q, wt_scales = dv.quantize_f8(weight, tile=dv.SCALE_BLOCK, want_columns=want_x)
         ctx.save_for_backward(t_q, t_scales, wt_q, wt_scales)
+        ctx.weight_shape = weight.shape
         return dv.product_f8(q, scales, w_q, w_scales, tile=dv.SCALE_BLOCK, dtype=x.dtype)
 
     @staticmethod
@@ -117,7 +118,9 @@ class _LinearF8(torch.autograd.Function):
         grad_x = grad_weight = None
         if want_x:
             grad_x = dv.product_f8(g_q, g_scales, wt_q, wt_scales, tile=dv.SCALE_BLOCK, dtype=dtype)
-        if want_weight:
+        if want_weight and grad_out.shape[0] == 0:  # a sum of nothing
+            grad_weight = grad_out.new_zeros(ctx.weight_shape)
+        elif want_weight:
             grad_weight = dv.product_f8(gt_q, gt_scales, t_q, t_scales, tile=1, dtype=dtype)
         return grad_x, grad_weight
 

@@ -862,6 +862,7 @@ dv_status dv_rms_norm(const void *x, int64_t ld_x, const void *residual, int64_t
     DV_CHECK(aligned(name, "total", total, elt));
     DV_CHECK(aligned(name, "out", out, elt));
     DV_CHECK(aligned(name, "q", q, 8));
+    DV_CHECK(aligned(name, "scales", scales, 4));
     if (rows == 0)
         return DV_OK;
     if (!out && !q)
@@ -965,6 +966,8 @@ dv_status dv_quantize_f8(const void *x, int64_t ld_x, int32_t dtype, int32_t row
     DV_CHECK(aligned(name, "x", x, element_size(dtype)));
     DV_CHECK(aligned(name, "q", q, 16));
     DV_CHECK(aligned(name, "t_q", t_q, 16));
+    DV_CHECK(aligned(name, "scales", scales, 4));
+    DV_CHECK(aligned(name, "t_scales", t_scales, 4));
     if (rows == 0)
         return DV_OK;
     if (!q && !t_q)
@@ -1016,6 +1019,8 @@ dv_status dv_product_f8(const void *a, int64_t ld_a, const float *a_scales, cons
     const size_t elt = element_size(dtype);
     DV_CHECK(aligned(name, "a", a, 16));
     DV_CHECK(aligned(name, "b", b, 16));
+    DV_CHECK(aligned(name, "a_scales", a_scales, 4));
+    DV_CHECK(aligned(name, "b_scales", b_scales, 4));
     DV_CHECK(aligned(name, "out", out, elt));
     if (rows == 0)
         return DV_OK;

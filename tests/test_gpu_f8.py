@@ -205,3 +205,18 @@ def test_product_error_on_normal_values(dv):
     want, _ = product_reference(a, sa, b, sb, 128, BF)
     off = dv.product_f8(a.to(DEV), sa.to(DEV), b.to(DEV), sb.to(DEV)).cpu().double() - want
     assert float(off.norm() / want.norm()) < 2.0 ** -9
+
+
+def test_product_of_rows_far_apart(dv):
+    """The widest row stride: 255 rows of a tile lie 2^30 bytes apart."""
+    rng = np.random.default_rng(6)
+    M, N, K = 300, 270, 256
+    a, sa, b, sb = operands(rng, M, N, K, 128)
+    wide = torch.empty((N - 1) * (1 << 22) + K, dtype=torch.uint8, device=DEV)
+    far = torch.as_strided(wide, (N, K), (1 << 22, 1))
+    far.copy_(b.view(torch.uint8))
+    far = torch.as_strided(wide.view(dv.F8), (N, K), (1 << 22, 1))
+    for rows, dtype in ((M, BF), (M, F32), (7, BF)):
+        args = (a[:rows].to(DEV), sa[:, :rows].contiguous().to(DEV))
+        want = dv.product_f8(*args, b.to(DEV), sb.to(DEV), dtype=dtype)
+        assert torch.equal(dv.product_f8(*args, far, sb.to(DEV), dtype=dtype), want)

@@ -231,3 +231,9 @@ def test_autograd_of_the_8_bit_product(dv, dtype):
     only = x.to(DEV).requires_grad_()
     dva.linear_f8(only, w.to(DEV)).backward(g.to(DEV))
     assert torch.equal(only.grad, a.grad)
+    only = w.to(DEV).requires_grad_()
+    dva.linear_f8(x.to(DEV), only).backward(g.to(DEV))
+    assert torch.equal(only.grad, b.grad)
+    none, only = x[:0].to(DEV).requires_grad_(), w.to(DEV).requires_grad_()
+    dva.linear_f8(none, only).sum().backward()
+    assert none.grad.shape == (0, D) and (only.grad == 0).all()

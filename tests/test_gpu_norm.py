@@ -172,3 +172,29 @@ def test_against_differences(dv):
     size_w = float((gw.cpu().double().abs() * u.abs()).sum()) + 1
     assert abs(float((gx.cpu().double() * v).sum()) - along_x) < 1e-5 * size_x
     assert abs(float((gw.cpu().double() * u).sum()) - along_w) < 1e-5 * size_w
+
+
+def test_every_result_of_one_call(dv):
+    """The C call with both results, the sum over its residual and rstd: each as by itself."""
+    rng = np.random.default_rng(12)
+    N, D = 37, 700
+    x, _ = rows(rng, N, D, BF)
+    res, _ = rows(rng, N, D, BF)
+    x, res, w = x.contiguous(), res.contiguous(), torch.ones(D, dtype=BF, device=DEV)
+    out, total, rstd = dv.rms_norm(x, w, 1e-5, residual=res, want_rstd=True)
+    q, scales, _ = dv.rms_norm_f8(x, w, 1e-5, residual=res)
+    o2, r2, q2, s2 = (torch.empty_like(t) for t in (out, rstd, q, scales))
+    st = dv.lib.dv_rms_norm(x.data_ptr(), D, res.data_ptr(), D, w.data_ptr(), dv.DV_BF16, N, D, 1e-5, res.data_ptr(),
+                            o2.data_ptr(), r2.data_ptr(), q2.data_ptr(), s2.data_ptr(), torch.cuda.current_stream().cuda_stream)
+    assert st == dv.DV_OK
+    assert torch.equal(o2, out) and torch.equal(r2, rstd) and torch.equal(s2, scales) and torch.equal(res, total)
+    assert torch.equal(q2.view(torch.uint8), q.view(torch.uint8))
+
+
+def test_a_row_added_to_itself_in_place(dv):
+    x = torch.from_numpy(np.random.default_rng(13).normal(size=(9, 300))).float().to(DEV)
+    w = torch.ones(300, device=DEV)
+    want, total, _ = dv.rms_norm(x, w, residual=x)
+    y = x.clone()
+    out, t, _ = dv.rms_norm(y, w, residual=y, total=y)
+    assert torch.equal(out, want) and torch.equal(t, total) and t.data_ptr() == y.data_ptr()

@@ -22,7 +22,7 @@ def norm(x=P, ldx=64, res=P + GB, ldr=64, w=P + 2 * GB, dt=1, N=8, D=64, eps=1e-
     (dict(x=None), INVALID), (dict(w=None), INVALID), (dict(q=None), INVALID), (dict(s=None), INVALID),
     (dict(out=None, q=None, s=None), INVALID), (dict(x=P + 1), INVALID), (dict(res=P + GB + 1), INVALID),
     (dict(w=P + 2 * GB + 2, dt=0), INVALID), (dict(total=P + 3 * GB + 1), INVALID), (dict(out=P + 4 * GB + 1), INVALID),
-    (dict(q=P + 6 * GB + 4), INVALID),
+    (dict(q=P + 6 * GB + 4), INVALID), (dict(s=P + 7 * GB + 2), INVALID),
     (dict(N=-1), SHAPE), (dict(N=(1 << 20) + 1), SHAPE), (dict(D=0), SHAPE), (dict(D=65537, ldx=70000, ldr=70000), SHAPE),
     (dict(ldx=63), SHAPE), (dict(ldr=63), SHAPE), (dict(eps=-1.0), SHAPE), (dict(eps=float("nan")), SHAPE),
     (dict(eps=float("inf")), SHAPE), (dict(dt=2), DTYPE),
@@ -62,7 +62,7 @@ def quantize(x=P, ld=200, dt=1, N=300, K=200, tile=1, q=P + GB, s=P + 2 * GB, tq
 @pytest.mark.parametrize("kw,status", [
     (dict(x=None), INVALID), (dict(q=None), INVALID), (dict(s=None), INVALID), (dict(tq=None), INVALID), (dict(ts=None), INVALID),
     (dict(q=None, s=None, tq=None, ts=None), INVALID), (dict(x=P + 1), INVALID), (dict(q=P + GB + 8), INVALID),
-    (dict(tq=P + 3 * GB + 8), INVALID),
+    (dict(tq=P + 3 * GB + 8), INVALID), (dict(s=P + 2 * GB + 1), INVALID), (dict(ts=P + 4 * GB + 2), INVALID),
     (dict(N=-1), SHAPE), (dict(N=(1 << 24) + 1), SHAPE), (dict(K=0), SHAPE), (dict(ld=199), SHAPE), (dict(tile=0), SHAPE),
     (dict(tile=64), SHAPE), (dict(N=1 << 24, K=1 << 14, ld=1 << 14), SHAPE), (dict(dt=5), DTYPE),
     (dict(q=P), ALIAS), (dict(s=P + 64), ALIAS), (dict(tq=P + GB + 16), ALIAS), (dict(ts=P + 2 * GB + 4), ALIAS),
@@ -81,6 +81,7 @@ def product(a=P, lda=256, sa=P + GB, b=P + 2 * GB, ldb=256, sb=P + 3 * GB, tile=
 @pytest.mark.parametrize("kw,status", [
     (dict(a=None), INVALID), (dict(sa=None), INVALID), (dict(b=None), INVALID), (dict(sb=None), INVALID), (dict(out=None), INVALID),
     (dict(a=P + 8), INVALID), (dict(b=P + 2 * GB + 8), INVALID), (dict(out=P + 4 * GB + 1), INVALID),
+    (dict(sa=P + GB + 2), INVALID), (dict(sb=P + 3 * GB + 1), INVALID),
     (dict(M=-1), SHAPE), (dict(N=0), SHAPE), (dict(M=1 << 20, N=1 << 16, ldo=1 << 16), SHAPE), (dict(K=0), SHAPE),
     (dict(K=200), SHAPE), (dict(K=(1 << 22) + 128, lda=1 << 23, ldb=1 << 23), SHAPE), (dict(lda=255), SHAPE), (dict(ldb=240), SHAPE),
     (dict(lda=264), SHAPE), (dict(ldb=257), SHAPE), (dict(ldb=(1 << 22) + 16), SHAPE), (dict(ldo=299), SHAPE), (dict(tile=2), SHAPE),
