@@ -171,83 +171,47 @@ __device__ __forceinline__ void read8(float (&x)[8], const T *row, int c, int n)
     raw.to(x);
 }
 
-// Blocks take every gridDim.x-th row.  HELD: a row's h and g stay in registers, else
-// (the longest rows) they are read again.  Each block's share of dw goes to `partial`
-// [gridDim.x][hidden].
+// Blocks take every gridDim.x-th row.  HELD: a row's h and g stay in registers and the block's
+// share of dw goes to `partial` [gridDim.x][hidden]; else (the longest rows, whose share of dw has no
+// registers left either: norm_weight_part_kernel) they are read again.
 template <typename T, int THREADS, int NV, bool HELD>
 __global__ __launch_bounds__(THREADS) void norm_grad_kernel(const T *grad_out, int64_t ld_g, const T *total, int64_t ld_h,
                                                             const T *weight, const float *rstd, const T *grad_total,
                                                             int64_t ld_gt, int rows, int hidden, T *grad_x, float *partial)
 {
+    constexpr int kHeld = HELD ? NV : 1;
     __shared__ float sums[2][THREADS / kWave];
-    float dw[NV][8];
+    float dw[kHeld][8];
 #pragma unroll
-    for (int v = 0; v < NV; ++v)
+    for (int v = 0; v < kHeld; ++v)
 #pragma unroll
         for (int e = 0; e < 8; ++e)
             dw[v][e] = 0.f;
+    const auto column = [](int v) { return (v * THREADS + (int)threadIdx.x) * 8; };
     int half = 0;
     for (int64_t row = blockIdx.x; row < rows; row += gridDim.x) {
         const T *gr = grad_out + row * ld_g, *hr = total + row * ld_h;
+        const T *const dr = grad_total ? grad_total + row * ld_gt : nullptr;
         const float r = rstd[row];
-        Raw8<T> raw_h[HELD ? NV : 1], raw_g[HELD ? NV : 1], raw_d[HELD ? NV : 1];
-        if constexpr (HELD) {
-#pragma unroll
-            for (int v = 0; v < NV; ++v) {
-                const int c = (v * THREADS + threadIdx.x) * 8;
-                raw_h[v].load(hr, c, hidden);
-                raw_g[v].load(gr, c, hidden);
-            }
-            if (grad_total && grad_x)
-#pragma unroll
-                for (int v = 0; v < NV; ++v)
-                    raw_d[v].load(grad_total + row * ld_gt, (v * THREADS + threadIdx.x) * 8, hidden);
-        }
-        float h[HELD ? NV : 1][8], g[HELD ? NV : 1][8];
-        float sum = 0.f;
-#pragma unroll
-        for (int v = 0; v < NV; ++v) {
-            const int at = HELD ? v : 0;
-            if constexpr (!HELD) {
-                raw_h[at].load(hr, (v * THREADS + threadIdx.x) * 8, hidden);
-                raw_g[at].load(gr, (v * THREADS + threadIdx.x) * 8, hidden);
-            }
+        Raw8<T> raw_h[kHeld], raw_g[kHeld], raw_d[kHeld];
+        float h[kHeld][8], g[kHeld][8];
+        // h r and g w of vector v
+        const auto take = [&](int v, int at) {
+            float w[8];
+            read8(w, weight, column(v), hidden);
             raw_h[at].to(h[at]);
             raw_g[at].to(g[at]);
-            float w[8];
-            read8(w, weight, (v * THREADS + threadIdx.x) * 8, hidden);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 h[at][e] *= r;
-                dw[v][e] = __builtin_fmaf(g[at][e], h[at][e], dw[v][e]);
+                if constexpr (HELD)
+                    dw[at][e] = __builtin_fmaf(g[at][e], h[at][e], dw[at][e]);
                 g[at][e] *= w[e];
-                sum = __builtin_fmaf(g[at][e], h[at][e], sum);
             }
-        }
-        if (!grad_x)
-            continue;
-        sum = row_sum<THREADS>(sum, sums[half]);
-        half ^= 1;  // the next row's sums meet elsewhere: its barrier comes after everyone has read these
-        const float k = sum / (float)hidden;
-#pragma unroll
-        for (int v = 0; v < NV; ++v) {
-            const int at = HELD ? v : 0;
-            const int c = (v * THREADS + threadIdx.x) * 8;
-            if constexpr (!HELD) {
-                read8(h[at], hr, c, hidden);
-                read8(g[at], gr, c, hidden);
-                float w[8];
-                read8(w, weight, c, hidden);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    h[at][e] *= r;
-                    g[at][e] *= w[e];
-                }
-            }
+        };
+        const auto finish = [&](int v, int at, float k) {
             float d[8];
-            if (grad_total) {
-                if constexpr (!HELD)
-                    raw_d[at].load(grad_total + row * ld_gt, c, hidden);
+            if (dr) {
                 raw_d[at].to(d);
             } else {
 #pragma unroll
@@ -257,13 +221,100 @@ __global__ __launch_bounds__(THREADS) void norm_grad_kernel(const T *grad_out, i
 #pragma unroll
             for (int e = 0; e < 8; ++e)
                 d[e] = __builtin_fmaf(r, g[at][e] - h[at][e] * k, d[e]);
-            store8(grad_x + row * hidden, c, hidden, d);
+            store8(grad_x + row * hidden, column(v), hidden, d);
+        };
+        float sum = 0.f;
+        if constexpr (HELD) {
+#pragma unroll
+            for (int v = 0; v < NV; ++v) {
+                raw_h[v].load(hr, column(v), hidden);
+                raw_g[v].load(gr, column(v), hidden);
+            }
+            if (dr && grad_x)
+#pragma unroll
+                for (int v = 0; v < NV; ++v)
+                    raw_d[v].load(dr, column(v), hidden);
+#pragma unroll
+            for (int v = 0; v < NV; ++v) {
+                take(v, v);
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    sum = __builtin_fmaf(g[v][e], h[v][e], sum);
+            }
+        } else {
+#pragma unroll 1
+            for (int v = 0; v < NV; ++v) {
+                raw_h[0].load(hr, column(v), hidden);
+                raw_g[0].load(gr, column(v), hidden);
+                take(v, 0);
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    sum = __builtin_fmaf(g[0][e], h[0][e], sum);
+            }
+        }
+        if (!grad_x)
+            continue;
+        sum = row_sum<THREADS>(sum, sums[half]);
+        half ^= 1;  // the next row's sums meet elsewhere: its barrier comes after everyone has read these
+        const float k = sum / (float)hidden;
+        if constexpr (HELD) {
+#pragma unroll
+            for (int v = 0; v < NV; ++v)
+                finish(v, v, k);
+        } else {
+#pragma unroll 1
+            for (int v = 0; v < NV; ++v) {
+                raw_h[0].load(hr, column(v), hidden);
+                raw_g[0].load(gr, column(v), hidden);
+                if (dr)
+                    raw_d[0].load(dr, column(v), hidden);
+                take(v, 0);
+                finish(v, 0, k);
+            }
         }
     }
-    if (partial)
+    if constexpr (HELD)
+        if (partial)
 #pragma unroll
-        for (int v = 0; v < NV; ++v)
-            store8(partial + (int64_t)blockIdx.x * hidden, (v * THREADS + threadIdx.x) * 8, hidden, dw[v]);
+            for (int v = 0; v < NV; ++v)
+                store8(partial + (int64_t)blockIdx.x * hidden, column(v), hidden, dw[v]);
+}
+
+// The shares of dw of the longest rows: a block takes 2,048 columns of every gridDim.y-th row, four of
+// them at a time, and leaves its share as norm_grad_kernel's blocks do.
+template <typename T>
+__global__ __launch_bounds__(256) void norm_weight_part_kernel(const T *grad_out, int64_t ld_g, const T *total, int64_t ld_h,
+                                                               const float *rstd, int rows, int hidden, float *partial)
+{
+    constexpr int kAtOnce = 4;
+    const int c = (blockIdx.x * 256 + (int)threadIdx.x) * 8;
+    float dw[8] = {};
+    for (int64_t from = blockIdx.y; from < rows; from += (int64_t)gridDim.y * kAtOnce) {
+        Raw8<T> raw_h[kAtOnce], raw_g[kAtOnce];
+        float r[kAtOnce];
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) {
+            const int64_t row = from + (int64_t)k * gridDim.y;
+            r[k] = 0.f;
+            raw_h[k].zero();
+            raw_g[k].zero();
+            if (row < rows) {
+                raw_h[k].load(total + row * ld_h, c, hidden);
+                raw_g[k].load(grad_out + row * ld_g, c, hidden);
+                r[k] = rstd[row];
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) {
+            float h[8], g[8];
+            raw_h[k].to(h);
+            raw_g[k].to(g);
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                dw[e] = __builtin_fmaf(g[e], h[e] * r[k], dw[e]);
+        }
+    }
+    store8(partial + (int64_t)blockIdx.y * hidden, c, hidden, dw);
 }
 
 // dw: the blocks' shares added.  A block takes 64 columns, 16 lanes a share with 4 of them each
@@ -384,10 +435,14 @@ hipError_t launch_grad(const NormGradArgs &a, float *partial, hipStream_t stream
             go(norm_grad_kernel<T, 512, 2, true>, 512);
         else if (a.hidden <= 16384)
             go(norm_grad_kernel<T, 1024, 2, true>, 1024);
-        else if (a.hidden <= 32768)
-            go(norm_grad_kernel<T, 1024, 4, false>, 1024);
-        else
-            go(norm_grad_kernel<T, 1024, 8, false>, 1024);
+        else {
+            if (a.grad_x)
+                a.hidden <= 32768 ? go(norm_grad_kernel<T, 1024, 4, false>, 1024) : go(norm_grad_kernel<T, 1024, 8, false>, 1024);
+            if (a.grad_weight)
+                norm_weight_part_kernel<T><<<dim3((unsigned)((a.hidden + 2047) / 2048), (unsigned)blocks), 256, 0, stream>>>(
+                    static_cast<const T *>(a.grad_out), a.ld_grad_out, static_cast<const T *>(a.total), a.ld_total, a.rstd,
+                    a.rows, a.hidden, partial);
+        }
     }
     if (a.grad_weight)
         norm_weight_kernel<T><<<(unsigned)((a.hidden + 63) / 64), 1024, 0, stream>>>(
