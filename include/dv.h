@@ -624,7 +624,8 @@ DV_API dv_status dv_embed_backward(const void *grad_out, int64_t ld_grad_out, in
  * A block of values x is quantized as
  *     scale = max(largest |x| of the block, 2^-100) / 448   (in fp32)
  *     q     = the e4m3 value nearest to the fp32 quotient x / scale, ties to even;
- * a block that holds an infinity or a NaN becomes NaN, its scale too.
+ * a block that holds an infinity or a NaN becomes NaN, its scale too.  A zero of
+ * either sign becomes +0; what rounds to zero keeps its sign.
  */
 
 /*

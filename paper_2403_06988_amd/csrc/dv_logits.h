@@ -30,6 +30,7 @@ struct BlockScale {
     // x / scale correctly rounded: one Newton step on the product with the correctly rounded
     // reciprocal.  Quotients of bf16 values often lie on the border between two
     // e4m3 values (448 = 7 * 64), where a product alone would fall to either side.
+    // The step makes +0 of -0.
     __device__ __forceinline__ float quotient(float x) const
     {
         const float t = x * inv;

@@ -75,6 +75,19 @@ def test_quantize_borders(dv, tile):
         assert torch.equal(ts.cpu(), want_ts) and same(tq, want_t)
 
 
+@pytest.mark.parametrize("tile", (1, 128))
+@pytest.mark.parametrize("dtype", (torch.float32, torch.bfloat16), ids=("fp32", "bf16"))
+def test_quantize_zeros_sign(dv, tile, dtype):
+    """A zero of either sign becomes +0; what rounds to zero keeps its sign."""
+    t = torch.zeros(128, 128, dtype=dtype)
+    t[::2] = -0.0
+    t[5, 3], t[5, 4] = 448.0, -2.0 ** -20        # the block's scale is 1, e4m3's least value 2^-9
+    q = dv.quantize_f8(t.to(DEV), tile=tile)[0].view(torch.uint8).cpu()
+    want = torch.zeros(128, 128, dtype=torch.uint8)
+    want[5, 3], want[5, 4] = 0x7E, 0x80
+    assert torch.equal(q, want)
+
+
 @pytest.mark.parametrize("tile", [1, 128])
 def test_quantize_special_values(dv, tile):
     t = torch.from_numpy(np.random.default_rng(2).normal(size=(300, 300))).float()
