@@ -706,6 +706,9 @@ DV_API size_t dv_product_f8_workspace_bytes(int32_t rows, int32_t cols, int32_t 
  * out [rows][ld_out] of `dtype`.  A head's logits: a the hidden states, b the
  * weights by tiles.  Gradients of out = x w^T: of x, a = the gradient's q, b = w's
  * t_q by tiles; of w, a = the gradient's t_q, b = x's t_q by rows.
+ * Scales of any size: what fp32 can hold is not lost where a_scales b_scales, or a
+ * block's sum under one of them, would leave its range (a tile of results that meets
+ * such scales is summed twice).
  * Products of fp32 results, and of bf16 results of at most 256 rows, are exact and
  * their sums in fp32.  bf16 results of more rows: of eight neighbouring products
  * what lies below 2^-13 of the largest is cut off before the sum (at most 7 * 2^-13

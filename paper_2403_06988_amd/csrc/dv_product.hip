@@ -4,7 +4,7 @@
 //
 // sb is one number for 128 n (tiles), or one for each n.  A block's sum of 128 products leaves
 // the matrix instruction (16 x 16 x 128) in fp32 and is added to the result's sum under
-// its scale.
+// its scales; where these might leave fp32's range on the way and the result not, in more steps (Factors).
 //
 // Operands stand in LDS as the bf16 ones of dv_gemm.h do: a stage is 128 bytes of every row,
 // here 128 k.  b (whose index n runs along a row of the result) is the instruction's first
@@ -26,6 +26,43 @@ struct ProductShape {
     int rows, cols;
     int blocks;        // of 128 k
 };
+
+// Scales lie from 2^-109 to 2^119 (a caller's own anywhere): sa sb, or by rows a block's sum under
+// sb, may be subnormal or past the largest where the result is neither.  Where no scale is such
+// (is_far), which is nearly always, a tile is summed the short way:
+//     tiles     sum * (sa sb), sa sb a normal number: one rounding
+//     by rows   (sum * sb) * sa, sb from 2^-109 (a block of zeros' scale is above) to 2^103: a sum is
+//               a multiple of 2^-18 and at most 2^25
+// A block that has met one that is sums its tile again the long way (FAR): sa sb, or sa, in two factors, a
+// power of two from 2^-100 to 2^95, under which a sum is exact, and the rest, which is at least 1/4
+// (by rows 1) unless the power is the least: what leaves the range then is the result.
+struct alignas(8) Factors {
+    float power, rest;
+
+    __device__ __forceinline__ Factors(float mantissa, int exponent)
+    {
+        const int e = exponent < -100 ? -100 : exponent > 95 ? 95 : exponent;
+        const int left = exponent - e < 127 ? exponent - e : 127;  // past it every sum but 0 is infinite
+        power = __builtin_ldexpf(1.f, e);
+        rest = __builtin_ldexpf(mantissa, left);
+    }
+    static __device__ __forceinline__ Factors of(float s)
+    {
+        return Factors(2.f * __builtin_amdgcn_frexp_mantf(s), __builtin_amdgcn_frexp_expf(s) - 1);
+    }
+    static __device__ __forceinline__ Factors of(float s, float t)
+    {
+        return Factors(__builtin_amdgcn_frexp_mantf(s) * __builtin_amdgcn_frexp_mantf(t),
+                       __builtin_amdgcn_frexp_expf(s) + __builtin_amdgcn_frexp_expf(t));
+    }
+};
+// Whether a scale asks for the long way: sa sb by tiles, sb by rows.
+template <bool TILES>
+__device__ __forceinline__ bool is_far(float s)
+{
+    s = __builtin_fabsf(s);
+    return TILES ? !(s >= 0x1p-126f && s <= 0x1.fffffep127f) : !(s >= 0x1p-109f && s < 0x1p103f);
+}
 
 // A lane's 32 e4m3 values of a fragment (16 rows of 128 k), as the 8-bit matrix instruction
 // takes them, or (EXACT) as bf16, which holds each of them.
@@ -102,10 +139,13 @@ struct Product8 {
         return f.v;
     }
 
-    // acc += the tile at i0 of b and j0 of a, over `stages` blocks of 128 k from `from` on.
-    static __device__ __forceinline__ void run(f32x4 (&acc)[kTm][kTn], const ProductShape &g, int i0, int j0, int from,
+    // acc += the tile at i0 of b and j0 of a, over `stages` blocks of 128 k from `from` on.  Whether one of this
+    // lane's scales asked for the long way.
+    template <bool FAR>
+    static __device__ __forceinline__ bool run(f32x4 (&acc)[kTm][kTn], const ProductShape &g, int i0, int j0, int from,
                                                int stages, char *lds)
     {
+        bool far = false;
         const int lane = threadIdx.x & (kWave - 1);
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
         const int wm = wave / WN, wn = wave % WN;
@@ -151,7 +191,14 @@ struct Product8 {
         }
         const int iw = i0 + wm * (BM / WM);
         const float *sb_tile = g.sb + (int64_t)((iw < g.cols ? iw : g.cols - 1) / kScaleBlock) * g.blocks;
-        float scale[kTn], next_scale[kTn], next_sb = 1.f;
+        float scale[kTn], power[kTn], next_scale[kTn], next_sb = 1.f;
+        // by rows: the wave's scales of b, of the stage in this buffer
+        const auto check_sb = [&](const char *tile) {
+#pragma unroll
+            for (int i = 0; i < BM / WM; i += kWave)
+                far |= is_far<false>(*reinterpret_cast<const float *>(tile + G::kStageBytes + (wm * (BM / WM) + i + lane) * 4));
+        };
+        static_assert(TILES || BM / WM % kWave == 0, "each lane has as many of them");
         const auto load_scales = [&](int kb) {
             const float *p = g.sa + (int64_t)kb * g.rows;
 #pragma unroll
@@ -188,14 +235,27 @@ struct Product8 {
             const auto add = [&](int i, int j) {
                 const f32x4 x = p[(i * kTn + j) & 3];
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    acc[i][j][e] = __builtin_fmaf(TILES ? x[e] : x[e] * sb[i & 3][e], scale[j], acc[i][j][e]);
+                for (int e = 0; e < 4; ++e) {
+                    const float y = FAR ? x[e] * power[j] : x[e];
+                    acc[i][j][e] = __builtin_fmaf(TILES ? y : y * sb[i & 3][e], scale[j], acc[i][j][e]);
+                }
                 // here, not where the compiler would sink it to: that takes registers for every product
                 asm volatile("" : "+v"(acc[i][j]));
             };
 #pragma unroll
-            for (int j = 0; j < kTn; ++j)
-                scale[j] = TILES ? next_scale[j] * next_sb : next_scale[j];
+            for (int j = 0; j < kTn; ++j) {
+                if constexpr (FAR) {
+                    const Factors f = TILES ? Factors::of(next_scale[j], next_sb) : Factors::of(next_scale[j]);
+                    power[j] = f.power;
+                    scale[j] = f.rest;
+                } else {
+                    scale[j] = TILES ? next_scale[j] * next_sb : next_scale[j];
+                    if constexpr (TILES)
+                        far |= is_far<true>(scale[j]);
+                }
+            }
+            if constexpr (!FAR && !TILES)
+                check_sb(tile);
             if (s + 1 < stages)
                 load_scales(from + s + 1);
 #pragma unroll
@@ -234,6 +294,7 @@ struct Product8 {
             for (int l = kLag; l > 0; --l)
                 add((kTm * kTn - l) / kTn, (kTm * kTn - l) % kTn);
         }
+        return far;
     }
 
     // 4 bytes a lane from base + offset to LDS, as Gemm::load_to_lds
@@ -261,17 +322,19 @@ struct Product8 {
 // ahead, so that what waits for it leaves the later blocks of b on their way.  An a row's 16-byte unit u stands
 // at place u ^ (row mod 16): the 16 rows that are read at once meet distinct banks.
 //
-// 128,256 x 4,096: 16 rows 101 us (5.3 TB/s; loads alone in this pattern 95), 32 rows 109, 64 rows
-// 124 (4.4 TB/s); 1 x 1,024 x 32,000 9.5 us, most of them the call.
+// Scales always go the long way (Factors): four multiplications more a fragment, in time that the loads take anyway.
+//
+// 128,256 x 4,096: 16 rows 101 us (5.3 TB/s; loads alone in this pattern 95), 32 rows 110, 64 rows
+// 130 (4.1 TB/s); 1 x 1,024 x 32,000 9.3 us, most of them the call.
 template <typename T, int KN, int WAVES, int C, int D, bool TILES>
-__global__ __launch_bounds__(WAVES *kWave, KN == 1 ? 4 : 3) void stream8_kernel(ProductShape g, T *out, int64_t ld, int64_t split_stride,
-                                                               int split_blocks)
+__global__ __launch_bounds__(WAVES *kWave, KN == 1 || (KN == 4 && TILES) ? 4 : 3)  // two blocks of eight waves at once
+    void stream8_kernel(ProductShape g, T *out, int64_t ld, int64_t split_stride, int split_blocks)
 {
     static_assert(D % (2 * C) == 0, "a turn of b's places is a whole turn of the two chunks that are held");
     constexpr int kRows = 16 * KN, kThreads = WAVES * kWave, kCols = WAVES * 16;
     constexpr int kPitch = C * kScaleBlock * 2, kA = kRows * kPitch;
     constexpr int kScales = C * (kRows + (TILES ? 0 : kCols));  // of a chunk: a's, then b's by rows
-    constexpr int kBuffer = kA + kScales * 4;
+    constexpr int kBuffer = kA + (kScales + C * kRows) * 4;     // a's in two factors
     constexpr int kPieces = kRows * C * 8;                      // of 16 e4m3 values, in a chunk of a
     constexpr int kMine = (kPieces + kThreads - 1) / kThreads;
     constexpr int kMyScales = (kScales + kThreads - 1) / kThreads;
@@ -358,8 +421,11 @@ __global__ __launch_bounds__(WAVES *kWave, KN == 1 ? 4 : 3) void stream8_kernel(
 #pragma unroll
         for (int m = 0; m < kMyScales; ++m) {
             const int at = m * kThreads + threadIdx.x;
-            if (at < kScales)
-                reinterpret_cast<float *>(buffer + kA)[at] = TILES ? scales[m] * from.tile_scales[TILES ? m : 0] : scales[m];
+            if (at < C * kRows)
+                reinterpret_cast<Factors *>(buffer + kA)[at] =
+                    TILES ? Factors::of(scales[m], from.tile_scales[TILES ? m : 0]) : Factors::of(scales[m]);
+            else if (at < kScales)
+                reinterpret_cast<float *>(buffer + kA)[C * kRows + at] = scales[m];
         }
     };
     const auto barrier = [&] {  // LDS is written and read; loads stay on their way
@@ -397,14 +463,15 @@ __global__ __launch_bounds__(WAVES *kWave, KN == 1 ? 4 : 3) void stream8_kernel(
             constexpr int kTurn = D / C;  // chunks: an even number, so that a chunk's buffer is known here
             static_assert(kTurn % 2 == 0, "two buffers");
             const char *const buffer = lds + i / C % 2 * kBuffer;
-            const float *const sc = reinterpret_cast<const float *>(buffer + kA);
+            const Factors *const sc = reinterpret_cast<const Factors *>(buffer + kA);
             Fragment8<true> fb;
             fb.set(x[i]);
             if (ALL || kb + D < blocks)
                 x[i] = load_b(kb + D);
             f32x4 sb = {1.f, 1.f, 1.f, 1.f};
             if constexpr (!TILES)
-                sb = *reinterpret_cast<const f32x4 *>(sc + C * kRows + i % C * kCols + wave * 16 + (lane >> 4) * 4);
+                sb = *reinterpret_cast<const f32x4 *>(reinterpret_cast<const float *>(sc + C * kRows) + i % C * kCols + wave * 16 +
+                                                      (lane >> 4) * 4);
 #pragma unroll
             for (int j = 0; j < KN; ++j) {
                 f32x4 p = {0.f, 0.f, 0.f, 0.f};
@@ -413,10 +480,12 @@ __global__ __launch_bounds__(WAVES *kWave, KN == 1 ? 4 : 3) void stream8_kernel(
                     const bf16x8 fa = *reinterpret_cast<const bf16x8 *>(buffer + j * 16 * kPitch + i % C * 256 + place[h]);
                     p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb.part[h], fa, p, 0, 0, 0);
                 }
-                const float sa = sc[i % C * kRows + j * 16 + (lane & 15)];
+                const Factors sa = sc[i % C * kRows + j * 16 + (lane & 15)];
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    acc[j][e] = __builtin_fmaf(TILES ? p[e] : p[e] * sb[e], sa, acc[j][e]);
+                for (int e = 0; e < 4; ++e) {
+                    const float y = p[e] * sa.power;
+                    acc[j][e] = __builtin_fmaf(TILES ? y : y * sb[e], sa.rest, acc[j][e]);
+                }
                 if constexpr (KN > 2)
                     asm volatile("" : "+v"(acc[j]));  // added here, as in Product8
             }
@@ -477,7 +546,14 @@ __global__ __launch_bounds__(WM *WN *kWave, 2) void product8_kernel(ProductShape
     const int from = blockIdx.y * split_stages;
     const int stages = g.blocks - from < split_stages ? g.blocks - from : split_stages;
     f32x4 acc[P::kTm][P::kTn] = {};
-    P::run(acc, g, ti * BM, tj * BN, from, stages, lds);
+    if (__syncthreads_or(P::template run<false>(acc, g, ti * BM, tj * BN, from, stages, lds))) {
+#pragma unroll
+        for (int i = 0; i < P::kTm; ++i)
+#pragma unroll
+            for (int j = 0; j < P::kTn; ++j)
+                acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        P::template run<true>(acc, g, ti * BM, tj * BN, from, stages, lds);
+    }
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
     const int wm = wave / WN, wn = wave % WN;
     out += blockIdx.y * split_stride;
