@@ -105,7 +105,7 @@ class _LinearF8(torch.autograd.Function):
         q, scales, t_q, t_scales = dv.quantize_f8(x, want_columns=want_weight)
         w_q, w_scales, wt_q, wt_scales = dv.quantize_f8(weight, tile=dv.SCALE_BLOCK, want_columns=want_x)
         ctx.save_for_backward(t_q, t_scales, wt_q, wt_scales)
-        ctx.weight_shape = weight.shape
+        ctx.weight_shape, ctx.weight_dtype = weight.shape, weight.dtype
         return dv.product_f8(q, scales, w_q, w_scales, tile=dv.SCALE_BLOCK, dtype=x.dtype)
 
     @staticmethod
@@ -114,14 +114,13 @@ class _LinearF8(torch.autograd.Function):
         t_q, t_scales, wt_q, wt_scales = ctx.saved_tensors
         want_x, want_weight = ctx.needs_input_grad
         g_q, g_scales, gt_q, gt_scales = dv.quantize_f8(grad_out.contiguous(), want_rows=want_x, want_columns=want_weight)
-        dtype = grad_out.dtype
         grad_x = grad_weight = None
         if want_x:
-            grad_x = dv.product_f8(g_q, g_scales, wt_q, wt_scales, tile=dv.SCALE_BLOCK, dtype=dtype)
+            grad_x = dv.product_f8(g_q, g_scales, wt_q, wt_scales, tile=dv.SCALE_BLOCK, dtype=grad_out.dtype)
         if want_weight and grad_out.shape[0] == 0:  # a sum of nothing
-            grad_weight = grad_out.new_zeros(ctx.weight_shape)
+            grad_weight = grad_out.new_zeros(ctx.weight_shape, dtype=ctx.weight_dtype)
         elif want_weight:
-            grad_weight = dv.product_f8(gt_q, gt_scales, t_q, t_scales, tile=1, dtype=dtype)
+            grad_weight = dv.product_f8(gt_q, gt_scales, t_q, t_scales, tile=1, dtype=ctx.weight_dtype)
         return grad_x, grad_weight
 
 
@@ -150,5 +149,6 @@ def linear_f8(x, weight):
     """x weight^T [N][V] of x [N][D] and weight [V][D], all three products (this
     and both gradients') of 8-bit operands: x and the gradient with a scale for
     every 128 elements along the products' sums, the weight for every 128 x 128.
-    Sums are in fp32, results in the inputs' type."""
+    Sums are in fp32, the result and x's gradient in x's type, the weight's in the
+    weight's, which may be another."""
     return _LinearF8.apply(x, weight)
