@@ -151,4 +151,6 @@ def linear_f8(x, weight):
     every 128 elements along the products' sums, the weight for every 128 x 128.
     Sums are in fp32, the result and x's gradient in x's type, the weight's in the
     weight's, which may be another."""
+    if x.dim() != 2 or weight.dim() != 2 or weight.shape[1] != x.shape[1]:  # (padded to whole blocks both might fit)
+        raise ValueError(f"x must be [N][D] and weight must be [V][D], got {list(x.shape)} and {list(weight.shape)}")
     return _LinearF8.apply(x, weight)
