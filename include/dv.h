@@ -690,10 +690,19 @@ DV_API dv_status dv_quantize_f8(const void *x, int64_t ld_x, int32_t dtype, int3
 
 /*
  * dv_product_f8_workspace_bytes -- device workspace of dv_product_f8 (sums of
- * parts of a long depth).  Returns 0 when an argument is outside its limit, and
- * may return 0 otherwise: then none is needed.
+ * parts of a long depth) with these sizes.  Returns 0 when an argument is outside its limit, and
+ * may return 0 otherwise: then none is needed.  It falls where more rows fill the
+ * card without parts: a workspace for calls of different rows takes the next query.
  */
 DV_API size_t dv_product_f8_workspace_bytes(int32_t rows, int32_t cols, int32_t depth);
+
+/*
+ * dv_product_f8_workspace_bytes_up_to -- device workspace that serves
+ * dv_product_f8 with any rows up to `rows`; for one cols and depth it never falls
+ * as rows grow.  (It looks at every 128 rows: a question for when memory is
+ * laid out, up to some milliseconds at 2^20 rows.)  0 as above.
+ */
+DV_API size_t dv_product_f8_workspace_bytes_up_to(int32_t rows, int32_t cols, int32_t depth);
 
 /*
  * dv_product_f8 -- the matrix product of two 8-bit operands:

@@ -35,7 +35,7 @@ __all__ = ["align", "validate_vocab", "masked_step", "masked_step_noalloc", "mas
            "head_loss_workspace_bytes", "head_loss_workspace_bytes_for", "head_loss_backward_workspace_bytes",
            "head_loss_backward_workspace_bytes_for", "distill_loss", "distill_loss_backward", "distill_loss_workspace_bytes", "embed", "embed_backward", "embed_backward_workspace_bytes",
            "rms_norm", "rms_norm_f8", "rms_norm_backward", "rms_norm_backward_workspace_bytes", "quantize_f8",
-           "product_f8", "product_f8_workspace_bytes", "adjust_logits", "DvError", "DEAD",
+           "product_f8", "product_f8_workspace_bytes", "product_f8_workspace_bytes_up_to", "adjust_logits", "DvError", "DEAD",
            "library_path", "lib"]
 
 DEAD = -1
@@ -131,6 +131,8 @@ def _load():
     lib.dv_quantize_f8.argtypes = [vp, i64, i32, i32, i32, i32, vp, vp, vp, vp, vp]
     lib.dv_product_f8_workspace_bytes.restype = sz
     lib.dv_product_f8_workspace_bytes.argtypes = [i32, i32, i32]
+    lib.dv_product_f8_workspace_bytes_up_to.restype = sz
+    lib.dv_product_f8_workspace_bytes_up_to.argtypes = [i32, i32, i32]
     lib.dv_product_f8.restype = ctypes.c_int
     lib.dv_product_f8.argtypes = [vp, i64, vp, vp, i64, vp, i32, i32, i32, i32, i32, vp, i64, vp, sz, vp]
     lib.dv_adjust_logits.restype = ctypes.c_int
@@ -721,6 +723,12 @@ def rms_norm_backward_workspace_bytes(rows: int, hidden: int) -> int:
 
 def product_f8_workspace_bytes(rows: int, cols: int, depth: int) -> int:
     return int(lib.dv_product_f8_workspace_bytes(rows, cols, depth))
+
+
+def product_f8_workspace_bytes_up_to(rows: int, cols: int, depth: int) -> int:
+    """Of calls of any number of rows up to ``rows`` (that of one number may be
+    less for more of them)."""
+    return int(lib.dv_product_f8_workspace_bytes_up_to(rows, cols, depth))
 
 
 F8 = torch.float8_e4m3fn

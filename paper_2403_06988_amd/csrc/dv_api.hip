@@ -997,6 +997,11 @@ size_t dv_product_f8_workspace_bytes(int32_t rows, int32_t cols, int32_t depth)
     return product_sizes_ok(rows, cols, depth) ? dv::product_f8_workspace_bytes(rows, cols, depth) : 0;
 }
 
+size_t dv_product_f8_workspace_bytes_up_to(int32_t rows, int32_t cols, int32_t depth)
+{
+    return product_sizes_ok(rows, cols, depth) ? dv::product_f8_workspace_bytes_up_to(rows, cols, depth) : 0;
+}
+
 dv_status dv_product_f8(const void *a, int64_t ld_a, const float *a_scales, const void *b, int64_t ld_b,
                         const float *b_scales, int32_t tile, int32_t rows, int32_t cols, int32_t depth, int32_t dtype,
                         void *out, int64_t ld_out, void *workspace, size_t workspace_bytes, void *stream)

@@ -195,6 +195,7 @@ struct ProductArgs {
     int64_t ld_out;
 };
 size_t product_f8_workspace_bytes(int rows, int cols, int depth);
+size_t product_f8_workspace_bytes_up_to(int rows, int cols, int depth);
 hipError_t launch_product_f8(const ProductArgs &a, void *workspace, hipStream_t stream);
 
 // ----------------------------------------------------------- adjusted logits

@@ -754,6 +754,22 @@ size_t product_f8_workspace_bytes(int rows, int cols, int depth)
     return f32 > bf16 ? f32 : bf16;
 }
 
+// The most of any call of up to `rows` rows.  Between two multiples of 128 rows (32 and 64 below that) only the
+// cost of the parts' sums changes with the rows, so that the splits only fall: the first row's, for all of them.
+size_t product_f8_workspace_bytes_up_to(int rows, int cols, int depth)
+{
+    size_t most = 0;
+    for (int64_t first = 1, last; first <= rows; first = last + 1) {
+        last = first <= 32 ? 32 : first <= kFewRows ? kFewRows : up_block(first);
+        const int end = (int)(last < rows ? last : rows);
+        for (int dtype : {0, 1}) {
+            const size_t bytes = parts_bytes(plan_f8((int)first, cols, depth, dtype), end, cols);
+            most = bytes > most ? bytes : most;
+        }
+    }
+    return most;
+}
+
 hipError_t launch_product_f8(const ProductArgs &a, void *workspace, hipStream_t stream)
 {
     const Plan8 plan = plan_f8(a.rows, a.cols, a.depth, a.dtype);

@@ -12,3 +12,43 @@ def test_linear_f8_refuses_other_depths(x, w):
     """Operands are padded to whole blocks of 128: rows of 100 and 120 would both be 128 long."""
     with pytest.raises(ValueError, match="weight must be"):
         dva.linear_f8(torch.zeros(x), torch.zeros(w))
+
+
+def product(M, N, K, ws, nb):
+    """The call with fake pointers, its result where its workspace is: refused as overlapping, past the workspace's checks."""
+    P, GB = 0x7F0000000000, 1 << 30
+    return dv.lib.dv_product_f8(P, K, P + 200 * GB, P + 20 * GB, K, P + 300 * GB, 128, M, N, K, dv.DV_BF16, ws, N, ws, nb, None)
+
+
+@pytest.mark.parametrize("N,K", [(32000, 4096), (1024, 8192), (1, 128), (257, 1 << 17), (4096, 32000), (128256, 1024)])
+def test_a_products_workspace_for_every_smaller_batch(N, K):
+    """One size serves calls of up to as many rows, and never falls; that of a call's own rows may."""
+    up_to, own = dv.product_f8_workspace_bytes_up_to, dv.product_f8_workspace_bytes
+    rows = sorted({r for c in (1, 16, 32, 64, 128, 192, 256, 512, 640, 1000, 1024, 2048, 4096, 5000) for r in (c - 1, c, c + 1)})
+    most, sizes = 0, []
+    for r in rows:
+        most = max(most, own(r, N, K))
+        sizes.append(up_to(r, N, K))
+        assert sizes[-1] >= most
+    assert sizes == sorted(sizes)
+    for r in rows[1:]:
+        if own(r, N, K):
+            assert product(r, N, K, 0x7F0000000000 + (100 << 30), sizes[-1]) == 4     # DV_ERR_ALIAS: the workspace is enough
+    if (N, K) == (32000, 4096):
+        assert own(64, N, K) > own(65, N, K)
+
+
+def test_a_products_workspace_up_to_every_row():
+    """Row by row where the plan changes often."""
+    for N, K in ((130, 6016), (1024, 8192), (4096, 2048)):
+        most = last = 0
+        for r in range(0, 1400):
+            most = max(most, dv.product_f8_workspace_bytes(r, N, K))
+            now = dv.product_f8_workspace_bytes_up_to(r, N, K)
+            assert now >= most and now >= last
+            last = now
+
+
+def test_workspace_up_to_outside_the_limits():
+    q = dv.product_f8_workspace_bytes_up_to
+    assert q(-1, 8, 128) == q(8, 0, 128) == q(8, 8, 100) == q(8, 8, 0) == q(1 << 20, 1 << 16, 128) == 0
