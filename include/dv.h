@@ -79,6 +79,7 @@ extern "C" {
 #define DV_MAX_DEPTH  4194304      /* depth       in [128, DV_MAX_DEPTH] */
 #define DV_MAX_BIAS   1024         /* num_bias    in [0, DV_MAX_BIAS]    */
 #define DV_MAX_HISTORY 1048575     /* max_history in [0, DV_MAX_HISTORY] */
+#define DV_EXACT_SUMS 256          /* beside dv_product_f8's dtype: no products are cut */
 #define DV_SCALE_BLOCK 128         /* columns, or rows and columns, of an 8-bit operand's scale */
 
 typedef enum dv_status {
@@ -719,7 +720,8 @@ DV_API size_t dv_product_f8_workspace_bytes_up_to(int32_t rows, int32_t cols, in
  * block's sum under one of them, would leave its range (a tile of results that meets
  * such scales is summed twice).
  * Products of fp32 results, and of bf16 results of at most 256 rows, are exact and
- * their sums in fp32.  bf16 results of more rows: of eight neighbouring products
+ * their sums in fp32; with dtype DV_BF16 | DV_EXACT_SUMS those of more rows are too, at about
+ * half the rate.  bf16 results of more rows without it: of eight neighbouring products
  * what lies below 2^-13 of the largest is cut off before the sum (at most 7 * 2^-13
  * of the magnitudes; 1.4e-5 of a sum of normal values, before the result's
  * rounding by 2^-9).

@@ -41,6 +41,7 @@ __all__ = ["align", "validate_vocab", "masked_step", "masked_step_noalloc", "mas
 DEAD = -1
 DV_OK = 0
 DV_F32, DV_BF16 = 0, 1
+DV_EXACT_SUMS = 256   # beside the type of a product of 8-bit operands
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.environ.get("DV_LIBRARY", os.path.join(_HERE, "libdv.so"))
@@ -864,13 +865,19 @@ def quantize_f8(x, tile=1, want_rows=True, want_columns=False, q=None, scales=No
     return q, scales, t_q, t_scales
 
 
-def product_f8(a, a_scales, b, b_scales, tile=128, dtype=torch.bfloat16, out=None, workspace=None, stream=None):
+def product_f8(a, a_scales, b, b_scales, tile=128, dtype=torch.bfloat16, out=None, workspace=None, stream=None, exact=False):
     """a b^T of two 8-bit operands: a [M][K] with scales by rows [K/128][M], b
     [N][K] with scales by tiles ([ceil(N/128)][K/128], ``tile`` 128) or by rows
     ([K/128][N], ``tile`` 1), as ``quantize_f8`` and ``rms_norm_f8`` give them (K a
     multiple of 128, float8_e4m3fn, row starts on 16-byte boundaries).  Returns
     out [M][N] in ``dtype`` (float32 or bfloat16); a given ``out`` may have any
-    row stride, and its type is the result's."""
+    row stride, and its type is the result's.
+
+    Products of float32 results and of at most 256 rows are exact, their sums in
+    fp32.  bfloat16 results of more rows lose of eight neighbouring products what
+    lies below 2^-13 of the largest (for normal values 1.4e-5 of the result, which
+    is then rounded by up to 2^-9), unless ``exact`` asks for the same sums there,
+    at about half the rate."""
     dev = b.device
     ld_a, ld_b = _matrix(a, "a", dev, F8), _matrix(b, "b", dev, F8)
     (M, K), N = a.shape, b.shape[0]
@@ -889,7 +896,7 @@ def product_f8(a, a_scales, b, b_scales, tile=128, dtype=torch.bfloat16, out=Non
     need = product_f8_workspace_bytes(M, N, K)
     workspace, nbytes = _scratch(workspace, need, dev, stream) if need else (None, 0)
     _run(lib.dv_product_f8, "dv_product_f8", dev, stream, _ptr(a), ld_a, _ptr(a_scales), _ptr(b), ld_b, _ptr(b_scales),
-         int(tile), M, N, K, _code(out.dtype), _ptr(out), ld_out, _ptr(workspace), nbytes)
+         int(tile), M, N, K, _code(out.dtype) | (DV_EXACT_SUMS if exact else 0), _ptr(out), ld_out, _ptr(workspace), nbytes)
     return out
 
 

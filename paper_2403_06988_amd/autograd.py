@@ -100,28 +100,28 @@ class _RmsNorm(torch.autograd.Function):
 
 class _LinearF8(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, weight):
-        want_x, want_weight = ctx.needs_input_grad
+    def forward(ctx, x, weight, exact):
+        want_x, want_weight = ctx.needs_input_grad[:2]
         q, scales, t_q, t_scales = dv.quantize_f8(x, want_columns=want_weight)
         w_q, w_scales, wt_q, wt_scales = dv.quantize_f8(weight, tile=dv.SCALE_BLOCK, want_columns=want_x)
         ctx.save_for_backward(t_q, t_scales, wt_q, wt_scales)
-        ctx.weight_shape, ctx.weight_dtype = weight.shape, weight.dtype
-        return dv.product_f8(q, scales, w_q, w_scales, tile=dv.SCALE_BLOCK, dtype=x.dtype)
+        ctx.weight_shape, ctx.weight_dtype, ctx.exact = weight.shape, weight.dtype, exact
+        return dv.product_f8(q, scales, w_q, w_scales, tile=dv.SCALE_BLOCK, dtype=x.dtype, exact=exact)
 
     @staticmethod
     @once_differentiable
     def backward(ctx, grad_out):
         t_q, t_scales, wt_q, wt_scales = ctx.saved_tensors
-        want_x, want_weight = ctx.needs_input_grad
+        want_x, want_weight = ctx.needs_input_grad[:2]
         g_q, g_scales, gt_q, gt_scales = dv.quantize_f8(grad_out.contiguous(), want_rows=want_x, want_columns=want_weight)
         grad_x = grad_weight = None
         if want_x:
-            grad_x = dv.product_f8(g_q, g_scales, wt_q, wt_scales, tile=dv.SCALE_BLOCK, dtype=grad_out.dtype)
+            grad_x = dv.product_f8(g_q, g_scales, wt_q, wt_scales, tile=dv.SCALE_BLOCK, dtype=grad_out.dtype, exact=ctx.exact)
         if want_weight and grad_out.shape[0] == 0:  # a sum of nothing
             grad_weight = grad_out.new_zeros(ctx.weight_shape, dtype=ctx.weight_dtype)
         elif want_weight:
-            grad_weight = dv.product_f8(gt_q, gt_scales, t_q, t_scales, tile=1, dtype=ctx.weight_dtype)
-        return grad_x, grad_weight
+            grad_weight = dv.product_f8(gt_q, gt_scales, t_q, t_scales, tile=1, dtype=ctx.weight_dtype, exact=ctx.exact)
+        return grad_x, grad_weight, None
 
 
 def embed(weight, ids, scale=1.0):
@@ -145,12 +145,13 @@ def rms_norm(x, weight, eps=1e-6, residual=None):
     return _RmsNorm.apply(x, residual, weight, eps)
 
 
-def linear_f8(x, weight):
+def linear_f8(x, weight, exact=False):
     """x weight^T [N][V] of x [N][D] and weight [V][D], all three products (this
     and both gradients') of 8-bit operands: x and the gradient with a scale for
     every 128 elements along the products' sums, the weight for every 128 x 128.
     Sums are in fp32, the result and x's gradient in x's type, the weight's in the
-    weight's, which may be another."""
+    weight's, which may be another.  ``exact``: bfloat16 results with the sums of
+    float32 ones, as ``dv.product_f8``."""
     if x.dim() != 2 or weight.dim() != 2 or weight.shape[1] != x.shape[1]:  # (padded to whole blocks both might fit)
         raise ValueError(f"x must be [N][D] and weight must be [V][D], got {list(x.shape)} and {list(weight.shape)}")
-    return _LinearF8.apply(x, weight)
+    return _LinearF8.apply(x, weight, exact)

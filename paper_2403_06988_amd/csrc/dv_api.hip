@@ -1010,6 +1010,9 @@ dv_status dv_product_f8(const void *a, int64_t ld_a, const float *a_scales, cons
     const char *name = "dv_product_f8";
     if (!b || !b_scales || (rows > 0 && (!a || !a_scales || !out)))
         return fail(DV_ERR_INVALID_ARG, "%s: b and b_scales must be non-NULL, a, a_scales and out when rows > 0", name);
+    const bool exact = dtype >= 0 && (dtype & DV_EXACT_SUMS);
+    if (exact)
+        dtype -= DV_EXACT_SUMS;
     DV_CHECK(train_sizes(name, {0, 1, dtype}));
     DV_CHECK(tile_arg(name, tile));
     if (!product_sizes_ok(rows, cols, depth))
@@ -1037,7 +1040,7 @@ dv_status dv_product_f8(const void *a, int64_t ld_a, const float *a_scales, cons
                          range_of(a_scales, scale_bytes(rows, depth, 1)), range_of(b_scales, scale_bytes(cols, depth, tile))};
     DV_CHECK(no_overlap(name, outs, ins));
     const dv::ProductArgs p{static_cast<const uint8_t *>(a), ld_a, a_scales, static_cast<const uint8_t *>(b), ld_b, b_scales,
-                            tile != 1, rows, cols, depth, dtype, out, ld_out};
+                            tile != 1, rows, cols, depth, dtype, exact, out, ld_out};
     return hip_status(dv::launch_product_f8(p, workspace, static_cast<hipStream_t>(stream)), "dv_product_f8 launch");
 }
 

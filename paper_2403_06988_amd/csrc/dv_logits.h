@@ -191,6 +191,7 @@ struct ProductArgs {
     bool tiles;
     int rows, cols, depth;
     int dtype;  // of the result
+    bool exact; // exact sums, whatever the type and rows
     void *out;
     int64_t ld_out;
 };

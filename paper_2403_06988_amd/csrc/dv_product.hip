@@ -637,13 +637,15 @@ constexpr int kFewRows = 64, kMostSplits = 16;
 // them before it adds them up in fp32: at most 7 * 2^-13 of the magnitudes, 1.4e-5 of a sum of
 // normal values (measured), where a bf16 result's own rounding is 1.7e-3.  fp32
 // results take the products of the same values as bf16, which lose nothing (half the rate: 4,096 in each direction
-// 126 us against 63), and so do bf16 results of a decode step's at most 256 rows, whose time is mostly b's.
-bool exact_sums(int rows, int dtype) { return dtype == 0 || rows <= 256; }
+// 126 us against 63), and so does a call that asks for it.  So do bf16 results of at most 256 rows, a decode step's,
+// whose tokens are chosen by differences of logits.  That is for the sums' sake, at a price (x 128,256 x 4,096):
+// 65 to 128 rows 161-164 us, by 8-bit instructions 142-150; 129 to 256 rows 283-289, by these 162-172.
+bool exact_sums(int rows, int dtype, bool asked) { return asked || dtype == 0 || rows <= 256; }
 
-Plan8 plan_f8(int rows, int cols, int depth, int dtype)
+Plan8 plan_f8(int rows, int cols, int depth, bool exact)
 {
     const int blocks = depth / kScaleBlock;
-    Plan8 best{exact_sums(rows, dtype), 0, 0, 1, blocks};
+    Plan8 best{exact, 0, 0, 1, blocks};
     if (rows <= kFewRows) {
         best.waves = rows <= 32 ? 4 : 8;
         const int64_t n = (cols + best.waves * 16 - 1) / (best.waves * 16);
@@ -749,9 +751,9 @@ hipError_t launch_product(const ProductArgs &a, const Plan8 &plan, void *workspa
 
 size_t product_f8_workspace_bytes(int rows, int cols, int depth)
 {
-    const size_t f32 = parts_bytes(plan_f8(rows, cols, depth, 0), rows, cols);
-    const size_t bf16 = parts_bytes(plan_f8(rows, cols, depth, 1), rows, cols);
-    return f32 > bf16 ? f32 : bf16;
+    const size_t exact = parts_bytes(plan_f8(rows, cols, depth, true), rows, cols);
+    const size_t cut = exact_sums(rows, 1, false) ? 0 : parts_bytes(plan_f8(rows, cols, depth, false), rows, cols);
+    return exact > cut ? exact : cut;
 }
 
 // The most of any call of up to `rows` rows.  Between two multiples of 128 rows (32 and 64 below that) only the
@@ -762,8 +764,8 @@ size_t product_f8_workspace_bytes_up_to(int rows, int cols, int depth)
     for (int64_t first = 1, last; first <= rows; first = last + 1) {
         last = first <= 32 ? 32 : first <= kFewRows ? kFewRows : up_block(first);
         const int end = (int)(last < rows ? last : rows);
-        for (int dtype : {0, 1}) {
-            const size_t bytes = parts_bytes(plan_f8((int)first, cols, depth, dtype), end, cols);
+        for (bool exact : {true, exact_sums((int)first, 1, false)}) {
+            const size_t bytes = parts_bytes(plan_f8((int)first, cols, depth, exact), end, cols);
             most = bytes > most ? bytes : most;
         }
     }
@@ -772,7 +774,7 @@ size_t product_f8_workspace_bytes_up_to(int rows, int cols, int depth)
 
 hipError_t launch_product_f8(const ProductArgs &a, void *workspace, hipStream_t stream)
 {
-    const Plan8 plan = plan_f8(a.rows, a.cols, a.depth, a.dtype);
+    const Plan8 plan = plan_f8(a.rows, a.cols, a.depth, exact_sums(a.rows, a.dtype, a.exact));
     return a.dtype == 1 ? launch_product<__bf16>(a, plan, workspace, stream) : launch_product<float>(a, plan, workspace, stream);
 }
 

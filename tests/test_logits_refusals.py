@@ -52,3 +52,13 @@ def test_a_products_workspace_up_to_every_row():
 def test_workspace_up_to_outside_the_limits():
     q = dv.product_f8_workspace_bytes_up_to
     assert q(-1, 8, 128) == q(8, 0, 128) == q(8, 8, 100) == q(8, 8, 0) == q(1 << 20, 1 << 16, 128) == 0
+
+
+def test_exact_sums_of_no_other_type():
+    """The choice stands beside a type; other bits are refused as types are."""
+    P, GB = 0x7F0000000000, 1 << 30
+    call = lambda dt: dv.lib.dv_product_f8(P, 256, P + GB, P + 2 * GB, 256, P + 3 * GB, 128, 8, 300, 256, dt, P + 16, 300,  # noqa: E731
+                                           P + 5 * GB, 1 << 50, None)
+    assert call(dv.DV_BF16 | dv.DV_EXACT_SUMS) == call(dv.DV_F32 | dv.DV_EXACT_SUMS) == 4      # as far as the overlap
+    for dt in (2 | dv.DV_EXACT_SUMS, 2 * dv.DV_EXACT_SUMS, -1, dv.DV_EXACT_SUMS << 1 | dv.DV_BF16):
+        assert call(dt) == 3                                                                    # DV_ERR_DTYPE
