@@ -861,6 +861,7 @@ dv_status dv_rms_norm(const void *x, int64_t ld_x, const void *residual, int64_t
     DV_CHECK(aligned(name, "weight", weight, elt));
     DV_CHECK(aligned(name, "total", total, elt));
     DV_CHECK(aligned(name, "out", out, elt));
+    DV_CHECK(aligned(name, "rstd", rstd, 4));
     DV_CHECK(aligned(name, "q", q, 8));
     DV_CHECK(aligned(name, "scales", scales, 4));
     if (rows == 0)
@@ -911,6 +912,7 @@ dv_status dv_rms_norm_backward(const void *grad_out, int64_t ld_grad_out, const 
     DV_CHECK(aligned(name, "grad_out", grad_out, elt));
     DV_CHECK(aligned(name, "total", total, elt));
     DV_CHECK(aligned(name, "weight", weight, elt));
+    DV_CHECK(aligned(name, "rstd", rstd, 4));
     DV_CHECK(aligned(name, "grad_total", grad_total, elt));
     DV_CHECK(aligned(name, "grad_x", grad_x, elt));
     DV_CHECK(aligned(name, "grad_weight", grad_weight, elt));
@@ -1074,6 +1076,15 @@ dv_status dv_adjust_logits(const void *logits, int64_t ld_logits, int32_t dtype,
     const size_t elt = element_size(dtype), n = (size_t)rows;
     DV_CHECK(aligned(name, "logits", logits, elt));
     DV_CHECK(aligned(name, "out", out, elt));
+    const struct {
+        const char *name;
+        const void *p;
+    } words[] = {{"history", history},       {"lengths", lengths},     {"prompt_lengths", prompt_lengths},
+                 {"repetition", repetition}, {"presence", presence},   {"frequency", frequency},
+                 {"bias_ids", bias_ids},     {"bias", bias},           {"allow", allow},
+                 {"states", states}};
+    for (const auto &w : words)
+        DV_CHECK(aligned(name, w.name, w.p, 4));
     if (rows == 0)
         return DV_OK;
     const bool in_place = out == logits && (ld_out == ld_logits || rows == 1);

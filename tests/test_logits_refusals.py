@@ -62,3 +62,34 @@ def test_exact_sums_of_no_other_type():
     assert call(dv.DV_BF16 | dv.DV_EXACT_SUMS) == call(dv.DV_F32 | dv.DV_EXACT_SUMS) == 4      # as far as the overlap
     for dt in (2 | dv.DV_EXACT_SUMS, 2 * dv.DV_EXACT_SUMS, -1, dv.DV_EXACT_SUMS << 1 | dv.DV_BF16):
         assert call(dt) == 3                                                                    # DV_ERR_DTYPE
+
+
+P, GB = 0x7F0000000000, 1 << 30
+
+
+def norm(rstd=P + 5 * GB):
+    return dv.lib.dv_rms_norm(P, 64, P + GB, 64, P + 2 * GB, 1, 8, 64, 1e-6, P + 2 * GB, P + 4 * GB, rstd, None, None, None)
+
+
+def norm_back(rstd=P + 3 * GB):
+    return dv.lib.dv_rms_norm_backward(P, 64, P + GB, 64, P + 2 * GB, rstd, None, 64, 1, 8, 64, P + 5 * GB, P + 5 * GB, P + 7 * GB,
+                                       1 << 40, None)
+
+
+def adjust(history=P + GB, lengths=P + 2 * GB, prompts=P + 3 * GB, repetition=P + 4 * GB, presence=P + 5 * GB, frequency=P + 6 * GB,
+           ids=P + 7 * GB, bias=P + 8 * GB, allow=P + 9 * GB, states=P + 10 * GB):
+    return dv.lib.dv_adjust_logits(P, 1000, 1, 8, 1000, history, 50, 50, lengths, prompts, repetition, presence, frequency, ids, bias, 4,
+                                   allow, 2, states, P + 2, 1000, None)
+
+
+@pytest.mark.parametrize("call,names", [(norm, ["rstd"]), (norm_back, ["rstd"]),
+                                        (adjust, ["history", "lengths", "prompts", "repetition", "presence", "frequency", "ids", "bias",
+                                                  "allow", "states"])])
+def test_arrays_of_four_bytes_off_their_alignment(call, names):
+    """fp32 and int32 arrays as the others (calls that a later check, the overlap's, would stop)."""
+    assert call() == 4                                              # DV_ERR_ALIAS
+    for name in names:
+        place = call.__defaults__[call.__code__.co_varnames.index(name)]
+        for off in (1, 2):
+            assert call(**{name: place + off}) == 1                 # DV_ERR_INVALID_ARG
+            assert b"aligned" in dv.lib.dv_last_error()
