@@ -325,9 +325,9 @@ struct Product8 {
 // Scales always go the long way (Factors): four multiplications more a fragment, in time that the loads take anyway.
 //
 // 128,256 x 4,096: 16 rows 101 us (5.3 TB/s; loads alone in this pattern 95), 32 rows 110, 64 rows
-// 130 (4.1 TB/s); 1 x 1,024 x 32,000 9.3 us, most of them the call.
+// 125 (4.3 TB/s); 1 x 1,024 x 32,000 9.0 us, most of them the call.
 template <typename T, int KN, int WAVES, int C, int D, bool TILES>
-__global__ __launch_bounds__(WAVES *kWave, KN == 1 || (KN == 4 && TILES) ? 4 : 3)  // two blocks of eight waves at once
+__global__ __launch_bounds__(WAVES *kWave, KN == 1 ? 4 : 3)
     void stream8_kernel(ProductShape g, T *out, int64_t ld, int64_t split_stride, int split_blocks)
 {
     static_assert(D % (2 * C) == 0, "a turn of b's places is a whole turn of the two chunks that are held");
