@@ -192,13 +192,11 @@ struct Product8 {
         const int iw = i0 + wm * (BM / WM);
         const float *sb_tile = g.sb + (int64_t)((iw < g.cols ? iw : g.cols - 1) / kScaleBlock) * g.blocks;
         float scale[kTn], power[kTn], next_scale[kTn], next_sb = 1.f;
-        // by rows: the wave's scales of b, of the stage in this buffer
+        // by rows: b's scales of the stage in this buffer, 64 of them a wave
         const auto check_sb = [&](const char *tile) {
-#pragma unroll
-            for (int i = 0; i < BM / WM; i += kWave)
-                far |= is_far<false>(*reinterpret_cast<const float *>(tile + G::kStageBytes + (wm * (BM / WM) + i + lane) * 4));
+            far |= is_far<false>(*reinterpret_cast<const float *>(tile + G::kStageBytes + (wave * kWave % BM + lane) * 4));
         };
-        static_assert(TILES || BM / WM % kWave == 0, "each lane has as many of them");
+        static_assert(TILES || (BM % kWave == 0 && BM / kWave <= kWaves), "the waves check all of them");
         const auto load_scales = [&](int kb) {
             const float *p = g.sa + (int64_t)kb * g.rows;
 #pragma unroll
