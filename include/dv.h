@@ -642,7 +642,9 @@ DV_API dv_status dv_embed_backward(const void *grad_out, int64_t ld_grad_out, in
  * `dtype`; rstd [rows] fp32; q and scales (both or none) = y as an 8-bit operand by
  * rows, quantized from fp32.  q 8-byte aligned.  total may be the residual or x
  * itself (the same address, row stride D).  At least one of out and q is wanted.
- * eps >= 0 and finite.  A row of zeros with eps = 0 gives NaN.
+ * eps >= 0 and finite.  A row of zeros with eps = 0 gives NaN.  rstd is infinite where it
+ * passes fp32's largest (a root mean square below 2^-128, eps = 0 or hardly more): out is
+ * as defined there, the gradients are not.
  * rows = 0 is valid and enqueues nothing.
  * Errors as dv_head_loss (no workspace).
  */

@@ -9,7 +9,8 @@
 //
 // Memory-bound: each row is read once and held in registers, 8 columns a lane and
 // vector, by one wave (up to 1,024 columns) or one block; a row's loads are all asked for before the first
-// is needed.  8,192 x 4,096 bf16 with a residual 43 us (6.3 TB/s), its gradients 46 (5.8
+// is needed.  Gradients of more than 16,384 columns have no registers for that: rows are read twice for dh and a
+// third time for dw (512 x 65,536 bf16 65 us).  8,192 x 4,096 bf16 with a residual 43 us (6.3 TB/s), its gradients 46 (5.8
 // TB/s) and 6 to join the weight's; 2,304 x 4,096 to e4m3 13 us; 1 x 1,024 2.7.
 #include "dv_logits.h"
 

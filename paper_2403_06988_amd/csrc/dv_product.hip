@@ -531,7 +531,7 @@ __global__ __launch_bounds__(WAVES *kWave, KN == 1 ? 4 : 3)
 }
 
 // 8-bit instructions: 8,192 x 32,000 x 4,096 1.04 ms (2.06 PFLOP/s), 8,192 x 4,096 x 32,000 0.98 (2.19), b by rows
-// 32,000 x 4,096 x 8,192 1.16; bound by the matrix instructions and the adds under the scales, which hardly overlap (without
+// 32,000 x 4,096 x 8,192 1.19; bound by the matrix instructions and the adds under the scales, which hardly overlap (without
 // the adds 2.85 PFLOP/s).  Exact: 4,096 in each direction 126 us (1.09 PFLOP/s).
 template <typename T, int BM, int BN, int WM, int WN, bool TILES, bool EXACT>
 __global__ __launch_bounds__(WM *WN *kWave, 2) void product8_kernel(ProductShape g, T *out, int64_t ld, int64_t split_stride,
